@@ -414,6 +414,158 @@ int fkv_read_kv(fkv_ctx *ctx, const double *pts_dev, int64_t n_streams, int64_t 
                 int64_t pt_stride, const int64_t *req_dev, int64_t n_req, void *out_dev,
                 int dtype, void *stream);
 
+/* ------------------------------------------------ paged 8-bit cache ----- */
+
+/* The positions that are still attended to, held in 8 bits until they are
+ * archived (the paper keeps its exact window in the cache's own type and has
+ * no counterpart).  A page is `block` consecutive positions of one request;
+ * its codes for one head share a float32 scale, a value being code x scale.
+ * Requests reach their pages through a block table.  fkv_page_plan gives pages
+ * to new tokens, fkv_page_write quantises them, fkv_page_attend attends over
+ * them, and fkv_page_read rebuilds positions into the K/V cache that
+ * fkv_rvq_encode archives. */
+
+/* Formats of a code: FKV_E4M3, 1-4-3 bits, finite values up to 448 (the two
+ * NaN codes are never written, and a page that holds one in a written slot is
+ * not valid); FKV_INT8, -127 .. 127. */
+#define FKV_E4M3 0
+#define FKV_INT8 1
+
+#define FKV_PAGE_MAX_REQ 16384         /* requests a call */
+#define FKV_PAGE_MAX_LEN (1 << 30)     /* positions a request */
+
+/* A pool of pages on the device, caller-owned: K and V code tensors indexed by
+ * (page, head, position in the page) with `dim` contiguous bytes each and the
+ * same byte strides (multiples of 16, data 16-byte aligned), and their scales,
+ * indexed by (page, head).  dim is 64 or 128, block a multiple of 16 up to
+ * 1024.  Any order of the strides will do: [page][head][position][dim] and
+ * [page][position][head][dim] alike.  Scales lie in [2^-100, 2^100]. */
+typedef struct {
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    int format;             /* FKV_E4M3 or FKV_INT8 */
+    int n_heads;
+    int dim;
+    int block;
+    int64_t n_blocks;
+    int64_t stride_block;
+    int64_t stride_head;
+    int64_t stride_pos;
+    int64_t scale_stride_block;   /* in floats */
+    int64_t scale_stride_head;
+} fkv_pages;
+
+/* Vectors of a batch's tokens, device memory: `dim` contiguous elements by
+ * (token, head), element strides whose bytes are multiples of 16, data 16-byte
+ * aligned. */
+typedef struct {
+    void *data;
+    int dtype;              /* FKV_F32, FKV_F16 or FKV_BF16 */
+    int64_t stride_tok;
+    int64_t stride_head;
+} fkv_rows;
+
+/* Block tables and slot maps from request lengths, on the device.  For each
+ * request r < n_req (at most FKV_PAGE_MAX_REQ), kv_len_dev[r] positions are in
+ * its pages and n_new_dev[r] tokens follow, or n_new_dev[r] < 0: the request
+ * ends and gives its pages back.
+ *   table_dev   int32 [n_req][table_stride], `width` columns used: request r's
+ *               pages in order; entries of new pages are added, the others
+ *               left as they are (an ended request's too)
+ *   free_dev    int32 [n_free]: a stack of page ids whose first *taken_dev
+ *               entries have been given out.  Pages given back are put before
+ *               entry *taken_dev, in the order of the requests and of their
+ *               positions; new pages are then taken in the same order
+ *   taken_dev   int32, kv_len_dev int32 [n_req]; their new values go to
+ *               taken_out_dev and kv_len_out_dev, which may be the same arrays
+ *               (an ended request's length is 0)
+ *   cu_dev      int32 [n_req + 1]: request r's tokens are rows cu[r] .. cu[r+1]
+ *   slots_dev   int64 [rows]: page id x block + position in the page of each
+ *               token's place, -1 from row cu[n_req] on
+ *   pos_dev     int32 [rows]: its position in the request, -1 likewise
+ * A page belongs to one request.  A call that does not fit is not carried out:
+ * a negative length, one above FKV_PAGE_MAX_LEN, more than `width` pages, more
+ * tokens than rows, more pages than are free, or more given back than were
+ * taken.  It sets FKV_ERANGE in the status word, copies lengths and count, sets
+ * every cu to 0 and every slot and position to -1, and changes nothing else. */
+int fkv_page_plan(fkv_ctx *ctx, const int32_t *n_new_dev, const int32_t *kv_len_dev, int64_t n_req,
+                  int32_t *table_dev, int64_t table_stride, int64_t width, int32_t *free_dev, int64_t n_free,
+                  const int32_t *taken_dev, int block, int32_t *cu_dev, int64_t *slots_dev, int32_t *pos_dev,
+                  int64_t rows, int32_t *kv_len_out_dev, int32_t *taken_out_dev, void *stream);
+
+/* Quantise the K and V vectors of n_tok tokens (k and v: n_heads heads, the
+ * same dtype) into the slots slots_dev[t] (int64; negative: the token is
+ * skipped).  Tokens with consecutive slots form a run in each page; a page
+ * takes one run a call, and its rows before the run's first one are those
+ * written earlier (fkv_page_plan's slots are of this kind).  With amax the
+ * run's largest finite magnitude, its wanted scale is
+ *     FKV_E4M3: the smallest power of two not below amax / 448,
+ *     FKV_INT8: amax / 127 (rounded to float32),
+ * at least 2^-100.  A page without earlier rows takes the wanted scale; another
+ * keeps its own if that is as large, else its earlier rows' codes are rounded
+ * again, code x (old scale x (1 / new scale)).  A value x is stored as
+ * x x (1 / scale) rounded to the nearest code (ties to even), beyond the
+ * largest as the largest.  A NaN is stored as zero and sets FKV_ECORRUPT in the
+ * status word; a slot past the pool is skipped and sets FKV_ERANGE.  What two
+ * runs of one page in a call leave there is not specified. */
+int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, const fkv_rows *v,
+                   const int64_t *slots_dev, int64_t n_tok, void *stream);
+
+/* Options of fkv_page_attend. */
+typedef struct {
+    float scale;                 /* multiplies q.k */
+    float softcap;               /* cap > 0: s becomes cap tanh(s / cap); 0: none */
+    int causal;                  /* 1: no position after a row's own */
+    int64_t window;              /* w > 0: only the w positions up to the row's own, and */
+    int64_t sinks;               /*   the request's first `sinks` ones; 0: no window */
+    const float *slopes;         /* device, [n_q_heads], or NULL: adds slope x (j - p) */
+    const int32_t *prefix;       /* device, [n_req], or NULL: the first prefix[r] positions
+                                    are seen by every row of request r */
+} fkv_attend;
+
+/* Attention of a batch's query rows over the pages.  q: n_tok tokens of
+ * n_q_heads heads (FKV_F16 or FKV_BF16), n_q_heads a multiple of
+ * pages->n_heads: query head u reads KV head u / (n_q_heads / n_heads).
+ * Request r's tokens are rows cu_dev[r] .. cu_dev[r+1] of q and the last of its
+ * kv_len_dev[r] positions (all in the pages): token i lies at position
+ * p = kv_len[r] - n_new + i.  It sees position j < kv_len[r] if j < prefix[r],
+ * or if (j <= p, unless causal is 0) and (there is no window, or j > p - window,
+ * or j < sinks); a token at a negative position sees nothing.
+ *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q.k_j) + slope (j - p)
+ * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse_dev
+ * (float32 [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row
+ * that sees nothing gets zeros and -infinity.  What masked positions and slots
+ * past a request's end hold does not matter.  Sums, maxima and weights are held
+ * in float32; the weights are rounded to fp16 for the product with V.
+ * table_dev, table_stride and width as in fkv_page_plan.  max_new and max_len
+ * bound n_new and kv_len of every request (they size the launch).  A request
+ * whose numbers do not hold together (cu not increasing or past n_tok, a length
+ * past max_new, max_len or the table) is skipped, its rows left as they are, a
+ * page id outside the pool gives the row unspecified values, and either sets
+ * FKV_ERANGE in the status word.  Rows of no request are left as they are.
+ * workspace_dev: fkv_page_attend_workspace(...) bytes for the same arguments,
+ * 256-byte aligned (NULL when that is 0), the caller's own until the call has
+ * run: calls that may overlap need one each.  The bytes depend on the sizes
+ * alone, so a captured call can be replayed with other lengths. */
+int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pages, int64_t n_tok, int n_q_heads,
+                                  int64_t n_req, int64_t max_new, int64_t max_len, const fkv_attend *opt);
+int fkv_page_attend(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *q, int64_t n_tok, int n_q_heads,
+                    const int32_t *cu_dev, const int32_t *kv_len_dev, int64_t n_req, const int32_t *table_dev,
+                    int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len, const fkv_attend *opt,
+                    const fkv_rows *out, float *lse_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* Rebuild positions [t0, min(t1, kv_len_dev[r])) of every request r < n_req
+ * into layer `layer`, sequence r of k_out and v_out (either may be NULL; views
+ * of n_req sequences and the pages' heads and dim that hold t1 positions):
+ * code x scale, rounded to nearest-even into the view's dtype.  Other
+ * positions are left as they are.  A page id outside the pool, or a length
+ * past the table, leaves its positions as they are and sets FKV_ERANGE. */
+int fkv_page_read(fkv_ctx *ctx, const fkv_pages *pages, const int32_t *kv_len_dev, int64_t n_req,
+                  const int32_t *table_dev, int64_t table_stride, int64_t width, int64_t t0, int64_t t1,
+                  int64_t layer, fkv_cache *k_out, fkv_cache *v_out, void *stream);
+
 /* ------------------------------------------------- appendable streams --- */
 
 /* A set of n_streams symbol streams of equal length, owned by the library on

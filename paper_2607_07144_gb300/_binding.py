@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(_PKG, "libfkv.so")
 
 OK, EINVAL, ERANGE, ENOMEM, ECUDA, ECORRUPT, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
 F32, F16, BF16 = 0, 1, 2
+E4M3, INT8 = 0, 1
+_FORMAT = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
 _DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _ERRNAME = {EINVAL: "EINVAL", ERANGE: "ERANGE", ENOMEM: "ENOMEM", ECUDA: "ECUDA",
             ECORRUPT: "ECORRUPT", ETIMEOUT: "ETIMEOUT"}
@@ -41,6 +43,25 @@ class _Cache(ctypes.Structure):
                 ("seq", ctypes.c_int64), ("stride_layer", ctypes.c_int64),
                 ("stride_batch", ctypes.c_int64), ("stride_head", ctypes.c_int64),
                 ("stride_pos", ctypes.c_int64)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("format", ctypes.c_int), ("n_heads", ctypes.c_int),
+                ("dim", ctypes.c_int), ("block", ctypes.c_int), ("n_blocks", ctypes.c_int64),
+                ("stride_block", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_pos", ctypes.c_int64),
+                ("scale_stride_block", ctypes.c_int64), ("scale_stride_head", ctypes.c_int64)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("stride_tok", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
+class _Attend(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("causal", ctypes.c_int),
+                ("window", ctypes.c_int64), ("sinks", ctypes.c_int64), ("slopes", ctypes.c_void_p),
+                ("prefix", ctypes.c_void_p)]
 
 
 # name -> (restype, argtypes)
@@ -77,6 +98,12 @@ SIGNATURES = {
     "fkv_decode_kv_static": (_I, [_P, _P, _I64, _I64, _P, _P, _I64, _P]),
     "fkv_read_kv": (_I, [_P, _P, _I64, _I64, _I64, _P, _I64, _P, _I, _P]),
     "fkv_cache_upload": (_I, [_P, _P, _P, _I64, _I64, _P]),
+    "fkv_page_plan": (_I, [_P, _P, _P, _I64, _P, _I64, _I64, _P, _I64, _P, _I, _P, _P, _P, _I64, _P, _P, _P]),
+    "fkv_page_write": (_I, [_P, _P, _P, _P, _P, _I64, _P]),
+    "fkv_page_attend_workspace": (_I64, [_P, _P, _I64, _I, _I64, _I64, _I64, _P]),
+    "fkv_page_attend": (_I, [_P, _P, _P, _I64, _I, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _P, _P, _P, _P, _I64,
+                             _P]),
+    "fkv_page_read": (_I, [_P, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _P, _P, _P]),
     "fkv_streams_create": (_I, [_P, _I64, _I64, ctypes.POINTER(_P)]),
     "fkv_streams_destroy": (_I, [_P]),
     "fkv_streams_reset": (_I, [_P]),
@@ -151,6 +178,58 @@ def cache_view(t: torch.Tensor, host: bool = False) -> _Cache:
         raise ValueError("cache must be a %s tensor [layers, batch, heads, seq, dim] with contiguous dim"
                          % ("CPU" if host else "CUDA"))
     return _Cache(t.data_ptr(), _DTYPE[t.dtype], t.shape[1], t.shape[3], st[0], st[1], st[2], st[3])
+
+
+def _rows_view(t: torch.Tensor, dim: int, what: str) -> _Rows:
+    """fkv_rows view of a CUDA tensor [tokens, heads, dim] (contiguous dim)."""
+    st = t.stride()
+    if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1) or not t.is_cuda or t.shape[2] != dim or t.dtype not in _DTYPE:
+        raise ValueError("%s must be a CUDA tensor [tokens, heads, %d] with contiguous dim" % (what, dim))
+    # the stride of a dimension of one is never used, but has to be a valid one
+    return _Rows(t.data_ptr(), _DTYPE[t.dtype], st[0] if t.shape[0] > 1 else dim, st[1] if t.shape[1] > 1 else dim)
+
+
+def _array(t: torch.Tensor, dtype, numel: int, what: str):
+    """Pointer of a contiguous CUDA array of at least `numel` elements."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError("%s must be a contiguous CUDA %s tensor of %d elements" % (what, dtype, numel))
+    return t.data_ptr()
+
+
+def _table(t: torch.Tensor, n_req: int):
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] < n_req or (t.shape[1] > 1 and
+                                                                                        t.stride(1) != 1):
+        raise ValueError("block_table must be a CUDA int32 tensor [requests, pages]")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1]), t.shape[1]
+
+
+class Pages:
+    """A pool of 8-bit K/V pages (fkv_pages): codes k and v [n_blocks, heads,
+    block, dim], torch.float8_e4m3fn or torch.int8, of the same strides (any,
+    with a contiguous dim: [n_blocks, block, heads, dim] permuted will do), and
+    float32 scales [n_blocks, heads].  The tensors stay the caller's."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if (k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1 or
+                k.dtype not in _FORMAT or not all(t.is_cuda for t in (k, v, k_scale, v_scale))):
+            raise ValueError("k and v must be CUDA float8_e4m3fn or int8 tensors [blocks, heads, block, dim] of one "
+                             "shape and strides, with contiguous dim")
+        if (k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:2] or
+                v_scale.shape != k.shape[:2] or k_scale.stride() != v_scale.stride()):
+            raise ValueError("k_scale and v_scale must be float32 tensors [blocks, heads] of the same strides")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_blocks, self.heads, self.block, self.dim = k.shape
+        st, ss = k.stride(), k_scale.stride()
+        self._c = _Pages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _FORMAT[k.dtype],
+                         self.heads, self.dim, self.block, self.n_blocks, st[0], st[1], st[2], ss[0], ss[1])
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_blocks: int, heads: int, block: int, dim: int, dtype=torch.float8_e4m3fn, device="cuda"):
+        shape = (n_blocks, heads, block, dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
+                   torch.empty(shape[:2], dtype=torch.float32, device=device),
+                   torch.empty(shape[:2], dtype=torch.float32, device=device))
 
 
 class Context:
@@ -442,6 +521,94 @@ class Context:
         self._check(lib().fkv_read_kv(self._h, _ptr(pts), pts.shape[0], n_rec, _rows(pts, 2), _ptr(req),
                                       req.shape[0], _ptr(out), _DTYPE[out.dtype], _stream(stream)))
         return out
+
+    # -- paged 8-bit cache
+    def page_plan(self, n_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free: torch.Tensor,
+                  taken: torch.Tensor, block: int, cu: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor,
+                  kv_len_out: torch.Tensor = None, taken_out: torch.Tensor = None, stream=None):
+        """Pages, slots and positions of n_new[r] more tokens of every request
+        (n_new[r] < 0: it ends) whose first kv_len[r] positions are in pages of
+        `block`.  int32 arrays, slots int64; block_table [requests, pages] and the
+        stack `free` are updated, kv_len and taken in place unless their outputs
+        are given.  slots and positions may have more rows than there are tokens:
+        -1 behind the last."""
+        n = n_new.numel()
+        i32 = torch.int32
+        tp, ts, tw = _table(block_table, n)
+        if slots.numel() != positions.numel():
+            raise ValueError("slots and positions must have the same length")
+        kv_len_out = kv_len if kv_len_out is None else kv_len_out
+        taken_out = taken if taken_out is None else taken_out
+        self._check(lib().fkv_page_plan(
+            self._h, _array(n_new, i32, n, "n_new"), _array(kv_len, i32, n, "kv_len"), n, tp, ts, tw,
+            _array(free, i32, 0, "free"), free.numel(), _array(taken, i32, 1, "taken"), int(block),
+            _array(cu, i32, n + 1, "cu"), _array(slots, torch.int64, 0, "slots"),
+            _array(positions, i32, 0, "positions"), slots.numel(), _array(kv_len_out, i32, n, "kv_len_out"),
+            _array(taken_out, i32, 1, "taken_out"), _stream(stream)))
+
+    def page_write(self, pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
+        """Quantise k and v [tokens, heads, dim] into the pages' slots (int64 [tokens], negative: skipped)."""
+        ck, cv = _rows_view(k, pages.dim, "k"), _rows_view(v, pages.dim, "v")
+        n = k.shape[0]
+        if v.shape != k.shape or k.shape[1] != pages.heads:
+            raise ValueError("k and v must be [tokens, %d, %d]" % (pages.heads, pages.dim))
+        self._check(lib().fkv_page_write(self._h, pages._ref, ctypes.byref(ck), ctypes.byref(cv),
+                                         _array(slots, torch.int64, n, "slots"), n, _stream(stream)))
+
+    def page_attend(self, pages: Pages, q: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor,
+                    block_table: torch.Tensor, max_new: int, max_len: int, out: torch.Tensor = None,
+                    lse: torch.Tensor = None, scale: float = None, causal: bool = True, window: int = 0,
+                    sinks: int = 0, softcap: float = 0.0, slopes: torch.Tensor = None, prefix: torch.Tensor = None,
+                    workspace: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Attention of q [tokens, query heads, dim] (rows cu[r] .. cu[r+1] the
+        last tokens of request r's kv_len[r] positions) over the pages; scale
+        defaults to dim ** -0.5.  max_new and max_len bound every request's new
+        tokens and positions.  lse: float32 [tokens, query heads] or None.  The
+        workspace is taken from torch's allocator unless given."""
+        n = kv_len.numel()
+        cq = _rows_view(q, pages.dim, "q")
+        T, Hq = q.shape[0], q.shape[1]
+        if out is None:
+            out = torch.empty((T, Hq, pages.dim), dtype=q.dtype, device=q.device)
+        co = _rows_view(out, pages.dim, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+        i32, f32 = torch.int32, torch.float32
+        tp, ts, tw = _table(block_table, n)
+        opt = _Attend(pages.dim ** -0.5 if scale is None else scale, softcap, int(bool(causal)), int(window),
+                      int(sinks), None if slopes is None else _array(slopes, f32, Hq, "slopes"),
+                      None if prefix is None else _array(prefix, i32, n, "prefix"))
+        L, o = lib(), ctypes.byref(opt)
+        need = L.fkv_page_attend_workspace(self._h, pages._ref, T, Hq, n, int(max_new), int(max_len), o)
+        if need and workspace is None:
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            else:
+                with torch.cuda.stream(stream):          # the allocator reuses it in that stream's order
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        self._check(L.fkv_page_attend(
+            self._h, pages._ref, ctypes.byref(cq), T, Hq, _array(cu, i32, n + 1, "cu"),
+            _array(kv_len, i32, n, "kv_len"), n, tp, ts, tw, int(max_new), int(max_len), o, ctypes.byref(co),
+            None if lse is None else _array(lse, f32, T * Hq, "lse"), ws[0], ws[1], _stream(stream)))
+        return out
+
+    def page_read(self, pages: Pages, kv_len: torch.Tensor, block_table: torch.Tensor, t0: int, t1: int,
+                  layer: int = 0, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
+        """Rebuild positions [t0, min(t1, kv_len[r])) of request r into sequence r
+        of a layer of the caches k_out and v_out [layers, batch, heads, seq, dim]."""
+        n = kv_len.numel()
+        tp, ts, tw = _table(block_table, n)
+        for x in (k_out, v_out):
+            if x is not None and (x.dim() != 5 or x.shape[2] != pages.heads or x.shape[4] != pages.dim or
+                                  not 0 <= layer < x.shape[0]):
+                raise ValueError("caches must be [layers, batch, %d, seq, %d] and hold the layer"
+                                 % (pages.heads, pages.dim))
+        ck = cache_view(k_out) if k_out is not None else None
+        cv = cache_view(v_out) if v_out is not None else None
+        self._check(lib().fkv_page_read(self._h, pages._ref, _array(kv_len, torch.int32, n, "kv_len"), n, tp, ts, tw,
+                                        int(t0), int(t1), int(layer), ctypes.byref(ck) if ck else None,
+                                        ctypes.byref(cv) if cv else None, _stream(stream)))
 
 
 class Streams:

@@ -1016,6 +1016,239 @@ int fkv_read_kv(fkv_ctx *ctx, const double *pts_dev, int64_t n_streams, int64_t 
     return FKV_OK;
 }
 
+namespace {
+
+bool misaligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+// Reasons to refuse a paged call, or null.
+const char *check_device(const fkv_ctx *ctx)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device ? nullptr : "the context's device is not current";
+}
+
+const char *check_pages(const fkv_pages *p)
+{
+    if (!p || !p->k || !p->v || !p->k_scale || !p->v_scale)
+        return "null page pool";
+    if (p->format != FKV_E4M3 && p->format != FKV_INT8)
+        return "unknown page format";
+    if (p->dim != 64 && p->dim != 128)
+        return "pages hold heads of 64 or 128 dimensions";
+    if (p->block < 16 || p->block > 1024 || p->block % 16)
+        return "page size must be a multiple of 16 up to 1024";
+    if (p->n_heads < 1 || p->n_heads > 65535 || p->n_blocks < 1 || p->n_blocks > INT32_MAX)
+        return "bad page pool size";
+    const int64_t s[3] = {p->stride_block, p->stride_head, p->stride_pos};
+    for (int64_t x : s)
+        if (x < 0 || x % 16 || x >= (int64_t(1) << 40))
+            return "bad page stride";
+    if (p->scale_stride_block < 0 || p->scale_stride_head < 0)
+        return "bad scale stride";
+    if (misaligned(p->k, 16) || misaligned(p->v, 16) || misaligned(p->k_scale, 4) || misaligned(p->v_scale, 4))
+        return "misaligned page pool";
+    return nullptr;
+}
+
+const char *check_rows(const fkv_rows *x)
+{
+    if (!x || !x->data)
+        return "null token rows";
+    if (x->dtype != FKV_F32 && x->dtype != FKV_F16 && x->dtype != FKV_BF16)
+        return "unknown element type";
+    const int64_t esz = x->dtype == FKV_F32 ? 4 : 2;
+    if (misaligned(x->data, 16) || x->stride_tok < 0 || x->stride_head < 0 || (x->stride_tok * esz) % 16 ||
+        (x->stride_head * esz) % 16)
+        return "token rows must lie on 16-byte boundaries";
+    return nullptr;
+}
+
+const char *check_table(int64_t n_req, const int32_t *table, int64_t table_stride, int64_t width)
+{
+    if (n_req < 0 || n_req > FKV_PAGE_MAX_REQ)
+        return "request count outside [0, 16384]";
+    if (n_req > 0 && (!table || misaligned(table, 4) || width < 1 || width > INT32_MAX || table_stride < width))
+        return "bad block table";
+    return nullptr;
+}
+
+const char *check_attend(const fkv_attend *o)
+{
+    if (!o)
+        return "null attention options";
+    if (!isfinite(o->scale) || !isfinite(o->softcap) || o->softcap < 0.0f)
+        return "bad scale or softcap";
+    if ((o->causal != 0 && o->causal != 1) || o->window < 0 || o->sinks < 0)
+        return "bad mask";
+    if (misaligned(o->slopes, 4) || misaligned(o->prefix, 4))
+        return "misaligned mask array";
+    return nullptr;
+}
+
+const char *check_attend_sizes(const fkv_pages *p, int64_t n_tok, int n_q_heads, int64_t n_req, int64_t max_new,
+                               int64_t max_len)
+{
+    if (n_tok < 0 || n_tok > INT32_MAX || n_req < 0 || n_req > FKV_PAGE_MAX_REQ || max_new < 0 ||
+        max_new > FKV_PAGE_MAX_LEN || max_len < 0 || max_len > FKV_PAGE_MAX_LEN)
+        return "size out of range";
+    if (n_q_heads < p->n_heads || n_q_heads % p->n_heads || n_q_heads > 65535)
+        return "query heads must be a multiple of the pages' heads";
+    return nullptr;
+}
+
+// The pool as [page][head][position][dim] bytes, in boxes of 16 positions of
+// one head whose rows are swizzled by their own width.
+bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *map)
+{
+    const cuuint64_t D = static_cast<cuuint64_t>(p->dim);
+    const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(p->block), static_cast<cuuint64_t>(p->n_heads),
+                                static_cast<cuuint64_t>(p->n_blocks)};
+    // the stride of a dimension of one is never used, but has to be a valid one
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(p->stride_pos),
+                                   p->n_heads > 1 ? static_cast<cuuint64_t>(p->stride_head) : D,
+                                   p->n_blocks > 1 ? static_cast<cuuint64_t>(p->stride_block) : D};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), 16, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               p->dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+int fkv_page_plan(fkv_ctx *ctx, const int32_t *n_new_dev, const int32_t *kv_len_dev, int64_t n_req,
+                  int32_t *table_dev, int64_t table_stride, int64_t width, int32_t *free_dev, int64_t n_free,
+                  const int32_t *taken_dev, int block, int32_t *cu_dev, int64_t *slots_dev, int32_t *pos_dev,
+                  int64_t rows, int32_t *kv_len_out_dev, int32_t *taken_out_dev, void *stream)
+{
+    if (!ctx)
+        return FKV_EINVAL;
+    if (const char *why = check_table(n_req, table_dev, table_stride, width))
+        return fail(ctx, FKV_EINVAL, why);
+    if (block < 16 || block > 1024 || block % 16)
+        return fail(ctx, FKV_EINVAL, "page size must be a multiple of 16 up to 1024");
+    if (rows < 0 || rows > INT32_MAX || n_free < 0 || n_free > INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "size out of range");
+    const void *need[] = {taken_dev, cu_dev, taken_out_dev, n_new_dev, kv_len_dev, kv_len_out_dev};
+    for (int i = 0; i < 6; ++i)
+        if ((!need[i] && (i < 3 || n_req > 0)) || misaligned(need[i], 4))
+            return fail(ctx, FKV_EINVAL, "null or misaligned array");
+    if ((n_free > 0 && !free_dev) || misaligned(free_dev, 4) || (rows > 0 && (!slots_dev || !pos_dev)) ||
+        misaligned(slots_dev, 8) || misaligned(pos_dev, 4))
+        return fail(ctx, FKV_EINVAL, "null or misaligned array");
+    if (const char *why = check_device(ctx))
+        return fail(ctx, FKV_EINVAL, why);
+    CK(launch_page_plan(ctx, n_new_dev, kv_len_dev, n_req, table_dev, table_stride, width, free_dev, n_free,
+                        taken_dev, block, cu_dev, slots_dev, pos_dev, rows, kv_len_out_dev, taken_out_dev,
+                        as_stream(stream)),
+       "page plan launch");
+    return FKV_OK;
+}
+
+int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, const fkv_rows *v,
+                   const int64_t *slots_dev, int64_t n_tok, void *stream)
+{
+    if (!ctx)
+        return FKV_EINVAL;
+    if (n_tok < 0 || n_tok > INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "size out of range");
+    if (const char *why = check_pages(pages))
+        return fail(ctx, FKV_EINVAL, why);
+    if (n_tok == 0)
+        return FKV_OK;
+    if (const char *why = check_rows(k))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_rows(v))
+        return fail(ctx, FKV_EINVAL, why);
+    if (k->dtype != v->dtype)
+        return fail(ctx, FKV_EINVAL, "K and V types differ");
+    if (!slots_dev || misaligned(slots_dev, 8))
+        return fail(ctx, FKV_EINVAL, "bad slot map");
+    if (const char *why = check_device(ctx))
+        return fail(ctx, FKV_EINVAL, why);
+    CK(launch_page_write(ctx, pages, k, v, slots_dev, n_tok, as_stream(stream)), "page write launch");
+    return FKV_OK;
+}
+
+int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pages, int64_t n_tok, int n_q_heads,
+                                  int64_t n_req, int64_t max_new, int64_t max_len, const fkv_attend *opt)
+{
+    if (!ctx || check_pages(pages) || check_attend(opt) ||
+        check_attend_sizes(pages, n_tok, n_q_heads, n_req, max_new, max_len))
+        return 0;
+    return page_attend_workspace(ctx, pages, n_req, n_q_heads, n_tok, max_new, max_len, opt);
+}
+
+int fkv_page_attend(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *q, int64_t n_tok, int n_q_heads,
+                    const int32_t *cu_dev, const int32_t *kv_len_dev, int64_t n_req, const int32_t *table_dev,
+                    int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len, const fkv_attend *opt,
+                    const fkv_rows *out, float *lse_dev, void *workspace_dev, int64_t workspace_bytes, void *stream)
+{
+    if (!ctx)
+        return FKV_EINVAL;
+    if (const char *why = check_pages(pages))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_attend(opt))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_attend_sizes(pages, n_tok, n_q_heads, n_req, max_new, max_len))
+        return fail(ctx, FKV_EINVAL, why);
+    if (n_tok == 0 || n_req == 0 || max_new == 0)
+        return FKV_OK;
+    if (const char *why = check_table(n_req, table_dev, table_stride, width))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_rows(q))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_rows(out))
+        return fail(ctx, FKV_EINVAL, why);
+    if (q->dtype == FKV_F32 || out->dtype != q->dtype)
+        return fail(ctx, FKV_EINVAL, "queries are float16 or bfloat16, and outputs of their type");
+    if (!cu_dev || !kv_len_dev || misaligned(cu_dev, 4) || misaligned(kv_len_dev, 4) || misaligned(lse_dev, 4))
+        return fail(ctx, FKV_EINVAL, "null or misaligned array");
+    const int64_t need = page_attend_workspace(ctx, pages, n_req, n_q_heads, n_tok, max_new, max_len, opt);
+    if (need > 0 && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 256)))
+        return fail(ctx, FKV_EINVAL, "workspace missing, too small or misaligned");
+    if (const char *why = check_device(ctx))
+        return fail(ctx, FKV_EINVAL, why);
+    EncodeTiledFn enc = encode_tiled();
+    CUtensorMap mk, mv;
+    if (!enc || !page_map(enc, pages, pages->k, &mk) || !page_map(enc, pages, pages->v, &mv))
+        return fail(ctx, FKV_ECUDA, "cuTensorMapEncodeTiled failed");
+    CK(launch_page_attend(ctx, pages, q, n_tok, n_q_heads, cu_dev, kv_len_dev, n_req, table_dev, table_stride, width,
+                          max_new, max_len, opt, out, lse_dev, need ? workspace_dev : nullptr, mk, mv,
+                          as_stream(stream)),
+       "page attention launch");
+    return FKV_OK;
+}
+
+int fkv_page_read(fkv_ctx *ctx, const fkv_pages *pages, const int32_t *kv_len_dev, int64_t n_req,
+                  const int32_t *table_dev, int64_t table_stride, int64_t width, int64_t t0, int64_t t1,
+                  int64_t layer, fkv_cache *k_out, fkv_cache *v_out, void *stream)
+{
+    if (!ctx)
+        return FKV_EINVAL;
+    if (const char *why = check_pages(pages))
+        return fail(ctx, FKV_EINVAL, why);
+    if (const char *why = check_table(n_req, table_dev, table_stride, width))
+        return fail(ctx, FKV_EINVAL, why);
+    if (t0 < 0 || t1 < t0 || t1 > FKV_PAGE_MAX_LEN || layer < 0 || (!k_out && !v_out))
+        return fail(ctx, FKV_EINVAL, "bad position range, layer or outputs");
+    const fkv_cache *outs[2] = {k_out, v_out};
+    for (const fkv_cache *c : outs)
+        if (c && (!check_cache(ctx, c) || t1 > c->seq || n_req > c->batch))
+            return fail(ctx, FKV_EINVAL, "bad output cache view");
+    if (k_out && v_out && k_out->dtype != v_out->dtype)
+        return fail(ctx, FKV_EINVAL, "K and V types differ");
+    if (n_req == 0 || t1 == t0)
+        return FKV_OK;
+    if (!kv_len_dev || misaligned(kv_len_dev, 4))
+        return fail(ctx, FKV_EINVAL, "null or misaligned array");
+    if (const char *why = check_device(ctx))
+        return fail(ctx, FKV_EINVAL, why);
+    CK(launch_page_read(ctx, pages, kv_len_dev, n_req, table_dev, table_stride, width, t0, t1, layer, k_out, v_out,
+                        as_stream(stream)),
+       "page read launch");
+    return FKV_OK;
+}
+
 int fkv_streams_create(fkv_ctx *ctx, int64_t n_streams, int64_t capacity_symbols, fkv_streams **out)
 {
     if (!ctx || !out)
