@@ -86,10 +86,6 @@ struct RowMask {
         from = a.window ? p - a.window + 1 : 0;
         pre = on ? q.pre : 0;
     }
-    __device__ __forceinline__ bool sees(const AttendArgs &a, int j) const
-    {
-        return (j < hi && (j >= from || j < a.sinks)) || j < pre;
-    }
 };
 
 // Whether every row at positions pa .. pb sees all of [k0, k1).
@@ -97,12 +93,6 @@ __device__ __forceinline__ bool all_see(const AttendArgs &a, const Request &q, i
 {
     return pa >= 0 && k1 <= q.len &&
            (k1 <= q.pre || ((!a.causal || k1 - 1 <= pa) && (!a.window || k0 > pb - a.window || k1 <= a.sinks)));
-}
-
-__device__ __forceinline__ float cap_tanh(float s, float cap)
-{
-    // tanh x = 1 - 2 / (1 + e^2x): an absolute error of a few 2^-24
-    return cap * (1.0f - __fdividef(2.0f, 1.0f + ex2(s * (2.0f * kLog2e) / cap)));
 }
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
@@ -148,29 +138,39 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 // ------------------------------------------------------------------ steps --
-// Up to 16 rows (the query heads of a KV head, times the new tokens) against a
+// Up to 8 NT rows (the query heads of a KV head, times the new tokens) against a
 // share of the keys: bound by reading the pages.  A warp owns every fourth
 // group of 32 keys, loads it by TMA into a ring of its own and keeps its own
 // running maximum, sum and output, so nothing but the last merge joins the
-// warps.  Codes go from shared memory to the tensor cores' fragments through
-// registers (the contraction may run over the head dimension in any order, so a
-// lane takes 16 consecutive bytes of a key as four steps' operands; a value
-// row's 16 bytes are 16 columns of the result).  mma.sync, as 16 rows are an
-// eighth of what tcgen05 multiplies at least: its rate is four times what the
-// bytes leave time for.
+// warps.  Keys are the rows of the first product and dimensions those of the
+// second, so the pages' codes are both times the operand of 16 rows and the few
+// query rows the one of 8 columns:
+//     S[key][row] = K Q^T,    O^T[dim][row] = V^T P^T,
+// with a transpose of 8 x 8 weights between them.  Codes become fragments in
+// registers: the contraction may run over the dimensions in any order, so a lane
+// takes 16 consecutive bytes of a key as four steps' operands, and 16 bytes of a
+// value row as 16 rows of the result.  mma.sync, as these shapes are a sixteenth
+// of what tcgen05 multiplies at least; its rate leaves the bytes the bound.
 template <int D> struct StepShape {
     static constexpr int stages = D == 128 ? 3 : 6;
     static constexpr int smem = 4 * stages * 64 * D + 1024;
 };
 
-template <int D, int FMT, typename T>
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+template <int D, int FMT, typename T, int NT>
 __global__ void __launch_bounds__(128, 2)
     k_attend_step(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
 {
-    constexpr int ST = StepShape<D>::stages, NS = D / 64, UNIT = 16 * D, STAGE = 4 * UNIT, NO = D / 8;
+    constexpr int ST = StepShape<D>::stages, NS = D / 64, UNIT = 16 * D, STAGE = 4 * UNIT, MO = D / 16, R = 8 * NT;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
-    __shared__ float ml[4][2][16];
+    __shared__ float ml[4][2][R];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
 
@@ -183,13 +183,13 @@ __global__ void __launch_bounds__(128, 2)
             atomicOr(a.status, FKV_ST_RANGE);
         return;
     }
-    const int rows = q.nq * a.G, row0 = rt * 16;
+    const int rows = q.nq * a.G, row0 = rt * R;
     if (row0 >= rows)
         return;
-    const int ia = static_cast<int>(a.gdiv.div(row0)), ib = static_cast<int>(a.gdiv.div(min(row0 + 15, rows - 1)));
+    const int ia = static_cast<int>(a.gdiv.div(row0)), ib = static_cast<int>(a.gdiv.div(min(row0 + R - 1, rows - 1)));
     const int pa = q.p0 + ia, pb = q.p0 + ib;
     const Tiles tiles(a, q, pa, pb);
-    const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk);
+    const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk), n_it = max(0, i1 - i0);
 
     const uint32_t ring = sbase + warp * ST * STAGE, bar0 = smem_u32(bars) + warp * ST * 8;
     if (lane == 0) {
@@ -199,62 +199,65 @@ __global__ void __launch_bounds__(128, 2)
     }
     __syncwarp();
 
-    // page ids and scales of the next 16 iterations' units, two a lane pair
-    int id_c = -1, id_n = -1;
-    float ks_c = 0.0f, vs_c = 1.0f, ks_n = 0.0f, vs_n = 1.0f;
+    // A lane looks up one of the 32 units (16 keys) of the next 16 iterations:
+    // its page, place in it, and what its scales give the scores.
+    struct Unit {
+        int id, off;
+        float mul, lvs, ivs;
+    };
+    const float mul0 = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : a.scale * kLog2e;
     bool bad = false;
-    auto fetch = [&](int batch, int &id, float &ks, float &vs) {
+    auto fetch = [&](int batch) {
+        Unit u = {0, 0, 0.0f, 0.0f, 0.0f};
         const int it = i0 + batch * 16 + (lane >> 1);
-        id = -1, ks = 0.0f, vs = 1.0f;
         if (it < i1) {
             const int key = tiles.at(it) * kTile + warp * 32 + (lane & 1) * 16;
             if (key < tiles.lim) {
-                id = a.table[r * a.table_stride + a.div.div(key)];
-                if (id < 0 || id >= a.n_blocks) {
+                const int j = static_cast<int>(a.div.div(key));
+                u.off = key - j * a.block;
+                u.id = a.table[r * a.table_stride + j];
+                if (u.id < 0 || u.id >= a.n_blocks) {
                     bad = true;
-                    id = 0;
+                    u.id = 0;
                 }
-                ks = a.ks[id * a.scb + h * a.sch];
-                vs = a.vs[id * a.scb + h * a.sch];
+                u.mul = a.ks[u.id * a.scb + h * a.sch] * mul0;
+                const float vs = fmaxf(a.vs[u.id * a.scb + h * a.sch], FKV_PAGE_MIN_SCALE);
+                u.lvs = lg2(vs);
+                u.ivs = __frcp_rn(vs);
             }
         }
+        return u;
     };
-    const int n_it = max(0, i1 - i0);
-    fetch(0, id_c, ks_c, vs_c);
-    fetch(1, id_n, ks_n, vs_n);
-    // units of iteration `it` that hold keys to look at
-    auto units = [&](int it) {
-        const int key = tiles.at(i0 + it) * kTile + warp * 32;
-        return key >= tiles.lim ? 0 : (key + 16 >= tiles.lim ? 1 : 2);
-    };
+    Unit cur = fetch(0), nxt = fetch(1);
+    // keys of iteration `it` from the warp's first one on that are looked at
+    auto first_key = [&](int it) { return tiles.at(i0 + it) * kTile + warp * 32; };
     auto issue = [&](int it, int batch) {
-        const int nu = units(it);
-        const int from = (it & 15) * 2;
-        const int ids[2] = {__shfl_sync(~0u, (it >> 4) == batch ? id_c : id_n, from),
-                            __shfl_sync(~0u, (it >> 4) == batch ? id_c : id_n, from + 1)};
-        if (lane == 0 && nu) {
-            const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * STAGE;
-            mbar_arrive_expect_tx(bar, nu * 2 * UNIT);
-            const int key = tiles.at(i0 + it) * kTile + warp * 32;
-            for (int u = 0; u < nu; ++u) {
-                const int k0 = key + 16 * u, off = k0 - static_cast<int>(a.div.div(k0)) * a.block;
-                tma_load_4d(dst + u * UNIT, &mk, 0, off, h, ids[u], bar);
-                tma_load_4d(dst + (2 + u) * UNIT, &mv, 0, off, h, ids[u], bar);
-            }
+        const int nu = min(2, (tiles.lim - first_key(it) + 15) >> 4);
+        const int from = (it & 15) * 2 + (lane & 1);
+        const bool now = (it >> 4) == batch;
+        const int id = __shfl_sync(~0u, now ? cur.id : nxt.id, from), off = __shfl_sync(~0u, now ? cur.off : nxt.off, from);
+        const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * STAGE;
+        if (nu > 0) {
+            if (lane == 0)
+                mbar_arrive_expect_tx(bar, nu * 2 * UNIT);
+            __syncwarp();
+            // lanes 0 .. 3: units 0 and 1 of K, then of V
+            if (lane < 4 && (lane & 1) < nu)
+                tma_load_4d(dst + lane * UNIT, lane < 2 ? &mk : &mv, 0, off, h, id, bar);
         }
         __syncwarp();
     };
     for (int it = 0; it < min(ST - 1, n_it); ++it)
         issue(it, 0);
 
-    // the query rows as fp16 fragments: lane t's steps take 16 consecutive
-    // dimensions (two such pieces for D = 128) of rows gid and gid + 8
-    uint32_t qf[NS * 4][4];
-    float rowmul[2], slope[2];
-    int prow[2];
+    // the query rows as fp16 operands: lane t's steps take 16 consecutive
+    // dimensions (two such pieces for D = 128) of row gid
+    uint32_t qf[NT][NS * 4][2];
+    float rowmul[NT][2], slope[NT][2];
+    int prow[NT][2], hi[NT][2], from[NT][2], pre[NT][2];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int row = row0 + gid + 8 * half;
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + 8 * n + gid;
         const bool live = row < rows;
         const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
         const T *src = static_cast<const T *>(a.q) + (q.tok0 + i) * a.q_tok + (h * a.G + u) * a.q_head;
@@ -275,262 +278,331 @@ __global__ void __launch_bounds__(128, 2)
                 }
             }
         }
-        amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
         // bf16 rows: 2^(14 - exponent), so that fp16 holds them (see above)
         float up = 1.0f, down = 1.0f;
-        if (sizeof(T) == 2 && !(std::is_same<T, __half>::value) && amax > 0.0f) {
+        if (!std::is_same<T, __half>::value) {
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
             const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
             up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
             down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
         }
-        rowmul[half] = a.scale * down;
-        prow[half] = q.p0 + i;
-        slope[half] = a.slopes && live ? a.slopes[h * a.G + u] * kLog2e : 0.0f;
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                qf[s * 4 + kk][half] = pack_half(x[s][4 * kk] * up, x[s][4 * kk + 1] * up);
-                qf[s * 4 + kk][2 + half] = pack_half(x[s][4 * kk + 2] * up, x[s][4 * kk + 3] * up);
+                qf[n][s * 4 + kk][0] = pack_half(x[s][4 * kk] * up, x[s][4 * kk + 1] * up);
+                qf[n][s * 4 + kk][1] = pack_half(x[s][4 * kk + 2] * up, x[s][4 * kk + 3] * up);
             }
-    }
-    const RowMask mask0(a, q, prow[0], row0 + gid < rows), mask1(a, q, prow[1], row0 + gid + 8 < rows);
-
-    float o[NO][4];
+        // a lane's scores are of rows 2t and 2t + 1
 #pragma unroll
-    for (int n = 0; n < NO; ++n)
-        o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        for (int c = 0; c < 2; ++c) {
+            rowmul[n][c] = __shfl_sync(~0u, down, (2 * t + c) * 4);
+            const int rw = row0 + 8 * n + 2 * t + c;
+            const bool on = rw < rows;
+            const int ii = on ? static_cast<int>(a.gdiv.div(rw)) : 0;
+            prow[n][c] = q.p0 + ii;
+            slope[n][c] = a.slopes && on ? a.slopes[h * a.G + rw - ii * a.G] * kLog2e : 0.0f;
+            const RowMask m(a, q, prow[n][c], on);
+            hi[n][c] = m.hi, from[n][c] = m.from, pre[n][c] = m.pre;
+        }
+    }
+
+    float o[NT][MO][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int d = 0; d < MO; ++d)
+            o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.0f;
+    }
 
     int batch = 0;
     for (int it = 0; it < n_it; ++it) {
         if ((it >> 4) != batch) {
             batch = it >> 4;
-            id_c = id_n, ks_c = ks_n, vs_c = vs_n;
-            fetch(batch + 1, id_n, ks_n, vs_n);
+            cur = nxt;
+            nxt = fetch(batch + 1);
         }
         if (it + ST - 1 < n_it)
             issue(it + ST - 1, batch);
-        const int nu = units(it);
-        if (!nu)
+        const int key = first_key(it), nu = min(2, (tiles.lim - key + 15) >> 4);
+        if (nu <= 0)
             break;                      // the last tile's end
-        if (!mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status))
+        if (!mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status)) {
+            // give the loads in flight a while to land before the memory is used again
+            for (int k = it + 1; k < min(n_it, it + ST); ++k)
+                mbar_wait(bar0 + 8 * (k % ST), (k / ST) & 1, a.status, 2000000);
             break;
+        }
         const uint32_t kt = ring + (it % ST) * STAGE, vt = kt + 2 * UNIT;
-        const int key = tiles.at(i0 + it) * kTile + warp * 32;
 
-        float sc[4][4];
+        float sc[2][NT][4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
-            if ((n >> 1) < nu) {
-                const int kr = 8 * n + gid;
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                sc[u][n][0] = sc[u][n][1] = sc[u][n][2] = sc[u][n][3] = 0.0f;
+            if (u < nu) {
+                const int kr = 16 * u + gid;            // and kr + 8
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const int c = NS * t + s;
-                    const uint32_t at = D == 128 ? kr * 128 + ((c ^ (kr & 7)) << 4) : kr * 64 + ((c ^ ((kr >> 1) & 3)) << 4);
-                    const uint4 w = lds128(kt + at);
-                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+                    uint4 w0, w1;
+                    if (D == 128) {
+                        const uint32_t at = kt + kr * 128 + ((c ^ (kr & 7)) << 4);
+                        w0 = lds128(at), w1 = lds128(at + 1024);
+                    } else {
+                        const uint32_t at = kt + kr * 64 + ((c ^ ((kr >> 1) & 3)) << 4);
+                        w0 = lds128(at), w1 = lds128(at + 512);
+                    }
+                    const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        uint32_t b0, b1;
-                        codes4_half<FMT>(ww[kk], b0, b1);
-                        mma16816(sc[n], qf[s * 4 + kk], b0, b1);
+                        uint32_t f[4];
+                        codes4_half<FMT>(x0[kk], f[0], f[2]);
+                        codes4_half<FMT>(x1[kk], f[1], f[3]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma16816(sc[u][n], f, qf[n][s * 4 + kk][0], qf[n][s * 4 + kk][1]);
                     }
                 }
             }
         }
 
-        // scores, masks and the value scales' logarithms
-        const bool full = all_see(a, q, pa, pb, key, key + 16 * nu);
-        float mx[2] = {-INFINITY, -INFINITY}, ivs[2];
+        // scores in base 2 with the value scales' logarithms
+        float mx[NT][2], ivs[2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            mx[n][0] = mx[n][1] = -INFINITY;
+        const bool full = nu == 2 && all_see(a, q, pa, pb, key, key + 32);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const float ks = __shfl_sync(~0u, ks_c, (it & 15) * 2 + u);
-            const float vs = fmaxf(__shfl_sync(~0u, vs_c, (it & 15) * 2 + u), FKV_PAGE_MIN_SCALE);
-            const float lvs = lg2(vs);
-            ivs[u] = __frcp_rn(vs);
+            const int at = (it & 15) * 2 + u;
+            const float mul = __shfl_sync(~0u, cur.mul, at), lvs = __shfl_sync(~0u, cur.lvs, at);
+            ivs[u] = __shfl_sync(~0u, cur.ivs, at);
 #pragma unroll
-            for (int n = 2 * u; n < 2 * u + 2; ++n)
+            for (int n = 0; n < NT; ++n) {
+                float x[4];
+                if (a.softcap > 0.0f) {
+                    const float cap = a.softcap * kLog2e;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // tanh y = 1 - 2 / (1 + e^2y): an absolute error of a few 2^-24
+                        const float z = ex2(sc[u][n][e] * (mul * rowmul[n][e & 1]));
+                        x[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + z), cap + lvs);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = fmaf(sc[u][n][e], mul * rowmul[n][e & 1], lvs);
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = fmaf(slope[n][e & 1],
+                                    static_cast<float>(key + 16 * u + gid + 8 * (e >> 1) - prow[n][e & 1]), x[e]);
+                }
+                if (!full) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = key + 16 * u + gid + 8 * (e >> 1), c = e & 1;
+                        const bool see = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c];
+                        x[e] = see && u < nu ? x[e] : -INFINITY;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int half = e >> 1, j = key + 8 * n + 2 * t + (e & 1);
-                    float x = sc[n][e] * (ks * rowmul[half]);
-                    if (a.softcap > 0.0f)
-                        x = cap_tanh(x, a.softcap);
-                    x = x * kLog2e;
-                    if (a.slopes)
-                        x += slope[half] * static_cast<float>(j - prow[half]);
-                    x += lvs;
-                    if (u >= nu || (!full && !(half ? mask1 : mask0).sees(a, j)))
-                        x = -INFINITY;
-                    sc[n][e] = x;
-                    mx[half] = fmaxf(mx[half], x);
+                    sc[u][n][e] = x[e];
+                    mx[n][e & 1] = fmaxf(mx[n][e & 1], x[e]);
                 }
+            }
         }
-        float alpha[2], mref[2];
+        bool grown = false;
+        float mref[NT][2], alpha[NT][2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            mx[half] = fmaxf(mx[half], __shfl_xor_sync(~0u, mx[half], 1));
-            mx[half] = fmaxf(mx[half], __shfl_xor_sync(~0u, mx[half], 2));
-            const float mn = fmaxf(m[half], mx[half]);
-            mref[half] = mn == -INFINITY ? 0.0f : mn;
-            alpha[half] = ex2(m[half] - mref[half]);
-            m[half] = mn;
-            l[half] *= alpha[half];
-        }
-        if (__any_sync(~0u, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NO; ++n) {
-                o[n][0] *= alpha[0], o[n][1] *= alpha[0];
-                o[n][2] *= alpha[1], o[n][3] *= alpha[1];
+            for (int c = 0; c < 2; ++c) {
+                float x = mx[n][c];
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                const float mn = fmaxf(m[n][c], x);
+                grown |= mn != m[n][c];
+                mref[n][c] = (mn == -INFINITY ? 0.0f : mn) - kPBits;
+                alpha[n][c] = ex2(m[n][c] - kPBits - mref[n][c]);
+                m[n][c] = mn;
+            }
+        if (__any_sync(~0u, grown)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                l[n][0] *= alpha[n][0], l[n][1] *= alpha[n][1];
+#pragma unroll
+                for (int d = 0; d < MO; ++d) {
+                    o[n][d][0] *= alpha[n][0], o[n][d][1] *= alpha[n][1];
+                    o[n][d][2] *= alpha[n][0], o[n][d][3] *= alpha[n][1];
+                }
             }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (u >= nu)
                 break;
-            uint32_t pf[4];
+            uint32_t pf[NT][2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int n = 2 * u + x;
+            for (int n = 0; n < NT; ++n) {
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    p[e] = ex2(sc[n][e] - mref[e >> 1] + kPBits);
-                l[0] += (p[0] + p[1]) * ivs[u];
-                l[1] += (p[2] + p[3]) * ivs[u];
-                pf[2 * x] = pack_half(p[0], p[1]);
-                pf[2 * x + 1] = pack_half(p[2], p[3]);
+                    p[e] = ex2(sc[u][n][e] - mref[n][e & 1]);
+                l[n][0] = fmaf(p[0] + p[2], ivs[u], l[n][0]);
+                l[n][1] = fmaf(p[1] + p[3], ivs[u], l[n][1]);
+                pf[n][0] = transpose8(pack_half(p[0], p[1]));
+                pf[n][1] = transpose8(pack_half(p[2], p[3]));
             }
-            // value rows 2t, 2t + 1, 2t + 8, 2t + 9 of the unit; those behind the
-            // request's end hold any bytes, NaN codes among them: read as zeros
-            const int vr[4] = {2 * t, 2 * t + 1, 2 * t + 8, 2 * t + 9};
-            const bool tail = key + 16 * u + 16 > q.len;
+            // value rows 2t, 2t + 1, 2t + 8, 2t + 9 of the unit, D / 8 dimensions
+            // each; rows behind the request's end hold any bytes, NaN codes among
+            // them: read as zeros
             uint32_t w[4][D / 32];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int row = 16 * u + vr[x];
+                const int row = 16 * u + 2 * t + (x & 1) + 8 * (x >> 1);
                 if (D == 128) {
                     const uint4 v = lds128(vt + row * 128 + ((gid ^ (row & 7)) << 4));
                     w[x][0] = v.x, w[x][1] = v.y;
-                    if (D == 128)
-                        w[x][D / 32 - 2] = v.z, w[x][D / 32 - 1] = v.w;
+                    w[x][D / 32 - 2] = v.z, w[x][D / 32 - 1] = v.w;
                 } else {
                     const uint2 v = lds64(vt + row * 64 + ((((gid >> 1) ^ ((row >> 1) & 3)) << 4) | (gid & 1) << 3));
                     w[x][0] = v.x, w[x][1] = v.y;
                 }
-                if (tail && key + row >= q.len) {
+            }
+            if (key + 16 * u + 16 > q.len) {
 #pragma unroll
-                    for (int k = 0; k < D / 32; ++k)
-                        w[x][k] = 0;
+                for (int x = 0; x < 4; ++x)
+                    if (key + 16 * u + 2 * t + (x & 1) + 8 * (x >> 1) >= q.len) {
+#pragma unroll
+                        for (int k = 0; k < D / 32; ++k)
+                            w[x][k] = 0;
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // rows gid and gid + 8 of the tile: dimensions 4k + 2e and the next
+                    const int sel = e ? 0x7362 : 0x5140;
+                    uint32_t f[4];
+                    codes4_half<FMT>(__byte_perm(w[0][k], w[1][k], sel), f[0], f[1]);
+                    codes4_half<FMT>(__byte_perm(w[2][k], w[3][k], sel), f[2], f[3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        mma16816(o[n][2 * k + e], f, pf[n][0], pf[n][1]);
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-                uint32_t b0[4], b1[4];
-                codes4_half<FMT>(__byte_perm(w[0][k], w[1][k], 0x5140), b0[0], b0[1]);
-                codes4_half<FMT>(__byte_perm(w[0][k], w[1][k], 0x7362), b0[2], b0[3]);
-                codes4_half<FMT>(__byte_perm(w[2][k], w[3][k], 0x5140), b1[0], b1[1]);
-                codes4_half<FMT>(__byte_perm(w[2][k], w[3][k], 0x7362), b1[2], b1[3]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    mma16816(o[4 * k + c], pf, b0[c], b1[c]);
-            }
         }
         __syncwarp();                  // the stage is free: the next issue may overwrite it
     }
 
     // merge the warps: a row's largest m, then sums and outputs against it
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        l[half] += __shfl_xor_sync(~0u, l[half], 1);
-        l[half] += __shfl_xor_sync(~0u, l[half], 2);
-        if (t == 0) {
-            ml[warp][0][gid + 8 * half] = m[half];
-            ml[warp][1][gid + 8 * half] = l[half];
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float x = l[n][c];
+            x += __shfl_xor_sync(~0u, x, 4);
+            x += __shfl_xor_sync(~0u, x, 8);
+            x += __shfl_xor_sync(~0u, x, 16);
+            if (gid == 0) {
+                ml[warp][0][8 * n + 2 * t + c] = m[n][c];
+                ml[warp][1][8 * n + 2 * t + c] = x;
+            }
         }
-    }
+    if (bad)
+        atomicOr(a.status, FKV_ST_RANGE);
     __syncthreads();                   // every ring is read: its memory takes the outputs
     float *mo = reinterpret_cast<float *>(raw + (sbase - smem_u32(raw)));
     constexpr int LD = D + 4;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        float *dst = mo + (warp * 16 + gid + 8 * half) * LD;
-        // n-tile n, column c of the fragments is dimension c * (D / 8) + n
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NO; ++n) {
-            dst[2 * t * NO + n] = o[n][2 * half];
-            dst[(2 * t + 1) * NO + n] = o[n][2 * half + 1];
+        for (int c = 0; c < 2; ++c) {
+            float *dst = mo + (warp * R + 8 * n + 2 * t + c) * LD + gid * (D / 8);
+#pragma unroll
+            for (int d = 0; d < MO; ++d)
+                *reinterpret_cast<float2 *>(dst + 2 * d) = make_float2(o[n][d][c], o[n][d][2 + c]);
         }
-    }
     __syncthreads();
-    if (bad)
-        atomicOr(a.status, FKV_ST_RANGE);
-    // thread: row tid / 8, dimensions (tid % 8) * D / 8 on
-    {
-        const int row = tid >> 3, c = (tid & 7) * (D / 8);
-        if (row0 + row < rows) {
-            float mt = -INFINITY;
+    constexpr int TPR = 128 / R, E = D / TPR;      // threads a row, dimensions a thread
+    const int row = tid / TPR, c = (tid % TPR) * E;
+    if (row0 + row >= rows)
+        return;
+    float mt = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                mt = fmaxf(mt, ml[w][0][row]);
-            const float mref = mt == -INFINITY ? 0.0f : mt;
-            float lt = 0.0f, f[4];
+    for (int w = 0; w < 4; ++w)
+        mt = fmaxf(mt, ml[w][0][row]);
+    const float mref = mt == -INFINITY ? 0.0f : mt;
+    float lt = 0.0f, f[4];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                f[w] = ex2(ml[w][0][row] - mref);
-                lt += ml[w][1][row] * f[w];
-            }
-            const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
-            const float lse2 = lt > 0.0f ? mref - kPBits + log2f(lt) : -INFINITY;
-            const int i = static_cast<int>(a.gdiv.div(row0 + row)), u = row0 + row - i * a.G;
-            const int64_t tok = q.tok0 + i, head = h * a.G + u, flat = tok * (a.H * a.G) + head;
-            float x[D / 8];
+    for (int w = 0; w < 4; ++w) {
+        f[w] = ex2(ml[w][0][row] - mref);
+        lt += ml[w][1][row] * f[w];
+    }
+    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
+    const float lse2 = lt > 0.0f ? mref - kPBits + log2f(lt) : -INFINITY;
+    const int i = static_cast<int>(a.gdiv.div(row0 + row));
+    const int64_t tok = q.tok0 + i, head = h * a.G + row0 + row - i * a.G, flat = tok * (a.H * a.G) + head;
+    float x[E];
 #pragma unroll
-            for (int k = 0; k < D / 8; ++k) {
-                x[k] = 0.0f;
+    for (int k = 0; k < E; ++k)
+        x[k] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    x[k] += mo[(w * 16 + row) * LD + c + k] * f[w];
-                x[k] *= inv;
-            }
-            if (a.splits == 1) {
-                T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + c;
-                T y[D / 8];
+    for (int w = 0; w < 4; ++w)
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k)
-                    y[k] = from_float<T>(x[k]);
-#pragma unroll
-                for (int k = 0; k < D / 64; ++k)
-                    reinterpret_cast<uint4 *>(dst)[k] = reinterpret_cast<const uint4 *>(y)[k];
-                if (a.lse && c == 0)
-                    a.lse[flat] = lse2 / kLog2e;
-            } else {
-                const int64_t at = split * a.T * (a.H * a.G) + flat;
-                float *dst = a.ws_o + at * D + c;
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k)
-                    reinterpret_cast<float4 *>(dst)[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-                if (c == 0)
-                    a.ws_lse[at] = lse2;
-            }
+        for (int k = 0; k < E; k += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(mo + (w * R + row) * LD + c + k);
+            x[k] = fmaf(v.x, f[w], x[k]), x[k + 1] = fmaf(v.y, f[w], x[k + 1]);
+            x[k + 2] = fmaf(v.z, f[w], x[k + 2]), x[k + 3] = fmaf(v.w, f[w], x[k + 3]);
         }
+    if (a.splits == 1) {
+        T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + c;
+#pragma unroll
+        for (int k = 0; k < E; k += 4) {
+            T y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                y[e] = from_float<T>(x[k + e] * inv);
+            *reinterpret_cast<uint2 *>(dst + k) = *reinterpret_cast<const uint2 *>(y);
+        }
+        if (a.lse && c == 0)
+            a.lse[flat] = lse2 / kLog2e;
+    } else {
+        const int64_t at = split * a.T * (a.H * a.G) + flat;
+#pragma unroll
+        for (int k = 0; k < E; k += 4)
+            *reinterpret_cast<float4 *>(a.ws_o + at * D + c + k) =
+                make_float4(x[k] * inv, x[k + 1] * inv, x[k + 2] * inv, x[k + 3] * inv);
+        if (c == 0)
+            a.ws_lse[at] = lse2;
     }
 }
 
 // --------------------------------------------------------------- combine --
-// A warp per query row: the splits' outputs weighted by 2^(lse - largest).
+// A block per query row: the splits' outputs weighted by 2^(lse - largest).
+// Its four warps take every fourth split (two at a time for 64 dimensions), so
+// that the loads of a row are in flight together: latency bounds the call.
+constexpr int kMaxSplits = 64;
+
 template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_combine(const AttendArgs a)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t Hq = a.H * a.G, row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    // rows behind the last request's are no one's, and rows of a request that
+    constexpr int L = D / 4, P = 128 / L;          // lanes a row of 4 dimensions each, splits at a time
+    __shared__ float w_s[kMaxSplits];
+    __shared__ float4 part[P][L];
+    const int tid = threadIdx.x, lane = tid & 31, g = tid / L, c = tid % L;
+    const int64_t Hq = a.H * a.G, row = blockIdx.x, tok = row / Hq, head = row - tok * Hq;
+    // rows behind the last request's are no one's, and those of a request that
     // was skipped have no partial results: both are left as they are
-    if (row >= a.T * Hq)
-        return;
-    const int64_t tok = row / Hq, head = row - tok * Hq;
     int lo = 0, hi = a.n_req;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -542,40 +614,46 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
     Request q;
     if (!q.load(a, lo) || tok < q.tok0 || tok >= q.tok0 + q.nq)
         return;
-    float mx = -INFINITY;
-    for (int s = lane; s < a.splits; s += 32)
-        mx = fmaxf(mx, a.ws_lse[s * a.T * Hq + row]);
+    if (tid < kMaxSplits)
+        w_s[tid] = tid < a.splits ? a.ws_lse[tid * a.T * Hq + row] : -INFINITY;
+    __syncthreads();
+    float mx = fmaxf(w_s[lane], w_s[lane + 32]);
 #pragma unroll
     for (int o = 16; o; o >>= 1)
         mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
     const float mref = mx == -INFINITY ? 0.0f : mx;
-    constexpr int E = D / 32;
-    float x[E], sum = 0.0f;
+    float sum = ex2(w_s[lane] - mref) + ex2(w_s[lane + 32] - mref);
 #pragma unroll
-    for (int k = 0; k < E; ++k)
-        x[k] = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const int64_t at = s * a.T * Hq + row;
-        const float w = ex2(a.ws_lse[at] - mref);
-        if (w == 0.0f)
-            continue;
-        sum += w;
+    for (int o = 16; o; o >>= 1)
+        sum += __shfl_xor_sync(~0u, sum, o);
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int s = g; s < a.splits; s += P) {
+        const float w = ex2(w_s[s] - mref);
+        const float4 v = *reinterpret_cast<const float4 *>(a.ws_o + (s * a.T * Hq + row) * D + 4 * c);
+        // a split without a visible key has weight zero (its output is zeros)
+        x.x = fmaf(w, v.x, x.x), x.y = fmaf(w, v.y, x.y), x.z = fmaf(w, v.z, x.z), x.w = fmaf(w, v.w, x.w);
+    }
+    part[g][c] = x;
+    __syncthreads();
+    if (g != 0)
+        return;
 #pragma unroll
-        for (int k = 0; k < E; ++k)
-            x[k] += w * a.ws_o[at * D + lane * E + k];
+    for (int k = 1; k < P; ++k) {
+        const float4 v = part[k][c];
+        x.x += v.x, x.y += v.y, x.z += v.z, x.w += v.w;
     }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + lane * E;
-#pragma unroll
-    for (int k = 0; k < E; ++k)
-        dst[k] = from_float<T>(x[k] * inv);
-    if (a.lse && lane == 0)
+    const T y[4] = {from_float<T>(x.x * inv), from_float<T>(x.y * inv), from_float<T>(x.z * inv), from_float<T>(x.w * inv)};
+    *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + 4 * c) =
+        *reinterpret_cast<const uint2 *>(y);
+    if (a.lse && c == 0)
         a.lse[row] = sum > 0.0f ? (mref + log2f(sum)) / kLog2e : -INFINITY;
 }
 
 // ------------------------------------------------------------------ launch --
 struct Plan {
-    int row_tiles, splits, chunk;
+    int nt, row_tiles, splits, chunk;
 };
 
 // How many shares the keys are split into.  A block's time is its keys plus a
@@ -585,7 +663,8 @@ struct Plan {
 Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t max_new, int64_t max_len, int window)
 {
     Plan p;
-    p.row_tiles = static_cast<int>((max_new * G + 15) / 16);
+    p.nt = max_new * G <= 8 ? 1 : 2;
+    p.row_tiles = static_cast<int>((max_new * G + 8 * p.nt - 1) / (8 * p.nt));
     const int64_t blocks = n_req * H * p.row_tiles, slots = ctx->sms * 2;
     int64_t span = max_len;
     if (window && window + max_new + 2 * kTile < span)
@@ -594,7 +673,7 @@ Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t max_new, i
     double best = 0.0;
     p.splits = 1;
     p.chunk = tiles > 0 ? tiles : 1;
-    for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
         const int chunk = (tiles + s - 1) / s;
         const int64_t waves = (blocks * s + slots - 1) / slots;
         const double cost = waves * (chunk * kTile + 384.0) + (s > 1 ? 512.0 + 8.0 * s : 0.0);
@@ -613,28 +692,35 @@ int window_of(const fkv_attend *opt)
     return opt->window >= FKV_PAGE_MAX_LEN ? 0 : static_cast<int>(opt->window);
 }
 
-template <int D, int FMT, typename T>
-cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+template <int D, int FMT, typename T, int NT>
+cudaError_t step_rows(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
-    const void *fn = reinterpret_cast<const void *>(k_attend_step<D, FMT, T>);
-    cudaError_t e = kernel_use(ctx, fn, 128, StepShape<D>::smem, nullptr);
+    const void *fn = reinterpret_cast<const void *>(k_attend_step<D, FMT, T, NT>);
+    const cudaError_t e = kernel_use(ctx, fn, 128, StepShape<D>::smem, nullptr);
     if (e != cudaSuccess)
         return e;
     const dim3 grid(static_cast<unsigned>(a.n_req * a.row_tiles * a.splits), a.H);
-    k_attend_step<D, FMT, T><<<grid, 128, StepShape<D>::smem, st>>>(a, mk, mv);
-    e = cudaGetLastError();
+    k_attend_step<D, FMT, T, NT><<<grid, 128, StepShape<D>::smem, st>>>(a, mk, mv);
+    return cudaGetLastError();
+}
+
+template <int D, int FMT, typename T>
+cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUtensorMap &mk, const CUtensorMap &mv,
+                    cudaStream_t st)
+{
+    const cudaError_t e = nt == 1 ? step_rows<D, FMT, T, 1>(ctx, a, mk, mv, st) : step_rows<D, FMT, T, 2>(ctx, a, mk, mv, st);
     if (e != cudaSuccess || a.splits == 1)
         return e;
-    k_attend_combine<D, T><<<static_cast<unsigned>((a.T * a.H * a.G + 3) / 4), 128, 0, st>>>(a);
+    k_attend_combine<D, T><<<static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st>>>(a);
     return cudaGetLastError();
 }
 
 template <int D, int FMT>
-cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, const CUtensorMap &mk, const CUtensorMap &mv,
+cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, const CUtensorMap &mk, const CUtensorMap &mv,
                     cudaStream_t st)
 {
-    return dtype == FKV_F16 ? step_as<D, FMT, __half>(ctx, a, mk, mv, st)
-                            : step_as<D, FMT, __nv_bfloat16>(ctx, a, mk, mv, st);
+    return dtype == FKV_F16 ? step_as<D, FMT, __half>(ctx, a, nt, mk, mv, st)
+                            : step_as<D, FMT, __nv_bfloat16>(ctx, a, nt, mk, mv, st);
 }
 
 }  // namespace
@@ -675,6 +761,6 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_pages *pg, const fk
     a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * T * n_q_heads * pg->dim : nullptr;
     const bool i8 = pg->format == FKV_INT8;
     if (pg->dim == 64)
-        return i8 ? step_dt<64, FKV_INT8>(ctx, a, q->dtype, mk, mv, st) : step_dt<64, FKV_E4M3>(ctx, a, q->dtype, mk, mv, st);
-    return i8 ? step_dt<128, FKV_INT8>(ctx, a, q->dtype, mk, mv, st) : step_dt<128, FKV_E4M3>(ctx, a, q->dtype, mk, mv, st);
+        return i8 ? step_dt<64, FKV_INT8>(ctx, a, q->dtype, p.nt, mk, mv, st) : step_dt<64, FKV_E4M3>(ctx, a, q->dtype, p.nt, mk, mv, st);
+    return i8 ? step_dt<128, FKV_INT8>(ctx, a, q->dtype, p.nt, mk, mv, st) : step_dt<128, FKV_E4M3>(ctx, a, q->dtype, p.nt, mk, mv, st);
 }
