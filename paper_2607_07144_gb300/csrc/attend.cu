@@ -12,88 +12,15 @@
 // the second product is sum P_j c'_j with P rounded to fp16 (relative 2^-11, an
 // eighth of a bf16 result's own rounding; P spans 2^8 .. 2^-24, so nothing above
 // 2^-32 of the largest weight is lost), and the sum of the weights is
-// sum P_j / vs, from the unrounded P_j, in fp32.  So pages of any scales mix in
+// sum P_j / vs, from the unrounded P_j, in fp32 (as vref / vs of a first page's vref).  So pages of any scales mix in
 // one accumulator without a rounding of V.
-#include <type_traits>
-
-#include "paged.cuh"
+#include "attend.cuh"
 
 using namespace fkvd;
 
 namespace {
 
-constexpr int kTile = 128;         // keys a tile: the unit of the visible range and of the splits
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kPBits = 8.0f;     // P is at most 2^8
-
-struct AttendArgs {
-    const void *q;
-    void *out;
-    float *lse;
-    const int *cu, *kv_len, *table;
-    const float *ks, *vs, *slopes;
-    const int *prefix;
-    float *ws_o, *ws_lse;
-    unsigned *status;
-    int64_t q_tok, q_head, o_tok, o_head, table_stride, scb, sch, n_blocks, T;
-    int n_req, H, G, block, width, max_new, max_len, window, sinks, causal;
-    int splits, chunk, row_tiles;
-    float scale, softcap;
-    FastDiv div, gdiv;
-};
-
-// What one request's rows see.
-struct Request {
-    int tok0, nq, len, pre, p0;
-    // false: the request's numbers do not hold together; it is reported and skipped
-    __device__ __forceinline__ bool load(const AttendArgs &a, int r)
-    {
-        const int c0 = a.cu[r], c1 = a.cu[r + 1];
-        len = a.kv_len[r];
-        tok0 = c0;
-        nq = c1 - c0;
-        pre = a.prefix ? min(max(a.prefix[r], 0), len) : 0;
-        p0 = len - nq;
-        return c0 >= 0 && c1 >= c0 && c1 <= a.T && nq <= a.max_new && len >= 0 && len <= a.max_len &&
-               static_cast<int64_t>(len) <= static_cast<int64_t>(a.width) * a.block;
-    }
-};
-
-// The tiles that rows at positions pa .. pb see: those of the first `lo`
-// positions (prefix, sinks), then those from the window's beginning on.
-struct Tiles {
-    int n_lo, hi0, n, lim;
-    __device__ __forceinline__ Tiles(const AttendArgs &a, const Request &q, int pa, int pb)
-    {
-        const int end = pb < 0 ? 0 : (a.causal ? min(q.len, pb + 1) : q.len);
-        const int lo = pb < 0 ? 0 : max(q.pre, a.window ? min(a.sinks, end) : 0);
-        const int begin = a.window ? max(0, pa - a.window + 1) : 0;
-        lim = max(end, lo);
-        n_lo = (lo + kTile - 1) / kTile;
-        hi0 = max(n_lo, begin / kTile);
-        n = n_lo + max(0, (end + kTile - 1) / kTile - hi0);
-    }
-    __device__ __forceinline__ int at(int i) const { return i < n_lo ? i : hi0 + i - n_lo; }
-};
-
-// The keys that one row sees: j < hi and (j >= from or j < sinks), or j < pre.
-struct RowMask {
-    int hi, from, pre;
-    __device__ __forceinline__ RowMask(const AttendArgs &a, const Request &q, int p, bool live)
-    {
-        const bool on = live && p >= 0;
-        hi = on ? (a.causal ? min(q.len, p + 1) : q.len) : 0;
-        from = a.window ? p - a.window + 1 : 0;
-        pre = on ? q.pre : 0;
-    }
-};
-
-// Whether every row at positions pa .. pb sees all of [k0, k1).
-__device__ __forceinline__ bool all_see(const AttendArgs &a, const Request &q, int pa, int pb, int k0, int k1)
-{
-    return pa >= 0 && k1 <= q.len &&
-           (k1 <= q.pre || ((!a.causal || k1 - 1 <= pa) && (!a.window || k0 > pb - a.window || k1 <= a.sinks)));
-}
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
 {
@@ -125,17 +52,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
-
-__device__ __forceinline__ uint32_t pack_half(float a, float b)
-{
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
-// Finished (or partial) row: o, lse to the outputs or to the workspace.
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 // ------------------------------------------------------------------ steps --
 // Up to 8 NT rows (the query heads of a KV head, times the new tokens) against a
@@ -207,6 +123,12 @@ __global__ void __launch_bounds__(128, 2)
     };
     const float mul0 = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : a.scale * kLog2e;
     bool bad = false;
+    float vref = 1.0f;
+    if (n_it > 0) {
+        const int64_t id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
+        if (id >= 0 && id < a.n_blocks)
+            vref = value_scale(a.vs[id * a.scb + h * a.sch]);
+    }
     auto fetch = [&](int batch) {
         Unit u = {0, 0, 0.0f, 0.0f, 0.0f};
         const int it = i0 + batch * 16 + (lane >> 1);
@@ -221,9 +143,9 @@ __global__ void __launch_bounds__(128, 2)
                     u.id = 0;
                 }
                 u.mul = a.ks[u.id * a.scb + h * a.sch] * mul0;
-                const float vs = fmaxf(a.vs[u.id * a.scb + h * a.sch], FKV_PAGE_MIN_SCALE);
+                const float vs = value_scale(a.vs[u.id * a.scb + h * a.sch]);
                 u.lvs = lg2(vs);
-                u.ivs = __frcp_rn(vs);
+                u.ivs = share_of(vref, vs);
             }
         }
         return u;
@@ -549,8 +471,8 @@ __global__ void __launch_bounds__(128, 2)
         f[w] = ex2(ml[w][0][row] - mref);
         lt += ml[w][1][row] * f[w];
     }
-    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
-    const float lse2 = lt > 0.0f ? mref - kPBits + log2f(lt) : -INFINITY;
+    const float inv = lt > 0.0f ? vref / lt : 0.0f;
+    const float lse2 = lt > 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
     const int i = static_cast<int>(a.gdiv.div(row0 + row));
     const int64_t tok = q.tok0 + i, head = h * a.G + row0 + row - i * a.G, flat = tok * (a.H * a.G) + head;
     float x[E];
@@ -656,16 +578,20 @@ struct Plan {
     int nt, row_tiles, splits, chunk;
 };
 
-// How many shares the keys are split into.  A block's time is its keys plus a
-// fixed part (its launch, the first loads' latency and the merge: about that
-// of 384 keys); the blocks run in waves of `slots`.  The split with the least
-// waves x time wins; joining the partial results costs another part a split.
-Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t max_new, int64_t max_len, int window)
+// Which kernel serves the call, and how many shares the keys are split into.
+// Up to 16 rows a KV head (nt = 1 or 2 columns of 8) go to the step kernel, more
+// to the tensor-memory one (nt = 0).  A block's time is its keys plus a fixed
+// part (its launch, the first loads' latency and its end: about that of 384
+// keys); the blocks run in waves of `slots`.  The split with the least waves x
+// time wins; joining the partial results costs another part a split.
+Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t T, int64_t max_new, int64_t max_len, int window)
 {
     Plan p;
-    p.nt = max_new * G <= 8 ? 1 : 2;
-    p.row_tiles = static_cast<int>((max_new * G + 8 * p.nt - 1) / (8 * p.nt));
-    const int64_t blocks = n_req * H * p.row_tiles, slots = ctx->sms * 2;
+    const int64_t most = max_new * G;
+    p.nt = most <= 8 ? 1 : most <= 16 ? 2 : 0;
+    const int per = p.nt ? 8 * p.nt : prompt_rows();
+    p.row_tiles = static_cast<int>((most + per - 1) / per);
+    const int64_t blocks = n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 2 : ctx->sms;
     int64_t span = max_len;
     if (window && window + max_new + 2 * kTile < span)
         span = window + max_new + 2 * kTile;
@@ -673,7 +599,9 @@ Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t max_new, i
     double best = 0.0;
     p.splits = 1;
     p.chunk = tiles > 0 ? tiles : 1;
-    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+    // partial results are indexed by (split, row) of a grid dimension
+    const int most_splits = T * H * G < (int64_t(1) << 30) ? kMaxSplits : 1;
+    for (int s = 1; s <= most_splits && s <= tiles; ++s) {
         const int chunk = (tiles + s - 1) / s;
         const int64_t waves = (blocks * s + slots - 1) / slots;
         const double cost = waves * (chunk * kTile + 384.0) + (s > 1 ? 512.0 + 8.0 * s : 0.0);
@@ -708,7 +636,9 @@ template <int D, int FMT, typename T>
 cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUtensorMap &mk, const CUtensorMap &mv,
                     cudaStream_t st)
 {
-    const cudaError_t e = nt == 1 ? step_rows<D, FMT, T, 1>(ctx, a, mk, mv, st) : step_rows<D, FMT, T, 2>(ctx, a, mk, mv, st);
+    const cudaError_t e = nt == 0   ? launch_attend_prompt(ctx, a, D, FMT, std::is_same<T, __half>::value ? FKV_F16 : FKV_BF16, st)
+                          : nt == 1 ? step_rows<D, FMT, T, 1>(ctx, a, mk, mv, st)
+                                    : step_rows<D, FMT, T, 2>(ctx, a, mk, mv, st);
     if (e != cudaSuccess || a.splits == 1)
         return e;
     k_attend_combine<D, T><<<static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st>>>(a);
@@ -728,7 +658,7 @@ cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, 
 int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pg, int64_t n_req, int n_q_heads, int64_t T,
                               int64_t max_new, int64_t max_len, const fkv_attend *opt)
 {
-    const Plan p = plan_of(ctx, n_req, pg->n_heads, n_q_heads / pg->n_heads, max_new, max_len, window_of(opt));
+    const Plan p = plan_of(ctx, n_req, pg->n_heads, n_q_heads / pg->n_heads, T, max_new, max_len, window_of(opt));
     if (p.splits == 1)
         return 0;
     return (static_cast<int64_t>(p.splits) * T * n_q_heads * (pg->dim + 1) * 4 + 255) / 256 * 256;
@@ -741,7 +671,8 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_pages *pg, const fk
                                const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
     AttendArgs a;
-    a.q = q->data, a.out = out->data, a.lse = lse;
+    a.q = q->data, a.out = out->data, a.lse = lse, a.pool_k = pg->k, a.pool_v = pg->v;
+    a.sb = pg->stride_block, a.sh = pg->stride_head, a.st = pg->stride_pos;
     a.cu = cu, a.kv_len = kv_len, a.table = table;
     a.ks = pg->k_scale, a.vs = pg->v_scale, a.slopes = opt->slopes, a.prefix = opt->prefix;
     a.status = ctx->d_status;
@@ -755,7 +686,7 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_pages *pg, const fk
     a.causal = opt->causal;
     a.scale = opt->scale, a.softcap = opt->softcap;
     a.div = FastDiv::make(pg->block), a.gdiv = FastDiv::make(a.G);
-    const Plan p = plan_of(ctx, n_req, a.H, a.G, max_new, max_len, a.window);
+    const Plan p = plan_of(ctx, n_req, a.H, a.G, T, max_new, max_len, a.window);
     a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk;
     a.ws_o = static_cast<float *>(ws);
     a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * T * n_q_heads * pg->dim : nullptr;

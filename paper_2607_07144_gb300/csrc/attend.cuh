@@ -1,0 +1,105 @@
+// What the two attention kernels over the paged cache share (attend.cu,
+// attend_prompt.cu): arguments, the visible range of a request's rows, and how
+// the value scales enter.
+#pragma once
+
+#include <type_traits>
+
+#include "paged.cuh"
+
+namespace fkvd {
+
+constexpr int kTile = 128;         // keys a tile: the unit of the visible range and of the splits
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttendArgs {
+    const void *q, *pool_k, *pool_v;
+    void *out;
+    float *lse;
+    const int *cu, *kv_len, *table;
+    const float *ks, *vs, *slopes;
+    const int *prefix;
+    float *ws_o, *ws_lse;
+    unsigned *status;
+    int64_t q_tok, q_head, o_tok, o_head, table_stride, sb, sh, st, scb, sch, n_blocks, T;
+    int n_req, H, G, block, width, max_new, max_len, window, sinks, causal;
+    int splits, chunk, row_tiles;
+    float scale, softcap;
+    FastDiv div, gdiv;
+};
+
+// What one request's rows see.
+struct Request {
+    int tok0, nq, len, pre, p0;
+    // false: the request's numbers do not hold together; it is reported and skipped
+    __device__ __forceinline__ bool load(const AttendArgs &a, int r)
+    {
+        const int c0 = a.cu[r], c1 = a.cu[r + 1];
+        len = a.kv_len[r];
+        tok0 = c0;
+        nq = c1 - c0;
+        pre = a.prefix ? min(max(a.prefix[r], 0), len) : 0;
+        p0 = len - nq;
+        return c0 >= 0 && c1 >= c0 && c1 <= a.T && nq <= a.max_new && len >= 0 && len <= a.max_len &&
+               static_cast<int64_t>(len) <= static_cast<int64_t>(a.width) * a.block;
+    }
+};
+
+// The tiles that rows at positions pa .. pb see: those of the first `lo`
+// positions (prefix, sinks), then those from the window's beginning on.
+struct Tiles {
+    int n_lo, hi0, n, lim;
+    __device__ __forceinline__ Tiles(const AttendArgs &a, const Request &q, int pa, int pb)
+    {
+        const int end = pb < 0 ? 0 : (a.causal ? min(q.len, pb + 1) : q.len);
+        const int lo = pb < 0 ? 0 : max(q.pre, a.window ? min(a.sinks, end) : 0);
+        const int begin = a.window ? max(0, pa - a.window + 1) : 0;
+        lim = max(end, lo);
+        n_lo = (lo + kTile - 1) / kTile;
+        hi0 = max(n_lo, begin / kTile);
+        n = n_lo + max(0, (end + kTile - 1) / kTile - hi0);
+    }
+    __device__ __forceinline__ int at(int i) const { return i < n_lo ? i : hi0 + i - n_lo; }
+};
+
+// The keys that one row sees: j < hi and (j >= from or j < sinks), or j < pre.
+struct RowMask {
+    int hi, from, pre;
+    __device__ __forceinline__ RowMask(const AttendArgs &a, const Request &q, int p, bool live)
+    {
+        const bool on = live && p >= 0;
+        hi = on ? (a.causal ? min(q.len, p + 1) : q.len) : 0;
+        from = a.window ? p - a.window + 1 : 0;
+        pre = on ? q.pre : 0;
+    }
+};
+
+// Whether every row at positions pa .. pb sees all of [k0, k1).
+__device__ __forceinline__ bool all_see(const AttendArgs &a, const Request &q, int pa, int pb, int k0, int k1)
+{
+    return pa >= 0 && k1 <= q.len &&
+           (k1 <= q.pre || ((!a.causal || k1 - 1 <= pa) && (!a.window || k0 > pb - a.window || k1 <= a.sinks)));
+}
+
+__device__ __forceinline__ uint32_t pack_half(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// The sum of weights counts each page's share as vref / vs, vref being the
+// scale of the share's first page, so that it stays in range whatever the
+// scales' size; the ratio is held below 2^100.
+__device__ __forceinline__ float value_scale(float vs) { return fmaxf(vs, FKV_PAGE_MIN_SCALE); }
+__device__ __forceinline__ float share_of(float vref, float vs) { return fminf(__fdividef(vref, vs), 0x1p100f); }
+
+}  // namespace fkvd
+
+// Rows of 256 (attend_prompt.cu): a.row_tiles, splits and chunk as for the steps.
+int prompt_rows();
+cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const fkvd::AttendArgs &a, int dim, int format, int dtype,
+                                 cudaStream_t st);

@@ -1,0 +1,614 @@
+// Attention over the paged 8-bit cache for many rows a KV head (attend.cu has the
+// mathematics): both products on the 5th-generation tensor cores.
+//
+// A block takes 256 rows of one KV head (its query heads, times new tokens) and
+// walks its share of the keys in tiles of 128.  Four warps load the pages' codes
+// and write them as fp16 tiles to shared memory (codes are exact in fp16; each
+// tile is converted once for 256 rows), one thread issues the tcgen05.mma, and
+// two groups of four warps, a thread a row, do the softmax of 128 rows each: the
+// one's products run while the other exponentiates.  S = Q K^T and then P (fp16,
+// in place of S) and O stay in tensor memory: P is the second product's first
+// operand from there, and V is read as it lies, [key][dimension], by a transposed
+// descriptor.  A row's reference maximum moves only when it would grow by more
+// than 2^8 (P then spans 2^14 .. 2^-24), so O is rarely rescaled.
+#include "attend.cuh"
+
+using namespace fkvd;
+
+namespace {
+
+constexpr int kRows = 256, kThreads = 512;
+constexpr float kPBits = 6.0f, kSlack = 8.0f;    // P is at most 2^(kPBits + kSlack)
+
+template <int D> struct PromptShape {
+    static constexpr int half = 128 * 128;                   // 64 dimensions of 128 rows in fp16
+    static constexpr int tile = half * (D / 64);             // 128 rows
+    static constexpr int off_q = 0, off_k = 2 * tile, off_v = 4 * tile, smem = 6 * tile + 1024;
+};
+
+enum { K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_EMPTY = 6, SC_FULL = 8, S_FULL = 12, P_FULL = 14, O_FULL = 16, Q_FULL = 18,
+       DRAIN = 19, N_BARS = 20 };
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+                 "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+// The largest of each 16 of 64 columns (tcgen05.ld.red).
+__device__ __forceinline__ void tmem_max4x16(uint32_t taddr, float *m)
+{
+    float x[64];
+    asm volatile(
+        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, %64, [%68+0];\n\t"
+        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, %65, [%68+16];\n\t"
+        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, %66, [%68+32];\n\t"
+        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, %67, [%68+48];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31]), "=f"(x[32]), "=f"(x[33]), "=f"(x[34]), "=f"(x[35]), "=f"(x[36]), "=f"(x[37]), "=f"(x[38]), "=f"(x[39]), "=f"(x[40]), "=f"(x[41]), "=f"(x[42]), "=f"(x[43]), "=f"(x[44]), "=f"(x[45]), "=f"(x[46]), "=f"(x[47]), "=f"(x[48]), "=f"(x[49]), "=f"(x[50]), "=f"(x[51]), "=f"(x[52]), "=f"(x[53]), "=f"(x[54]), "=f"(x[55]), "=f"(x[56]), "=f"(x[57]), "=f"(x[58]), "=f"(x[59]), "=f"(x[60]), "=f"(x[61]), "=f"(x[62]), "=f"(x[63]), "=f"(m[0]), "=f"(m[1]), "=f"(m[2]), "=f"(m[3])
+        : "r"(taddr));
+}
+
+// Waits for this thread's loads; the registers pass through, so that nothing
+// reads them earlier.
+__device__ __forceinline__ void tmem_wait_ld(float *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// D[tmem] (+)= A[tmem] B[smem], A fp16 pairs in 32-bit columns.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// A [keys][dimensions] tile as the second operand with its dimensions outermost:
+// 64 dimensions a 128-byte swizzled row, 8 keys a 1024-byte atom; the next 64
+// dimensions `half` bytes on.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t half)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(half >> 4) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// Two fp32 fused multiply-adds, or additions, in one instruction.
+__device__ __forceinline__ void fma2(float &x, float &y, float a, float b, float m, float c)
+{
+    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %4};\n\tmov.b64 u, {%5, %5};\n\t"
+        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "f"(a), "f"(b), "f"(m), "f"(c));
+}
+__device__ __forceinline__ void add2(float &x, float &y, float a, float b)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\t"
+        "add.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+
+// One group's softmax of a tile: see k_attend_prompt.
+struct Row {
+    float m, l;                 // reference maximum and the sum of weights
+    float down;                 // what a score is multiplied by for the row's power of two
+    int p, hi, from, pre;       // position and visible keys
+    float slope;
+};
+
+template <int D, int FMT, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs a)
+{
+    using S = PromptShape<D>;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[N_BARS];
+    __shared__ float4 scales[4][8];           // of the last four tiles' units of 16 keys: multiplier, log2 vs, vref / vs
+    __shared__ uint32_t tmem_slot;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
+    const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
+    auto bar = [&](int i) { return smem_u32(bars) + 8 * i; };
+
+    // the last rows of a causal prompt see the most keys: they go first
+    int x = blockIdx.x;
+    const int h = x % a.H;
+    x /= a.H;
+    const int split = x % a.splits;
+    x /= a.splits;
+    const int r = x % a.n_req, rt = a.row_tiles - 1 - x / a.n_req;
+    Request q;
+    if (!q.load(a, r)) {
+        if (tid == 0)
+            atomicOr(a.status, FKV_ST_RANGE);
+        return;
+    }
+    const int rows = q.nq * a.G, row0 = rt * kRows;
+    if (row0 >= rows)
+        return;
+    const int groups = rows - row0 > 128 ? 2 : 1;
+    const int pa = q.p0 + static_cast<int>(a.gdiv.div(row0));
+    const int pb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + kRows, rows) - 1));
+    const Tiles tiles(a, q, pa, pb);
+    const int i0 = split * a.chunk, n_it = max(0, min(tiles.n, i0 + a.chunk) - i0);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(K_FULL + i), 4);
+            mbar_init(bar(K_EMPTY + i), 1);
+            mbar_init(bar(V_FULL + i), 4);
+            mbar_init(bar(V_EMPTY + i), 1);
+            mbar_init(bar(S_FULL + i), 1);
+            mbar_init(bar(P_FULL + i), 128);
+            mbar_init(bar(O_FULL + i), 1);
+        }
+        for (int i = 0; i < 4; ++i)
+            mbar_init(bar(SC_FULL + i), 4);
+        mbar_init(bar(Q_FULL), 128 * groups);
+        mbar_init(bar(DRAIN), 1);
+        fence_mbar_init();
+    }
+    if (warp == 12)
+        tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    // the scale of the share's first page (share_of)
+    float vref = 1.0f;
+    if (n_it > 0) {
+        const int64_t id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
+        if (id >= 0 && id < a.n_blocks)
+            vref = value_scale(a.vs[id * a.scb + h * a.sch]);
+    }
+
+    if (group == 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        // ---------------------------------------------------- MMA issuer
+        if (warp == 12 && lane == 0 && n_it > 0) {
+            constexpr uint32_t id_s = idesc_f16_f32(128, 128), id_o = idesc_f16_f32(128, D) | 1u << 16;
+            const uint32_t s_t[2] = {tmem, tmem + 128}, o_t[2] = {tmem + 256, tmem + 384};
+            auto scores = [&](int w, int j) {
+                const uint32_t qb = sbase + S::off_q + w * S::tile, kb = sbase + S::off_k + (j & 1) * S::tile;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (k >> 2) * S::half + (k & 3) * 32;
+                    umma_f16(s_t[w], sdesc_sw128(qb + off), sdesc_sw128(kb + off), id_s, k > 0);
+                }
+                umma_commit(bar(S_FULL + w));
+            };
+            bool ok = mbar_wait(bar(Q_FULL), 0, a.status) && mbar_wait(bar(K_FULL), 0, a.status);
+            if (ok) {
+                tc_fence_after();
+                for (int w = 0; w < groups; ++w)
+                    scores(w, 0);
+                umma_commit(bar(K_EMPTY));
+            }
+            for (int j = 0; j < n_it && ok; ++j) {
+                for (int w = 0; w < groups && ok; ++w) {
+                    ok = mbar_wait(bar(P_FULL + w), j & 1, a.status) &&
+                         (w > 0 || mbar_wait(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
+                    if (!ok)
+                        break;
+                    tc_fence_after();
+                    const uint32_t vb = sbase + S::off_v + (j & 1) * S::tile;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        umma_f16_ts(o_t[w], s_t[w] + 8 * k, sdesc_mn_sw128(vb + k * 2048, S::half), id_o, j > 0 || k > 0);
+                    if (w == groups - 1)
+                        umma_commit(bar(V_EMPTY + (j & 1)));
+                    if (j + 1 == n_it) {
+                        umma_commit(bar(O_FULL + w));
+                        continue;
+                    }
+                    ok = w > 0 || mbar_wait(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
+                    if (!ok)
+                        break;
+                    tc_fence_after();
+                    scores(w, j + 1);
+                    if (w == groups - 1)
+                        umma_commit(bar(K_EMPTY + ((j + 1) & 1)));
+                }
+            }
+            // every MMA has completed before tensor memory is released
+            umma_commit(bar(DRAIN));
+            mbar_wait(bar(DRAIN), 0, a.status);
+        }
+    } else if (group == 2) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+        // ---------------------------------------------------- codes to fp16 tiles
+        // warp w takes keys 32w .. 32w + 31 of a tile, two units of one page each
+        constexpr int C = D / 16, RP = 32 / C, NL = 16 / RP;      // pieces a row, rows at a time, loads a unit
+        const int w = warp & 3, c = lane % C, r0 = lane / C;
+        const float mul0 = fabsf(a.scale) * (a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : kLog2e);
+        const uint8_t *const pk = static_cast<const uint8_t *>(a.pool_k) + h * a.sh + c * 16;
+        const uint8_t *const pv = static_cast<const uint8_t *>(a.pool_v) + h * a.sh + c * 16;
+        bool bad = false;
+        // page ids (-1: no key of the unit is looked at) of tile j's two units
+        auto pages = [&](int j, int *id) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                id[u] = -1;
+                if (j < n_it) {
+                    const int key = tiles.at(i0 + j) * kTile + 32 * w + 16 * u;
+                    if (key < tiles.lim) {
+                        id[u] = a.table[r * a.table_stride + a.div.div(key)];
+                        if (id[u] < 0 || id[u] >= a.n_blocks) {
+                            bad = true;
+                            id[u] = 0;
+                        }
+                    }
+                }
+            }
+        };
+        auto load = [&](const uint8_t *pool, int j, const int *id, uint4 (*v)[NL]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int key = j < n_it ? tiles.at(i0 + j) * kTile + 32 * w + 16 * u : 0;
+                const int off = key - static_cast<int>(a.div.div(key)) * a.block;
+                const uint8_t *p = pool + id[u] * a.sb + (off + r0) * a.st;
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    v[u][i] = id[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p + i * RP * a.st)) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto store = [&](uint32_t tile, const uint4 (*v)[NL], int zero_from) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const int key = 32 * w + 16 * u + r0 + i * RP;
+                    uint32_t f[8];
+                    codes4_half<FMT>(v[u][i].x, f[0], f[1]);
+                    codes4_half<FMT>(v[u][i].y, f[2], f[3]);
+                    codes4_half<FMT>(v[u][i].z, f[4], f[5]);
+                    codes4_half<FMT>(v[u][i].w, f[6], f[7]);
+                    if (key >= zero_from) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            f[k] = 0;
+                    }
+                    // 16-byte pieces 2c and 2c + 1 of the row; the upper 64 dimensions
+                    // take them the other way round, so that eight lanes' stores
+                    // meet all banks
+                    const uint32_t at = tile + (c >> 2) * S::half + key * 128;
+                    const int flip = D == 128 ? c >> 2 : 0, p0 = (2 * (c & 3) + flip) ^ (key & 7), p1 = p0 ^ 1;
+                    if (flip) {
+                        sts128(at + p0 * 16, f[4], f[5], f[6], f[7]);
+                        sts128(at + p1 * 16, f[0], f[1], f[2], f[3]);
+                    } else {
+                        sts128(at + p0 * 16, f[0], f[1], f[2], f[3]);
+                        sts128(at + p1 * 16, f[4], f[5], f[6], f[7]);
+                    }
+                }
+        };
+        int id[2], nid[2];
+        uint4 kr[2][NL], vr[2][NL];
+        pages(0, id);
+        load(pk, 0, id, kr);
+        load(pv, 0, id, vr);
+        for (int j = 0; j < n_it; ++j) {
+            pages(j + 1, nid);
+            // lanes 0 and 1: the scales of the warp's units
+            if (lane < 2) {
+                const int mine = id[lane & 1];
+                float ks = 0.0f, vs = 1.0f;
+                if (mine >= 0) {
+                    ks = a.ks[mine * a.scb + h * a.sch];
+                    vs = value_scale(a.vs[mine * a.scb + h * a.sch]);
+                }
+                scales[j & 3][2 * w + lane] = make_float4(ks * mul0, lg2(vs), share_of(vref, vs), 0.0f);
+            }
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(SC_FULL + (j & 3)));
+            const int st = j & 1;
+            if (j >= 2 && !mbar_wait(bar(K_EMPTY + st), ((j >> 1) - 1) & 1, a.status))
+                break;
+            store(sbase + S::off_k + st * S::tile, kr, 128);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(K_FULL + st));
+            load(pk, j + 1, nid, kr);
+            if (j >= 2 && !mbar_wait(bar(V_EMPTY + st), ((j >> 1) - 1) & 1, a.status))
+                break;
+            // rows behind the request's end hold any bytes, NaN codes among them
+            store(sbase + S::off_v + st * S::tile, vr, q.len - tiles.at(i0 + j) * kTile);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(V_FULL + st));
+            load(pv, j + 1, nid, vr);
+            id[0] = nid[0], id[1] = nid[1];
+        }
+        if (bad)
+            atomicOr(a.status, FKV_ST_RANGE);
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+        // ---------------------------------------------------- softmax
+        const int w = group, row = row0 + 128 * w + (tid & 127), local = tid & 127;
+        const bool live = row < rows;
+        if (w < groups) {
+            const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
+            const int64_t tok = q.tok0 + i, head = h * a.G + u;
+            Row st;
+            st.m = -INFINITY, st.l = 0.0f, st.down = 1.0f;
+            st.p = q.p0 + i;
+            const RowMask mask(a, q, st.p, live);
+            st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
+            st.slope = a.slopes && live ? a.slopes[head] * kLog2e : 0.0f;
+            // the query row as fp16 (a negative scale turns its sign)
+            {
+                const T *src = static_cast<const T *>(a.q) + tok * a.q_tok + head * a.q_head;
+                uint4 v[D / 8];
+                float amax = 0.0f;
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k) {
+                    v[k] = live ? reinterpret_cast<const uint4 *>(src)[k] : make_uint4(0, 0, 0, 0);
+                    const T *y = reinterpret_cast<const T *>(&v[k]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        amax = fmaxf(amax, fabsf(static_cast<float>(y[e])));
+                }
+                float up = a.scale < 0.0f ? -1.0f : 1.0f;
+                if (!std::is_same<T, __half>::value) {
+                    const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
+                    up *= __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
+                    st.down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
+                }
+                const uint32_t at = sbase + S::off_q + w * S::tile + local * 128;
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k) {
+                    const T *y = reinterpret_cast<const T *>(&v[k]);
+                    uint32_t f[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        f[e] = pack_half(static_cast<float>(y[2 * e]) * up, static_cast<float>(y[2 * e + 1]) * up);
+                    sts128(at + (k >> 3) * S::half + (((k & 7) ^ (local & 7)) << 4), f[0], f[1], f[2], f[3]);
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(bar(Q_FULL));
+            }
+            // the group's own range of positions, for tiles that need no mask
+            const int ga = q.p0 + static_cast<int>(a.gdiv.div(row0 + 128 * w));
+            const int gb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + 128 * w + 128, rows) - 1));
+            const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+            const uint32_t s_t = tmem + 128 * w + lanes, o_t = tmem + 256 + 128 * w + lanes;
+            bool ok = true;
+            for (int j = 0; j < n_it; ++j) {
+                ok = mbar_wait(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status) &&
+                     mbar_wait(bar(S_FULL + w), j & 1, a.status);
+                if (!ok)
+                    break;
+                tc_fence_after();
+                const int key = tiles.at(i0 + j) * kTile;
+                const float4 *sc = scales[j & 3];
+                const bool full = all_see(a, q, ga, gb, key, key + kTile);
+                const bool masked = !full || a.slopes != nullptr;      // a unit's largest is not its largest product
+                // The tile is read twice, for the reference maximum and for the weights,
+                // 32 columns at a time: 128 scores and their weights at once do not fit a
+                // thread's registers.  32 products of columns c on to scores:
+                auto scores = [&](float *s, int c) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const float mul = sc[c / 16 + n].x * st.down, lvs = sc[c / 16 + n].y;
+                        if (a.softcap > 0.0f) {
+                            const float cap = a.softcap * kLog2e;
+                            // tanh y = 1 - 2 / (1 + e^2y)
+#pragma unroll
+                            for (int e = 16 * n; e < 16 * n + 16; ++e)
+                                s[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + ex2(s[e] * mul)), cap + lvs);
+                        } else {
+#pragma unroll
+                            for (int e = 16 * n; e < 16 * n + 16; e += 2)
+                                fma2(s[e], s[e + 1], s[e], s[e + 1], mul, lvs);
+                        }
+                    }
+                    if (a.slopes) {
+                        const float at = static_cast<float>(key + c - st.p);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            s[e] = fmaf(st.slope, at + static_cast<float>(e), s[e]);
+                    }
+                    if (!full) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int jj = key + c + e;
+                            const bool see = (jj < st.hi && (jj >= st.from || jj < a.sinks)) || jj < st.pre;
+                            s[e] = see ? s[e] : -INFINITY;
+                        }
+                    }
+                };
+                float mx = -INFINITY;
+                if (masked) {
+#pragma unroll 1
+                    for (int c = 0; c < 128; c += 32) {
+                        float s[32];
+                        tmem_ld32(s_t + c, s);
+                        tmem_wait_ld(s);
+                        scores(s, c);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            mx = fmaxf(mx, s[e]);
+                    }
+                } else {
+                    // scores grow with the products: the largest product of each page's 16
+                    float y[8];
+                    tmem_max4x16(s_t, y);
+                    tmem_max4x16(s_t + 64, y + 4);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        float z = y[n] * (sc[n].x * st.down);
+                        if (a.softcap > 0.0f)
+                            z = a.softcap * kLog2e * (1.0f - __fdividef(2.0f, 1.0f + ex2(z)));
+                        mx = fmaxf(mx, z + sc[n].y);
+                    }
+                }
+                const bool move = mx > st.m + kSlack;
+                if (__any_sync(~0u, move)) {
+                    const float to = move ? mx : st.m;
+                    const float f = move ? ex2(st.m - to) : 1.0f;
+                    st.m = to;
+                    st.l *= f;
+                    // the products so far are done: their commit came before this tile's scores'
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            float o[32];
+                            tmem_ld32(o_t + c, o);
+                            tmem_wait_ld(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                o[e] *= f;
+                            tmem_st32(o_t + c, o);
+                        }
+                    }
+                }
+                const float mref = (st.m == -INFINITY ? 0.0f : st.m) - kPBits;
+                // weights; the tile's first columns, read by then, take them as fp16 pairs
+                const bool plain = !masked && a.softcap == 0.0f;
+                float s[2][32];
+                tmem_ld32(s_t, s[0]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float *v = s[k & 1];
+                    tmem_wait_ld(v);
+                    if (k < 3)
+                        tmem_ld32(s_t + 32 * (k + 1), s[(k + 1) & 1]);
+                    if (!plain)
+                        scores(v, 32 * k);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const float4 u = sc[2 * k + n];
+                        const float mul = plain ? u.x * st.down : 1.0f, off = (plain ? u.y : 0.0f) - mref;
+                        float sx = 0.0f, sy = 0.0f;
+#pragma unroll
+                        for (int e = 16 * n; e < 16 * n + 16; e += 2) {
+                            float y0, y1;
+                            fma2(y0, y1, v[e], v[e + 1], mul, off);
+                            y0 = ex2(y0), y1 = ex2(y1);
+                            add2(sx, sy, y0, y1);
+                            p[e >> 1] = pack_half(y0, y1);
+                        }
+                        st.l = fmaf(sx + sy, u.z, st.l);
+                    }
+                    tmem_st16(s_t + 16 * k, p);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar(P_FULL + w));
+            }
+            if (n_it > 0 && ok)
+                ok = mbar_wait(bar(O_FULL + w), 0, a.status);
+            tc_fence_after();
+            const float inv = st.l > 0.0f ? vref / st.l : 0.0f;
+            const float lse2 = st.l > 0.0f ? st.m - kPBits + log2f(st.l) - log2f(vref) : -INFINITY;
+            const int64_t flat = tok * (a.H * a.G) + head, at = split * a.T * (a.H * a.G) + flat;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                float o[32];
+                tmem_ld32(o_t + 32 * k, o);
+                tmem_wait_ld(o);
+                if (!live)
+                    continue;
+                // a row that saw nothing has no products either: tensor memory holds anything
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    o[e] = st.l > 0.0f ? o[e] * inv : 0.0f;
+                if (a.splits == 1) {
+                    T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + 32 * k;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        T y[8];
+#pragma unroll
+                        for (int f = 0; f < 8; ++f)
+                            y[f] = from_float<T>(o[e + f]);
+                        *reinterpret_cast<uint4 *>(dst + e) = *reinterpret_cast<const uint4 *>(y);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4 *>(a.ws_o + at * D + 32 * k + e) =
+                            make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            if (live) {
+                if (a.splits > 1)
+                    a.ws_lse[at] = lse2;
+                else if (a.lse)
+                    a.lse[flat] = lse2 / kLog2e;
+            }
+            tc_fence_before();
+        }
+    }
+    __syncthreads();
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int D, int FMT, typename T> cudaError_t prompt_as(const fkv_ctx *ctx, const AttendArgs &a, cudaStream_t st)
+{
+    const void *fn = reinterpret_cast<const void *>(k_attend_prompt<D, FMT, T>);
+    const cudaError_t e = kernel_use(ctx, fn, kThreads, PromptShape<D>::smem, nullptr);
+    if (e != cudaSuccess)
+        return e;
+    const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.row_tiles) * a.n_req * a.splits * a.H);
+    k_attend_prompt<D, FMT, T><<<grid, kThreads, PromptShape<D>::smem, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <int D, int FMT> cudaError_t prompt_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, cudaStream_t st)
+{
+    return dtype == FKV_F16 ? prompt_as<D, FMT, __half>(ctx, a, st) : prompt_as<D, FMT, __nv_bfloat16>(ctx, a, st);
+}
+
+}  // namespace
+
+int prompt_rows() { return kRows; }
+
+cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const AttendArgs &a, int dim, int format, int dtype, cudaStream_t st)
+{
+    if (dim == 64)
+        return format == FKV_INT8 ? prompt_dt<64, FKV_INT8>(ctx, a, dtype, st) : prompt_dt<64, FKV_E4M3>(ctx, a, dtype, st);
+    return format == FKV_INT8 ? prompt_dt<128, FKV_INT8>(ctx, a, dtype, st) : prompt_dt<128, FKV_E4M3>(ctx, a, dtype, st);
+}

@@ -186,6 +186,21 @@ def test_scales_of_any_size_mix(fkv, ctx, where):
     b.check(ctx)
 
 
+@pytest.mark.parametrize("lens", [[(5000, 1)], [(900, 40)], [(3000, 300)]])
+def test_pages_of_zeros(fkv, ctx, lens):
+    """Values that are all zero, in pages of the smallest scale, at the first and at every page."""
+    for every in (False, True):
+        b = Batch(fkv, 21, lens, 1, 2, 128, 16, "e4m3", "bf16")
+        for r in range(len(lens)):
+            ids = b.table[r] if every else b.table[r, :2]
+            b.codes[1][ids], b.scale[1][ids] = 0, np.float32(paged.FLOOR)
+            b.pages.v.view(torch.uint8)[torch.from_numpy(ids).cuda()] = 0
+        b.pages.v_scale.copy_(torch.from_numpy(b.scale[1]))
+        b.check(ctx, rows=[0, 5, 39, 299])
+        if every:
+            assert not b.run(ctx)[0][:sum(b.new)].any()
+
+
 def test_queries_of_any_size(fkv, ctx):
     b = Batch(fkv, 7, [(300, 2), (150, 30)], 2, 2, 64, 16, "int8", "bf16")
     b.q[0] *= 2.0 ** 60
