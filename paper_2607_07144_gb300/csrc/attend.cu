@@ -471,8 +471,8 @@ __global__ void __launch_bounds__(128, 2)
         f[w] = ex2(ml[w][0][row] - mref);
         lt += ml[w][1][row] * f[w];
     }
-    const float inv = lt > 0.0f ? vref / lt : 0.0f;
-    const float lse2 = lt > 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
+    const float inv = lt != 0.0f ? vref / lt : 0.0f;
+    const float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
     const int i = static_cast<int>(a.gdiv.div(row0 + row));
     const int64_t tok = q.tok0 + i, head = h * a.G + row0 + row - i * a.G, flat = tok * (a.H * a.G) + head;
     float x[E];
@@ -565,12 +565,12 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
         const float4 v = part[k][c];
         x.x += v.x, x.y += v.y, x.z += v.z, x.w += v.w;
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
     const T y[4] = {from_float<T>(x.x * inv), from_float<T>(x.y * inv), from_float<T>(x.z * inv), from_float<T>(x.w * inv)};
     *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + 4 * c) =
         *reinterpret_cast<const uint2 *>(y);
     if (a.lse && c == 0)
-        a.lse[row] = sum > 0.0f ? (mref + log2f(sum)) / kLog2e : -INFINITY;
+        a.lse[row] = sum != 0.0f ? (mref + log2f(sum)) / kLog2e : -INFINITY;
 }
 
 // ------------------------------------------------------------------ launch --

@@ -9,8 +9,10 @@
 // one's products run while the other exponentiates.  S = Q K^T and then P (fp16,
 // in place of S) and O stay in tensor memory: P is the second product's first
 // operand from there, and V is read as it lies, [key][dimension], by a transposed
-// descriptor.  A row's reference maximum moves only when it would grow by more
-// than 2^8 (P then spans 2^14 .. 2^-24), so O is rarely rescaled.
+// descriptor.  A tile is read once, against the row's reference exponent from the
+// tiles before: only when weights come out above 2^15 does the reference move up
+// to the largest score seen (O and what has been written of P are then scaled by
+// the power of two between them, exactly), so no pass looks for the maximum.
 #include "attend.cuh"
 
 using namespace fkvd;
@@ -18,7 +20,8 @@ using namespace fkvd;
 namespace {
 
 constexpr int kRows = 256, kThreads = 512;
-constexpr float kPBits = 6.0f, kSlack = 8.0f;    // P is at most 2^(kPBits + kSlack)
+constexpr float kPBits = 6.0f;          // a reference gives its own score the weight 2^6
+constexpr float kMostSum = 32768.0f;    // of 16 weights: each then fits fp16
 
 template <int D> struct PromptShape {
     static constexpr int half = 128 * 128;                   // 64 dimensions of 128 rows in fp16
@@ -48,20 +51,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
                  "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
-// The largest of each 16 of 64 columns (tcgen05.ld.red).
-__device__ __forceinline__ void tmem_max4x16(uint32_t taddr, float *m)
-{
-    float x[64];
-    asm volatile(
-        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, %64, [%68+0];\n\t"
-        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, %65, [%68+16];\n\t"
-        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, %66, [%68+32];\n\t"
-        "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 {%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, %67, [%68+48];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31]), "=f"(x[32]), "=f"(x[33]), "=f"(x[34]), "=f"(x[35]), "=f"(x[36]), "=f"(x[37]), "=f"(x[38]), "=f"(x[39]), "=f"(x[40]), "=f"(x[41]), "=f"(x[42]), "=f"(x[43]), "=f"(x[44]), "=f"(x[45]), "=f"(x[46]), "=f"(x[47]), "=f"(x[48]), "=f"(x[49]), "=f"(x[50]), "=f"(x[51]), "=f"(x[52]), "=f"(x[53]), "=f"(x[54]), "=f"(x[55]), "=f"(x[56]), "=f"(x[57]), "=f"(x[58]), "=f"(x[59]), "=f"(x[60]), "=f"(x[61]), "=f"(x[62]), "=f"(x[63]), "=f"(m[0]), "=f"(m[1]), "=f"(m[2]), "=f"(m[3])
-        : "r"(taddr));
-}
-
 // Waits for this thread's loads; the registers pass through, so that nothing
 // reads them earlier.
 __device__ __forceinline__ void tmem_wait_ld(float *r)
@@ -69,6 +58,15 @@ __device__ __forceinline__ void tmem_wait_ld(float *r)
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
                  :
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr)
                  : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -127,7 +125,7 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b)
 
 // One group's softmax of a tile: see k_attend_prompt.
 struct Row {
-    float m, l;                 // reference maximum and the sum of weights
+    float m, l;                 // reference exponent and the sum of weights
     float down;                 // what a score is multiplied by for the row's power of two
     int p, hi, from, pre;       // position and visible keys
     float slope;
@@ -260,21 +258,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const uint8_t *const pk = static_cast<const uint8_t *>(a.pool_k) + h * a.sh + c * 16;
         const uint8_t *const pv = static_cast<const uint8_t *>(a.pool_v) + h * a.sh + c * 16;
         bool bad = false;
-        // page ids (-1: no key of the unit is looked at) of tile j's two units
-        auto pages = [&](int j, int *id) {
+        // Page ids (-1: no key of the unit is looked at) of a tile's two units.  They
+        // are asked for two tiles ahead and checked a tile later, the scales (by
+        // lanes 0 and 1, a unit each) and the codes one tile ahead, so that nothing
+        // here waits for memory.
+        auto ask = [&](int j, int *id) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 id[u] = -1;
                 if (j < n_it) {
                     const int key = tiles.at(i0 + j) * kTile + 32 * w + 16 * u;
-                    if (key < tiles.lim) {
+                    if (key < tiles.lim)
                         id[u] = a.table[r * a.table_stride + a.div.div(key)];
-                        if (id[u] < 0 || id[u] >= a.n_blocks) {
-                            bad = true;
-                            id[u] = 0;
-                        }
-                    }
                 }
+            }
+        };
+        auto check = [&](int j, int *id) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (j < n_it && tiles.at(i0 + j) * kTile + 32 * w + 16 * u < tiles.lim && (id[u] < 0 || id[u] >= a.n_blocks)) {
+                    bad = true;
+                    id[u] = 0;
+                }
+        };
+        auto ask_scales = [&](const int *id, float &ks, float &vs) {
+            const int mine = lane & 1 ? id[1] : id[0];
+            ks = 0.0f, vs = 1.0f;
+            if (lane < 2 && mine >= 0) {
+                ks = a.ks[mine * a.scb + h * a.sch];
+                vs = a.vs[mine * a.scb + h * a.sch];
             }
         };
         auto load = [&](const uint8_t *pool, int j, const int *id, uint4 (*v)[NL]) {
@@ -318,23 +330,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     }
                 }
         };
-        int id[2], nid[2];
+        int nid[2], nnid[2];
+        float ks, vs;
         uint4 kr[2][NL], vr[2][NL];
-        pages(0, id);
-        load(pk, 0, id, kr);
-        load(pv, 0, id, vr);
+        ask(0, nnid);
+        check(0, nnid);
+        ask(1, nid);
+        load(pk, 0, nnid, kr);
+        load(pv, 0, nnid, vr);
+        ask_scales(nnid, ks, vs);
+        check(1, nid);
         for (int j = 0; j < n_it; ++j) {
-            pages(j + 1, nid);
-            // lanes 0 and 1: the scales of the warp's units
+            // nid: checked ids of tile j + 1
+            ask(j + 2, nnid);
             if (lane < 2) {
-                const int mine = id[lane & 1];
-                float ks = 0.0f, vs = 1.0f;
-                if (mine >= 0) {
-                    ks = a.ks[mine * a.scb + h * a.sch];
-                    vs = value_scale(a.vs[mine * a.scb + h * a.sch]);
-                }
+                vs = value_scale(vs);
                 scales[j & 3][2 * w + lane] = make_float4(ks * mul0, lg2(vs), share_of(vref, vs), 0.0f);
             }
+            ask_scales(nid, ks, vs);
             __syncwarp();
             if (lane == 0)
                 mbar_arrive(bar(SC_FULL + (j & 3)));
@@ -356,7 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (lane == 0)
                 mbar_arrive(bar(V_FULL + st));
             load(pv, j + 1, nid, vr);
-            id[0] = nid[0], id[1] = nid[1];
+            check(j + 2, nnid);
+            nid[0] = nnid[0], nid[1] = nnid[1];
         }
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);
@@ -369,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
             const int64_t tok = q.tok0 + i, head = h * a.G + u;
             Row st;
-            st.m = -INFINITY, st.l = 0.0f, st.down = 1.0f;
+            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f;
             st.p = q.p0 + i;
             const RowMask mask(a, q, st.p, live);
             st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
@@ -421,10 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const int key = tiles.at(i0 + j) * kTile;
                 const float4 *sc = scales[j & 3];
                 const bool full = all_see(a, q, ga, gb, key, key + kTile);
-                const bool masked = !full || a.slopes != nullptr;      // a unit's largest is not its largest product
-                // The tile is read twice, for the reference maximum and for the weights,
-                // 32 columns at a time: 128 scores and their weights at once do not fit a
-                // thread's registers.  32 products of columns c on to scores:
+                // 32 products of columns c on to scores
                 auto scores = [&](float *s, int c) {
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
@@ -456,81 +467,93 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         }
                     }
                 };
-                float mx = -INFINITY;
-                if (masked) {
-#pragma unroll 1
-                    for (int c = 0; c < 128; c += 32) {
-                        float s[32];
-                        tmem_ld32(s_t + c, s);
-                        tmem_wait_ld(s);
-                        scores(s, c);
+                // Weights of 32 columns from products (mul, off) or scores (1, -reference);
+                // the tile's first columns, read by then, take them as fp16 pairs.
+                auto weights = [&](float *v, int k, float mul0, float mul1, float off0, float off1) {
+                    uint32_t p[16];
+                    float sum[2];
+                    auto evaluate = [&](float base) {
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            float sx = 0.0f, sy = 0.0f;
+#pragma unroll
+                            for (int e = 16 * n; e < 16 * n + 16; e += 2) {
+                                float y0, y1;
+                                fma2(y0, y1, v[e], v[e + 1], n ? mul1 : mul0, (n ? off1 : off0) - base);
+                                y0 = ex2(y0), y1 = ex2(y1);
+                                add2(sx, sy, y0, y1);
+                                p[e >> 1] = pack_half(y0, y1);
+                            }
+                            sum[n] = sx + sy;
+                        }
+                    };
+                    evaluate(st.m);
+                    // (not <=: a sum that is no number is looked at as well)
+                    const bool over = !(fmaxf(sum[0], sum[1]) <= kMostSum) || st.m == -INFINITY;
+                    if (__any_sync(~0u, over)) {
+                        float mx = -INFINITY;
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            mx = fmaxf(mx, s[e]);
+                            mx = fmaxf(mx, fmaf(v[e], e < 16 ? mul0 : mul1, e < 16 ? off0 : off1));
+                        // the reference: a score's weight is 2^(score - m); an integer
+                        const float to = over && mx > -INFINITY ? ceilf(mx) - kPBits : st.m;
+                        const float f = to == st.m || st.m == -INFINITY ? (to == st.m ? 1.0f : 0.0f) : ex2(st.m - to);
+                        st.m = to;
+                        st.l *= f;
+                        // the products so far are done: their commit came before this tile's scores'
+                        if (j > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                float o[32];
+                                tmem_ld32(o_t + c, o);
+                                tmem_wait_ld(o);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    o[e] *= f;
+                                tmem_st32(o_t + c, o);
+                            }
+                        }
+#pragma unroll 1
+                        for (int c = 0; c < k; ++c) {
+                            uint32_t w16[16];
+                            tmem_wait_st();
+                            tmem_ld16(s_t + 16 * c, w16);
+                            const __half2 f2 = __float2half2_rn(f);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const __half2 y = __hmul2(*reinterpret_cast<__half2 *>(&w16[e]), f2);
+                                w16[e] = *reinterpret_cast<const uint32_t *>(&y);
+                            }
+                            tmem_st16(s_t + 16 * c, w16);
+                        }
+                        evaluate(st.m == -INFINITY ? 0.0f : st.m);
+                    }
+                    st.l = fmaf(sum[0], sc[2 * k].z, fmaf(sum[1], sc[2 * k + 1].z, st.l));
+                    tmem_st16(s_t + 16 * k, p);
+                };
+                if (full && a.softcap == 0.0f && !a.slopes) {
+#pragma unroll 1
+                    for (int k = 0; k < 4; k += 2) {
+                        float s[2][32];
+                        tmem_ld32(s_t + 32 * k, s[0]);
+                        tmem_ld32(s_t + 32 * k + 32, s[1]);
+                        tmem_wait_ld(s[0]);
+                        tmem_wait_ld(s[1]);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float4 u0 = sc[2 * (k + e)], u1 = sc[2 * (k + e) + 1];
+                            weights(s[e], k + e, u0.x * st.down, u1.x * st.down, u0.y, u1.y);
+                        }
                     }
                 } else {
-                    // scores grow with the products: the largest product of each page's 16
-                    float y[8];
-                    tmem_max4x16(s_t, y);
-                    tmem_max4x16(s_t + 64, y + 4);
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        float z = y[n] * (sc[n].x * st.down);
-                        if (a.softcap > 0.0f)
-                            z = a.softcap * kLog2e * (1.0f - __fdividef(2.0f, 1.0f + ex2(z)));
-                        mx = fmaxf(mx, z + sc[n].y);
-                    }
-                }
-                const bool move = mx > st.m + kSlack;
-                if (__any_sync(~0u, move)) {
-                    const float to = move ? mx : st.m;
-                    const float f = move ? ex2(st.m - to) : 1.0f;
-                    st.m = to;
-                    st.l *= f;
-                    // the products so far are done: their commit came before this tile's scores'
-                    if (j > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            float o[32];
-                            tmem_ld32(o_t + c, o);
-                            tmem_wait_ld(o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                o[e] *= f;
-                            tmem_st32(o_t + c, o);
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        float s[32];
+                        tmem_ld32(s_t + 32 * k, s);
+                        tmem_wait_ld(s);
+                        scores(s, 32 * k);
+                        weights(s, k, 1.0f, 1.0f, 0.0f, 0.0f);
                     }
-                }
-                const float mref = (st.m == -INFINITY ? 0.0f : st.m) - kPBits;
-                // weights; the tile's first columns, read by then, take them as fp16 pairs
-                const bool plain = !masked && a.softcap == 0.0f;
-                float s[2][32];
-                tmem_ld32(s_t, s[0]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float *v = s[k & 1];
-                    tmem_wait_ld(v);
-                    if (k < 3)
-                        tmem_ld32(s_t + 32 * (k + 1), s[(k + 1) & 1]);
-                    if (!plain)
-                        scores(v, 32 * k);
-                    uint32_t p[16];
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const float4 u = sc[2 * k + n];
-                        const float mul = plain ? u.x * st.down : 1.0f, off = (plain ? u.y : 0.0f) - mref;
-                        float sx = 0.0f, sy = 0.0f;
-#pragma unroll
-                        for (int e = 16 * n; e < 16 * n + 16; e += 2) {
-                            float y0, y1;
-                            fma2(y0, y1, v[e], v[e + 1], mul, off);
-                            y0 = ex2(y0), y1 = ex2(y1);
-                            add2(sx, sy, y0, y1);
-                            p[e >> 1] = pack_half(y0, y1);
-                        }
-                        st.l = fmaf(sx + sy, u.z, st.l);
-                    }
-                    tmem_st16(s_t + 16 * k, p);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -539,8 +562,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (n_it > 0 && ok)
                 ok = mbar_wait(bar(O_FULL + w), 0, a.status);
             tc_fence_after();
-            const float inv = st.l > 0.0f ? vref / st.l : 0.0f;
-            const float lse2 = st.l > 0.0f ? st.m - kPBits + log2f(st.l) - log2f(vref) : -INFINITY;
+            const float inv = st.l != 0.0f ? vref / st.l : 0.0f;
+            const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - log2f(vref) : -INFINITY;
             const int64_t flat = tok * (a.H * a.G) + head, at = split * a.T * (a.H * a.G) + flat;
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {
@@ -552,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 // a row that saw nothing has no products either: tensor memory holds anything
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                    o[e] = st.l > 0.0f ? o[e] * inv : 0.0f;
+                    o[e] = st.l != 0.0f ? o[e] * inv : 0.0f;
                 if (a.splits == 1) {
                     T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + 32 * k;
 #pragma unroll
