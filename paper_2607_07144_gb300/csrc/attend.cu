@@ -67,9 +67,11 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
 // takes 16 consecutive bytes of a key as four steps' operands, and 16 bytes of a
 // value row as 16 rows of the result.  mma.sync, as these shapes are a sixteenth
 // of what tcgen05 multiplies at least; its rate leaves the bytes the bound.
-template <int D> struct StepShape {
-    static constexpr int stages = D == 128 ? 3 : 6;
-    static constexpr int smem = 4 * stages * 64 * D + 1024;
+template <int D, int NT> struct StepShape {
+    static constexpr int stages = D == 128 ? 2 : 4, ring = 4 * stages * 64 * D;
+    // more than 8 rows: the query operands, [column tile][step][lane]
+    static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0, ml = 4 * 2 * 8 * NT * 4;
+    static constexpr int smem = ring + q + ml + 1024;
 };
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
@@ -80,15 +82,18 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 }
 
 template <int D, int FMT, typename T, int NT>
-__global__ void __launch_bounds__(128, 2)
+__global__ void __launch_bounds__(128, 3)
     k_attend_step(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
 {
-    constexpr int ST = StepShape<D>::stages, NS = D / 64, UNIT = 16 * D, STAGE = 4 * UNIT, MO = D / 16, R = 8 * NT;
+    constexpr int ST = StepShape<D, NT>::stages, NS = D / 64, UNIT = 16 * D, STAGE = 4 * UNIT, MO = D / 16, R = 8 * NT;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
-    __shared__ float ml[4][2][R];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
+    uint8_t *const base = raw + (sbase - smem_u32(raw));
+    uint2 *const q_s = reinterpret_cast<uint2 *>(base + StepShape<D, NT>::ring);
+    typedef float RowPair[2][R];                 // a warp's maxima and sums
+    RowPair *const ml = reinterpret_cast<RowPair *>(base + StepShape<D, NT>::ring + StepShape<D, NT>::q);
 
     const int h = blockIdx.y;
     const int split = blockIdx.x % a.splits, rr = blockIdx.x / a.splits;
@@ -174,7 +179,7 @@ __global__ void __launch_bounds__(128, 2)
 
     // the query rows as fp16 operands: lane t's steps take 16 consecutive
     // dimensions (two such pieces for D = 128) of row gid
-    uint32_t qf[NT][NS * 4][2];
+    uint32_t qf[NT > 1 ? 1 : NS * 4][2];
     float rowmul[NT][2], slope[NT][2];
     int prow[NT][2], hi[NT][2], from[NT][2], pre[NT][2];
 #pragma unroll
@@ -213,8 +218,14 @@ __global__ void __launch_bounds__(128, 2)
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                qf[n][s * 4 + kk][0] = pack_half(x[s][4 * kk] * up, x[s][4 * kk + 1] * up);
-                qf[n][s * 4 + kk][1] = pack_half(x[s][4 * kk + 2] * up, x[s][4 * kk + 3] * up);
+                const uint32_t f0 = pack_half(x[s][4 * kk] * up, x[s][4 * kk + 1] * up);
+                const uint32_t f1 = pack_half(x[s][4 * kk + 2] * up, x[s][4 * kk + 3] * up);
+                if (NT > 1) {
+                    if (warp == n % 4)
+                        q_s[(n * NS * 4 + s * 4 + kk) * 32 + lane] = make_uint2(f0, f1);
+                } else {
+                    qf[s * 4 + kk][0] = f0, qf[s * 4 + kk][1] = f1;
+                }
             }
         // a lane's scores are of rows 2t and 2t + 1
 #pragma unroll
@@ -229,6 +240,9 @@ __global__ void __launch_bounds__(128, 2)
             hi[n][c] = m.hi, from[n][c] = m.from, pre[n][c] = m.pre;
         }
     }
+
+    if (NT > 1)
+        __syncthreads();
 
     float o[NT][MO][4];
     float m[NT][2], l[NT][2];
@@ -263,33 +277,39 @@ __global__ void __launch_bounds__(128, 2)
 
         float sc[2][NT][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
                 sc[u][n][0] = sc[u][n][1] = sc[u][n][2] = sc[u][n][3] = 0.0f;
-            if (u < nu) {
-                const int kr = 16 * u + gid;            // and kr + 8
+        // both units' keys gid and gid + 8; a unit that was not loaded gives
+        // products of any bytes, which no row sees
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const int c = NS * t + s;
-                    uint4 w0, w1;
-                    if (D == 128) {
-                        const uint32_t at = kt + kr * 128 + ((c ^ (kr & 7)) << 4);
-                        w0 = lds128(at), w1 = lds128(at + 1024);
-                    } else {
-                        const uint32_t at = kt + kr * 64 + ((c ^ ((kr >> 1) & 3)) << 4);
-                        w0 = lds128(at), w1 = lds128(at + 512);
-                    }
-                    const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+        for (int s = 0; s < NS; ++s) {
+            const int c = NS * t + s;
+            uint4 w[2][2];
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        uint32_t f[4];
-                        codes4_half<FMT>(x0[kk], f[0], f[2]);
-                        codes4_half<FMT>(x1[kk], f[1], f[3]);
+            for (int u = 0; u < 2; ++u) {
+                const int kr = 16 * u + gid;
+                const uint32_t at = D == 128 ? kt + kr * 128 + ((c ^ (kr & 7)) << 4) : kt + kr * 64 + ((c ^ ((kr >> 1) & 3)) << 4);
+                w[u][0] = lds128(at), w[u][1] = lds128(at + 8 * D);
+            }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma16816(sc[u][n], f, qf[n][s * 4 + kk][0], qf[n][s * 4 + kk][1]);
-                    }
+            for (int kk = 0; kk < 4; ++kk) {
+                uint32_t f[2][4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    codes4_half<FMT>(reinterpret_cast<const uint32_t *>(&w[u][0])[kk], f[u][0], f[u][2]);
+                    codes4_half<FMT>(reinterpret_cast<const uint32_t *>(&w[u][1])[kk], f[u][1], f[u][3]);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint2 qv;
+                    if (NT > 1)
+                        qv = q_s[(n * NS * 4 + s * 4 + kk) * 32 + lane];
+                    else
+                        qv = make_uint2(qf[s * 4 + kk][0], qf[s * 4 + kk][1]);
+                    mma16816(sc[0][n], f[0], qv.x, qv.y);
+                    mma16816(sc[1][n], f[1], qv.x, qv.y);
                 }
             }
         }
@@ -300,6 +320,14 @@ __global__ void __launch_bounds__(128, 2)
         for (int n = 0; n < NT; ++n)
             mx[n][0] = mx[n][1] = -INFINITY;
         const bool full = nu == 2 && all_see(a, q, pa, pb, key, key + 32);
+        float bias[NT][2];
+        if (a.slopes) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    bias[n][c] = slope[n][c] * static_cast<float>(key + gid - prow[n][c]);
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int at = (it & 15) * 2 + u;
@@ -324,8 +352,7 @@ __global__ void __launch_bounds__(128, 2)
                 if (a.slopes) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        x[e] = fmaf(slope[n][e & 1],
-                                    static_cast<float>(key + 16 * u + gid + 8 * (e >> 1) - prow[n][e & 1]), x[e]);
+                        x[e] = fmaf(slope[n][e & 1], static_cast<float>(16 * u + 8 * (e >> 1)), x[e] + bias[n][e & 1]);
                 }
                 if (!full) {
 #pragma unroll
@@ -444,7 +471,7 @@ __global__ void __launch_bounds__(128, 2)
     if (bad)
         atomicOr(a.status, FKV_ST_RANGE);
     __syncthreads();                   // every ring is read: its memory takes the outputs
-    float *mo = reinterpret_cast<float *>(raw + (sbase - smem_u32(raw)));
+    float *mo = reinterpret_cast<float *>(base);
     constexpr int LD = D + 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -579,7 +606,7 @@ struct Plan {
 };
 
 // Which kernel serves the call, and how many shares the keys are split into.
-// Up to 16 rows a KV head (nt = 1 or 2 columns of 8) go to the step kernel, more
+// Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step kernel, more
 // to the tensor-memory one (nt = 0).  A block's time is its keys plus a fixed
 // part (its launch, the first loads' latency and its end: about that of 384
 // keys); the blocks run in waves of `slots`.  The split with the least waves x
@@ -588,10 +615,10 @@ Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t T, int64_t
 {
     Plan p;
     const int64_t most = max_new * G;
-    p.nt = most <= 8 ? 1 : most <= 16 ? 2 : 0;
+    p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
-    const int64_t blocks = n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 2 : ctx->sms;
+    const int64_t blocks = n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
     int64_t span = max_len;
     if (window && window + max_new + 2 * kTile < span)
         span = window + max_new + 2 * kTile;
@@ -624,11 +651,11 @@ template <int D, int FMT, typename T, int NT>
 cudaError_t step_rows(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
     const void *fn = reinterpret_cast<const void *>(k_attend_step<D, FMT, T, NT>);
-    const cudaError_t e = kernel_use(ctx, fn, 128, StepShape<D>::smem, nullptr);
+    const cudaError_t e = kernel_use(ctx, fn, 128, StepShape<D, NT>::smem, nullptr);
     if (e != cudaSuccess)
         return e;
     const dim3 grid(static_cast<unsigned>(a.n_req * a.row_tiles * a.splits), a.H);
-    k_attend_step<D, FMT, T, NT><<<grid, 128, StepShape<D>::smem, st>>>(a, mk, mv);
+    k_attend_step<D, FMT, T, NT><<<grid, 128, StepShape<D, NT>::smem, st>>>(a, mk, mv);
     return cudaGetLastError();
 }
 

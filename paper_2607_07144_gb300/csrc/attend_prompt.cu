@@ -39,12 +39,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
                  : "r"(taddr)
                  : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *r)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-                 "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31])
-                 : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -74,6 +68,28 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// mbar_wait for warps that share their schedulers with working ones: the
+// hardware suspends a waiting thread for up to 10 ms a try instead of polling
+// (polls took a fifth of the instruction issue), 200 tries being the 2 s limit.
+__device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, unsigned *status)
+{
+#pragma unroll 1
+    for (int i = 0; i < 200; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(10000000u)
+            : "memory");
+        if (ok)
+            return true;
+    }
+    atomicOr(status, FKV_ST_TIMEOUT);
+    return false;
 }
 
 // D[tmem] (+)= A[tmem] B[smem], A fp16 pairs in 32-bit columns.
@@ -137,7 +153,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     using S = PromptShape<D>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
-    __shared__ float4 scales[4][8];           // of the last four tiles' units of 16 keys: multiplier, log2 vs, vref / vs
+    // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and vref / vs
+    __shared__ float k_scales[4][8];
+    __shared__ float2 v_scales[4][8];
     __shared__ uint32_t tmem_slot;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
@@ -167,9 +185,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(K_FULL + i), 4);
+            mbar_init(bar(K_FULL + i), 2);
             mbar_init(bar(K_EMPTY + i), 1);
-            mbar_init(bar(V_FULL + i), 4);
+            mbar_init(bar(V_FULL + i), 2);
             mbar_init(bar(V_EMPTY + i), 1);
             mbar_init(bar(S_FULL + i), 1);
             mbar_init(bar(P_FULL + i), 128);
@@ -211,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 }
                 umma_commit(bar(S_FULL + w));
             };
-            bool ok = mbar_wait(bar(Q_FULL), 0, a.status) && mbar_wait(bar(K_FULL), 0, a.status);
+            bool ok = mbar_park(bar(Q_FULL), 0, a.status) && mbar_park(bar(K_FULL), 0, a.status);
             if (ok) {
                 tc_fence_after();
                 for (int w = 0; w < groups; ++w)
@@ -220,8 +238,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             }
             for (int j = 0; j < n_it && ok; ++j) {
                 for (int w = 0; w < groups && ok; ++w) {
-                    ok = mbar_wait(bar(P_FULL + w), j & 1, a.status) &&
-                         (w > 0 || mbar_wait(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
+                    ok = mbar_park(bar(P_FULL + w), j & 1, a.status) &&
+                         (w > 0 || mbar_park(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
                     if (!ok)
                         break;
                     tc_fence_after();
@@ -235,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         umma_commit(bar(O_FULL + w));
                         continue;
                     }
-                    ok = w > 0 || mbar_wait(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
+                    ok = w > 0 || mbar_park(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
                     if (!ok)
                         break;
                     tc_fence_after();
@@ -246,131 +264,116 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             }
             // every MMA has completed before tensor memory is released
             umma_commit(bar(DRAIN));
-            mbar_wait(bar(DRAIN), 0, a.status);
+            mbar_park(bar(DRAIN), 0, a.status);
         }
     } else if (group == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         // ---------------------------------------------------- codes to fp16 tiles
-        // warp w takes keys 32w .. 32w + 31 of a tile, two units of one page each
-        constexpr int C = D / 16, RP = 32 / C, NL = 16 / RP;      // pieces a row, rows at a time, loads a unit
-        const int w = warp & 3, c = lane % C, r0 = lane / C;
+        // warps 0 and 1 take K's keys 0 .. 63 and 64 .. 127 of a tile, 2 and 3 V's:
+        // four units of 16 keys, each of one page
+        // A lane moves 16-byte piece c of rows r0, r0 + RP, ...; eight lanes that
+        // store together hold four pieces of two rows of different parity, which
+        // the swizzle puts on different banks.
+        constexpr int RP = 512 / D, NL = 16 / RP;                 // rows at a time, loads a unit
+        const int w = warp & 1;
+        const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+        const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+        const bool v_side = warp & 2;
+        const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
+        const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
         const float mul0 = fabsf(a.scale) * (a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : kLog2e);
-        const uint8_t *const pk = static_cast<const uint8_t *>(a.pool_k) + h * a.sh + c * 16;
-        const uint8_t *const pv = static_cast<const uint8_t *>(a.pool_v) + h * a.sh + c * 16;
+        const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
+        // where the lane's first row's two 16-byte halves go in a tile
+        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
+        const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
+        const int64_t row_step = RP * a.st;
         bool bad = false;
-        // Page ids (-1: no key of the unit is looked at) of a tile's two units.  They
-        // are asked for two tiles ahead and checked a tile later, the scales (by
-        // lanes 0 and 1, a unit each) and the codes one tile ahead, so that nothing
-        // here waits for memory.
-        auto ask = [&](int j, int *id) {
+        // Lane u < 4 looks after unit u: its page id (-1: no key of it is looked at)
+        // is asked for two tiles ahead and checked a tile later, its scale and the
+        // codes one tile ahead, so that nothing here waits for memory.
+        auto first = [&](int j) { return tiles.at(i0 + j) * kTile + 64 * w; };
+        auto ask = [&](int j) {
+            const int key = first(j) + 16 * lane;
+            return j < n_it && lane < 4 && key < tiles.lim ? a.table[r * a.table_stride + a.div.div(key)] : -1;
+        };
+        auto check = [&](int j, int id) {
+            if (j < n_it && lane < 4 && first(j) + 16 * lane < tiles.lim && (id < 0 || id >= a.n_blocks)) {
+                bad = true;
+                return 0;
+            }
+            return id;
+        };
+        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 0.0f; };
+        uint4 v[4][NL];
+        auto load = [&](int j, int id) {
+            // the unit's first row in the pool, from the lane that knows its page
+            int64_t from = -1;
+            if (id >= 0) {
+                const int key = first(j) + 16 * lane;
+                from = id * a.sb + (key - static_cast<int>(a.div.div(key)) * a.block) * a.st;
+            }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                id[u] = -1;
-                if (j < n_it) {
-                    const int key = tiles.at(i0 + j) * kTile + 32 * w + 16 * u;
-                    if (key < tiles.lim)
-                        id[u] = a.table[r * a.table_stride + a.div.div(key)];
+            for (int u = 0; u < 4; ++u) {
+                const int64_t at = __shfl_sync(~0u, from, u);
+                const uint8_t *p = pool + at;
+#pragma unroll
+                for (int i = 0; i < NL; ++i, p += row_step)
+                    v[u][i] = at >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        int nid = check(0, ask(0)), nnid;
+        load(0, nid);
+        float scale = ask_scale(nid);
+        nid = check(1, ask(1));
+        for (int j = 0; j < n_it; ++j) {
+            // nid: checked ids of tile j + 1
+            nnid = ask(j + 2);
+            if (lane < 4) {
+                if (v_side) {
+                    const float vs = value_scale(scale);
+                    v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vref, vs));
+                } else {
+                    k_scales[j & 3][4 * w + lane] = scale * mul0;
                 }
             }
-        };
-        auto check = [&](int j, int *id) {
+            scale = ask_scale(nid);
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(SC_FULL + (j & 3)));
+            const int st = j & 1;
+            if (j >= 2 && !mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status))
+                break;
+            const int first_key = first(j);
+            if (v_side && first_key + 64 > q.len) {
+                // rows behind the request's end hold any bytes, NaN codes among them
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (j < n_it && tiles.at(i0 + j) * kTile + 32 * w + 16 * u < tiles.lim && (id[u] < 0 || id[u] >= a.n_blocks)) {
-                    bad = true;
-                    id[u] = 0;
-                }
-        };
-        auto ask_scales = [&](const int *id, float &ks, float &vs) {
-            const int mine = lane & 1 ? id[1] : id[0];
-            ks = 0.0f, vs = 1.0f;
-            if (lane < 2 && mine >= 0) {
-                ks = a.ks[mine * a.scb + h * a.sch];
-                vs = a.vs[mine * a.scb + h * a.sch];
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < NL; ++i)
+                        if (first_key + 16 * u + r0 + i * RP >= q.len)
+                            v[u][i] = make_uint4(0, 0, 0, 0);
             }
-        };
-        auto load = [&](const uint8_t *pool, int j, const int *id, uint4 (*v)[NL]) {
+            const uint32_t tile = at0 + st * S::tile;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int key = j < n_it ? tiles.at(i0 + j) * kTile + 32 * w + 16 * u : 0;
-                const int off = key - static_cast<int>(a.div.div(key)) * a.block;
-                const uint8_t *p = pool + id[u] * a.sb + (off + r0) * a.st;
-#pragma unroll
-                for (int i = 0; i < NL; ++i)
-                    v[u][i] = id[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p + i * RP * a.st)) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        auto store = [&](uint32_t tile, const uint4 (*v)[NL], int zero_from) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
-                    const int key = 32 * w + 16 * u + r0 + i * RP;
                     uint32_t f[8];
                     codes4_half<FMT>(v[u][i].x, f[0], f[1]);
                     codes4_half<FMT>(v[u][i].y, f[2], f[3]);
                     codes4_half<FMT>(v[u][i].z, f[4], f[5]);
                     codes4_half<FMT>(v[u][i].w, f[6], f[7]);
-                    if (key >= zero_from) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            f[k] = 0;
-                    }
-                    // 16-byte pieces 2c and 2c + 1 of the row; the upper 64 dimensions
-                    // take them the other way round, so that eight lanes' stores
-                    // meet all banks
-                    const uint32_t at = tile + (c >> 2) * S::half + key * 128;
-                    const int flip = D == 128 ? c >> 2 : 0, p0 = (2 * (c & 3) + flip) ^ (key & 7), p1 = p0 ^ 1;
-                    if (flip) {
-                        sts128(at + p0 * 16, f[4], f[5], f[6], f[7]);
-                        sts128(at + p1 * 16, f[0], f[1], f[2], f[3]);
-                    } else {
-                        sts128(at + p0 * 16, f[0], f[1], f[2], f[3]);
-                        sts128(at + p1 * 16, f[4], f[5], f[6], f[7]);
-                    }
+                    // the row's place in its group of eight turns with i for RP = 4
+                    const uint32_t at = tile + (16 * u + i * RP) * 128, x = RP == 4 && (i & 1) ? sw ^ 64 : sw;
+                    sts128(at + x, f[0], f[1], f[2], f[3]);
+                    sts128(at + (x ^ 16), f[4], f[5], f[6], f[7]);
                 }
-        };
-        int nid[2], nnid[2];
-        float ks, vs;
-        uint4 kr[2][NL], vr[2][NL];
-        ask(0, nnid);
-        check(0, nnid);
-        ask(1, nid);
-        load(pk, 0, nnid, kr);
-        load(pv, 0, nnid, vr);
-        ask_scales(nnid, ks, vs);
-        check(1, nid);
-        for (int j = 0; j < n_it; ++j) {
-            // nid: checked ids of tile j + 1
-            ask(j + 2, nnid);
-            if (lane < 2) {
-                vs = value_scale(vs);
-                scales[j & 3][2 * w + lane] = make_float4(ks * mul0, lg2(vs), share_of(vref, vs), 0.0f);
-            }
-            ask_scales(nid, ks, vs);
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(bar(SC_FULL + (j & 3)));
-            const int st = j & 1;
-            if (j >= 2 && !mbar_wait(bar(K_EMPTY + st), ((j >> 1) - 1) & 1, a.status))
-                break;
-            store(sbase + S::off_k + st * S::tile, kr, 128);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0)
-                mbar_arrive(bar(K_FULL + st));
-            load(pk, j + 1, nid, kr);
-            if (j >= 2 && !mbar_wait(bar(V_EMPTY + st), ((j >> 1) - 1) & 1, a.status))
-                break;
-            // rows behind the request's end hold any bytes, NaN codes among them
-            store(sbase + S::off_v + st * S::tile, vr, q.len - tiles.at(i0 + j) * kTile);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(bar(V_FULL + st));
-            load(pv, j + 1, nid, vr);
-            check(j + 2, nnid);
-            nid[0] = nnid[0], nid[1] = nnid[1];
+                mbar_arrive(bar(full_bar + st));
+            load(j + 1, nid);
+            nid = check(j + 2, nnid);
         }
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);
@@ -427,140 +430,141 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const uint32_t s_t = tmem + 128 * w + lanes, o_t = tmem + 256 + 128 * w + lanes;
             bool ok = true;
             for (int j = 0; j < n_it; ++j) {
-                ok = mbar_wait(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status) &&
-                     mbar_wait(bar(S_FULL + w), j & 1, a.status);
+                ok = mbar_park(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status);
+                if (!ok)
+                    break;
+                const int key = tiles.at(i0 + j) * kTile;
+                const float *const km = k_scales[j & 3];
+                const float2 *const vm = v_scales[j & 3];
+                const bool full = all_see(a, q, ga, gb, key, key + kTile);
+                const bool plain = full && a.softcap == 0.0f && !a.slopes;
+                ok = mbar_park(bar(S_FULL + w), j & 1, a.status);
                 if (!ok)
                     break;
                 tc_fence_after();
-                const int key = tiles.at(i0 + j) * kTile;
-                const float4 *sc = scales[j & 3];
-                const bool full = all_see(a, q, ga, gb, key, key + kTile);
-                // 32 products of columns c on to scores
-                auto scores = [&](float *s, int c) {
+                // 64 columns at a time, a second time where the reference has to move first
+#pragma unroll 1
+                for (int k = 0, again = 0; k < 2;) {
+                    float s[64];
+                    tmem_ld32(s_t + 64 * k, s);
+                    tmem_ld32(s_t + 64 * k + 32, s + 32);
+                    tmem_wait_ld(s);
+                    tmem_wait_ld(s + 32);
+                    float mul[4], off[4];
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const float mul = sc[c / 16 + n].x * st.down, lvs = sc[c / 16 + n].y;
+                    for (int n = 0; n < 4; ++n) {
+                        mul[n] = km[4 * k + n] * st.down;
+                        off[n] = vm[4 * k + n].x;
+                    }
+                    if (!plain) {
+                        // products to scores in base 2
                         if (a.softcap > 0.0f) {
                             const float cap = a.softcap * kLog2e;
                             // tanh y = 1 - 2 / (1 + e^2y)
 #pragma unroll
-                            for (int e = 16 * n; e < 16 * n + 16; ++e)
-                                s[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + ex2(s[e] * mul)), cap + lvs);
+                            for (int e = 0; e < 64; ++e)
+                                s[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + ex2(s[e] * mul[e / 16])), cap + off[e / 16]);
                         } else {
 #pragma unroll
-                            for (int e = 16 * n; e < 16 * n + 16; e += 2)
-                                fma2(s[e], s[e + 1], s[e], s[e + 1], mul, lvs);
+                            for (int e = 0; e < 64; e += 2)
+                                fma2(s[e], s[e + 1], s[e], s[e + 1], mul[e / 16], off[e / 16]);
                         }
-                    }
-                    if (a.slopes) {
-                        const float at = static_cast<float>(key + c - st.p);
+                        if (a.slopes) {
+                            const float at = static_cast<float>(key + 64 * k - st.p);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            s[e] = fmaf(st.slope, at + static_cast<float>(e), s[e]);
-                    }
-                    if (!full) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int jj = key + c + e;
-                            const bool see = (jj < st.hi && (jj >= st.from || jj < a.sinks)) || jj < st.pre;
-                            s[e] = see ? s[e] : -INFINITY;
+                            for (int e = 0; e < 64; ++e)
+                                s[e] = fmaf(st.slope, at + static_cast<float>(e), s[e]);
                         }
-                    }
-                };
-                // Weights of 32 columns from products (mul, off) or scores (1, -reference);
-                // the tile's first columns, read by then, take them as fp16 pairs.
-                auto weights = [&](float *v, int k, float mul0, float mul1, float off0, float off1) {
-                    uint32_t p[16];
-                    float sum[2];
-                    auto evaluate = [&](float base) {
+                        if (!full) {
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            float sx = 0.0f, sy = 0.0f;
-#pragma unroll
-                            for (int e = 16 * n; e < 16 * n + 16; e += 2) {
-                                float y0, y1;
-                                fma2(y0, y1, v[e], v[e + 1], n ? mul1 : mul0, (n ? off1 : off0) - base);
-                                y0 = ex2(y0), y1 = ex2(y1);
-                                add2(sx, sy, y0, y1);
-                                p[e >> 1] = pack_half(y0, y1);
+                            for (int e = 0; e < 64; ++e) {
+                                const int jj = key + 64 * k + e;
+                                const bool see = (jj < st.hi && (jj >= st.from || jj < a.sinks)) || jj < st.pre;
+                                s[e] = see ? s[e] : -INFINITY;
                             }
-                            sum[n] = sx + sy;
                         }
-                    };
-                    evaluate(st.m);
-                    // (not <=: a sum that is no number is looked at as well)
-                    const bool over = !(fmaxf(sum[0], sum[1]) <= kMostSum) || st.m == -INFINITY;
-                    if (__any_sync(~0u, over)) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+                            mul[n] = 1.0f, off[n] = 0.0f;
+                    }
+                    if (again) {
+                        // A score's weight is 2^(score - m); m an integer.  All of the
+                        // warp's rows move up to what they have seen: one at a time they
+                        // would each bring the warp here.
                         float mx = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            mx = fmaxf(mx, fmaf(v[e], e < 16 ? mul0 : mul1, e < 16 ? off0 : off1));
-                        // the reference: a score's weight is 2^(score - m); an integer
-                        const float to = over && mx > -INFINITY ? ceilf(mx) - kPBits : st.m;
-                        const float f = to == st.m || st.m == -INFINITY ? (to == st.m ? 1.0f : 0.0f) : ex2(st.m - to);
+                        for (int e = 0; e < 64; ++e)
+                            mx = fmaxf(mx, fmaf(s[e], mul[e / 16], off[e / 16]));
+                        const float to = fmaxf(st.m, mx > -INFINITY ? ceilf(mx) - kPBits : st.m);
+                        const float f = to == st.m ? 1.0f : ex2(st.m - to);
                         st.m = to;
                         st.l *= f;
                         // the products so far are done: their commit came before this tile's scores'
                         if (j > 0) {
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                float o[32];
-                                tmem_ld32(o_t + c, o);
-                                tmem_wait_ld(o);
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(o_t + c, o);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    o[e] *= f;
-                                tmem_st32(o_t + c, o);
+                                for (int e = 0; e < 16; ++e)
+                                    o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st16(o_t + c, o);
                             }
                         }
-#pragma unroll 1
-                        for (int c = 0; c < k; ++c) {
-                            uint32_t w16[16];
-                            tmem_wait_st();
-                            tmem_ld16(s_t + 16 * c, w16);
+                        if (k > 0) {
                             const __half2 f2 = __float2half2_rn(f);
+#pragma unroll 1
+                            for (int c = 0; c < 32; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(s_t + c, o);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const __half2 y = __hmul2(*reinterpret_cast<__half2 *>(&w16[e]), f2);
-                                w16[e] = *reinterpret_cast<const uint32_t *>(&y);
+                                for (int e = 0; e < 16; ++e) {
+                                    const __half2 y = __hmul2(*reinterpret_cast<__half2 *>(&o[e]), f2);
+                                    o[e] = *reinterpret_cast<const uint32_t *>(&y);
+                                }
+                                tmem_st16(s_t + c, o);
                             }
-                            tmem_st16(s_t + 16 * c, w16);
                         }
-                        evaluate(st.m == -INFINITY ? 0.0f : st.m);
+                        tmem_wait_st();
                     }
-                    st.l = fmaf(sum[0], sc[2 * k].z, fmaf(sum[1], sc[2 * k + 1].z, st.l));
-                    tmem_st16(s_t + 16 * k, p);
-                };
-                if (full && a.softcap == 0.0f && !a.slopes) {
-#pragma unroll 1
-                    for (int k = 0; k < 4; k += 2) {
-                        float s[2][32];
-                        tmem_ld32(s_t + 32 * k, s[0]);
-                        tmem_ld32(s_t + 32 * k + 32, s[1]);
-                        tmem_wait_ld(s[0]);
-                        tmem_wait_ld(s[1]);
+                    const float base = again && st.m == -INFINITY ? 0.0f : st.m;
+                    uint32_t p[32];
+                    float sum[4];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float4 u0 = sc[2 * (k + e)], u1 = sc[2 * (k + e) + 1];
-                            weights(s[e], k + e, u0.x * st.down, u1.x * st.down, u0.y, u1.y);
+                    for (int n = 0; n < 4; ++n) {
+                        float sx = 0.0f, sy = 0.0f;
+                        const float o = off[n] - base;
+#pragma unroll
+                        for (int e = 16 * n; e < 16 * n + 16; e += 2) {
+                            float y0, y1;
+                            fma2(y0, y1, s[e], s[e + 1], mul[n], o);
+                            y0 = ex2(y0), y1 = ex2(y1);
+                            add2(sx, sy, y0, y1);
+                            p[e >> 1] = pack_half(y0, y1);
                         }
+                        sum[n] = sx + sy;
                     }
-                } else {
-#pragma unroll 1
-                    for (int k = 0; k < 4; ++k) {
-                        float s[32];
-                        tmem_ld32(s_t + 32 * k, s);
-                        tmem_wait_ld(s);
-                        scores(s, 32 * k);
-                        weights(s, k, 1.0f, 1.0f, 0.0f, 0.0f);
+                    // (not <=: a sum that is no number is looked at as well)
+                    if (!again && __any_sync(~0u, !(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) <= kMostSum) ||
+                                                      st.m == -INFINITY)) {
+                        again = 1;
+                        continue;
                     }
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        st.l = fmaf(sum[n], vm[4 * k + n].y, st.l);
+                    // fp16 pairs in the tile's first columns, which have been read
+                    tmem_st16(s_t + 32 * k, p);
+                    tmem_st16(s_t + 32 * k + 16, p + 16);
+                    tmem_wait_st();
+                    ++k;
+                    again = 0;
                 }
-                tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(bar(P_FULL + w));
             }
             if (n_it > 0 && ok)
-                ok = mbar_wait(bar(O_FULL + w), 0, a.status);
+                ok = mbar_park(bar(O_FULL + w), 0, a.status);
             tc_fence_after();
             const float inv = st.l != 0.0f ? vref / st.l : 0.0f;
             const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - log2f(vref) : -INFINITY;
