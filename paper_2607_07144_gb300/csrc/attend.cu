@@ -561,7 +561,9 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
             hi = mid;
     }
     Request q;
-    if (!q.load(a, lo) || tok < q.tok0 || tok >= q.tok0 + q.nq)
+    const bool mine = q.load(a, lo) && tok >= q.tok0 && tok < q.tok0 + q.nq;
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the partial results are written
+    if (!mine)
         return;
     if (tid < kMaxSplits)
         w_s[tid] = tid < a.splits ? a.ws_lse[tid * a.T * Hq + row] : -INFINITY;
@@ -668,8 +670,7 @@ cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUten
                                     : step_rows<D, FMT, T, 2>(ctx, a, mk, mv, st);
     if (e != cudaSuccess || a.splits == 1)
         return e;
-    k_attend_combine<D, T><<<static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch_after(k_attend_combine<D, T>, static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st, a);
 }
 
 template <int D, int FMT>

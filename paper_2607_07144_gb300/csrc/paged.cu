@@ -1,42 +1,31 @@
 // The paged 8-bit K/V cache: block tables and slot maps from request lengths
 // (k_page_plan), quantising writes (k_page_write) and the way back to a K/V
 // cache (k_page_read).  Attention over the pages is in attend.cu.
-#include <cooperative_groups.h>
-
 #include "paged.cuh"
 
-namespace cg = cooperative_groups;
 using namespace fkvd;
 
 namespace {
 
 // ------------------------------------------------------------------ plan --
-// One cluster of 8 blocks does a whole call: every block scans its share of
-// the requests (tokens, blocks that come back, blocks needed), the shares'
-// totals are exchanged through distributed shared memory, and the tokens are
-// then spread over all threads, each finding its request by a binary search
-// over the shares' prefix sums where they lie.  A second launch, or a grid-wide
-// counter in a workspace that two graphs could share, is not needed; what
-// bounds the call is the chain scan, exchange, exchange, store.
-constexpr int kPlanBlocks = 8, kPlanThreads = 512;
-constexpr int kPlanShare = FKV_PAGE_MAX_REQ / kPlanBlocks;   // requests a block can hold
-
-struct PlanSmem {
-    int cu[kPlanShare + 1];     // tokens before request i of this block's share
-    int need[kPlanShare + 1];   // new blocks before it
-    int back[kPlanShare + 1];   // returned blocks before it
-    long long tot[3];           // the share's totals
-    int warp[3][kPlanThreads / 32];
-    int carry[3];
-    int bad;                    // a length or the table's width does not fit
-};
+// One block scans the requests (tokens, pages given back, pages needed), a
+// consecutive share a thread, and does everything that is counted in pages: the
+// stack, the tables, the lengths.  The tokens' slots and positions follow from
+// those; a few are written by the same block, more by a second launch that
+// starts while the first one ends (one block's stores would take 160 us for half
+// a million tokens where the second launch takes 6).  Latency bounds both: each
+// is a chain of three or four loads.
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanSmem = (FKV_PAGE_MAX_REQ + 1) * 3 * sizeof(int);
+constexpr int kSlotThreads = 256, kSlotRows = 4;       // the second launch: rows a thread
 
 struct PlanArgs {
     const int *n_new, *kv_len, *taken;
     int *table, *free_ids, *cu, *positions, *kv_len_out, *taken_out;
     int64_t *slots;
     int64_t table_stride, n_free, rows;
-    int n_req, width, block;
+    int n_req, width, block, share;
+    bool with_rows;              // the plan's block writes slots and positions itself
     FastDiv div;
     unsigned *status;
 };
@@ -46,181 +35,168 @@ __device__ __forceinline__ int blocks_of(const PlanArgs &a, int tokens)
     return static_cast<int>(a.div.div(static_cast<unsigned>(tokens) + a.block - 1));
 }
 
-__global__ void __cluster_dims__(kPlanBlocks, 1, 1) __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
+// The last i < n with first[i] <= x (first[0] <= x).
+__device__ __forceinline__ int last_from(const int *first, int n, int x)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    PlanSmem &s = *reinterpret_cast<PlanSmem *>(raw);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int me = cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int share = (a.n_req + kPlanBlocks - 1) / kPlanBlocks;
-    const int r0 = min(me * share, a.n_req), r1 = min(r0 + share, a.n_req);
-    if (tid == 0) {
-        s.bad = 0;
-        s.carry[0] = s.carry[1] = s.carry[2] = 0;
-        s.tot[0] = s.tot[1] = s.tot[2] = 0;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= x)
+            lo = mid;
+        else
+            hi = mid;
     }
+    return lo;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
+{
+    extern __shared__ int sums[];            // n_req + 1 sums each of tokens, pages needed and pages given back
+    __shared__ long long part[3][32];
+    __shared__ int bad_s;
+    int *const cu = sums, *const need = sums + a.n_req + 1, *const back = need + a.n_req + 1;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r0 = min(tid * a.share, a.n_req), r1 = min(r0 + a.share, a.n_req);
     const int taken0 = *a.taken;
+    if (tid == 0)
+        bad_s = 0;
     __syncthreads();
 
-    // this share's exclusive sums, kPlanThreads requests at a time
-    for (int base = r0; base < r1; base += kPlanThreads) {
-        const int r = base + tid;
-        int v[3] = {0, 0, 0};
-        if (r < r1) {
-            const int nn = a.n_new[r], len = a.kv_len[r];
-            // 2^30: sums of a block's width stay inside 31 bits
-            if (len < 0 || nn > (1 << 30) || len > (1 << 30) || blocks_of(a, max(len, 0)) > a.width) {
-                s.bad = 1;
-            } else if (nn < 0) {
-                v[2] = blocks_of(a, len);
-            } else {
-                const int nb = blocks_of(a, len + nn);
-                if (nb > a.width)
-                    s.bad = 1;
-                v[0] = nn;
-                v[1] = nb - blocks_of(a, len);
-            }
+    // this thread's requests: tokens, pages needed, pages given back
+    auto count = [&](int r, int &tokens, int &pages, int &back) {
+        const int nn = a.n_new[r], len = a.kv_len[r];
+        tokens = pages = back = 0;
+        if (len < 0 || len > FKV_PAGE_MAX_LEN || nn > FKV_PAGE_MAX_LEN - len || blocks_of(a, len) > a.width)
+            return false;
+        if (nn < 0) {
+            back = blocks_of(a, len);
+            return true;
         }
-        int inc[3];
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            int x = v[c];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(~0u, x, o);
-                if (lane >= o)
-                    x += y;
-            }
-            inc[c] = x;
-            if (lane == 31)
-                s.warp[c][warp] = x;
-            // a share's tokens and blocks are counted in 64 bits beside the 32-bit prefix sums
-            long long w = v[c];
-#pragma unroll
-            for (int o = 16; o; o >>= 1)
-                w += __shfl_xor_sync(~0u, w, o);
-            if (lane == 0 && w)
-                atomicAdd(reinterpret_cast<unsigned long long *>(&s.tot[c]), static_cast<unsigned long long>(w));
-        }
-        __syncthreads();
-        int pre[3];
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            int x = s.carry[c];
-            for (int w = 0; w < warp; ++w)
-                x += s.warp[c][w];
-            pre[c] = x + inc[c] - v[c];
-        }
-        if (r < r1) {
-            s.cu[r - r0] = pre[0];
-            s.need[r - r0] = pre[1];
-            s.back[r - r0] = pre[2];
-        }
-        __syncthreads();
-        if (tid == kPlanThreads - 1) {
-#pragma unroll
-            for (int c = 0; c < 3; ++c)
-                s.carry[c] = pre[c] + v[c];
-        }
-        __syncthreads();
+        const int nb = blocks_of(a, len + nn);
+        tokens = nn;
+        pages = nb - blocks_of(a, len);
+        return nb <= a.width;
+    };
+    long long sum[3] = {0, 0, 0};
+    for (int r = r0; r < r1; ++r) {
+        int t, p, b;
+        if (!count(r, t, p, b))
+            bad_s = 1;
+        sum[0] += t, sum[1] += p, sum[2] += b;
     }
-    cluster.sync();
-
-    // every block's totals: what lies before this share, and the whole call's
-    long long before[3] = {0, 0, 0}, all[3] = {0, 0, 0};
-    int first_tok[kPlanBlocks + 1];
-    int bad = 0;
+    long long before[3], all[3];
 #pragma unroll
-    for (int b = 0; b < kPlanBlocks; ++b) {
-        const PlanSmem *o = cluster.map_shared_rank(&s, b);
-        bad |= o->bad;
+    for (int c = 0; c < 3; ++c) {
+        long long x = sum[c];
 #pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            const long long t = o->tot[c];
-            if (b < me)
-                before[c] += t;
-            if (c == 0)
-                first_tok[b] = static_cast<int>(min(all[0], 0x7fffffffll));
-            all[c] += t;
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o)
+                x += y;
         }
+        if (lane == 31)
+            part[c][warp] = x;
+        before[c] = x - sum[c];
     }
-    first_tok[kPlanBlocks] = static_cast<int>(min(all[0], 0x7fffffffll));
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+        long long x = part[c][lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o)
+                x += y;
+        }
+        const long long prev = __shfl_sync(~0u, x, warp > 0 ? warp - 1 : 0);
+        before[c] += warp > 0 ? prev : 0;
+        all[c] = __shfl_sync(~0u, x, 31);
+    }
     const long long taken1 = taken0 - all[2];
     // all or nothing: a call that does not fit leaves lengths, table and stack as they are
-    if (taken0 < 0 || taken0 > a.n_free || taken1 < 0 || taken1 + all[1] > a.n_free || all[0] > a.rows)
-        bad = 1;
-    const int64_t gtid = static_cast<int64_t>(me) * kPlanThreads + tid, gsize = kPlanBlocks * kPlanThreads;
+    const bool bad = bad_s || taken0 < 0 || taken0 > a.n_free || taken1 < 0 || taken1 + all[1] > a.n_free || all[0] > a.rows;
+    const int tokens = bad ? 0 : static_cast<int>(all[0]), pages = bad ? 0 : static_cast<int>(all[1]);
 
-    // blocks that come back go onto the stack before any is taken from it.  The
-    // lengths' new values wait until every thread has read the old ones: the
-    // outputs may be the inputs' own arrays.
-    if (!bad) {
-        for (int r = r0 + warp; r < r1; r += kPlanThreads / 32) {
-            if (a.n_new[r] >= 0)
-                continue;
-            const int nb = blocks_of(a, a.kv_len[r]);
-            const long long at = taken1 + before[2] + s.back[r - r0];
-            for (int j = lane; j < nb; j += 32)
-                a.free_ids[at + j] = a.table[r * a.table_stride + j];
+    for (int r = r0; r < r1; ++r) {
+        int t, p, b;
+        count(r, t, p, b);
+        cu[r] = bad ? 0 : static_cast<int>(before[0]);
+        need[r] = bad ? 0 : static_cast<int>(before[1]);
+        back[r] = bad ? 0 : static_cast<int>(before[2]);
+        before[0] += t, before[1] += p, before[2] += b;
+    }
+    if (tid == 0)
+        cu[a.n_req] = tokens;
+    __syncthreads();
+    // pages that come back go onto the stack before any is taken from it
+    for (int i = tid; i < (bad ? 0 : all[2]); i += kPlanThreads) {
+        const int r = last_from(back, a.n_req, i);
+        a.free_ids[taken1 + i] = a.table[r * a.table_stride + i - back[r]];
+    }
+    __syncthreads();
+    for (int r = tid; r <= a.n_req; r += kPlanThreads)
+        a.cu[r] = cu[r];
+    for (int i = tid; i < pages; i += kPlanThreads) {
+        const int r = last_from(need, a.n_req, i);
+        a.table[r * a.table_stride + blocks_of(a, a.kv_len[r]) + i - need[r]] = a.free_ids[taken1 + i];
+    }
+    if (a.with_rows) {
+        for (int t = tid; t < a.rows; t += kPlanThreads) {
+            int64_t slot = -1;
+            int pos = -1;
+            if (t < tokens) {
+                const int r = last_from(cu, a.n_req, t), len = a.kv_len[r], had = blocks_of(a, len);
+                pos = len + t - cu[r];
+                const int j = static_cast<int>(a.div.div(pos));
+                const int id = j < had ? a.table[r * a.table_stride + j] : a.free_ids[taken1 + need[r] + j - had];
+                slot = id < 0 ? -1 : static_cast<int64_t>(id) * a.block + pos - j * a.block;
+            }
+            a.slots[t] = slot;
+            a.positions[t] = pos;
         }
     }
-    for (int r = r0 + tid; r < r1; r += kPlanThreads)
-        a.cu[r] = bad ? 0 : static_cast<int>(before[0] + s.cu[r - r0]);
-    if (gtid == 0)
-        a.cu[a.n_req] = bad ? 0 : static_cast<int>(all[0]);
-    cluster.sync();
-
-    const int total = bad ? 0 : static_cast<int>(all[0]);
-    for (int64_t t = gtid; t < a.rows; t += gsize) {
-        int64_t slot = -1;
-        int pos = -1;
-        if (t < total) {
-            int b = 0;
-#pragma unroll
-            for (int i = 1; i < kPlanBlocks; ++i)
-                b += first_tok[i] <= t;
-            // a share without tokens starts where the next one does: the last
-            // share whose first token is t or before holds it
-            const PlanSmem *o = cluster.map_shared_rank(&s, b);
-            const int o0 = min(b * share, a.n_req), on = min(o0 + share, a.n_req) - o0;
-            const int rel = static_cast<int>(t) - first_tok[b];
-            int lo = 0, hi = on;          // the last request whose first token is rel or before
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (o->cu[mid] <= rel)
-                    lo = mid;
-                else
-                    hi = mid;
-            }
-            const int r = o0 + lo, len = a.kv_len[r];
-            pos = len + rel - o->cu[lo];
-            const int j = static_cast<int>(a.div.div(pos)), off = pos - j * a.block, had = blocks_of(a, len);
-            int id;
-            if (j < had) {
-                id = a.table[r * a.table_stride + j];
-            } else {
-                long long need0 = o->need[lo];
-                for (int i = 0; i < b; ++i)
-                    need0 += cluster.map_shared_rank(&s, i)->tot[1];
-                id = a.free_ids[taken1 + need0 + j - had];
-                if (off == 0 || rel == o->cu[lo])
-                    a.table[r * a.table_stride + j] = id;
-            }
-            slot = id < 0 ? -1 : static_cast<int64_t>(id) * a.block + off;
-        }
-        a.slots[t] = slot;
-        a.positions[t] = pos;
-    }
-    cluster.sync();
-    // no block reads lengths, the taken count or another's shared memory from here on
-    for (int r = r0 + tid; r < r1; r += kPlanThreads) {
+    __syncthreads();
+    // nothing reads lengths or the taken count from here on: the outputs may be
+    // the inputs' own arrays
+    for (int r = tid; r < a.n_req; r += kPlanThreads) {
         const int nn = a.n_new[r], len = a.kv_len[r];
         a.kv_len_out[r] = bad ? len : (nn < 0 ? 0 : len + nn);
     }
-    if (gtid == 0) {
+    if (tid == 0) {
         *a.taken_out = bad ? taken0 : static_cast<int>(taken1 + all[1]);
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);
+    }
+}
+
+// Slots and positions from the plan's tables, lengths and sums: a token's
+// request is searched for among those that the block's tokens span.
+__global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanArgs a)
+{
+    __shared__ int span[2];
+    const int tid = threadIdx.x;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * (kSlotThreads * kSlotRows);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the plan has run
+    const int tokens = a.cu[a.n_req];
+    if (tid < 2 && t0 < tokens)
+        span[tid] = last_from(a.cu, a.n_req, static_cast<int>(tid ? min(t0 + kSlotThreads * kSlotRows, static_cast<int64_t>(tokens)) - 1 : t0));
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSlotRows; ++i) {
+        const int64_t t = t0 + i * kSlotThreads + tid;
+        if (t >= a.rows)
+            return;
+        int64_t slot = -1;
+        int pos = -1;
+        if (t < tokens) {
+            const int lo = span[0], r = lo + last_from(a.cu + lo, span[1] - lo + 1, static_cast<int>(t));
+            const int c0 = a.cu[r];
+            pos = a.kv_len_out[r] - (a.cu[r + 1] - c0) + static_cast<int>(t) - c0;
+            const int j = static_cast<int>(a.div.div(pos)), id = a.table[r * a.table_stride + j];
+            slot = id < 0 ? -1 : static_cast<int64_t>(id) * a.block + pos - j * a.block;
+        }
+        a.slots[t] = slot;
+        a.positions[t] = pos;
     }
 }
 
@@ -341,94 +317,149 @@ struct WriteArgs {
     int64_t x_tok[2], x_head[2];
     const int64_t *slots;
     int64_t T, sb, sh, st, scb, sch, n_blocks;
-    int block, stretch;
+    int block, stretch, heads;
     unsigned *status;
 };
 
-constexpr int kWriteThreads = 128;
+// 16 elements as they lie in memory.
+template <typename T> struct Raw {
+    uint4 v[sizeof(T)];
+};
 
-// A block per (stretch of tokens, head, K or V).  A run of tokens with
-// consecutive slots inside one page belongs to the block whose stretch holds
-// its first token, which therefore reads and writes that page and its scale
-// alone: no atomics, and the same result in any order of the blocks.  Bound by
-// the bytes of long calls and by latency for a step's: a run is read for its
-// largest magnitude, then read again (from L1) to be rounded.
-template <int D, int FMT, typename T> __global__ void __launch_bounds__(kWriteThreads) k_page_write(WriteArgs a)
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *p)
 {
-    constexpr int C = D / 16, R = kWriteThreads / C;       // 16-element chunks a row, rows at a time
-    __shared__ float red[kWriteThreads / 32];
-    __shared__ int len_s;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = tid % C, row0 = tid / C;
-    const int kv = blockIdx.z, h = blockIdx.y;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.stretch, t1 = min(t0 + a.stretch, a.T);
-    const T *x = static_cast<const T *>(a.x[kv]) + h * a.x_head[kv] + c * 16;
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)); ++i)
+        r.v[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    return r;
+}
+
+// A run of tokens with consecutive slots inside one page belongs to the group of
+// GT threads whose stretch of tokens holds its first one, for one head and K or
+// V; the group reads and writes that page and its scale alone: no atomics, and
+// the same result in any order of the groups.  A few tokens (a step's) get a
+// warp each, many a block of 128 threads for as many tokens as a page holds,
+// which keeps up to four rows a thread in registers between the search for the
+// largest magnitude and the rounding (longer runs are read again).  Bytes bound
+// long calls, the chain slot, page, store a step's.
+template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT) k_page_write(WriteArgs a)
+{
+    constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
+    __shared__ float red[GT / 32];
+    const int lane = threadIdx.x & 31, tid = GT == 32 ? lane : threadIdx.x, c = tid % C, row0 = tid / C;
+    int64_t t0, item = blockIdx.x;
+    if (GT == 32)
+        item = item * 8 + (threadIdx.x >> 5);
+    const int h = static_cast<int>(item % a.heads);
+    item /= a.heads;
+    const int kv = item & 1;
+    t0 = (item >> 1) * a.stretch;
+    if (t0 >= a.T)
+        return;
+    const int64_t t1 = min(t0 + a.stretch, a.T);
+    const T *const x = static_cast<const T *>(a.x[kv]) + h * a.x_head[kv] + c * 16;
     bool nan = false, range = false;
-    for (int64_t t = t0; t < t1; ++t) {
-        const int64_t slot = a.slots[t];
-        if (slot < 0)
-            continue;
-        const int64_t blk = slot / a.block;
-        const int off = static_cast<int>(slot - blk * a.block);
-        if (t > 0 && off != 0 && a.slots[t - 1] == slot - 1)
-            continue;
-        if (blk >= a.n_blocks) {
-            range = true;
-            continue;
+    for (int64_t base = t0; base < t1; base += 32) {
+        // a lane a token: which of them begin a run (every warp of a group finds the same)
+        const int64_t mine = base + lane;
+        int64_t slot_l = -1;
+        bool lead = false;
+        if (mine < t1) {
+            slot_l = a.slots[mine];
+            const int64_t prev = mine > 0 ? a.slots[mine - 1] : -2;
+            lead = slot_l >= 0 && (prev != slot_l - 1 || slot_l % a.block == 0);
         }
-        // the run's length: consecutive slots up to the page's end
-        const int most = static_cast<int>(min(static_cast<int64_t>(a.block - off), a.T - t));
-        if (tid == 0)
-            len_s = most;
-        __syncthreads();
-        for (int i = tid; i < most; i += kWriteThreads)
-            if (a.slots[t + i] != slot + i) {
-                atomicMin(&len_s, i);
-                break;
+        unsigned leads = __ballot_sync(~0u, lead);
+        while (leads) {
+            const int who = __ffs(leads) - 1;
+            leads &= leads - 1;
+            const int64_t t = base + who, slot = __shfl_sync(~0u, slot_l, who), blk = slot / a.block;
+            if (blk >= a.n_blocks) {
+                range = true;
+                continue;
             }
-        __syncthreads();
-        const int len = len_s;
-        float amax = 0.0f;
-        for (int i = row0; i < len; i += R) {
-            float v[16];
-            load16<T>(x + (t + i) * a.x_tok[kv], v);
+            const int off = static_cast<int>(slot - blk * a.block);
+            // the run's length: consecutive slots up to the page's end
+            const int most = static_cast<int>(min(static_cast<int64_t>(a.block - off), a.T - t));
+            int len = most;
+            for (int i = 0; i < most; i += 32) {
+                const unsigned off_run = __ballot_sync(~0u, i + lane < most && a.slots[t + i + lane] != slot + i + lane);
+                if (off_run) {
+                    len = i + __ffs(off_run) - 1;
+                    break;
+                }
+            }
+            float *const sp = a.scale[kv] + blk * a.scb + h * a.sch;
+            const float was = off > 0 ? *sp : 0.0f;
+            uint8_t *const page = a.pool[kv] + blk * a.sb + h * a.sh + c * 16;
+            Raw<T> keep[KEEP];
+            float amax = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-                amax = fmaxf(amax, finite_abs(v[k]));
-        }
+            for (int k = 0; k < KEEP; ++k)
+                if (row0 + k * R < len)
+                    keep[k] = load_raw<T>(x + (t + row0 + k * R) * a.x_tok[kv]);
 #pragma unroll
-        for (int o = 16; o; o >>= 1)
-            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
-        if (lane == 0)
-            red[warp] = amax;
-        __syncthreads();
+            for (int k = 0; k < KEEP; ++k)
+                if (row0 + k * R < len) {
+                    float v[16];
+                    load16<T>(reinterpret_cast<const T *>(&keep[k]), v);
 #pragma unroll
-        for (int w = 0; w < kWriteThreads / 32; ++w)
-            amax = fmaxf(amax, red[w]);
-        float *sp = a.scale[kv] + blk * a.scb + h * a.sch;
-        uint8_t *page = a.pool[kv] + blk * a.sb + h * a.sh + c * 16;
-        const float want = amax > 0.0f ? scale_of<FMT>(amax) : FKV_PAGE_MIN_SCALE;
-        const float was = off > 0 ? *sp : 0.0f;
-        // a page's scale never shrinks while it has rows
-        const float now = was >= want ? was : want;
-        const float inv = __frcp_rn(now);
-        for (int i = row0; i < len; i += R) {
-            float v[16];
-            load16<T>(x + (t + i) * a.x_tok[kv], v);
-            nan |= drop_nan(v);
-            *reinterpret_cast<uint4 *>(page + (off + i) * a.st) = codes16<FMT>(v, inv);
-        }
-        if (now != was) {
-            const float ratio = __fmul_rn(was, inv);
-            for (int i = row0; i < off; i += R) {
-                uint4 *p = reinterpret_cast<uint4 *>(page + i * a.st);
+                    for (int e = 0; e < 16; ++e)
+                        amax = fmaxf(amax, finite_abs(v[e]));
+                }
+            for (int i = row0 + KEEP * R; i < len; i += R) {
                 float v[16];
-                values16<FMT>(*p, v);
-                *p = codes16<FMT>(v, ratio);
+                load16<T>(x + (t + i) * a.x_tok[kv], v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    amax = fmaxf(amax, finite_abs(v[e]));
             }
+#pragma unroll
+            for (int o = 16; o; o >>= 1)
+                amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
+            if (GT > 32) {
+                if (lane == 0)
+                    red[threadIdx.x >> 5] = amax;
+                __syncthreads();           // (also: every thread has read the page's old scale)
+#pragma unroll
+                for (int w = 0; w < GT / 32; ++w)
+                    amax = fmaxf(amax, red[w]);
+            } else {
+                __syncwarp();
+            }
+            const float want = amax > 0.0f ? scale_of<FMT>(amax) : FKV_PAGE_MIN_SCALE;
+            // a page's scale never shrinks while it has rows
+            const float now = was >= want ? was : want;
+            const float inv = __frcp_rn(now);
+#pragma unroll
+            for (int k = 0; k < KEEP; ++k)
+                if (row0 + k * R < len) {
+                    float v[16];
+                    load16<T>(reinterpret_cast<const T *>(&keep[k]), v);
+                    nan |= drop_nan(v);
+                    *reinterpret_cast<uint4 *>(page + (off + row0 + k * R) * a.st) = codes16<FMT>(v, inv);
+                }
+            for (int i = row0 + KEEP * R; i < len; i += R) {
+                float v[16];
+                load16<T>(x + (t + i) * a.x_tok[kv], v);
+                nan |= drop_nan(v);
+                *reinterpret_cast<uint4 *>(page + (off + i) * a.st) = codes16<FMT>(v, inv);
+            }
+            if (now != was) {
+                const float ratio = __fmul_rn(was, inv);
+                for (int i = row0; i < off; i += R) {
+                    uint4 *p = reinterpret_cast<uint4 *>(page + i * a.st);
+                    float v[16];
+                    values16<FMT>(*p, v);
+                    *p = codes16<FMT>(v, ratio);
+                }
+                if (tid == 0)
+                    *sp = now;
+            }
+            if (GT > 32)
+                __syncthreads();           // red is free
         }
-        __syncthreads();       // every thread has read the old scale, red and len_s
-        if (tid == 0)
-            *sp = now;
     }
     if (nan)
         atomicOr(a.status, FKV_ST_CORRUPT);
@@ -517,15 +548,19 @@ template <int D, int FMT, typename T> __global__ void __launch_bounds__(256) k_p
     }
 }
 
-template <int FMT, typename T>
-cudaError_t write_as(const fkv_ctx *ctx, const WriteArgs &a, int dim, dim3 grid, cudaStream_t st)
+template <int D, int FMT, typename T> cudaError_t write_by(const WriteArgs &a, int64_t items, cudaStream_t st)
 {
-    (void)ctx;
-    if (dim == 64)
-        k_page_write<64, FMT, T><<<grid, kWriteThreads, 0, st>>>(a);
+    if (a.stretch == 1)
+        k_page_write<D, FMT, T, 32><<<static_cast<unsigned>((items + 7) / 8), 256, 0, st>>>(a);
     else
-        k_page_write<128, FMT, T><<<grid, kWriteThreads, 0, st>>>(a);
+        k_page_write<D, FMT, T, 128><<<static_cast<unsigned>(items), 128, 0, st>>>(a);
     return cudaGetLastError();
+}
+
+template <int FMT, typename T> cudaError_t write_as(const WriteArgs &a, int dim, cudaStream_t st)
+{
+    const int64_t items = (a.T + a.stretch - 1) / a.stretch * 2 * a.heads;
+    return dim == 64 ? write_by<64, FMT, T>(a, items, st) : write_by<128, FMT, T>(a, items, st);
 }
 
 template <int FMT, typename T> cudaError_t read_as(const ReadArgs &a, int dim, dim3 grid, cudaStream_t st)
@@ -552,12 +587,20 @@ cudaError_t launch_page_plan(const fkv_ctx *ctx, const int32_t *n_new, const int
     a.n_req = static_cast<int>(n_req), a.width = static_cast<int>(width), a.block = block;
     a.div = FastDiv::make(block);
     a.status = ctx->d_status;
-    const void *fn = reinterpret_cast<const void *>(k_page_plan);
-    const cudaError_t e = kernel_use(ctx, fn, kPlanThreads, sizeof(PlanSmem), nullptr);
+    a.share = (a.n_req + kPlanThreads - 1) / kPlanThreads;
+    // one launch while the block's own stores take less than a second launch
+    // does (about 4 us: 4096 rows)
+    a.with_rows = rows <= 4 * kPlanThreads;
+    const size_t smem = (static_cast<size_t>(a.n_req) + 1) * 3 * sizeof(int);
+    cudaError_t e = kernel_use(ctx, reinterpret_cast<const void *>(k_page_plan), kPlanThreads, kPlanSmem, nullptr);
     if (e != cudaSuccess)
         return e;
-    k_page_plan<<<kPlanBlocks, kPlanThreads, sizeof(PlanSmem), st>>>(a);
-    return cudaGetLastError();
+    k_page_plan<<<1, kPlanThreads, smem, st>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || a.with_rows)
+        return e;
+    const int64_t per = kSlotThreads * kSlotRows;
+    return launch_after(k_page_slots, static_cast<unsigned>((rows + per - 1) / per), kSlotThreads, 0, st, a);
 }
 
 cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
@@ -577,18 +620,18 @@ cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_
     a.scb = p->scale_stride_block, a.sch = p->scale_stride_head;
     a.n_blocks = p->n_blocks, a.block = p->block;
     a.status = ctx->d_status;
-    // one token a block while that keeps the blocks to a few waves, else 16
-    a.stretch = T * p->n_heads * 2 <= static_cast<int64_t>(ctx->sms) * 64 ? 1 : 16;
-    const dim3 grid(static_cast<unsigned>((T + a.stretch - 1) / a.stretch), p->n_heads, 2);
+    // a warp a token while that fills the device up to a few times over, else a
+    // block for as many tokens as a page holds
+    a.heads = p->n_heads;
+    a.stretch = T * p->n_heads * 2 <= static_cast<int64_t>(ctx->sms) * 64 ? 1 : p->block;
     const bool i8 = p->format == FKV_INT8;
     switch (k->dtype) {
     case FKV_F32:
-        return i8 ? write_as<FKV_INT8, float>(ctx, a, p->dim, grid, st) : write_as<FKV_E4M3, float>(ctx, a, p->dim, grid, st);
+        return i8 ? write_as<FKV_INT8, float>(a, p->dim, st) : write_as<FKV_E4M3, float>(a, p->dim, st);
     case FKV_F16:
-        return i8 ? write_as<FKV_INT8, __half>(ctx, a, p->dim, grid, st) : write_as<FKV_E4M3, __half>(ctx, a, p->dim, grid, st);
+        return i8 ? write_as<FKV_INT8, __half>(a, p->dim, st) : write_as<FKV_E4M3, __half>(a, p->dim, st);
     default:
-        return i8 ? write_as<FKV_INT8, __nv_bfloat16>(ctx, a, p->dim, grid, st)
-                  : write_as<FKV_E4M3, __nv_bfloat16>(ctx, a, p->dim, grid, st);
+        return i8 ? write_as<FKV_INT8, __nv_bfloat16>(a, p->dim, st) : write_as<FKV_E4M3, __nv_bfloat16>(a, p->dim, st);
     }
 }
 

@@ -8,6 +8,21 @@
 #define FKV_PAGE_MIN_SCALE 7.888609052210118e-31f
 
 #ifdef __CUDACC__
+// Launch `kernel` so that its blocks may be scheduled while the stream's
+// previous kernel ends; it waits (griddepcontrol.wait) before it reads what that
+// one wrote.
+template <typename... Args, typename... Given>
+cudaError_t launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Given &...args)
+{
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid, cfg.blockDim = block, cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cfg.attrs = &at, cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 namespace fkvd {
 
 // Two e4m3 codes (the lower byte first) as two fp16, exactly.
