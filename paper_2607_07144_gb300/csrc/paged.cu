@@ -1,6 +1,8 @@
 // The paged 8-bit K/V cache: block tables and slot maps from request lengths
 // (k_page_plan), quantising writes (k_page_write) and the way back to a K/V
 // cache (k_page_read).  Attention over the pages is in attend.cu.
+#include <type_traits>
+
 #include "paged.cuh"
 
 using namespace fkvd;
@@ -8,14 +10,15 @@ using namespace fkvd;
 namespace {
 
 // ------------------------------------------------------------------ plan --
-// One block scans the requests (tokens, pages given back, pages needed), a
+// A block scans the requests (tokens, pages given back, pages needed), a
 // consecutive share a thread, and does everything that is counted in pages: the
 // stack, the tables, the lengths.  The tokens' slots and positions follow from
 // those; a few are written by the same block, more by a second launch that
-// starts while the first one ends (one block's stores would take 160 us for half
-// a million tokens where the second launch takes 6).  Latency bounds both: each
-// is a chain of three or four loads.
-constexpr int kPlanThreads = 1024;
+// starts while the first one ends.  Where there is that much to do, the first
+// launch is a cluster of eight blocks, which all scan and share the pages: no
+// counter in memory orders them, so calls (and graphs) that overlap share
+// nothing.  Latency bounds both launches: each is a chain of three or four loads.
+constexpr int kPlanThreads = 1024, kPlanCluster = 8;
 constexpr int kPlanSmem = (FKV_PAGE_MAX_REQ + 1) * 3 * sizeof(int);
 constexpr int kSlotThreads = 256, kSlotRows = 4;       // the second launch: rows a thread
 
@@ -57,6 +60,16 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
     int *const cu = sums, *const need = sums + a.n_req + 1, *const back = need + a.n_req + 1;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r0 = min(tid * a.share, a.n_req), r1 = min(r0 + a.share, a.n_req);
+    // of all the launch's threads
+    const int blocks = static_cast<int>(gridDim.x), gtid = static_cast<int>(blockIdx.x) * kPlanThreads + tid, gsize = blocks * kPlanThreads;
+    auto sync = [&]() {
+        if (blocks > 1) {
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        } else {
+            __syncthreads();
+        }
+    };
     const int taken0 = *a.taken;
     if (tid == 0)
         bad_s = 0;
@@ -129,16 +142,27 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
         cu[a.n_req] = tokens;
     __syncthreads();
     // pages that come back go onto the stack before any is taken from it
-    for (int i = tid; i < (bad ? 0 : all[2]); i += kPlanThreads) {
+    for (int i = gtid; i < (bad ? 0 : all[2]); i += gsize) {
         const int r = last_from(back, a.n_req, i);
         a.free_ids[taken1 + i] = a.table[r * a.table_stride + i - back[r]];
     }
-    __syncthreads();
-    for (int r = tid; r <= a.n_req; r += kPlanThreads)
+    sync();
+    for (int r = gtid; r <= a.n_req; r += gsize)
         a.cu[r] = cu[r];
-    for (int i = tid; i < pages; i += kPlanThreads) {
-        const int r = last_from(need, a.n_req, i);
-        a.table[r * a.table_stride + blocks_of(a, a.kv_len[r]) + i - need[r]] = a.free_ids[taken1 + i];
+    for (int i = gtid; i < pages; i += 4 * gsize) {
+        // four at a time, their loads in flight together
+        int id[4], len[4], r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int x = min(i + k * gsize, pages - 1);
+            r[k] = last_from(need, a.n_req, x);
+            id[k] = a.free_ids[taken1 + x];
+            len[k] = a.kv_len[r[k]];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k * gsize < pages)
+                a.table[r[k] * a.table_stride + blocks_of(a, len[k]) + i + k * gsize - need[r[k]]] = id[k];
     }
     if (a.with_rows) {
         for (int t = tid; t < a.rows; t += kPlanThreads) {
@@ -155,48 +179,58 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
             a.positions[t] = pos;
         }
     }
-    __syncthreads();
+    sync();
     // nothing reads lengths or the taken count from here on: the outputs may be
     // the inputs' own arrays
-    for (int r = tid; r < a.n_req; r += kPlanThreads) {
+    for (int r = gtid; r < a.n_req; r += gsize) {
         const int nn = a.n_new[r], len = a.kv_len[r];
         a.kv_len_out[r] = bad ? len : (nn < 0 ? 0 : len + nn);
     }
-    if (tid == 0) {
+    if (gtid == 0) {
         *a.taken_out = bad ? taken0 : static_cast<int>(taken1 + all[1]);
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);
     }
 }
 
-// Slots and positions from the plan's tables, lengths and sums: a token's
-// request is searched for among those that the block's tokens span.
+// Slots and positions from the plan's tables, lengths and sums.  A token's
+// request is searched for in the sums, which a block first copies to shared
+// memory (up to kSlotSums of them; more are searched where they lie).
+constexpr int kSlotSums = 8192;
+
 __global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanArgs a)
 {
-    __shared__ int span[2];
+    extern __shared__ int sums[];
     const int tid = threadIdx.x;
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * (kSlotThreads * kSlotRows);
     asm volatile("griddepcontrol.wait;" ::: "memory");     // the plan has run
-    const int tokens = a.cu[a.n_req];
-    if (tid < 2 && t0 < tokens)
-        span[tid] = last_from(a.cu, a.n_req, static_cast<int>(tid ? min(t0 + kSlotThreads * kSlotRows, static_cast<int64_t>(tokens)) - 1 : t0));
-    __syncthreads();
+    const bool copied = a.n_req < kSlotSums;
+    if (copied) {
+        for (int i = tid; i <= a.n_req; i += kSlotThreads)
+            sums[i] = a.cu[i];
+        __syncthreads();
+    }
+    const int *const cu = copied ? sums : a.cu;
+    const int tokens = cu[a.n_req];
+    int r[kSlotRows], id[kSlotRows], pos[kSlotRows];
+#pragma unroll
+    for (int i = 0; i < kSlotRows; ++i) {
+        const int t = static_cast<int>(min(t0 + i * kSlotThreads + tid, static_cast<int64_t>(tokens) - 1));
+        r[i] = t >= 0 ? last_from(cu, a.n_req, t) : 0;
+        pos[i] = t >= 0 ? a.kv_len_out[r[i]] - cu[r[i] + 1] + t : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kSlotRows; ++i)
+        id[i] = tokens > 0 ? a.table[r[i] * a.table_stride + a.div.div(pos[i])] : -1;
 #pragma unroll
     for (int i = 0; i < kSlotRows; ++i) {
         const int64_t t = t0 + i * kSlotThreads + tid;
         if (t >= a.rows)
             return;
-        int64_t slot = -1;
-        int pos = -1;
-        if (t < tokens) {
-            const int lo = span[0], r = lo + last_from(a.cu + lo, span[1] - lo + 1, static_cast<int>(t));
-            const int c0 = a.cu[r];
-            pos = a.kv_len_out[r] - (a.cu[r + 1] - c0) + static_cast<int>(t) - c0;
-            const int j = static_cast<int>(a.div.div(pos)), id = a.table[r * a.table_stride + j];
-            slot = id < 0 ? -1 : static_cast<int64_t>(id) * a.block + pos - j * a.block;
-        }
-        a.slots[t] = slot;
-        a.positions[t] = pos;
+        const bool live = t < tokens;
+        const int off = pos[i] - static_cast<int>(a.div.div(pos[i])) * a.block;
+        a.slots[t] = live && id[i] >= 0 ? static_cast<int64_t>(id[i]) * a.block + off : -1;
+        a.positions[t] = live ? pos[i] : -1;
     }
 }
 
@@ -335,6 +369,55 @@ template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *p)
     return r;
 }
 
+// The largest magnitude of some elements, two at a time for 16-bit types; a NaN
+// makes it NaN.
+template <typename T> struct Largest {
+    uint32_t m = 0;
+    __device__ __forceinline__ void take(const Raw<T> &r)
+    {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&r);
+#pragma unroll
+        for (int i = 0; i < 4 * static_cast<int>(sizeof(T)); ++i) {
+            if (std::is_same<T, float>::value)
+                // magnitudes compare as integers do, NaN above infinity
+                m = max(m, w[i] & 0x7fffffffu);
+            else if (std::is_same<T, __half>::value)
+                asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
+            else
+                asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
+        }
+    }
+    __device__ __forceinline__ float value() const
+    {
+        if (std::is_same<T, float>::value)
+            return __uint_as_float(m);
+        if (std::is_same<T, __half>::value) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&m));
+            return f.x != f.x || f.y != f.y ? __uint_as_float(0x7fffffffu) : fmaxf(f.x, f.y);
+        }
+        const uint32_t b = max(m & 0xffffu, m >> 16);
+        return __uint_as_float(b << 16);
+    }
+};
+
+// codes16 of values of at most the scale's range: no limits to look at, and an
+// int8's rounding is an addition of 1.5 2^23, whose sum's low byte is the code.
+template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *x, float inv)
+{
+    if (FMT == FKV_E4M3)
+        return codes16<FMT>(x, inv);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            q[k] = __float_as_uint(__fadd_rn(__fmul_rn(x[4 * i + k], inv), 12582912.0f));
+        w[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A run of tokens with consecutive slots inside one page belongs to the group of
 // GT threads whose stretch of tokens holds its first one, for one head and K or
 // V; the group reads and writes that page and its scale alone: no atomics, and
@@ -346,7 +429,7 @@ template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *p)
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT) k_page_write(WriteArgs a)
 {
     constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
-    __shared__ float red[GT / 32];
+    __shared__ uint32_t red[GT / 32];
     const int lane = threadIdx.x & 31, tid = GT == 32 ? lane : threadIdx.x, c = tid % C, row0 = tid / C;
     int64_t t0, item = blockIdx.x;
     if (GT == 32)
@@ -394,58 +477,66 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
             const float was = off > 0 ? *sp : 0.0f;
             uint8_t *const page = a.pool[kv] + blk * a.sb + h * a.sh + c * 16;
             Raw<T> keep[KEEP];
-            float amax = 0.0f;
+            Largest<T> most_v;
 #pragma unroll
             for (int k = 0; k < KEEP; ++k)
                 if (row0 + k * R < len)
                     keep[k] = load_raw<T>(x + (t + row0 + k * R) * a.x_tok[kv]);
 #pragma unroll
             for (int k = 0; k < KEEP; ++k)
-                if (row0 + k * R < len) {
+                if (row0 + k * R < len)
+                    most_v.take(keep[k]);
+            for (int i = row0 + KEEP * R; i < len; i += R)
+                most_v.take(load_raw<T>(x + (t + i) * a.x_tok[kv]));
+            // as integers: magnitudes, a NaN above all
+            uint32_t amax_u = __float_as_uint(most_v.value());
+            auto join = [&]() {
+                amax_u = __reduce_max_sync(~0u, amax_u);
+                if (GT > 32) {
+                    __syncthreads();       // red is free (also: every thread has read the page's old scale)
+                    if (lane == 0)
+                        red[threadIdx.x >> 5] = amax_u;
+                    __syncthreads();
+#pragma unroll
+                    for (int w = 0; w < GT / 32; ++w)
+                        amax_u = max(amax_u, red[w]);
+                }
+            };
+            join();
+            const bool odd = amax_u >= 0x7f800000u;          // infinities or NaN among the values
+            if (odd) {
+                // rare: the largest finite magnitude
+                float amax = 0.0f;
+                for (int i = row0; i < len; i += R) {
                     float v[16];
-                    load16<T>(reinterpret_cast<const T *>(&keep[k]), v);
+                    load16<T>(x + (t + i) * a.x_tok[kv], v);
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         amax = fmaxf(amax, finite_abs(v[e]));
                 }
-            for (int i = row0 + KEEP * R; i < len; i += R) {
-                float v[16];
-                load16<T>(x + (t + i) * a.x_tok[kv], v);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    amax = fmaxf(amax, finite_abs(v[e]));
+                amax_u = __float_as_uint(amax);
+                join();
             }
-#pragma unroll
-            for (int o = 16; o; o >>= 1)
-                amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
-            if (GT > 32) {
-                if (lane == 0)
-                    red[threadIdx.x >> 5] = amax;
-                __syncthreads();           // (also: every thread has read the page's old scale)
-#pragma unroll
-                for (int w = 0; w < GT / 32; ++w)
-                    amax = fmaxf(amax, red[w]);
-            } else {
-                __syncwarp();
-            }
-            const float want = amax > 0.0f ? scale_of<FMT>(amax) : FKV_PAGE_MIN_SCALE;
+            const float want = amax_u ? scale_of<FMT>(__uint_as_float(amax_u)) : FKV_PAGE_MIN_SCALE;
             // a page's scale never shrinks while it has rows
             const float now = was >= want ? was : want;
             const float inv = __frcp_rn(now);
+            if (!odd) {
 #pragma unroll
-            for (int k = 0; k < KEEP; ++k)
-                if (row0 + k * R < len) {
-                    float v[16];
-                    load16<T>(reinterpret_cast<const T *>(&keep[k]), v);
-                    nan |= drop_nan(v);
-                    *reinterpret_cast<uint4 *>(page + (off + row0 + k * R) * a.st) = codes16<FMT>(v, inv);
-                }
-            for (int i = row0 + KEEP * R; i < len; i += R) {
+                for (int k = 0; k < KEEP; ++k)
+                    if (row0 + k * R < len) {
+                        float v[16];
+                        load16<T>(reinterpret_cast<const T *>(&keep[k]), v);
+                        *reinterpret_cast<uint4 *>(page + (off + row0 + k * R) * a.st) = codes16_inside<FMT>(v, inv);
+                    }
+            }
+            for (int i = odd ? row0 : row0 + KEEP * R; i < len; i += R) {
                 float v[16];
                 load16<T>(x + (t + i) * a.x_tok[kv], v);
                 nan |= drop_nan(v);
                 *reinterpret_cast<uint4 *>(page + (off + i) * a.st) = codes16<FMT>(v, inv);
             }
+            __syncwarp();
             if (now != was) {
                 const float ratio = __fmul_rn(was, inv);
                 for (int i = row0; i < off; i += R) {
@@ -457,8 +548,6 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
                 if (tid == 0)
                     *sp = now;
             }
-            if (GT > 32)
-                __syncthreads();           // red is free
         }
     }
     if (nan)
@@ -595,12 +684,22 @@ cudaError_t launch_page_plan(const fkv_ctx *ctx, const int32_t *n_new, const int
     cudaError_t e = kernel_use(ctx, reinterpret_cast<const void *>(k_page_plan), kPlanThreads, kPlanSmem, nullptr);
     if (e != cudaSuccess)
         return e;
-    k_page_plan<<<1, kPlanThreads, smem, st>>>(a);
-    e = cudaGetLastError();
-    if (e != cudaSuccess || a.with_rows)
+    if (a.with_rows) {
+        k_page_plan<<<1, kPlanThreads, smem, st>>>(a);
+        return cudaGetLastError();
+    }
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = kPlanCluster, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kPlanCluster), cfg.blockDim = dim3(kPlanThreads), cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cfg.attrs = &at, cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, k_page_plan, a);
+    if (e != cudaSuccess)
         return e;
     const int64_t per = kSlotThreads * kSlotRows;
-    return launch_after(k_page_slots, static_cast<unsigned>((rows + per - 1) / per), kSlotThreads, 0, st, a);
+    const size_t sums = a.n_req < kSlotSums ? (static_cast<size_t>(a.n_req) + 1) * sizeof(int) : 0;
+    return launch_after(k_page_slots, static_cast<unsigned>((rows + per - 1) / per), kSlotThreads, sums, st, a);
 }
 
 cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
