@@ -468,32 +468,48 @@ typedef struct {
 } fkv_rows;
 
 /* Block tables and slot maps from request lengths, on the device.  For each
- * request r < n_req (at most FKV_PAGE_MAX_REQ), kv_len_dev[r] positions are in
- * its pages and n_new_dev[r] tokens follow, or n_new_dev[r] < 0: the request
- * ends and gives its pages back.
- *   table_dev   int32 [n_req][table_stride], `width` columns used: request r's
- *               pages in order; entries of new pages are added, the others
- *               left as they are (an ended request's too)
- *   free_dev    int32 [n_free]: a stack of page ids whose first *taken_dev
- *               entries have been given out.  Pages given back are put before
- *               entry *taken_dev, in the order of the requests and of their
- *               positions; new pages are then taken in the same order
- *   taken_dev   int32, kv_len_dev int32 [n_req]; their new values go to
- *               taken_out_dev and kv_len_out_dev, which may be the same arrays
- *               (an ended request's length is 0)
- *   cu_dev      int32 [n_req + 1]: request r's tokens are rows cu[r] .. cu[r+1]
- *   slots_dev   int64 [rows]: page id x block + position in the page of each
- *               token's place, -1 from row cu[n_req] on
- *   pos_dev     int32 [rows]: its position in the request, -1 likewise
+ * request r < n_req (at most FKV_PAGE_MAX_REQ), kv_len[r] positions are in its
+ * pages and n_new[r] tokens follow, or n_new[r] < 0: the request ends and gives
+ * its pages back.  All arrays are device memory:
+ *   table   [n_req][table_stride], `width` columns used: request r's pages in
+ *           order; entries of new pages are added, the others left as they are
+ *           (an ended request's too)
+ *   free    [n_free]: a stack of page ids whose first *taken entries have been
+ *           given out.  Pages given back are put before entry *taken, in the
+ *           order of the requests and of their positions; new pages are then
+ *           taken in the same order
+ *   taken, kv_len [n_req]: their new values go to taken_out and kv_len_out,
+ *           which may be the same arrays (an ended request's length is 0)
+ *   cu      [n_req + 1]: request r's tokens are rows cu[r] .. cu[r+1]
+ *   slots   [rows]: page id x block + position in the page of each token's
+ *           place, -1 from row cu[n_req] on
+ *   pos     [rows]: its position in the request, -1 likewise
  * A page belongs to one request.  A call that does not fit is not carried out:
- * a negative length, one above FKV_PAGE_MAX_LEN, more than `width` pages, more
- * tokens than rows, more pages than are free, or more given back than were
- * taken.  It sets FKV_ERANGE in the status word, copies lengths and count, sets
- * every cu to 0 and every slot and position to -1, and changes nothing else. */
-int fkv_page_plan(fkv_ctx *ctx, const int32_t *n_new_dev, const int32_t *kv_len_dev, int64_t n_req,
-                  int32_t *table_dev, int64_t table_stride, int64_t width, int32_t *free_dev, int64_t n_free,
-                  const int32_t *taken_dev, int block, int32_t *cu_dev, int64_t *slots_dev, int32_t *pos_dev,
-                  int64_t rows, int32_t *kv_len_out_dev, int32_t *taken_out_dev, void *stream);
+ * a negative length, one that is or becomes more than FKV_PAGE_MAX_LEN, more
+ * than `width` pages, more tokens than rows, more pages than are free, or more
+ * given back than were taken.  It sets FKV_ERANGE in the status word, copies
+ * lengths and count, sets every cu to 0 and every slot and position to -1, and
+ * changes nothing else. */
+typedef struct {
+    const int32_t *n_new;
+    const int32_t *kv_len;
+    int32_t *table;
+    int32_t *free;
+    const int32_t *taken;
+    int32_t *cu;
+    int64_t *slots;
+    int32_t *pos;
+    int32_t *kv_len_out;
+    int32_t *taken_out;
+    int64_t n_req;
+    int64_t table_stride;
+    int64_t width;
+    int64_t n_free;
+    int64_t rows;
+    int64_t block;          /* positions a page, as fkv_pages */
+} fkv_plan;
+
+int fkv_page_plan(fkv_ctx *ctx, const fkv_plan *plan, void *stream);
 
 /* Quantise the K and V vectors of n_tok tokens (k and v: n_heads heads, the
  * same dtype) into the slots slots_dev[t] (int64; negative: the token is
@@ -513,48 +529,64 @@ int fkv_page_plan(fkv_ctx *ctx, const int32_t *n_new_dev, const int32_t *kv_len_
 int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, const fkv_rows *v,
                    const int64_t *slots_dev, int64_t n_tok, void *stream);
 
-/* Options of fkv_page_attend. */
-typedef struct {
-    float scale;                 /* multiplies q.k */
-    float softcap;               /* cap > 0: s becomes cap tanh(s / cap); 0: none */
-    int causal;                  /* 1: no position after a row's own */
-    int64_t window;              /* w > 0: only the w positions up to the row's own, and */
-    int64_t sinks;               /*   the request's first `sinks` ones; 0: no window */
-    const float *slopes;         /* device, [n_q_heads], or NULL: adds slope x (j - p) */
-    const int32_t *prefix;       /* device, [n_req], or NULL: the first prefix[r] positions
-                                    are seen by every row of request r */
-} fkv_attend;
-
 /* Attention of a batch's query rows over the pages.  q: n_tok tokens of
  * n_q_heads heads (FKV_F16 or FKV_BF16), n_q_heads a multiple of
  * pages->n_heads: query head u reads KV head u / (n_q_heads / n_heads).
- * Request r's tokens are rows cu_dev[r] .. cu_dev[r+1] of q and the last of its
- * kv_len_dev[r] positions (all in the pages): token i lies at position
+ * Request r's tokens are rows cu[r] .. cu[r+1] of q and the last of its
+ * kv_len[r] positions (all in the pages): token i lies at position
  * p = kv_len[r] - n_new + i.  It sees position j < kv_len[r] if j < prefix[r],
  * or if (j <= p, unless causal is 0) and (there is no window, or j > p - window,
  * or j < sinks); a token at a negative position sees nothing.
- *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q.k_j) + slope (j - p)
- * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse_dev
- * (float32 [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row
- * that sees nothing gets zeros and -infinity.  What masked positions and slots
- * past a request's end hold does not matter.  Sums, maxima and weights are held
- * in float32; the weights are rounded to fp16 for the product with V.
- * table_dev, table_stride and width as in fkv_page_plan.  max_new and max_len
- * bound n_new and kv_len of every request (they size the launch).  A request
- * whose numbers do not hold together (cu not increasing or past n_tok, a length
- * past max_new, max_len or the table) is skipped, its rows left as they are, a
- * page id outside the pool gives the row unspecified values, and either sets
+ *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q.k_j) + slope (j - p),
+ *     f(s) = cap tanh(s / cap) if softcap = cap > 0, else s,
+ * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse (float32
+ * [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row that sees
+ * nothing gets zeros and -infinity.  What masked positions and slots past a
+ * request's end hold does not matter.  Sums, maxima and weights are held in
+ * float32; the weights are rounded to fp16 for the product with V.
+ * table, table_stride and width as in fkv_page_plan.  max_new and max_len bound
+ * n_new and kv_len of every request (they size the launch).  A request whose
+ * numbers do not hold together (cu not increasing or past n_tok, a length past
+ * max_new, max_len or the table) is skipped, its rows left as they are, a page
+ * id outside the pool gives the row unspecified values, and either sets
  * FKV_ERANGE in the status word.  Rows of no request are left as they are.
- * workspace_dev: fkv_page_attend_workspace(...) bytes for the same arguments,
- * 256-byte aligned (NULL when that is 0), the caller's own until the call has
- * run: calls that may overlap need one each.  The bytes depend on the sizes
- * alone, so a captured call can be replayed with other lengths. */
-int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pages, int64_t n_tok, int n_q_heads,
-                                  int64_t n_req, int64_t max_new, int64_t max_len, const fkv_attend *opt);
-int fkv_page_attend(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *q, int64_t n_tok, int n_q_heads,
-                    const int32_t *cu_dev, const int32_t *kv_len_dev, int64_t n_req, const int32_t *table_dev,
-                    int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len, const fkv_attend *opt,
-                    const fkv_rows *out, float *lse_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+ * workspace: fkv_page_attend_workspace(ctx, a) bytes, 256-byte aligned (NULL
+ * when that is 0), the caller's own until the call has run: calls that may
+ * overlap need one each.  The bytes depend on the sizes alone, so a captured
+ * call can be replayed with other lengths. */
+typedef struct {
+    const fkv_pages *pages;      /* host struct, read by the call */
+    const void *q;               /* vectors by (token, head) as fkv_rows: 16-byte */
+    void *out;                   /*   boundaries, element strides below */
+    float *lse;                  /* or NULL */
+    const int32_t *cu;           /* device, [n_req + 1] */
+    const int32_t *kv_len;       /* device, [n_req] */
+    const int32_t *table;        /* device, [n_req][table_stride] */
+    const float *slopes;         /* device, [n_q_heads], or NULL: adds slope x (j - p) */
+    const int32_t *prefix;       /* device, [n_req], or NULL: the first prefix[r] positions
+                                    are seen by every row of request r */
+    int64_t q_stride_tok;
+    int64_t q_stride_head;
+    int64_t out_stride_tok;
+    int64_t out_stride_head;
+    int64_t n_tok;
+    int64_t n_req;
+    int64_t table_stride;
+    int64_t width;
+    int64_t max_new;
+    int64_t max_len;
+    int64_t window;              /* w > 0: only the w positions up to the row's own, and */
+    int64_t sinks;               /*   the request's first `sinks` ones; 0: no window */
+    int32_t dtype;               /* of q and out: FKV_F16 or FKV_BF16 */
+    int32_t n_q_heads;
+    int32_t causal;              /* 1: no position after a row's own */
+    float scale;                 /* multiplies q.k */
+    float softcap;               /* cap > 0: s becomes cap tanh(s / cap); 0: none */
+    int32_t reserved;            /* 0 */
+} fkv_attend;
+
+int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_attend *a);
+int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Rebuild positions [t0, min(t1, kv_len_dev[r])) of every request r < n_req
  * into layer `layer`, sequence r of k_out and v_out (either may be NULL; views

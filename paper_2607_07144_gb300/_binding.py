@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 import numpy as np
@@ -53,15 +54,12 @@ class _Pages(ctypes.Structure):
                 ("scale_stride_block", ctypes.c_int64), ("scale_stride_head", ctypes.c_int64)]
 
 
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("stride_tok", ctypes.c_int64),
-                ("stride_head", ctypes.c_int64)]
-
-
-class _Attend(ctypes.Structure):
-    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("causal", ctypes.c_int),
-                ("window", ctypes.c_int64), ("sinks", ctypes.c_int64), ("slopes", ctypes.c_void_p),
-                ("prefix", ctypes.c_void_p)]
+# fkv_cache, fkv_rows, fkv_plan and fkv_attend, packed: filling a buffer takes a tenth of
+# the time of as many ctypes arguments
+_CACHE = struct.Struct("@Pi6q")
+_ROWS = struct.Struct("@Piqq")
+_PLAN = struct.Struct("@10P6q")
+_ATTEND = struct.Struct("@9P12q3i2fi")
 
 
 # name -> (restype, argtypes)
@@ -98,11 +96,10 @@ SIGNATURES = {
     "fkv_decode_kv_static": (_I, [_P, _P, _I64, _I64, _P, _P, _I64, _P]),
     "fkv_read_kv": (_I, [_P, _P, _I64, _I64, _I64, _P, _I64, _P, _I, _P]),
     "fkv_cache_upload": (_I, [_P, _P, _P, _I64, _I64, _P]),
-    "fkv_page_plan": (_I, [_P, _P, _P, _I64, _P, _I64, _I64, _P, _I64, _P, _I, _P, _P, _P, _I64, _P, _P, _P]),
+    "fkv_page_plan": (_I, [_P, _P, _P]),
     "fkv_page_write": (_I, [_P, _P, _P, _P, _P, _I64, _P]),
-    "fkv_page_attend_workspace": (_I64, [_P, _P, _I64, _I, _I64, _I64, _I64, _P]),
-    "fkv_page_attend": (_I, [_P, _P, _P, _I64, _I, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _P, _P, _P, _P, _I64,
-                             _P]),
+    "fkv_page_attend_workspace": (_I64, [_P, _P]),
+    "fkv_page_attend": (_I, [_P, _P, _P, _I64, _P]),
     "fkv_page_read": (_I, [_P, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _P, _P, _P]),
     "fkv_streams_create": (_I, [_P, _I64, _I64, ctypes.POINTER(_P)]),
     "fkv_streams_destroy": (_I, [_P]),
@@ -118,6 +115,8 @@ def lib():
     """The loaded library.  Raises if it has not been built: there is no
     fallback implementation."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -180,27 +179,30 @@ def cache_view(t: torch.Tensor, host: bool = False) -> _Cache:
     return _Cache(t.data_ptr(), _DTYPE[t.dtype], t.shape[1], t.shape[3], st[0], st[1], st[2], st[3])
 
 
-def _rows_view(t: torch.Tensor, dim: int, what: str) -> _Rows:
-    """fkv_rows view of a CUDA tensor [tokens, heads, dim] (contiguous dim)."""
-    st = t.stride()
-    if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1) or not t.is_cuda or t.shape[2] != dim or t.dtype not in _DTYPE:
+_I32, _INT64, _FLOAT = torch.int32, torch.int64, torch.float32
+
+
+def _vectors(t: torch.Tensor, dim: int, what: str):
+    """(pointer, dtype, shape, token stride, head stride) of a CUDA tensor [tokens, heads, dim] (contiguous dim)."""
+    shape, st, dt = t.shape, t.stride(), _DTYPE.get(t.dtype)
+    if len(st) != 3 or st[2] != 1 or shape[2] != dim or dt is None or not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor [tokens, heads, %d] with contiguous dim" % (what, dim))
     # the stride of a dimension of one is never used, but has to be a valid one
-    return _Rows(t.data_ptr(), _DTYPE[t.dtype], st[0] if t.shape[0] > 1 else dim, st[1] if t.shape[1] > 1 else dim)
+    return t.data_ptr(), dt, shape, st[0] if shape[0] > 1 else dim, st[1] if shape[1] > 1 else dim
 
 
 def _array(t: torch.Tensor, dtype, numel: int, what: str):
     """Pointer of a contiguous CUDA array of at least `numel` elements."""
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("%s must be a contiguous CUDA %s tensor of %d elements" % (what, dtype, numel))
     return t.data_ptr()
 
 
 def _table(t: torch.Tensor, n_req: int):
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] < n_req or (t.shape[1] > 1 and
-                                                                                        t.stride(1) != 1):
+    shape, st = t.shape, t.stride()
+    if t.dtype is not _I32 or len(shape) != 2 or shape[0] < n_req or (shape[1] > 1 and st[1] != 1) or not t.is_cuda:
         raise ValueError("block_table must be a CUDA int32 tensor [requests, pages]")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1]), t.shape[1]
+    return t.data_ptr(), st[0] if shape[0] > 1 else max(1, shape[1]), shape[1]
 
 
 class Pages:
@@ -223,6 +225,7 @@ class Pages:
         self._c = _Pages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _FORMAT[k.dtype],
                          self.heads, self.dim, self.block, self.n_blocks, st[0], st[1], st[2], ss[0], ss[1])
         self._ref = ctypes.byref(self._c)
+        self._addr = ctypes.addressof(self._c)
 
     @classmethod
     def empty(cls, n_blocks: int, heads: int, block: int, dim: int, dtype=torch.float8_e4m3fn, device="cuda"):
@@ -266,6 +269,12 @@ class Context:
         self._cb_arrays = None
         if rc != OK:
             raise FkvError(rc, "fkv_create(N=%d, r=%r, span_len=%d) rejected" % (self.N, self.r, self.L))
+        # argument blocks of the paged calls (calls on one context are serialised)
+        self._plan = ctypes.create_string_buffer(_PLAN.size)
+        self._rows = [ctypes.create_string_buffer(_ROWS.size) for _ in range(2)]
+        self._attend = ctypes.create_string_buffer(_ATTEND.size)
+        self._caches = [ctypes.create_string_buffer(_CACHE.size) for _ in range(2)]
+        self._attend_need = {}
         # symbols are uint8 up to N = 256, uint16 above; torch.int16 holds the
         # uint16 symbols bit for bit (every symbol is below 1024)
         self.sym_bytes = L.fkv_symbol_bytes(self._h)
@@ -532,28 +541,33 @@ class Context:
         stack `free` are updated, kv_len and taken in place unless their outputs
         are given.  slots and positions may have more rows than there are tokens:
         -1 behind the last."""
-        n = n_new.numel()
-        i32 = torch.int32
+        n, rows = n_new.numel(), slots.numel()
         tp, ts, tw = _table(block_table, n)
-        if slots.numel() != positions.numel():
+        if positions.numel() != rows:
             raise ValueError("slots and positions must have the same length")
-        kv_len_out = kv_len if kv_len_out is None else kv_len_out
-        taken_out = taken if taken_out is None else taken_out
-        self._check(lib().fkv_page_plan(
-            self._h, _array(n_new, i32, n, "n_new"), _array(kv_len, i32, n, "kv_len"), n, tp, ts, tw,
-            _array(free, i32, 0, "free"), free.numel(), _array(taken, i32, 1, "taken"), int(block),
-            _array(cu, i32, n + 1, "cu"), _array(slots, torch.int64, 0, "slots"),
-            _array(positions, i32, 0, "positions"), slots.numel(), _array(kv_len_out, i32, n, "kv_len_out"),
-            _array(taken_out, i32, 1, "taken_out"), _stream(stream)))
+        lp, kp = _array(kv_len, _I32, n, "kv_len"), _array(taken, _I32, 1, "taken")
+        _PLAN.pack_into(
+            self._plan, 0, _array(n_new, _I32, n, "n_new"), lp, tp, _array(free, _I32, 0, "free"), kp,
+            _array(cu, _I32, n + 1, "cu"), _array(slots, _INT64, 0, "slots"), _array(positions, _I32, 0, "positions"),
+            lp if kv_len_out is None else _array(kv_len_out, _I32, n, "kv_len_out"),
+            kp if taken_out is None else _array(taken_out, _I32, 1, "taken_out"), n, ts, tw, free.numel(), rows, block)
+        rc = lib().fkv_page_plan(self._h, self._plan, _stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def page_write(self, pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
         """Quantise k and v [tokens, heads, dim] into the pages' slots (int64 [tokens], negative: skipped)."""
-        ck, cv = _rows_view(k, pages.dim, "k"), _rows_view(v, pages.dim, "v")
-        n = k.shape[0]
-        if v.shape != k.shape or k.shape[1] != pages.heads:
+        kp, kd, shape, kt, kh = _vectors(k, pages.dim, "k")
+        vp, vd, vshape, vt, vh = _vectors(v, pages.dim, "v")
+        n = shape[0]
+        if vshape != shape or shape[1] != pages.heads:
             raise ValueError("k and v must be [tokens, %d, %d]" % (pages.heads, pages.dim))
-        self._check(lib().fkv_page_write(self._h, pages._ref, ctypes.byref(ck), ctypes.byref(cv),
-                                         _array(slots, torch.int64, n, "slots"), n, _stream(stream)))
+        _ROWS.pack_into(self._rows[0], 0, kp, kd, kt, kh)
+        _ROWS.pack_into(self._rows[1], 0, vp, vd, vt, vh)
+        rc = lib().fkv_page_write(self._h, pages._addr, self._rows[0], self._rows[1],
+                                  _array(slots, _INT64, n, "slots"), n, _stream(stream))
+        if rc != OK:
+            self._check(rc)
 
     def page_attend(self, pages: Pages, q: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor,
                     block_table: torch.Tensor, max_new: int, max_len: int, out: torch.Tensor = None,
@@ -566,31 +580,43 @@ class Context:
         tokens and positions.  lse: float32 [tokens, query heads] or None.  The
         workspace is taken from torch's allocator unless given."""
         n = kv_len.numel()
-        cq = _rows_view(q, pages.dim, "q")
-        T, Hq = q.shape[0], q.shape[1]
+        dim = pages.dim
+        qp, qd, shape, qt, qh = _vectors(q, dim, "q")
+        T, Hq = shape[0], shape[1]
         if out is None:
-            out = torch.empty((T, Hq, pages.dim), dtype=q.dtype, device=q.device)
-        co = _rows_view(out, pages.dim, "out")
-        if out.shape != q.shape:
-            raise ValueError("out must have q's shape")
-        i32, f32 = torch.int32, torch.float32
+            out = torch.empty((T, Hq, dim), dtype=q.dtype, device=q.device)
+        op, od, oshape, ot, oh = _vectors(out, dim, "out")
+        if oshape != shape or od != qd:
+            raise ValueError("out must have q's shape and type")
         tp, ts, tw = _table(block_table, n)
-        opt = _Attend(pages.dim ** -0.5 if scale is None else scale, softcap, int(bool(causal)), int(window),
-                      int(sinks), None if slopes is None else _array(slopes, f32, Hq, "slopes"),
-                      None if prefix is None else _array(prefix, i32, n, "prefix"))
-        L, o = lib(), ctypes.byref(opt)
-        need = L.fkv_page_attend_workspace(self._h, pages._ref, T, Hq, n, int(max_new), int(max_len), o)
-        if need and workspace is None:
+        buf = self._attend
+        _ATTEND.pack_into(
+            buf, 0, pages._addr, qp, op, 0 if lse is None else _array(lse, _FLOAT, T * Hq, "lse"),
+            _array(cu, _I32, n + 1, "cu"), _array(kv_len, _I32, n, "kv_len"), tp,
+            0 if slopes is None else _array(slopes, _FLOAT, Hq, "slopes"),
+            0 if prefix is None else _array(prefix, _I32, n, "prefix"), qt, qh, ot, oh, T, n, ts, tw, max_new, max_len,
+            window, sinks, qd, Hq, causal, dim ** -0.5 if scale is None else scale, softcap, 0)
+        L = lib()
+        # the workspace's size depends on these alone
+        key = (T, Hq, n, max_new, max_len, window, pages.heads, dim)
+        need = self._attend_need.get(key)
+        if need is None:
+            if len(self._attend_need) >= 4096:
+                self._attend_need.clear()
+            need = self._attend_need[key] = L.fkv_page_attend_workspace(self._h, buf)
+        ws = nb = 0
+        if workspace is not None:
+            ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        elif need:
             if stream is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
             else:
                 with torch.cuda.stream(stream):          # the allocator reuses it in that stream's order
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        self._check(L.fkv_page_attend(
-            self._h, pages._ref, ctypes.byref(cq), T, Hq, _array(cu, i32, n + 1, "cu"),
-            _array(kv_len, i32, n, "kv_len"), n, tp, ts, tw, int(max_new), int(max_len), o, ctypes.byref(co),
-            None if lse is None else _array(lse, f32, T * Hq, "lse"), ws[0], ws[1], _stream(stream)))
+            ws, nb = workspace.data_ptr(), need
+        rc = L.fkv_page_attend(self._h, buf, ws, nb, _stream(stream))
+        if rc != OK:
+            self._check(rc)
         return out
 
     def page_read(self, pages: Pages, kv_len: torch.Tensor, block_table: torch.Tensor, t0: int, t1: int,
@@ -599,16 +625,21 @@ class Context:
         of a layer of the caches k_out and v_out [layers, batch, heads, seq, dim]."""
         n = kv_len.numel()
         tp, ts, tw = _table(block_table, n)
-        for x in (k_out, v_out):
-            if x is not None and (x.dim() != 5 or x.shape[2] != pages.heads or x.shape[4] != pages.dim or
-                                  not 0 <= layer < x.shape[0]):
-                raise ValueError("caches must be [layers, batch, %d, seq, %d] and hold the layer"
-                                 % (pages.heads, pages.dim))
-        ck = cache_view(k_out) if k_out is not None else None
-        cv = cache_view(v_out) if v_out is not None else None
-        self._check(lib().fkv_page_read(self._h, pages._ref, _array(kv_len, torch.int32, n, "kv_len"), n, tp, ts, tw,
-                                        int(t0), int(t1), int(layer), ctypes.byref(ck) if ck else None,
-                                        ctypes.byref(cv) if cv else None, _stream(stream)))
+        views = [0, 0]
+        for i, x in enumerate((k_out, v_out)):
+            if x is None:
+                continue
+            shape, st, dt = x.shape, x.stride(), _DTYPE.get(x.dtype)
+            if (len(shape) != 5 or shape[2] != pages.heads or shape[4] != pages.dim or st[4] != 1 or dt is None or
+                    not 0 <= layer < shape[0] or not x.is_cuda):
+                raise ValueError("caches must be CUDA tensors [layers, batch, %d, seq, %d] with contiguous dim that "
+                                 "hold the layer" % (pages.heads, pages.dim))
+            _CACHE.pack_into(self._caches[i], 0, x.data_ptr(), dt, shape[1], shape[3], st[0], st[1], st[2], st[3])
+            views[i] = self._caches[i]
+        rc = lib().fkv_page_read(self._h, pages._addr, _array(kv_len, _I32, n, "kv_len"), n, tp, ts, tw, t0, t1, layer,
+                                 views[0] or None, views[1] or None, _stream(stream))
+        if rc != OK:
+            self._check(rc)
 
 
 class Streams:

@@ -21,6 +21,7 @@ using namespace fkvd;
 namespace {
 
 constexpr float kPBits = 8.0f;     // P is at most 2^8
+constexpr int kMaxCluster = 8;     // blocks of a portable cluster
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
 {
@@ -73,6 +74,35 @@ template <int D, int NT> struct StepShape {
     static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0, ml = 4 * 2 * 8 * NT * 4;
     static constexpr int smem = ring + q + ml + 1024;
 };
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The same place in the shared memory of the cluster's block `rank`.
+__device__ __forceinline__ uint32_t in_cluster(const float *p, int rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float ld_cluster(const float *p, int rank)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cluster(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(const float *p, int rank)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(in_cluster(p, rank))
+                 : "memory");
+    return v;
+}
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -485,7 +515,8 @@ __global__ void __launch_bounds__(128, 3)
     __syncthreads();
     constexpr int TPR = 128 / R, E = D / TPR;      // threads a row, dimensions a thread
     const int row = tid / TPR, c = (tid % TPR) * E;
-    if (row0 + row >= rows)
+    const bool live = row0 + row < rows;
+    if (!live && !a.cluster)
         return;
     float mt = -INFINITY;
 #pragma unroll
@@ -498,10 +529,10 @@ __global__ void __launch_bounds__(128, 3)
         f[w] = ex2(ml[w][0][row] - mref);
         lt += ml[w][1][row] * f[w];
     }
-    const float inv = lt != 0.0f ? vref / lt : 0.0f;
-    const float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
-    const int i = static_cast<int>(a.gdiv.div(row0 + row));
-    const int64_t tok = q.tok0 + i, head = h * a.G + row0 + row - i * a.G, flat = tok * (a.H * a.G) + head;
+    float inv = lt != 0.0f ? vref / lt : 0.0f;
+    float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
+    const int i = live ? static_cast<int>(a.gdiv.div(row0 + row)) : 0;
+    const int64_t tok = q.tok0 + i, head = h * a.G + (live ? row0 + row - i * a.G : 0), flat = tok * (a.H * a.G) + head;
     float x[E];
 #pragma unroll
     for (int k = 0; k < E; ++k)
@@ -514,7 +545,49 @@ __global__ void __launch_bounds__(128, 3)
             x[k] = fmaf(v.x, f[w], x[k]), x[k + 1] = fmaf(v.y, f[w], x[k + 1]);
             x[k + 2] = fmaf(v.z, f[w], x[k + 2]), x[k + 3] = fmaf(v.w, f[w], x[k + 3]);
         }
-    if (a.splits == 1) {
+    if (a.cluster) {
+        // the shares of a row meet in their cluster's shared memory: every block
+        // leaves its rows there, and the blocks take every splits-th row
+        float *const part = mo + 4 * R * LD, *const part_lse = part + R * D;
+#pragma unroll
+        for (int k = 0; k < E; k += 4)
+            *reinterpret_cast<float4 *>(part + row * D + c + k) = make_float4(x[k] * inv, x[k + 1] * inv, x[k + 2] * inv, x[k + 3] * inv);
+        if (c == 0)
+            part_lse[row] = lse2;
+        cluster_sync();
+        const bool mine = live && row % a.splits == split;
+        if (mine) {
+            float most = -INFINITY, sum = 0.0f, l_s[kMaxCluster];
+#pragma unroll
+            for (int s = 0; s < kMaxCluster; ++s) {
+                l_s[s] = s < a.splits ? ld_cluster(part_lse + row, s) : -INFINITY;
+                most = fmaxf(most, l_s[s]);
+            }
+            const float ref = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                x[k] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < kMaxCluster; ++s) {
+                if (s >= a.splits)
+                    break;
+                const float w = ex2(l_s[s] - ref);
+                sum += w;
+#pragma unroll
+                for (int k = 0; k < E; k += 4) {
+                    const float4 v = ld_cluster4(part + row * D + c + k, s);
+                    x[k] = fmaf(v.x, w, x[k]), x[k + 1] = fmaf(v.y, w, x[k + 1]);
+                    x[k + 2] = fmaf(v.z, w, x[k + 2]), x[k + 3] = fmaf(v.w, w, x[k + 3]);
+                }
+            }
+            inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+            lse2 = sum != 0.0f ? ref + log2f(sum) : -INFINITY;
+        }
+        cluster_sync();                // no block's memory goes before the others have read it
+        if (!mine)
+            return;
+    }
+    if (a.splits == 1 || a.cluster) {
         T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + c;
 #pragma unroll
         for (int k = 0; k < E; k += 4) {
@@ -603,50 +676,59 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
 }
 
 // ------------------------------------------------------------------ launch --
+// A window that holds every position is none.
+int window_of(const fkv_attend &c) { return c.window >= FKV_PAGE_MAX_LEN ? 0 : static_cast<int>(c.window); }
+
 struct Plan {
     int nt, row_tiles, splits, chunk;
+    bool cluster;                // the splits of a row are one cluster
+    bool fits;                   // the blocks are few enough for one launch
 };
 
 // Which kernel serves the call, and how many shares the keys are split into.
-// Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step kernel, more
-// to the tensor-memory one (nt = 0).  A block's time is its keys plus a fixed
-// part (its launch, the first loads' latency and its end: about that of 384
-// keys); the blocks run in waves of `slots`.  The split with the least waves x
-// time wins; joining the partial results costs another part a split.
-Plan plan_of(const fkv_ctx *ctx, int64_t n_req, int H, int G, int64_t T, int64_t max_new, int64_t max_len, int window)
+// Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step
+// kernel, more to the tensor-memory one (nt = 0).  A block's time is its keys
+// plus a fixed part (its launch, the first loads' latency and its end: about that
+// of 384 keys); the blocks run in waves of `slots`.  The split with the least
+// waves x time wins.  Up to eight shares of the step kernel are joined in their
+// cluster (about 100 keys' time) if all blocks run at once: where blocks queue,
+// those of a cluster hold their places until its last one is done (64 ragged
+// sequences of 16-32k positions: 561 us, and 499 with the shares joined by
+// another launch, which costs 512 keys' time and 8 a share).
+Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
 {
     Plan p;
-    const int64_t most = max_new * G;
+    const int H = c.pages->n_heads, G = c.n_q_heads / H, window = window_of(c);
+    const int64_t most = c.max_new * G;
     p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
-    const int64_t blocks = n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
-    int64_t span = max_len;
-    if (window && window + max_new + 2 * kTile < span)
-        span = window + max_new + 2 * kTile;
+    const int64_t blocks = c.n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
+    int64_t span = c.max_len;
+    if (window && window + c.max_new + 2 * kTile < span)
+        span = window + c.max_new + 2 * kTile;
     const int tiles = static_cast<int>((span + kTile - 1) / kTile);
     double best = 0.0;
     p.splits = 1;
     p.chunk = tiles > 0 ? tiles : 1;
-    // partial results are indexed by (split, row) of a grid dimension
-    const int most_splits = T * H * G < (int64_t(1) << 30) ? kMaxSplits : 1;
+    // blocks, and rows of partial results, are counted in a grid dimension
+    p.fits = blocks <= INT32_MAX;
+    const int64_t room = INT32_MAX / (blocks > 0 ? blocks : 1);
+    const int most_splits = c.n_tok * c.n_q_heads > INT32_MAX ? 1 : static_cast<int>(room < kMaxSplits ? room : kMaxSplits);
     for (int s = 1; s <= most_splits && s <= tiles; ++s) {
         const int chunk = (tiles + s - 1) / s;
         const int64_t waves = (blocks * s + slots - 1) / slots;
-        const double cost = waves * (chunk * kTile + 384.0) + (s > 1 ? 512.0 + 8.0 * s : 0.0);
+        const bool in_cluster = p.nt && s > 1 && s <= kMaxCluster && blocks * s <= slots;
+        const double join = s == 1 ? 0.0 : in_cluster ? 100.0 : 512.0 + 8.0 * s;
+        const double cost = waves * (chunk * kTile + 384.0) + join;
         if (s == 1 || cost < best) {
             best = cost;
             p.splits = (tiles + chunk - 1) / chunk;
             p.chunk = chunk;
         }
     }
+    p.cluster = p.nt && p.splits > 1 && p.splits <= kMaxCluster && blocks * p.splits <= slots;
     return p;
-}
-
-// A window that holds every position is none.
-int window_of(const fkv_attend *opt)
-{
-    return opt->window >= FKV_PAGE_MAX_LEN ? 0 : static_cast<int>(opt->window);
 }
 
 template <int D, int FMT, typename T, int NT>
@@ -656,9 +738,14 @@ cudaError_t step_rows(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap
     const cudaError_t e = kernel_use(ctx, fn, 128, StepShape<D, NT>::smem, nullptr);
     if (e != cudaSuccess)
         return e;
-    const dim3 grid(static_cast<unsigned>(a.n_req * a.row_tiles * a.splits), a.H);
-    k_attend_step<D, FMT, T, NT><<<grid, 128, StepShape<D, NT>::smem, st>>>(a, mk, mv);
-    return cudaGetLastError();
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = a.cluster ? a.splits : 1, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_req * a.row_tiles * a.splits), a.H), cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = StepShape<D, NT>::smem, cfg.stream = st;
+    cfg.attrs = &at, cfg.numAttrs = a.cluster ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, k_attend_step<D, FMT, T, NT>, a, mk, mv);
 }
 
 template <int D, int FMT, typename T>
@@ -668,7 +755,7 @@ cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUten
     const cudaError_t e = nt == 0   ? launch_attend_prompt(ctx, a, D, FMT, std::is_same<T, __half>::value ? FKV_F16 : FKV_BF16, st)
                           : nt == 1 ? step_rows<D, FMT, T, 1>(ctx, a, mk, mv, st)
                                     : step_rows<D, FMT, T, 2>(ctx, a, mk, mv, st);
-    if (e != cudaSuccess || a.splits == 1)
+    if (e != cudaSuccess || a.splits == 1 || a.cluster)
         return e;
     return launch_after(k_attend_combine<D, T>, static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st, a);
 }
@@ -683,43 +770,42 @@ cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, 
 
 }  // namespace
 
-int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pg, int64_t n_req, int n_q_heads, int64_t T,
-                              int64_t max_new, int64_t max_len, const fkv_attend *opt)
+int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_attend &c)
 {
-    const Plan p = plan_of(ctx, n_req, pg->n_heads, n_q_heads / pg->n_heads, T, max_new, max_len, window_of(opt));
-    if (p.splits == 1)
+    const Plan p = plan_of(ctx, c);
+    if (!p.fits)
+        return -1;
+    if (p.splits == 1 || p.cluster)
         return 0;
-    return (static_cast<int64_t>(p.splits) * T * n_q_heads * (pg->dim + 1) * 4 + 255) / 256 * 256;
+    return (static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * (c.pages->dim + 1) * 4 + 255) / 256 * 256;
 }
 
-cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_pages *pg, const fkv_rows *q, int64_t T, int n_q_heads,
-                               const int32_t *cu, const int32_t *kv_len, int64_t n_req, const int32_t *table,
-                               int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len,
-                               const fkv_attend *opt, const fkv_rows *out, float *lse, void *ws,
-                               const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws, const CUtensorMap &mk,
+                               const CUtensorMap &mv, cudaStream_t st)
 {
+    const fkv_pages *pg = c.pages;
     AttendArgs a;
-    a.q = q->data, a.out = out->data, a.lse = lse, a.pool_k = pg->k, a.pool_v = pg->v;
+    a.q = c.q, a.out = c.out, a.lse = c.lse, a.pool_k = pg->k, a.pool_v = pg->v;
     a.sb = pg->stride_block, a.sh = pg->stride_head, a.st = pg->stride_pos;
-    a.cu = cu, a.kv_len = kv_len, a.table = table;
-    a.ks = pg->k_scale, a.vs = pg->v_scale, a.slopes = opt->slopes, a.prefix = opt->prefix;
+    a.cu = c.cu, a.kv_len = c.kv_len, a.table = c.table;
+    a.ks = pg->k_scale, a.vs = pg->v_scale, a.slopes = c.slopes, a.prefix = c.prefix;
     a.status = ctx->d_status;
-    a.q_tok = q->stride_tok, a.q_head = q->stride_head, a.o_tok = out->stride_tok, a.o_head = out->stride_head;
-    a.table_stride = table_stride, a.scb = pg->scale_stride_block, a.sch = pg->scale_stride_head;
-    a.n_blocks = pg->n_blocks, a.T = T;
-    a.n_req = static_cast<int>(n_req), a.H = pg->n_heads, a.G = n_q_heads / pg->n_heads, a.block = pg->block;
-    a.width = static_cast<int>(width), a.max_new = static_cast<int>(max_new), a.max_len = static_cast<int>(max_len);
-    a.window = window_of(opt);
-    a.sinks = a.window ? static_cast<int>(opt->sinks < FKV_PAGE_MAX_LEN ? opt->sinks : FKV_PAGE_MAX_LEN) : 0;
-    a.causal = opt->causal;
-    a.scale = opt->scale, a.softcap = opt->softcap;
+    a.q_tok = c.q_stride_tok, a.q_head = c.q_stride_head, a.o_tok = c.out_stride_tok, a.o_head = c.out_stride_head;
+    a.table_stride = c.table_stride, a.scb = pg->scale_stride_block, a.sch = pg->scale_stride_head;
+    a.n_blocks = pg->n_blocks, a.T = c.n_tok;
+    a.n_req = static_cast<int>(c.n_req), a.H = pg->n_heads, a.G = c.n_q_heads / pg->n_heads, a.block = pg->block;
+    a.width = static_cast<int>(c.width), a.max_new = static_cast<int>(c.max_new), a.max_len = static_cast<int>(c.max_len);
+    a.window = window_of(c);
+    a.sinks = a.window ? static_cast<int>(c.sinks < FKV_PAGE_MAX_LEN ? c.sinks : FKV_PAGE_MAX_LEN) : 0;
+    a.causal = c.causal;
+    a.scale = c.scale, a.softcap = c.softcap;
     a.div = FastDiv::make(pg->block), a.gdiv = FastDiv::make(a.G);
-    const Plan p = plan_of(ctx, n_req, a.H, a.G, T, max_new, max_len, a.window);
-    a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk;
+    const Plan p = plan_of(ctx, c);
+    a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk, a.cluster = p.cluster;
     a.ws_o = static_cast<float *>(ws);
-    a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * T * n_q_heads * pg->dim : nullptr;
+    a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * pg->dim : nullptr;
     const bool i8 = pg->format == FKV_INT8;
     if (pg->dim == 64)
-        return i8 ? step_dt<64, FKV_INT8>(ctx, a, q->dtype, p.nt, mk, mv, st) : step_dt<64, FKV_E4M3>(ctx, a, q->dtype, p.nt, mk, mv, st);
-    return i8 ? step_dt<128, FKV_INT8>(ctx, a, q->dtype, p.nt, mk, mv, st) : step_dt<128, FKV_E4M3>(ctx, a, q->dtype, p.nt, mk, mv, st);
+        return i8 ? step_dt<64, FKV_INT8>(ctx, a, c.dtype, p.nt, mk, mv, st) : step_dt<64, FKV_E4M3>(ctx, a, c.dtype, p.nt, mk, mv, st);
+    return i8 ? step_dt<128, FKV_INT8>(ctx, a, c.dtype, p.nt, mk, mv, st) : step_dt<128, FKV_E4M3>(ctx, a, c.dtype, p.nt, mk, mv, st);
 }

@@ -24,6 +24,7 @@ struct AttendArgs {
     int64_t q_tok, q_head, o_tok, o_head, table_stride, sb, sh, st, scb, sch, n_blocks, T;
     int n_req, H, G, block, width, max_new, max_len, window, sinks, causal;
     int splits, chunk, row_tiles;
+    bool cluster;                // a row's splits are one cluster, which joins them
     float scale, softcap;
     FastDiv div, gdiv;
 };

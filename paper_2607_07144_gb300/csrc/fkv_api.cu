@@ -1072,28 +1072,42 @@ const char *check_table(int64_t n_req, const int32_t *table, int64_t table_strid
     return nullptr;
 }
 
-const char *check_attend(const fkv_attend *o)
+// What fkv_page_attend_workspace needs to hold, and the rest of a call.
+const char *check_attend_sizes(const fkv_attend *a)
 {
-    if (!o)
-        return "null attention options";
-    if (!isfinite(o->scale) || !isfinite(o->softcap) || o->softcap < 0.0f)
-        return "bad scale or softcap";
-    if ((o->causal != 0 && o->causal != 1) || o->window < 0 || o->sinks < 0)
-        return "bad mask";
-    if (misaligned(o->slopes, 4) || misaligned(o->prefix, 4))
-        return "misaligned mask array";
+    if (!a)
+        return "null arguments";
+    if (const char *why = check_pages(a->pages))
+        return why;
+    if (a->n_tok < 0 || a->n_tok > INT32_MAX || a->n_req < 0 || a->n_req > FKV_PAGE_MAX_REQ || a->max_new < 0 ||
+        a->max_new > FKV_PAGE_MAX_LEN || a->max_len < 0 || a->max_len > FKV_PAGE_MAX_LEN || a->window < 0 || a->sinks < 0)
+        return "size out of range";
+    const int H = a->pages->n_heads;
+    if (a->n_q_heads < H || a->n_q_heads % H || a->n_q_heads > 65535)
+        return "query heads must be a multiple of the pages' heads";
+    if (a->max_new * (a->n_q_heads / H) > INT32_MAX / 2)
+        return "too many new tokens for one launch";
     return nullptr;
 }
 
-const char *check_attend_sizes(const fkv_pages *p, int64_t n_tok, int n_q_heads, int64_t n_req, int64_t max_new,
-                               int64_t max_len)
+const char *check_attend(const fkv_attend *a)
 {
-    if (n_tok < 0 || n_tok > INT32_MAX || n_req < 0 || n_req > FKV_PAGE_MAX_REQ || max_new < 0 ||
-        max_new > FKV_PAGE_MAX_LEN || max_len < 0 || max_len > FKV_PAGE_MAX_LEN)
-        return "size out of range";
-    if (n_q_heads < p->n_heads || n_q_heads % p->n_heads || n_q_heads > 65535)
-        return "query heads must be a multiple of the pages' heads";
-    return nullptr;
+    if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.0f)
+        return "bad scale or softcap";
+    if ((a->causal != 0 && a->causal != 1) || a->reserved != 0)
+        return "bad mask";
+    if (a->dtype != FKV_F16 && a->dtype != FKV_BF16)
+        return "queries are float16 or bfloat16";
+    const fkv_rows q = {const_cast<void *>(a->q), a->dtype, a->q_stride_tok, a->q_stride_head};
+    const fkv_rows out = {a->out, a->dtype, a->out_stride_tok, a->out_stride_head};
+    if (const char *why = check_rows(&q))
+        return why;
+    if (const char *why = check_rows(&out))
+        return why;
+    if (!a->cu || !a->kv_len || misaligned(a->cu, 4) || misaligned(a->kv_len, 4) || misaligned(a->lse, 4) ||
+        misaligned(a->slopes, 4) || misaligned(a->prefix, 4))
+        return "null or misaligned array";
+    return check_table(a->n_req, a->table, a->table_stride, a->width);
 }
 
 // The pool as [page][head][position][dim] bytes, in boxes of 16 positions of
@@ -1115,32 +1129,28 @@ bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *ma
 
 }  // namespace
 
-int fkv_page_plan(fkv_ctx *ctx, const int32_t *n_new_dev, const int32_t *kv_len_dev, int64_t n_req,
-                  int32_t *table_dev, int64_t table_stride, int64_t width, int32_t *free_dev, int64_t n_free,
-                  const int32_t *taken_dev, int block, int32_t *cu_dev, int64_t *slots_dev, int32_t *pos_dev,
-                  int64_t rows, int32_t *kv_len_out_dev, int32_t *taken_out_dev, void *stream)
+int fkv_page_plan(fkv_ctx *ctx, const fkv_plan *p, void *stream)
 {
     if (!ctx)
         return FKV_EINVAL;
-    if (const char *why = check_table(n_req, table_dev, table_stride, width))
+    if (!p)
+        return fail(ctx, FKV_EINVAL, "null arguments");
+    if (const char *why = check_table(p->n_req, p->table, p->table_stride, p->width))
         return fail(ctx, FKV_EINVAL, why);
-    if (block < 16 || block > 1024 || block % 16)
+    if (p->block < 16 || p->block > 1024 || p->block % 16)
         return fail(ctx, FKV_EINVAL, "page size must be a multiple of 16 up to 1024");
-    if (rows < 0 || rows > INT32_MAX || n_free < 0 || n_free > INT32_MAX)
+    if (p->rows < 0 || p->rows > INT32_MAX || p->n_free < 0 || p->n_free > INT32_MAX)
         return fail(ctx, FKV_EINVAL, "size out of range");
-    const void *need[] = {taken_dev, cu_dev, taken_out_dev, n_new_dev, kv_len_dev, kv_len_out_dev};
+    const void *need[] = {p->taken, p->cu, p->taken_out, p->n_new, p->kv_len, p->kv_len_out};
     for (int i = 0; i < 6; ++i)
-        if ((!need[i] && (i < 3 || n_req > 0)) || misaligned(need[i], 4))
+        if ((!need[i] && (i < 3 || p->n_req > 0)) || misaligned(need[i], 4))
             return fail(ctx, FKV_EINVAL, "null or misaligned array");
-    if ((n_free > 0 && !free_dev) || misaligned(free_dev, 4) || (rows > 0 && (!slots_dev || !pos_dev)) ||
-        misaligned(slots_dev, 8) || misaligned(pos_dev, 4))
+    if ((p->n_free > 0 && !p->free) || misaligned(p->free, 4) || (p->rows > 0 && (!p->slots || !p->pos)) ||
+        misaligned(p->slots, 8) || misaligned(p->pos, 4))
         return fail(ctx, FKV_EINVAL, "null or misaligned array");
     if (const char *why = check_device(ctx))
         return fail(ctx, FKV_EINVAL, why);
-    CK(launch_page_plan(ctx, n_new_dev, kv_len_dev, n_req, table_dev, table_stride, width, free_dev, n_free,
-                        taken_dev, block, cu_dev, slots_dev, pos_dev, rows, kv_len_out_dev, taken_out_dev,
-                        as_stream(stream)),
-       "page plan launch");
+    CK(launch_page_plan(ctx, *p, as_stream(stream)), "page plan launch");
     return FKV_OK;
 }
 
@@ -1169,53 +1179,36 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
     return FKV_OK;
 }
 
-int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_pages *pages, int64_t n_tok, int n_q_heads,
-                                  int64_t n_req, int64_t max_new, int64_t max_len, const fkv_attend *opt)
+int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_attend *a)
 {
-    if (!ctx || check_pages(pages) || check_attend(opt) ||
-        check_attend_sizes(pages, n_tok, n_q_heads, n_req, max_new, max_len))
+    if (!ctx || check_attend_sizes(a))
         return 0;
-    return page_attend_workspace(ctx, pages, n_req, n_q_heads, n_tok, max_new, max_len, opt);
+    const int64_t need = page_attend_workspace(ctx, *a);
+    return need < 0 ? 0 : need;
 }
 
-int fkv_page_attend(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *q, int64_t n_tok, int n_q_heads,
-                    const int32_t *cu_dev, const int32_t *kv_len_dev, int64_t n_req, const int32_t *table_dev,
-                    int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len, const fkv_attend *opt,
-                    const fkv_rows *out, float *lse_dev, void *workspace_dev, int64_t workspace_bytes, void *stream)
+int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t workspace_bytes, void *stream)
 {
     if (!ctx)
         return FKV_EINVAL;
-    if (const char *why = check_pages(pages))
+    if (const char *why = check_attend_sizes(a))
         return fail(ctx, FKV_EINVAL, why);
-    if (const char *why = check_attend(opt))
-        return fail(ctx, FKV_EINVAL, why);
-    if (const char *why = check_attend_sizes(pages, n_tok, n_q_heads, n_req, max_new, max_len))
-        return fail(ctx, FKV_EINVAL, why);
-    if (n_tok == 0 || n_req == 0 || max_new == 0)
+    if (a->n_tok == 0 || a->n_req == 0 || a->max_new == 0)
         return FKV_OK;
-    if (const char *why = check_table(n_req, table_dev, table_stride, width))
+    if (const char *why = check_attend(a))
         return fail(ctx, FKV_EINVAL, why);
-    if (const char *why = check_rows(q))
-        return fail(ctx, FKV_EINVAL, why);
-    if (const char *why = check_rows(out))
-        return fail(ctx, FKV_EINVAL, why);
-    if (q->dtype == FKV_F32 || out->dtype != q->dtype)
-        return fail(ctx, FKV_EINVAL, "queries are float16 or bfloat16, and outputs of their type");
-    if (!cu_dev || !kv_len_dev || misaligned(cu_dev, 4) || misaligned(kv_len_dev, 4) || misaligned(lse_dev, 4))
-        return fail(ctx, FKV_EINVAL, "null or misaligned array");
-    const int64_t need = page_attend_workspace(ctx, pages, n_req, n_q_heads, n_tok, max_new, max_len, opt);
-    if (need > 0 && (!workspace_dev || workspace_bytes < need || misaligned(workspace_dev, 256)))
+    const int64_t need = page_attend_workspace(ctx, *a);
+    if (need < 0)
+        return fail(ctx, FKV_EINVAL, "too many requests times new tokens for one launch");
+    if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256)))
         return fail(ctx, FKV_EINVAL, "workspace missing, too small or misaligned");
     if (const char *why = check_device(ctx))
         return fail(ctx, FKV_EINVAL, why);
     EncodeTiledFn enc = encode_tiled();
     CUtensorMap mk, mv;
-    if (!enc || !page_map(enc, pages, pages->k, &mk) || !page_map(enc, pages, pages->v, &mv))
+    if (!enc || !page_map(enc, a->pages, a->pages->k, &mk) || !page_map(enc, a->pages, a->pages->v, &mv))
         return fail(ctx, FKV_ECUDA, "cuTensorMapEncodeTiled failed");
-    CK(launch_page_attend(ctx, pages, q, n_tok, n_q_heads, cu_dev, kv_len_dev, n_req, table_dev, table_stride, width,
-                          max_new, max_len, opt, out, lse_dev, need ? workspace_dev : nullptr, mk, mv,
-                          as_stream(stream)),
-       "page attention launch");
+    CK(launch_page_attend(ctx, *a, need ? workspace : nullptr, mk, mv, as_stream(stream)), "page attention launch");
     return FKV_OK;
 }
 

@@ -200,23 +200,17 @@ cudaError_t launch_read_kv(const fkv_ctx *c, const double *pts, int64_t n_stream
 int64_t read_order_ints(const fkv_ctx *c, int64_t n_req);
 
 // paged.cu, attend.cu: the paged 8-bit cache (arguments already checked)
-cudaError_t launch_page_plan(const fkv_ctx *c, const int32_t *n_new, const int32_t *kv_len, int64_t n_req,
-                             int32_t *table, int64_t table_stride, int64_t width, int32_t *free_ids, int64_t n_free,
-                             const int32_t *taken, int block, int32_t *cu, int64_t *slots, int32_t *positions,
-                             int64_t rows, int32_t *kv_len_out, int32_t *taken_out, cudaStream_t st);
+cudaError_t launch_page_plan(const fkv_ctx *c, const fkv_plan &p, cudaStream_t st);
 cudaError_t launch_page_write(const fkv_ctx *c, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
                               const int64_t *slots, int64_t n_tok, cudaStream_t st);
 cudaError_t launch_page_read(const fkv_ctx *c, const fkv_pages *p, const int32_t *kv_len, int64_t n_req,
                              const int32_t *table, int64_t table_stride, int64_t width, int64_t t0, int64_t t1,
                              int64_t layer, const fkv_cache *k_out, const fkv_cache *v_out, cudaStream_t st);
 // mk, mv: TMA maps over the pools as [page][head][position][dim] bytes, 16 positions a box
-int64_t page_attend_workspace(const fkv_ctx *c, const fkv_pages *p, int64_t n_req, int n_q_heads, int64_t n_tok,
-                              int64_t max_new, int64_t max_len, const fkv_attend *opt);
-cudaError_t launch_page_attend(const fkv_ctx *c, const fkv_pages *p, const fkv_rows *q, int64_t n_tok, int n_q_heads,
-                               const int32_t *cu, const int32_t *kv_len, int64_t n_req, const int32_t *table,
-                               int64_t table_stride, int64_t width, int64_t max_new, int64_t max_len,
-                               const fkv_attend *opt, const fkv_rows *out, float *lse, void *ws,
-                               const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st);
+// bytes, or -1: too many blocks for one launch
+int64_t page_attend_workspace(const fkv_ctx *c, const fkv_attend &a);
+cudaError_t launch_page_attend(const fkv_ctx *c, const fkv_attend &a, void *ws, const CUtensorMap &mk,
+                               const CUtensorMap &mv, cudaStream_t st);
 
 // ------------------------------------------------------- device helpers
 #ifdef __CUDACC__

@@ -663,18 +663,16 @@ template <int FMT, typename T> cudaError_t read_as(const ReadArgs &a, int dim, d
 
 }  // namespace
 
-cudaError_t launch_page_plan(const fkv_ctx *ctx, const int32_t *n_new, const int32_t *kv_len, int64_t n_req,
-                             int32_t *table, int64_t table_stride, int64_t width, int32_t *free_ids, int64_t n_free,
-                             const int32_t *taken, int block, int32_t *cu, int64_t *slots, int32_t *positions,
-                             int64_t rows, int32_t *kv_len_out, int32_t *taken_out, cudaStream_t st)
+cudaError_t launch_page_plan(const fkv_ctx *ctx, const fkv_plan &p, cudaStream_t st)
 {
     PlanArgs a;
-    a.n_new = n_new, a.kv_len = kv_len, a.taken = taken;
-    a.table = table, a.free_ids = free_ids, a.cu = cu, a.positions = positions;
-    a.kv_len_out = kv_len_out, a.taken_out = taken_out, a.slots = slots;
-    a.table_stride = table_stride, a.n_free = n_free, a.rows = rows;
-    a.n_req = static_cast<int>(n_req), a.width = static_cast<int>(width), a.block = block;
-    a.div = FastDiv::make(block);
+    a.n_new = p.n_new, a.kv_len = p.kv_len, a.taken = p.taken;
+    a.table = p.table, a.free_ids = p.free, a.cu = p.cu, a.positions = p.pos;
+    a.kv_len_out = p.kv_len_out, a.taken_out = p.taken_out, a.slots = p.slots;
+    a.table_stride = p.table_stride, a.n_free = p.n_free, a.rows = p.rows;
+    a.n_req = static_cast<int>(p.n_req), a.width = static_cast<int>(p.width), a.block = static_cast<int>(p.block);
+    const int64_t rows = p.rows;
+    a.div = FastDiv::make(static_cast<unsigned>(p.block));
     a.status = ctx->d_status;
     a.share = (a.n_req + kPlanThreads - 1) / kPlanThreads;
     // one launch while the block's own stores take less than a second launch
