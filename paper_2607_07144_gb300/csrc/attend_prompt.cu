@@ -139,6 +139,12 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b)
         : "f"(a), "f"(b));
 }
 
+// The word whose first n bits are set (none for n <= 0, all for n >= 32).
+__device__ __forceinline__ uint32_t below(int n)
+{
+    return static_cast<uint32_t>((1ull << max(0, min(32, n))) - 1);
+}
+
 // One group's softmax of a tile: see k_attend_prompt.
 struct Row {
     float m, l;                 // reference exponent and the sum of weights
@@ -182,6 +188,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int pb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + kRows, rows) - 1));
     const Tiles tiles(a, q, pa, pb);
     const int i0 = split * a.chunk, n_it = max(0, min(tiles.n, i0 + a.chunk) - i0);
+    // the first group's rows end earlier: tiles at the share's end that none of
+    // them sees are the second group's alone
+    int n_first = n_it;
+    if (groups == 2) {
+        const Tiles own(a, q, pa, q.p0 + static_cast<int>(a.gdiv.div(row0 + 127)));
+        while (n_first > 0 && tiles.at(i0 + n_first - 1) * kTile >= own.lim)
+            --n_first;
+    }
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -232,14 +246,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             bool ok = mbar_park(bar(Q_FULL), 0, a.status) && mbar_park(bar(K_FULL), 0, a.status);
             if (ok) {
                 tc_fence_after();
-                for (int w = 0; w < groups; ++w)
+                for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
                     scores(w, 0);
                 umma_commit(bar(K_EMPTY));
             }
             for (int j = 0; j < n_it && ok; ++j) {
-                for (int w = 0; w < groups && ok; ++w) {
+                bool have_v = false, have_k = false;
+                for (int w = j < n_first ? 0 : 1; w < groups && ok; ++w) {
                     ok = mbar_park(bar(P_FULL + w), j & 1, a.status) &&
-                         (w > 0 || mbar_park(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
+                         (have_v || mbar_park(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
+                    have_v = true;
                     if (!ok)
                         break;
                     tc_fence_after();
@@ -249,11 +265,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         umma_f16_ts(o_t[w], s_t[w] + 8 * k, sdesc_mn_sw128(vb + k * 2048, S::half), id_o, j > 0 || k > 0);
                     if (w == groups - 1)
                         umma_commit(bar(V_EMPTY + (j & 1)));
-                    if (j + 1 == n_it) {
+                    if (j + 1 == (w ? n_it : n_first)) {
                         umma_commit(bar(O_FULL + w));
                         continue;
                     }
-                    ok = w > 0 || mbar_park(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
+                    ok = have_k || mbar_park(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
+                    have_k = true;
                     if (!ok)
                         break;
                     tc_fence_after();
@@ -429,7 +446,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
             const uint32_t s_t = tmem + 128 * w + lanes, o_t = tmem + 256 + 128 * w + lanes;
             bool ok = true;
-            for (int j = 0; j < n_it; ++j) {
+            const int n_own = w ? n_it : n_first;
+            for (int j = 0; j < n_own; ++j) {
                 ok = mbar_park(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status);
                 if (!ok)
                     break;
@@ -444,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 tc_fence_after();
                 // 64 columns at a time, a second time where the reference has to move first
 #pragma unroll 1
-                for (int k = 0, again = 0; k < 2;) {
+                for (int k = 0, again = j == 0; k < 2;) {
                     float s[64];
                     tmem_ld32(s_t + 64 * k, s);
                     tmem_ld32(s_t + 64 * k + 32, s + 32);
@@ -476,11 +494,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                                 s[e] = fmaf(st.slope, at + static_cast<float>(e), s[e]);
                         }
                         if (!full) {
+                            // the visible keys as bits: ranges meet as words, and a
+                            // score's test is one bit (its three comparisons, short
+                            // cuts and all, took 80 cycles a score)
 #pragma unroll
-                            for (int e = 0; e < 64; ++e) {
-                                const int jj = key + 64 * k + e;
-                                const bool see = (jj < st.hi && (jj >= st.from || jj < a.sinks)) || jj < st.pre;
-                                s[e] = see ? s[e] : -INFINITY;
+                            for (int x = 0; x < 2; ++x) {
+                                const int j0 = key + 64 * k + 32 * x;
+                                const uint32_t vis = (below(st.hi - j0) & (~below(st.from - j0) | below(a.sinks - j0))) | below(st.pre - j0);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    s[32 * x + e] = vis >> e & 1 ? s[32 * x + e] : -INFINITY;
                             }
                         }
 #pragma unroll
@@ -563,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 tc_fence_before();
                 mbar_arrive(bar(P_FULL + w));
             }
-            if (n_it > 0 && ok)
+            if (n_own > 0 && ok)
                 ok = mbar_park(bar(O_FULL + w), 0, a.status);
             tc_fence_after();
             const float inv = st.l != 0.0f ? vref / st.l : 0.0f;
