@@ -92,16 +92,85 @@ __device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, unsigne
     return false;
 }
 
-// D[tmem] (+)= A[tmem] B[smem], A fp16 pairs in 32-bit columns.
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate)
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
+// A tile's MMAs are one statement each, from the low words of the first step's
+// descriptors (a descriptor's address counts 16 bytes, its high word is the
+// layout): the issuing warp shares its scheduler with five working ones, and what
+// it executes between two MMAs is what the tensor core waits for.  Measured beside
+// twenty busy warps: 161 cycles an MMA issued by a lane picked by its number, 89
+// by an elected one with 64-bit descriptors, 79 like this, of which the tensor
+// core itself takes 64.
+//
+// D[tmem] = A[smem] B[smem]^T over D dimensions: 128-byte swizzled rows of 64.
+template <int D> __device__ __forceinline__ void umma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc)
+{
+    if (D == 128)
+        asm volatile(
+            "{\n\t.reg .b64 x, y;\n\t.reg .b32 p, q, hi;\n\t.reg .pred f, t;\n\t"
+            "mov.b32 hi, 0x40004040;\n\tsetp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+            "mov.b64 x, {%1, hi};\n\tmov.b64 y, {%2, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, f;\n\t"
+            "add.u32 p, %1, 2;\n\tadd.u32 q, %2, 2;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 4;\n\tadd.u32 q, %2, 4;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 6;\n\tadd.u32 q, %2, 6;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 1024;\n\tadd.u32 q, %2, 1024;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 1026;\n\tadd.u32 q, %2, 1026;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 1028;\n\tadd.u32 q, %2, 1028;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 1030;\n\tadd.u32 q, %2, 1030;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "}" ::"r"(d), "r"(a), "r"(b), "r"(idesc) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .b64 x, y;\n\t.reg .b32 p, q, hi;\n\t.reg .pred f, t;\n\t"
+            "mov.b32 hi, 0x40004040;\n\tsetp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+            "mov.b64 x, {%1, hi};\n\tmov.b64 y, {%2, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, f;\n\t"
+            "add.u32 p, %1, 2;\n\tadd.u32 q, %2, 2;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 4;\n\tadd.u32 q, %2, 4;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "add.u32 p, %1, 6;\n\tadd.u32 q, %2, 6;\n\tmov.b64 x, {p, hi};\n\tmov.b64 y, {q, hi};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, t;\n\t"
+            "}" ::"r"(d), "r"(a), "r"(b), "r"(idesc) : "memory");
+}
+
+// D[tmem] (+)= A[tmem] B[smem] over 128 keys: A fp16 pairs in 32-bit columns, B
+// 16 keys (2048 bytes) a step.
+__device__ __forceinline__ void umma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate,
+                                             uint32_t b_hi)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
+        "{\n\t.reg .b64 y;\n\t.reg .b32 p, q;\n\t.reg .pred f, t;\n\t"
+        "setp.ne.b32 f, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "mov.b32 p, %1;\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, f;\n\t"
+        "add.u32 p, %1, 8;\n\tadd.u32 q, %2, 128;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 16;\n\tadd.u32 q, %2, 256;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 24;\n\tadd.u32 q, %2, 384;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 32;\n\tadd.u32 q, %2, 512;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 40;\n\tadd.u32 q, %2, 640;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 48;\n\tadd.u32 q, %2, 768;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "add.u32 p, %1, 56;\n\tadd.u32 q, %2, 896;\n\tmov.b64 y, {q, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [p], y, %3, t;\n\t"
+        "}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(b_hi) : "memory");
 }
 
 // A [keys][dimensions] tile as the second operand with its dimensions outermost:
@@ -231,56 +300,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     if (group == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ---------------------------------------------------- MMA issuer
-        if (warp == 12 && lane == 0 && n_it > 0) {
+        // The whole warp follows the loop and one elected thread issues.
+        if (warp == 12 && n_it > 0) {
             constexpr uint32_t id_s = idesc_f16_f32(128, 128), id_o = idesc_f16_f32(128, D) | 1u << 16;
-            const uint32_t s_t[2] = {tmem, tmem + 128}, o_t[2] = {tmem + 256, tmem + 384};
+            constexpr uint32_t step = S::tile >> 4;
+            const uint32_t q_d = static_cast<uint32_t>(sdesc_sw128(sbase + S::off_q));
+            const uint32_t k_d = static_cast<uint32_t>(sdesc_sw128(sbase + S::off_k));
+            const uint32_t v_d = static_cast<uint32_t>(sdesc_mn_sw128(sbase + S::off_v, S::half));
+            const uint32_t v_hi = static_cast<uint32_t>(sdesc_mn_sw128(0, S::half) >> 32);
             auto scores = [&](int w, int j) {
-                const uint32_t qb = sbase + S::off_q + w * S::tile, kb = sbase + S::off_k + (j & 1) * S::tile;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k >> 2) * S::half + (k & 3) * 32;
-                    umma_f16(s_t[w], sdesc_sw128(qb + off), sdesc_sw128(kb + off), id_s, k > 0);
+                if (elect_one()) {
+                    umma_tile_ss<D>(tmem + 128 * w, q_d + w * step, k_d + (j & 1) * step, id_s);
+                    umma_commit(bar(S_FULL + w));
                 }
-                umma_commit(bar(S_FULL + w));
+                __syncwarp();
             };
-            bool ok = mbar_park(bar(Q_FULL), 0, a.status) && mbar_park(bar(K_FULL), 0, a.status);
+            auto commit = [&](int b) {
+                if (elect_one())
+                    umma_commit(bar(b));
+                __syncwarp();
+            };
+            auto wait = [&](int b, int parity) { return __all_sync(~0u, mbar_park(bar(b), parity, a.status)); };
+            bool ok = wait(Q_FULL, 0) && wait(K_FULL, 0);
             if (ok) {
                 tc_fence_after();
                 for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
                     scores(w, 0);
-                umma_commit(bar(K_EMPTY));
+                commit(K_EMPTY);
             }
             for (int j = 0; j < n_it && ok; ++j) {
                 bool have_v = false, have_k = false;
-                for (int w = j < n_first ? 0 : 1; w < groups && ok; ++w) {
-                    ok = mbar_park(bar(P_FULL + w), j & 1, a.status) &&
-                         (have_v || mbar_park(bar(V_FULL + (j & 1)), (j >> 1) & 1, a.status));
+                for (int w = j < n_first ? 0 : 1; w < groups; ++w) {
+                    ok = wait(P_FULL + w, j & 1) && (have_v || wait(V_FULL + (j & 1), (j >> 1) & 1));
                     have_v = true;
                     if (!ok)
                         break;
                     tc_fence_after();
-                    const uint32_t vb = sbase + S::off_v + (j & 1) * S::tile;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        umma_f16_ts(o_t[w], s_t[w] + 8 * k, sdesc_mn_sw128(vb + k * 2048, S::half), id_o, j > 0 || k > 0);
-                    if (w == groups - 1)
-                        umma_commit(bar(V_EMPTY + (j & 1)));
-                    if (j + 1 == (w ? n_it : n_first)) {
-                        umma_commit(bar(O_FULL + w));
-                        continue;
+                    if (elect_one()) {
+                        umma_tile_ts(tmem + 256 + 128 * w, tmem + 128 * w, v_d + (j & 1) * step, id_o, j > 0, v_hi);
+                        if (w == groups - 1)
+                            umma_commit(bar(V_EMPTY + (j & 1)));
+                        if (j + 1 == (w ? n_it : n_first))
+                            umma_commit(bar(O_FULL + w));
                     }
-                    ok = have_k || mbar_park(bar(K_FULL + ((j + 1) & 1)), ((j + 1) >> 1) & 1, a.status);
+                    __syncwarp();
+                    if (j + 1 == (w ? n_it : n_first))
+                        continue;
+                    ok = have_k || wait(K_FULL + ((j + 1) & 1), ((j + 1) >> 1) & 1);
                     have_k = true;
                     if (!ok)
                         break;
                     tc_fence_after();
                     scores(w, j + 1);
                     if (w == groups - 1)
-                        umma_commit(bar(K_EMPTY + ((j + 1) & 1)));
+                        commit(K_EMPTY + ((j + 1) & 1));
                 }
             }
             // every MMA has completed before tensor memory is released
-            umma_commit(bar(DRAIN));
+            commit(DRAIN);
             mbar_park(bar(DRAIN), 0, a.status);
         }
     } else if (group == 2) {
@@ -460,9 +537,65 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 if (!ok)
                     break;
                 tc_fence_after();
-                // 64 columns at a time, a second time where the reference has to move first
+                // A tile that needs neither masks nor more than a multiplication, and
+                // whose rows have their reference: two halves of 64 columns, the second's
+                // products on their way while the first's weights are stored.
+                int k = 0, again = j == 0;
+                if (plain && j > 0) {
+                    float s[64], sum[4];
+                    uint32_t p[32];
+                    auto evaluate = [&](int half) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            float sx = 0.0f, sy = 0.0f;
+                            const float mul = km[4 * half + n] * st.down, o = vm[4 * half + n].x - st.m;
+#pragma unroll
+                            for (int e = 16 * n; e < 16 * n + 16; e += 2) {
+                                float y0, y1;
+                                fma2(y0, y1, s[e], s[e + 1], mul, o);
+                                y0 = ex2(y0), y1 = ex2(y1);
+                                add2(sx, sy, y0, y1);
+                                p[e >> 1] = pack_half(y0, y1);
+                            }
+                            sum[n] = sx + sy;
+                        }
+                        // (not <=: a sum that is no number is looked at as well)
+                        return __any_sync(~0u, !(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) <= kMostSum) ||
+                                                   st.m == -INFINITY);
+                    };
+                    tmem_ld32(s_t, s);
+                    tmem_ld32(s_t + 32, s + 32);
+                    tmem_wait_ld(s);
+                    tmem_wait_ld(s + 32);
+                    again = evaluate(0);
+                    if (!again) {
+                        tmem_ld32(s_t + 64, s);
+                        tmem_ld32(s_t + 96, s + 32);
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+                            st.l = fmaf(sum[n], vm[n].y, st.l);
+                        // fp16 pairs in the tile's first columns, which have been read
+                        tmem_st16(s_t, p);
+                        tmem_st16(s_t + 16, p + 16);
+                        tmem_wait_ld(s);
+                        tmem_wait_ld(s + 32);
+                        k = 1;
+                        again = evaluate(1);
+                        if (!again) {
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+                                st.l = fmaf(sum[n], vm[4 + n].y, st.l);
+                            tmem_st16(s_t + 32, p);
+                            tmem_st16(s_t + 48, p + 16);
+                            k = 2;
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                // Any other tile: a half at a time, a second time where the reference has
+                // to move first.
 #pragma unroll 1
-                for (int k = 0, again = j == 0; k < 2;) {
+                while (k < 2) {
                     float s[64];
                     tmem_ld32(s_t + 64 * k, s);
                     tmem_ld32(s_t + 64 * k + 32, s + 32);
