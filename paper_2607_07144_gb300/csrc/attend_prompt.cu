@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             mbar_init(bar(V_FULL + i), 2);
             mbar_init(bar(V_EMPTY + i), 1);
             mbar_init(bar(S_FULL + i), 1);
-            mbar_init(bar(P_FULL + i), 128);
+            mbar_init(bar(P_FULL + i), 4);
             mbar_init(bar(O_FULL + i), 1);
         }
         for (int i = 0; i < 4; ++i)
@@ -533,6 +533,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const float2 *const vm = v_scales[j & 3];
                 const bool full = all_see(a, q, ga, gb, key, key + kTile);
                 const bool plain = full && a.softcap == 0.0f && !a.slopes;
+                // before the scores are there: the pages' multipliers
+                float km_r[8], vo_r[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    km_r[n] = km[n] * st.down, vo_r[n] = vm[n].x;
                 ok = mbar_park(bar(S_FULL + w), j & 1, a.status);
                 if (!ok)
                     break;
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
                             float sx = 0.0f, sy = 0.0f;
-                            const float mul = km[4 * half + n] * st.down, o = vm[4 * half + n].x - st.m;
+                            const float mul = half ? km_r[4 + n] : km_r[n], o = (half ? vo_r[4 + n] : vo_r[n]) - st.m;
 #pragma unroll
                             for (int e = 16 * n; e < 16 * n + 16; e += 2) {
                                 float y0, y1;
@@ -717,7 +722,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     again = 0;
                 }
                 tc_fence_before();
-                mbar_arrive(bar(P_FULL + w));
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(bar(P_FULL + w));
             }
             if (n_own > 0 && ok)
                 ok = mbar_park(bar(O_FULL + w), 0, a.status);
