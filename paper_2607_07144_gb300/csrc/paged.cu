@@ -404,18 +404,20 @@ template <typename T> struct Largest {
 // int8's rounding is an addition of 1.5 2^23, whose sum's low byte is the code.
 template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *x, float inv)
 {
-    if (FMT == FKV_E4M3)
+    if (FMT == FKV_E4M3) {
         return codes16<FMT>(x, inv);
-    uint32_t w[4];
+    } else {
+        uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t q[4];
+        for (int i = 0; i < 4; ++i) {
+            uint32_t q[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            q[k] = __float_as_uint(__fadd_rn(__fmul_rn(x[4 * i + k], inv), 12582912.0f));
-        w[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            for (int k = 0; k < 4; ++k)
+                q[k] = __float_as_uint(__fadd_rn(__fmul_rn(x[4 * i + k], inv), 12582912.0f));
+            w[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // A run of tokens with consecutive slots inside one page belongs to the group of
@@ -426,7 +428,7 @@ template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *
 // which keeps up to four rows a thread in registers between the search for the
 // largest magnitude and the rounding (longer runs are read again).  Bytes bound
 // long calls, the chain slot, page, store a step's.
-template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT) k_page_write(WriteArgs a)
+template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT, GT == 32 || sizeof(T) == 4 ? 1 : 8) k_page_write(WriteArgs a)
 {
     constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
     __shared__ uint32_t red[GT / 32];
@@ -465,6 +467,13 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
             const int off = static_cast<int>(slot - blk * a.block);
             // the run's length: consecutive slots up to the page's end
             const int most = static_cast<int>(min(static_cast<int64_t>(a.block - off), a.T - t));
+            // a block loads the run's rows before it knows the length, as if it were as
+            // long as the page allows (a step's are mostly one row)
+            Raw<T> keep[KEEP];
+#pragma unroll
+            for (int k = 0; k < KEEP; ++k)
+                if ((GT > 32 || k == 0) && row0 + k * R < most)
+                    keep[k] = load_raw<T>(x + (t + row0 + k * R) * a.x_tok[kv]);
             int len = most;
             for (int i = 0; i < most; i += 32) {
                 const unsigned off_run = __ballot_sync(~0u, i + lane < most && a.slots[t + i + lane] != slot + i + lane);
@@ -476,12 +485,13 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
             float *const sp = a.scale[kv] + blk * a.scb + h * a.sch;
             const float was = off > 0 ? *sp : 0.0f;
             uint8_t *const page = a.pool[kv] + blk * a.sb + h * a.sh + c * 16;
-            Raw<T> keep[KEEP];
-            Largest<T> most_v;
+            if (GT == 32) {
 #pragma unroll
-            for (int k = 0; k < KEEP; ++k)
-                if (row0 + k * R < len)
-                    keep[k] = load_raw<T>(x + (t + row0 + k * R) * a.x_tok[kv]);
+                for (int k = 1; k < KEEP; ++k)
+                    if (row0 + k * R < len)
+                        keep[k] = load_raw<T>(x + (t + row0 + k * R) * a.x_tok[kv]);
+            }
+            Largest<T> most_v;
 #pragma unroll
             for (int k = 0; k < KEEP; ++k)
                 if (row0 + k * R < len)
