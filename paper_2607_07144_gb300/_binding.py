@@ -182,26 +182,27 @@ def cache_view(t: torch.Tensor, host: bool = False) -> _Cache:
 _I32, _INT64, _FLOAT = torch.int32, torch.int64, torch.float32
 
 
-def _vectors(t: torch.Tensor, dim: int, what: str):
+def _vectors(t: torch.Tensor, dim: int, what: str, dev: int):
     """(pointer, dtype, shape, token stride, head stride) of a CUDA tensor [tokens, heads, dim] (contiguous dim)."""
     shape, st, dt = t.shape, t.stride(), _DTYPE.get(t.dtype)
-    if len(st) != 3 or st[2] != 1 or shape[2] != dim or dt is None or not t.is_cuda:
-        raise ValueError("%s must be a CUDA tensor [tokens, heads, %d] with contiguous dim" % (what, dim))
+    if len(st) != 3 or st[2] != 1 or shape[2] != dim or dt is None or t.get_device() != dev:
+        raise ValueError("%s must be a tensor [tokens, heads, %d] with contiguous dim on cuda:%d" % (what, dim, dev))
     # the stride of a dimension of one is never used, but has to be a valid one
     return t.data_ptr(), dt, shape, st[0] if shape[0] > 1 else dim, st[1] if shape[1] > 1 else dim
 
 
-def _array(t: torch.Tensor, dtype, numel: int, what: str):
-    """Pointer of a contiguous CUDA array of at least `numel` elements."""
-    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError("%s must be a contiguous CUDA %s tensor of %d elements" % (what, dtype, numel))
+def _array(t: torch.Tensor, dtype, numel: int, what: str, dev: int):
+    """Pointer of a contiguous array of at least `numel` elements on device `dev`."""
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on cuda:%d" % (what, dtype, numel, dev))
     return t.data_ptr()
 
 
-def _table(t: torch.Tensor, n_req: int):
+def _table(t: torch.Tensor, n_req: int, dev: int):
     shape, st = t.shape, t.stride()
-    if t.dtype is not _I32 or len(shape) != 2 or shape[0] < n_req or (shape[1] > 1 and st[1] != 1) or not t.is_cuda:
-        raise ValueError("block_table must be a CUDA int32 tensor [requests, pages]")
+    if (t.dtype is not _I32 or len(shape) != 2 or shape[0] < n_req or (shape[1] > 1 and st[1] != 1) or
+            t.get_device() != dev):
+        raise ValueError("block_table must be an int32 tensor [requests, pages] on cuda:%d" % dev)
     return t.data_ptr(), st[0] if shape[0] > 1 else max(1, shape[1]), shape[1]
 
 
@@ -213,15 +214,18 @@ class Pages:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         if (k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1 or
-                k.dtype not in _FORMAT or not all(t.is_cuda for t in (k, v, k_scale, v_scale))):
-            raise ValueError("k and v must be CUDA float8_e4m3fn or int8 tensors [blocks, heads, block, dim] of one "
-                             "shape and strides, with contiguous dim")
+                k.dtype not in _FORMAT or not k.is_cuda or any(t.device != k.device for t in (v, k_scale, v_scale))):
+            raise ValueError("k and v must be float8_e4m3fn or int8 tensors [blocks, heads, block, dim] of one shape "
+                             "and strides, with contiguous dim, and all four on one CUDA device")
         if (k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:2] or
                 v_scale.shape != k.shape[:2] or k_scale.stride() != v_scale.stride()):
             raise ValueError("k_scale and v_scale must be float32 tensors [blocks, heads] of the same strides")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_blocks, self.heads, self.block, self.dim = k.shape
-        st, ss = k.stride(), k_scale.stride()
+        self.device = k.get_device()
+        ss = k_scale.stride()
+        # the stride of a dimension of one is never used, but has to be a valid one
+        st = [x if n > 1 else self.dim for x, n in zip(k.stride(), k.shape)]
         self._c = _Pages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _FORMAT[k.dtype],
                          self.heads, self.dim, self.block, self.n_blocks, st[0], st[1], st[2], ss[0], ss[1])
         self._ref = ctypes.byref(self._c)
@@ -269,6 +273,7 @@ class Context:
         self._cb_arrays = None
         if rc != OK:
             raise FkvError(rc, "fkv_create(N=%d, r=%r, span_len=%d) rejected" % (self.N, self.r, self.L))
+        self._dev = torch.cuda.current_device()
         # argument blocks of the paged calls (calls on one context are serialised)
         self._plan = ctypes.create_string_buffer(_PLAN.size)
         self._rows = [ctypes.create_string_buffer(_ROWS.size) for _ in range(2)]
@@ -531,7 +536,12 @@ class Context:
                                       req.shape[0], _ptr(out), _DTYPE[out.dtype], _stream(stream)))
         return out
 
-    # -- paged 8-bit cache
+    # -- paged 8-bit cache (all tensors on the context's device)
+    def _on(self, pages: Pages) -> int:
+        if pages.device != self._dev:
+            raise ValueError("the pages are on cuda:%d, the context on cuda:%d" % (pages.device, self._dev))
+        return self._dev
+
     def page_plan(self, n_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free: torch.Tensor,
                   taken: torch.Tensor, block: int, cu: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor,
                   kv_len_out: torch.Tensor = None, taken_out: torch.Tensor = None, stream=None):
@@ -542,30 +552,32 @@ class Context:
         are given.  slots and positions may have more rows than there are tokens:
         -1 behind the last."""
         n, rows = n_new.numel(), slots.numel()
-        tp, ts, tw = _table(block_table, n)
+        dev = self._dev
+        tp, ts, tw = _table(block_table, n, dev)
         if positions.numel() != rows:
             raise ValueError("slots and positions must have the same length")
-        lp, kp = _array(kv_len, _I32, n, "kv_len"), _array(taken, _I32, 1, "taken")
+        lp, kp = _array(kv_len, _I32, n, "kv_len", dev), _array(taken, _I32, 1, "taken", dev)
         _PLAN.pack_into(
-            self._plan, 0, _array(n_new, _I32, n, "n_new"), lp, tp, _array(free, _I32, 0, "free"), kp,
-            _array(cu, _I32, n + 1, "cu"), _array(slots, _INT64, 0, "slots"), _array(positions, _I32, 0, "positions"),
-            lp if kv_len_out is None else _array(kv_len_out, _I32, n, "kv_len_out"),
-            kp if taken_out is None else _array(taken_out, _I32, 1, "taken_out"), n, ts, tw, free.numel(), rows, block)
+            self._plan, 0, _array(n_new, _I32, n, "n_new", dev), lp, tp, _array(free, _I32, 0, "free", dev), kp,
+            _array(cu, _I32, n + 1, "cu", dev), _array(slots, _INT64, 0, "slots", dev), _array(positions, _I32, 0, "positions", dev),
+            lp if kv_len_out is None else _array(kv_len_out, _I32, n, "kv_len_out", dev),
+            kp if taken_out is None else _array(taken_out, _I32, 1, "taken_out", dev), n, ts, tw, free.numel(), rows, block)
         rc = lib().fkv_page_plan(self._h, self._plan, _stream(stream))
         if rc != OK:
             self._check(rc)
 
     def page_write(self, pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
         """Quantise k and v [tokens, heads, dim] into the pages' slots (int64 [tokens], negative: skipped)."""
-        kp, kd, shape, kt, kh = _vectors(k, pages.dim, "k")
-        vp, vd, vshape, vt, vh = _vectors(v, pages.dim, "v")
+        dev = self._on(pages)
+        kp, kd, shape, kt, kh = _vectors(k, pages.dim, "k", dev)
+        vp, vd, vshape, vt, vh = _vectors(v, pages.dim, "v", dev)
         n = shape[0]
         if vshape != shape or shape[1] != pages.heads:
             raise ValueError("k and v must be [tokens, %d, %d]" % (pages.heads, pages.dim))
         _ROWS.pack_into(self._rows[0], 0, kp, kd, kt, kh)
         _ROWS.pack_into(self._rows[1], 0, vp, vd, vt, vh)
         rc = lib().fkv_page_write(self._h, pages._addr, self._rows[0], self._rows[1],
-                                  _array(slots, _INT64, n, "slots"), n, _stream(stream))
+                                  _array(slots, _INT64, n, "slots", dev), n, _stream(stream))
         if rc != OK:
             self._check(rc)
 
@@ -579,22 +591,23 @@ class Context:
         defaults to dim ** -0.5.  max_new and max_len bound every request's new
         tokens and positions.  lse: float32 [tokens, query heads] or None.  The
         workspace is taken from torch's allocator unless given."""
+        dev = self._on(pages)
         n = kv_len.numel()
         dim = pages.dim
-        qp, qd, shape, qt, qh = _vectors(q, dim, "q")
+        qp, qd, shape, qt, qh = _vectors(q, dim, "q", dev)
         T, Hq = shape[0], shape[1]
         if out is None:
             out = torch.empty((T, Hq, dim), dtype=q.dtype, device=q.device)
-        op, od, oshape, ot, oh = _vectors(out, dim, "out")
+        op, od, oshape, ot, oh = _vectors(out, dim, "out", dev)
         if oshape != shape or od != qd:
             raise ValueError("out must have q's shape and type")
-        tp, ts, tw = _table(block_table, n)
+        tp, ts, tw = _table(block_table, n, dev)
         buf = self._attend
         _ATTEND.pack_into(
-            buf, 0, pages._addr, qp, op, 0 if lse is None else _array(lse, _FLOAT, T * Hq, "lse"),
-            _array(cu, _I32, n + 1, "cu"), _array(kv_len, _I32, n, "kv_len"), tp,
-            0 if slopes is None else _array(slopes, _FLOAT, Hq, "slopes"),
-            0 if prefix is None else _array(prefix, _I32, n, "prefix"), qt, qh, ot, oh, T, n, ts, tw, max_new, max_len,
+            buf, 0, pages._addr, qp, op, 0 if lse is None else _array(lse, _FLOAT, T * Hq, "lse", dev),
+            _array(cu, _I32, n + 1, "cu", dev), _array(kv_len, _I32, n, "kv_len", dev), tp,
+            0 if slopes is None else _array(slopes, _FLOAT, Hq, "slopes", dev),
+            0 if prefix is None else _array(prefix, _I32, n, "prefix", dev), qt, qh, ot, oh, T, n, ts, tw, max_new, max_len,
             window, sinks, qd, Hq, causal, dim ** -0.5 if scale is None else scale, softcap, 0)
         L = lib()
         # the workspace's size depends on these alone
@@ -623,20 +636,21 @@ class Context:
                   layer: int = 0, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
         """Rebuild positions [t0, min(t1, kv_len[r])) of request r into sequence r
         of a layer of the caches k_out and v_out [layers, batch, heads, seq, dim]."""
+        dev = self._on(pages)
         n = kv_len.numel()
-        tp, ts, tw = _table(block_table, n)
+        tp, ts, tw = _table(block_table, n, dev)
         views = [0, 0]
         for i, x in enumerate((k_out, v_out)):
             if x is None:
                 continue
             shape, st, dt = x.shape, x.stride(), _DTYPE.get(x.dtype)
             if (len(shape) != 5 or shape[2] != pages.heads or shape[4] != pages.dim or st[4] != 1 or dt is None or
-                    not 0 <= layer < shape[0] or not x.is_cuda):
+                    not 0 <= layer < shape[0] or x.get_device() != dev):
                 raise ValueError("caches must be CUDA tensors [layers, batch, %d, seq, %d] with contiguous dim that "
                                  "hold the layer" % (pages.heads, pages.dim))
             _CACHE.pack_into(self._caches[i], 0, x.data_ptr(), dt, shape[1], shape[3], st[0], st[1], st[2], st[3])
             views[i] = self._caches[i]
-        rc = lib().fkv_page_read(self._h, pages._addr, _array(kv_len, _I32, n, "kv_len"), n, tp, ts, tw, t0, t1, layer,
+        rc = lib().fkv_page_read(self._h, pages._addr, _array(kv_len, _I32, n, "kv_len", dev), n, tp, ts, tw, t0, t1, layer,
                                  views[0] or None, views[1] or None, _stream(stream))
         if rc != OK:
             self._check(rc)

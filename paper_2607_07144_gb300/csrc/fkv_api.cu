@@ -1171,6 +1171,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
         return fail(ctx, FKV_EINVAL, why);
     if (k->dtype != v->dtype)
         return fail(ctx, FKV_EINVAL, "K and V types differ");
+    if ((n_tok / pages->block + 1) * 2 * pages->n_heads > INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "too many tokens for one launch");
     if (!slots_dev || misaligned(slots_dev, 8))
         return fail(ctx, FKV_EINVAL, "bad slot map");
     if (const char *why = check_device(ctx))
@@ -1232,6 +1234,8 @@ int fkv_page_read(fkv_ctx *ctx, const fkv_pages *pages, const int32_t *kv_len_de
         return fail(ctx, FKV_EINVAL, "K and V types differ");
     if (n_req == 0 || t1 == t0)
         return FKV_OK;
+    if (n_req * (t1 / 16 + 1) > 8ll * INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "too many positions for one launch");
     if (!kv_len_dev || misaligned(kv_len_dev, 4))
         return fail(ctx, FKV_EINVAL, "null or misaligned array");
     if (const char *why = check_device(ctx))

@@ -250,6 +250,118 @@ def test_a_page_outside_the_pool_is_reported(fkv, ctx):
         b.table[1, 1] = keep
 
 
+def test_requests_without_positions(fkv, ctx):
+    """Lengths of zero: nothing to see, with new tokens and without."""
+    for lens in ([(0, 0), (0, 1)], [(-1, 1), (0, 2), (-9, 9)], [(-40, 40), (5, 3)]):
+        Batch(fkv, 22, lens, 2, 4, 64, 16, "int8", "f16").check(ctx)
+    b = Batch(fkv, 23, [(-2, 2)], 1, 1, 128, 16, "e4m3", "bf16")
+    out, lse = b.run(ctx, max_len=0)
+    assert ctx.sync_status() == 0 and not out.any() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_views_with_strides(fkv, ctx, new):
+    """K and V pages side by side in one tensor, queries and outputs as slices of wider rows."""
+    b = Batch(fkv, 24, [(300, new), (17, 1)], 3, 2, 128, 32, "e4m3", "bf16")
+    want, lse = b.run(ctx)
+    both = torch.stack([b.pages.k.view(torch.uint8), b.pages.v.view(torch.uint8)], 1)      # [pages, 2, heads, block, dim]
+    scales = torch.stack([b.pages.k_scale, b.pages.v_scale], 2)                             # [pages, heads, 2]
+    pages = fkv.Pages(both[:, 0].view(torch.float8_e4m3fn), both[:, 1].view(torch.float8_e4m3fn), scales[:, :, 0], scales[:, :, 1])
+    T = b.q.shape[0]
+    wide = torch.full((T, 14, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 4:10] = b.q
+    res = torch.full((T, 9, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.page_attend(pages, wide[:, 4:10], _i32(b.cu), _i32(b.len), _i32(np.hstack([b.table, b.table]))[:, :b.table.shape[1]],
+                    max(b.new), max(b.len), out=res[:, 2:8])
+    assert ctx.sync_status() == 0
+    assert torch.equal(res[:, 2:8], want) and (res[:, :2] == 7).all() and (res[:, 8:] == 7).all()
+
+
+@pytest.mark.parametrize("by_token", [False, True])
+def test_pages_past_four_gigabytes(fkv, ctx, by_token):
+    """Byte offsets that do not fit 32 bits: a pool of 5 GiB whose last pages are written, read and attended to."""
+    H, D, block = 2, 128, 64
+    nb = (5 << 30) // (H * D * block)
+    shape = (nb, block, H, D) if by_token else (nb, H, block, D)
+    pools = [torch.zeros(shape, dtype=torch.int8, device="cuda") for _ in range(2)]
+    views = [p.transpose(1, 2) if by_token else p for p in pools]
+    scale = [torch.zeros((nb, H), device="cuda") for _ in range(2)]
+    pages = fkv.Pages(views[0], views[1], scale[0], scale[1])
+    rng = np.random.default_rng(25)
+    n = 150
+    ids = np.array([nb - 1, nb - 3, nb // 2 + 7])
+    slots = ids[np.arange(n) // block] * block + np.arange(n) % block
+    kv = torch.from_numpy(rng.standard_normal((n, 2, H, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    ctx.page_write(pages, kv[:, 0], kv[:, 1], torch.from_numpy(slots).cuda())
+    small = [np.zeros((3, H, block, D), np.uint8) for _ in range(2)]
+    sc = [np.zeros((3, H), np.float32) for _ in range(2)]
+    for i in range(2):
+        paged.write(small[i], sc[i], kv[:, i].double().cpu().numpy(), np.arange(n), "int8")
+        at = torch.from_numpy(ids).cuda()
+        got = views[i][at].contiguous().view(torch.uint8).cpu().numpy()
+        for j in range(3):
+            m = min(block, n - j * block)
+            assert np.array_equal(got[j, :, :m], small[i][j, :, :m])
+        assert np.array_equal(scale[i][at].cpu().numpy(), sc[i])
+    table = _i32([ids])
+    out = torch.zeros((1, 1, H, n, D), dtype=torch.float32, device="cuda")
+    ctx.page_read(pages, _i32([n]), table, 0, n, 0, out, None)
+    want = paged.gather(small[0], sc[0], np.arange(3), n, "int8")
+    assert np.array_equal(out[0, 0].cpu().numpy(), want.astype(np.float32))
+    for new in (1, 40):
+        q = torch.from_numpy(rng.standard_normal((new, 2 * H, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+        o = ctx.page_attend(pages, q, _i32([0, new]), _i32([n]), table, new, n)
+        k, v = (paged.gather(small[i], sc[i], np.arange(3), n, "int8") for i in range(2))
+        w, _, mass, size = paged.attend(q.double().cpu().numpy(), k, v, D ** -0.5, paged.visible(new, n), p0=n - new)
+        bound = 2.0 ** -8 * np.abs(w) + (2.0 ** -11 + 2.0 ** -20 * (size + 24))[..., None] * mass
+        assert (np.abs(o.double().cpu().numpy() - w) <= bound * (1 + 2.0 ** -8)).all()
+    assert ctx.sync_status() == 0
+
+
+def test_first_calls_inside_a_capture():
+    """A fresh process captures every paged call before any has run, replays it twice, and gets what eager calls give."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2607_07144_gb300 as fkv
+i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+def state():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    p = fkv.Pages.empty(40, 2, 16, 64, torch.int8)
+    for t in (p.k, p.v): t.zero_()
+    return dict(p=p, new=i32([300, 1, 40]), ln=i32([0, 0, 0]), tab=torch.full((3, 24), -1, dtype=torch.int32, device="cuda"),
+                free=torch.arange(40, dtype=torch.int32, device="cuda"), taken=i32([0]), cu=i32([0] * 4),
+                slots=torch.zeros(5000, dtype=torch.int64, device="cuda"), pos=torch.zeros(5000, dtype=torch.int32, device="cuda"),
+                x=torch.randn((5000, 8, 64), generator=g, device="cuda", dtype=torch.float16),
+                o=torch.zeros((5000, 4, 64), dtype=torch.float16, device="cuda"),
+                s=torch.zeros((3, 4, 64), dtype=torch.float16, device="cuda"), one=i32([0, 1, 2, 3]),
+                k=torch.zeros((1, 3, 2, 320, 64), device="cuda"), v=torch.zeros((1, 3, 2, 320, 64), device="cuda"))
+def step(ctx, d):
+    ctx.page_plan(d["new"], d["ln"], d["tab"], d["free"], d["taken"], 16, d["cu"], d["slots"], d["pos"])
+    ctx.page_write(d["p"], d["x"][:, :2], d["x"][:, 2:4], d["slots"])
+    ctx.page_attend(d["p"], d["x"][:, 4:], d["cu"], d["ln"], d["tab"], 300, 320, out=d["o"])
+    ctx.page_attend(d["p"], d["x"][:3, 4:], d["one"], d["ln"], d["tab"], 1, 320, out=d["s"])
+    ctx.page_read(d["p"], d["ln"], d["tab"], 0, 320, 0, d["k"], d["v"])
+ctx = fkv.Context(256)
+a, b = state(), state()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step(ctx, a)
+for new in ([300, 1, 40], [5, 3, 1]):
+    for d in (a, b): d["new"].copy_(i32(new))
+    g.replay()
+    step(ctx, b)
+    assert ctx.sync_status() == 0
+    for n in ("ln", "tab", "taken", "cu", "slots", "pos", "o", "s", "k", "v"):
+        assert torch.equal(a[n], b[n]), n
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=280)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
+
+
 # ------------------------------------------------------------------ plans --
 def _plan(ctx, new, ln, table, free, taken, block, rows, in_place=False):
     t = dict(new=_i32(new), ln=_i32(ln), table=_i32(table), free=_i32(free), taken=_i32([taken]),
