@@ -289,13 +289,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
-    // the scale of the share's first page (share_of)
-    float vref = 1.0f;
-    if (n_it > 0) {
-        const int64_t id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
-        if (id >= 0 && id < a.n_blocks)
-            vref = value_scale(a.vs[id * a.scb + h * a.sch]);
-    }
+    // the id of the share's first page, whose value scale the sums of weights are
+    // counted against (share_of); asked for early, used late
+    int first_id = -1;
+    if (n_it > 0 && group < 3)
+        first_id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
+    auto first_scale = [&]() {
+        return first_id >= 0 && first_id < a.n_blocks ? value_scale(a.vs[first_id * a.scb + h * a.sch]) : 1.0f;
+    };
 
     if (group == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -415,10 +416,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     v[u][i] = at >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
             }
         };
-        int nid = check(0, ask(0)), nnid;
+        int nid = ask(0), nnid = ask(1);
+        nid = check(0, nid);
         load(0, nid);
         float scale = ask_scale(nid);
-        nid = check(1, ask(1));
+        const float vref = first_scale();
+        nid = check(1, nnid);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1
             nnid = ask(j + 2);
@@ -517,6 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 fence_proxy_async_smem();
                 mbar_arrive(bar(Q_FULL));
             }
+            const float vref = first_scale();
             // the group's own range of positions, for tiles that need no mask
             const int ga = q.p0 + static_cast<int>(a.gdiv.div(row0 + 128 * w));
             const int gb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + 128 * w + 128, rows) - 1));

@@ -10,17 +10,17 @@ using namespace fkvd;
 namespace {
 
 // ------------------------------------------------------------------ plan --
-// A block scans the requests (tokens, pages given back, pages needed), a
-// consecutive share a thread, and does everything that is counted in pages: the
-// stack, the tables, the lengths.  The tokens' slots and positions follow from
-// those; a few are written by the same block, more by a second launch that
-// starts while the first one ends.  Where there is that much to do, the first
-// launch is a cluster of eight blocks, which all scan and share the pages: no
-// counter in memory orders them, so calls (and graphs) that overlap share
-// nothing.  Latency bounds both launches: each is a chain of three or four loads.
-constexpr int kPlanThreads = 1024, kPlanCluster = 8;
-constexpr int kPlanSmem = (FKV_PAGE_MAX_REQ + 1) * 3 * sizeof(int);
-constexpr int kSlotThreads = 256, kSlotRows = 4;       // the second launch: rows a thread
+// Every block scans the requests (tokens, pages needed, pages given back; a
+// consecutive share a thread) and then does its part of the pages and of the
+// token rows from the inputs alone: a page given back in the call is looked up
+// where its request's table has it, not on the stack.  So blocks wait for one
+// another nowhere, and share no counter that overlapping calls or graphs would
+// share too.  Only what may be the inputs' own arrays, the lengths and the count,
+// has to come after: in the same block where one block does the call (up to 4096
+// rows), else in a second launch of one block, whose own scan runs while the
+// first launch does.  Latency bounds both: a chain of three or four loads.
+constexpr int kPlanThreads = 1024, kPlanRows = 4;      // rows a thread
+constexpr int kPlanSmem = FKV_PAGE_MAX_REQ * 3 * sizeof(int);
 
 struct PlanArgs {
     const int *n_new, *kv_len, *taken;
@@ -28,7 +28,6 @@ struct PlanArgs {
     int64_t *slots;
     int64_t table_stride, n_free, rows;
     int n_req, width, block, share;
-    bool with_rows;              // the plan's block writes slots and positions itself
     FastDiv div;
     unsigned *status;
 };
@@ -52,58 +51,74 @@ __device__ __forceinline__ int last_from(const int *first, int n, int x)
     return lo;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
+// What a call amounts to; all or nothing: one that does not fit has no tokens
+// and no pages.
+struct PlanTotals {
+    int tokens, pages, back;
+    int taken0, taken1;
+    bool bad;
+};
+
+// The requests' totals, and (cu not null) the sums before every request: n_req
+// each in cu, need and back.
+__device__ PlanTotals plan_scan(const PlanArgs &a, int *cu, int *need, int *back)
 {
-    extern __shared__ int sums[];            // n_req + 1 sums each of tokens, pages needed and pages given back
-    __shared__ long long part[3][32];
+    __shared__ int part[3][32];
     __shared__ int bad_s;
-    int *const cu = sums, *const need = sums + a.n_req + 1, *const back = need + a.n_req + 1;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r0 = min(tid * a.share, a.n_req), r1 = min(r0 + a.share, a.n_req);
-    // of all the launch's threads
-    const int blocks = static_cast<int>(gridDim.x), gtid = static_cast<int>(blockIdx.x) * kPlanThreads + tid, gsize = blocks * kPlanThreads;
-    auto sync = [&]() {
-        if (blocks > 1) {
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        } else {
-            __syncthreads();
-        }
-    };
-    const int taken0 = *a.taken;
+    PlanTotals p;
+    p.taken0 = *a.taken;
     if (tid == 0)
         bad_s = 0;
     __syncthreads();
-
-    // this thread's requests: tokens, pages needed, pages given back
-    auto count = [&](int r, int &tokens, int &pages, int &back) {
+    auto count = [&](int r, int *v) {
         const int nn = a.n_new[r], len = a.kv_len[r];
-        tokens = pages = back = 0;
+        v[0] = v[1] = v[2] = 0;
         if (len < 0 || len > FKV_PAGE_MAX_LEN || nn > FKV_PAGE_MAX_LEN - len || blocks_of(a, len) > a.width)
             return false;
         if (nn < 0) {
-            back = blocks_of(a, len);
+            v[2] = blocks_of(a, len);
             return true;
         }
         const int nb = blocks_of(a, len + nn);
-        tokens = nn;
-        pages = nb - blocks_of(a, len);
+        v[0] = nn;
+        v[1] = nb - blocks_of(a, len);
         return nb <= a.width;
     };
-    long long sum[3] = {0, 0, 0};
-    for (int r = r0; r < r1; ++r) {
-        int t, p, b;
-        if (!count(r, t, p, b))
-            bad_s = 1;
-        sum[0] += t, sum[1] += p, sum[2] += b;
+    // Sums are kept in 32 bits; one that does not fit makes the call one that does
+    // not either.
+    int sum[3];
+    bool over = false;
+    {
+        long long wide[3] = {0, 0, 0};
+        for (int r = r0; r < r1; ++r) {
+            int v[3];
+            if (!count(r, v))
+                over = true;
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+                wide[c] += v[c];
+        }
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            over |= wide[c] > 0x7fffffffll;
+            sum[c] = static_cast<int>(min(wide[c], 0x7fffffffll));
+        }
     }
-    long long before[3], all[3];
+    // whether a warp's values, each below 2^31, sum to less than that
+    auto fits = [](unsigned x) {
+        const long long hi = __reduce_add_sync(~0u, x >> 15), lo = __reduce_add_sync(~0u, x & 0x7fffu);
+        return (hi << 15) + lo <= 0x7fffffffll;
+    };
+    int before[3], all[3];
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
-        long long x = sum[c];
+        over |= !fits(sum[c]);
+        int x = sum[c];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(~0u, x, o);
+            const int y = __shfl_up_sync(~0u, x, o);
             if (lane >= o)
                 x += y;
         }
@@ -111,127 +126,135 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
             part[c][warp] = x;
         before[c] = x - sum[c];
     }
+    if (over)
+        bad_s = 1;
     __syncthreads();
+    over = bad_s;
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
-        long long x = part[c][lane];
+        int x = part[c][lane];
+        over |= !fits(x);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(~0u, x, o);
+            const int y = __shfl_up_sync(~0u, x, o);
             if (lane >= o)
                 x += y;
         }
-        const long long prev = __shfl_sync(~0u, x, warp > 0 ? warp - 1 : 0);
+        const int prev = __shfl_sync(~0u, x, warp > 0 ? warp - 1 : 0);
         before[c] += warp > 0 ? prev : 0;
         all[c] = __shfl_sync(~0u, x, 31);
     }
-    const long long taken1 = taken0 - all[2];
-    // all or nothing: a call that does not fit leaves lengths, table and stack as they are
-    const bool bad = bad_s || taken0 < 0 || taken0 > a.n_free || taken1 < 0 || taken1 + all[1] > a.n_free || all[0] > a.rows;
-    const int tokens = bad ? 0 : static_cast<int>(all[0]), pages = bad ? 0 : static_cast<int>(all[1]);
-
-    for (int r = r0; r < r1; ++r) {
-        int t, p, b;
-        count(r, t, p, b);
-        cu[r] = bad ? 0 : static_cast<int>(before[0]);
-        need[r] = bad ? 0 : static_cast<int>(before[1]);
-        back[r] = bad ? 0 : static_cast<int>(before[2]);
-        before[0] += t, before[1] += p, before[2] += b;
-    }
-    if (tid == 0)
-        cu[a.n_req] = tokens;
-    __syncthreads();
-    // pages that come back go onto the stack before any is taken from it
-    for (int i = gtid; i < (bad ? 0 : all[2]); i += gsize) {
-        const int r = last_from(back, a.n_req, i);
-        a.free_ids[taken1 + i] = a.table[r * a.table_stride + i - back[r]];
-    }
-    sync();
-    for (int r = gtid; r <= a.n_req; r += gsize)
-        a.cu[r] = cu[r];
-    for (int i = gtid; i < pages; i += 4 * gsize) {
-        // four at a time, their loads in flight together
-        int id[4], len[4], r[4];
+    const long long taken1 = static_cast<long long>(p.taken0) - all[2];
+    p.bad = over || p.taken0 < 0 || p.taken0 > a.n_free || taken1 < 0 || taken1 + all[1] > a.n_free || all[0] > a.rows;
+    p.taken1 = p.bad ? p.taken0 : static_cast<int>(taken1);
+    p.tokens = p.bad ? 0 : all[0];
+    p.pages = p.bad ? 0 : all[1];
+    p.back = p.bad ? 0 : all[2];
+    if (cu) {
+        for (int r = r0; r < r1; ++r) {
+            cu[r] = p.bad ? 0 : before[0];
+            need[r] = p.bad ? 0 : before[1];
+            back[r] = p.bad ? 0 : before[2];
+            if (r + 1 < r1) {
+                int v[3];
+                count(r, v);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int x = min(i + k * gsize, pages - 1);
-            r[k] = last_from(need, a.n_req, x);
-            id[k] = a.free_ids[taken1 + x];
-            len[k] = a.kv_len[r[k]];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (i + k * gsize < pages)
-                a.table[r[k] * a.table_stride + blocks_of(a, len[k]) + i + k * gsize - need[r[k]]] = id[k];
-    }
-    if (a.with_rows) {
-        for (int t = tid; t < a.rows; t += kPlanThreads) {
-            int64_t slot = -1;
-            int pos = -1;
-            if (t < tokens) {
-                const int r = last_from(cu, a.n_req, t), len = a.kv_len[r], had = blocks_of(a, len);
-                pos = len + t - cu[r];
-                const int j = static_cast<int>(a.div.div(pos));
-                const int id = j < had ? a.table[r * a.table_stride + j] : a.free_ids[taken1 + need[r] + j - had];
-                slot = id < 0 ? -1 : static_cast<int64_t>(id) * a.block + pos - j * a.block;
+                for (int c = 0; c < 3; ++c)
+                    before[c] += v[c];
             }
-            a.slots[t] = slot;
-            a.positions[t] = pos;
         }
+        __syncthreads();
     }
-    sync();
-    // nothing reads lengths or the taken count from here on: the outputs may be
-    // the inputs' own arrays
-    for (int r = gtid; r < a.n_req; r += gsize) {
+    return p;
+}
+
+// What may lie over the inputs: lengths and count.
+__device__ __forceinline__ void plan_finish(const PlanArgs &a, const PlanTotals &p)
+{
+    for (int r = threadIdx.x; r < a.n_req; r += kPlanThreads) {
         const int nn = a.n_new[r], len = a.kv_len[r];
-        a.kv_len_out[r] = bad ? len : (nn < 0 ? 0 : len + nn);
+        a.kv_len_out[r] = p.bad ? len : (nn < 0 ? 0 : len + nn);
     }
-    if (gtid == 0) {
-        *a.taken_out = bad ? taken0 : static_cast<int>(taken1 + all[1]);
-        if (bad)
+    if (threadIdx.x == 0) {
+        *a.taken_out = p.taken1 + p.pages;
+        if (p.bad)
             atomicOr(a.status, FKV_ST_RANGE);
     }
 }
 
-// Slots and positions from the plan's tables, lengths and sums.  A token's
-// request is searched for in the sums, which a block first copies to shared
-// memory (up to kSlotSums of them; more are searched where they lie).
-constexpr int kSlotSums = 8192;
-
-__global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanArgs a)
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanArgs a)
 {
-    extern __shared__ int sums[];
-    const int tid = threadIdx.x;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * (kSlotThreads * kSlotRows);
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // the plan has run
-    const bool copied = a.n_req < kSlotSums;
-    if (copied) {
-        for (int i = tid; i <= a.n_req; i += kSlotThreads)
-            sums[i] = a.cu[i];
+    extern __shared__ int sums[];            // n_req sums each of tokens, pages needed and pages given back
+    int *const cu = sums, *const need = sums + a.n_req, *const back = need + a.n_req;
+    const PlanTotals p = plan_scan(a, cu, need, back);
+    // of all the launch's threads
+    const int gtid = static_cast<int>(blockIdx.x) * kPlanThreads + threadIdx.x, gsize = static_cast<int>(gridDim.x) * kPlanThreads;
+
+    // the x-th page that comes back, and the x-th that is taken: off the stack
+    // once those that came back are used up
+    auto returned = [&](int x) {
+        const int r = last_from(back, a.n_req, x);
+        return a.table[r * a.table_stride + x - back[r]];
+    };
+    auto fresh = [&](int x) { return x < p.back ? returned(x) : a.free_ids[p.taken1 + x]; };
+
+    // the thread's first page of either kind: on their way while the rows are
+    // looked up
+    int page = 0, page_r = 0, page_len = 0, page_back = 0;
+    if (gtid < p.pages) {
+        page_r = last_from(need, a.n_req, gtid);
+        page = fresh(gtid);
+        page_len = a.kv_len[page_r];
+    }
+    if (gtid < p.back)
+        page_back = returned(gtid);
+    for (int r = gtid; r <= a.n_req; r += gsize)
+        a.cu[r] = r < a.n_req ? cu[r] : p.tokens;
+    // the rows, whose loads are in flight together
+    for (int64_t t0 = gtid; t0 < a.rows; t0 += static_cast<int64_t>(kPlanRows) * gsize) {
+        int id[kPlanRows], pos[kPlanRows];
+#pragma unroll
+        for (int k = 0; k < kPlanRows; ++k) {
+            const int64_t t = t0 + static_cast<int64_t>(k) * gsize;
+            id[k] = pos[k] = -1;
+            if (t < p.tokens) {
+                const int r = last_from(cu, a.n_req, static_cast<int>(t)), len = a.kv_len[r], had = blocks_of(a, len);
+                pos[k] = len + static_cast<int>(t) - cu[r];
+                const int j = static_cast<int>(a.div.div(pos[k]));
+                id[k] = j < had ? a.table[r * a.table_stride + j] : fresh(need[r] + j - had);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kPlanRows; ++k) {
+            const int64_t t = t0 + static_cast<int64_t>(k) * gsize;
+            if (t < a.rows) {
+                const int off = pos[k] - static_cast<int>(a.div.div(pos[k])) * a.block;
+                a.slots[t] = id[k] < 0 ? -1 : static_cast<int64_t>(id[k]) * a.block + off;
+                a.positions[t] = pos[k];
+            }
+        }
+    }
+    if (gtid < p.pages)
+        a.table[page_r * a.table_stride + blocks_of(a, page_len) + gtid - need[page_r]] = page;
+    if (gtid < p.back)
+        a.free_ids[p.taken1 + gtid] = page_back;
+    for (int i = gtid + gsize; i < p.pages; i += gsize) {
+        const int r = last_from(need, a.n_req, i), id = fresh(i);
+        a.table[r * a.table_stride + blocks_of(a, a.kv_len[r]) + i - need[r]] = id;
+    }
+    for (int i = gtid + gsize; i < p.back; i += gsize)
+        a.free_ids[p.taken1 + i] = returned(i);
+    if (gridDim.x == 1) {
         __syncthreads();
+        plan_finish(a, p);
     }
-    const int *const cu = copied ? sums : a.cu;
-    const int tokens = cu[a.n_req];
-    int r[kSlotRows], id[kSlotRows], pos[kSlotRows];
-#pragma unroll
-    for (int i = 0; i < kSlotRows; ++i) {
-        const int t = static_cast<int>(min(t0 + i * kSlotThreads + tid, static_cast<int64_t>(tokens) - 1));
-        r[i] = t >= 0 ? last_from(cu, a.n_req, t) : 0;
-        pos[i] = t >= 0 ? a.kv_len_out[r[i]] - cu[r[i] + 1] + t : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < kSlotRows; ++i)
-        id[i] = tokens > 0 ? a.table[r[i] * a.table_stride + a.div.div(pos[i])] : -1;
-#pragma unroll
-    for (int i = 0; i < kSlotRows; ++i) {
-        const int64_t t = t0 + i * kSlotThreads + tid;
-        if (t >= a.rows)
-            return;
-        const bool live = t < tokens;
-        const int off = pos[i] - static_cast<int>(a.div.div(pos[i])) * a.block;
-        a.slots[t] = live && id[i] >= 0 ? static_cast<int64_t>(id[i]) * a.block + off : -1;
-        a.positions[t] = live ? pos[i] : -1;
-    }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan_finish(PlanArgs a)
+{
+    const PlanTotals p = plan_scan(a, nullptr, nullptr, nullptr);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // no block reads the inputs from here on
+    plan_finish(a, p);
 }
 
 // ----------------------------------------------------------------- write --
@@ -681,33 +704,21 @@ cudaError_t launch_page_plan(const fkv_ctx *ctx, const fkv_plan &p, cudaStream_t
     a.kv_len_out = p.kv_len_out, a.taken_out = p.taken_out, a.slots = p.slots;
     a.table_stride = p.table_stride, a.n_free = p.n_free, a.rows = p.rows;
     a.n_req = static_cast<int>(p.n_req), a.width = static_cast<int>(p.width), a.block = static_cast<int>(p.block);
-    const int64_t rows = p.rows;
     a.div = FastDiv::make(static_cast<unsigned>(p.block));
     a.status = ctx->d_status;
     a.share = (a.n_req + kPlanThreads - 1) / kPlanThreads;
-    // one launch while the block's own stores take less than a second launch
-    // does (about 4 us: 4096 rows)
-    a.with_rows = rows <= 4 * kPlanThreads;
-    const size_t smem = (static_cast<size_t>(a.n_req) + 1) * 3 * sizeof(int);
+    const int64_t per = kPlanThreads * kPlanRows, want = (a.rows + per - 1) / per;
+    // a block an SM at most; each scans all requests
+    const int blocks = static_cast<int>(want < 1 ? 1 : want < ctx->sms ? want : ctx->sms);
+    const size_t smem = static_cast<size_t>(a.n_req) * 3 * sizeof(int);
     cudaError_t e = kernel_use(ctx, reinterpret_cast<const void *>(k_page_plan), kPlanThreads, kPlanSmem, nullptr);
     if (e != cudaSuccess)
         return e;
-    if (a.with_rows) {
-        k_page_plan<<<1, kPlanThreads, smem, st>>>(a);
-        return cudaGetLastError();
-    }
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = kPlanCluster, at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kPlanCluster), cfg.blockDim = dim3(kPlanThreads), cfg.dynamicSmemBytes = smem, cfg.stream = st;
-    cfg.attrs = &at, cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, k_page_plan, a);
-    if (e != cudaSuccess)
+    k_page_plan<<<blocks, kPlanThreads, smem, st>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || blocks == 1)
         return e;
-    const int64_t per = kSlotThreads * kSlotRows;
-    const size_t sums = a.n_req < kSlotSums ? (static_cast<size_t>(a.n_req) + 1) * sizeof(int) : 0;
-    return launch_after(k_page_slots, static_cast<unsigned>((rows + per - 1) / per), kSlotThreads, sums, st, a);
+    return launch_after(k_page_plan_finish, 1, kPlanThreads, 0, st, a);
 }
 
 cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
