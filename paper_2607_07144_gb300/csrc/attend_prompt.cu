@@ -407,13 +407,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const int key = first(j) + 16 * lane;
                 from = id * a.sb + (key - static_cast<int>(a.div.div(key)) * a.block) * a.st;
             }
+            // all of them before the first load: a shuffle behind one waits for it as well
+            int64_t at[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                at[u] = __shfl_sync(~0u, from, u);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t at = __shfl_sync(~0u, from, u);
-                const uint8_t *p = pool + at;
+                const uint8_t *p = pool + at[u];
 #pragma unroll
                 for (int i = 0; i < NL; ++i, p += row_step)
-                    v[u][i] = at >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+                    v[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
             }
         };
         int nid = ask(0), nnid = ask(1);
