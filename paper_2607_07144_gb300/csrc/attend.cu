@@ -12,7 +12,8 @@
 // the second product is sum P_j c'_j with P rounded to fp16 (relative 2^-11, an
 // eighth of a bf16 result's own rounding; P spans 2^8 .. 2^-24, so nothing above
 // 2^-32 of the largest weight is lost), and the sum of the weights is
-// sum P_j / vs, from the unrounded P_j, in fp32 (as vref / vs of a first page's vref).  So pages of any scales mix in
+// sum P_j / vs, from the unrounded P_j, in fp32 (as vref / vs, vref the share's first
+// page's scale, which stays in range).  So pages of any scales mix in
 // one accumulator without a rounding of V.
 #include "attend.cuh"
 
@@ -150,49 +151,43 @@ __global__ void __launch_bounds__(128, 3)
     }
     __syncwarp();
 
-    // A lane looks up one of the 32 units (16 keys) of the next 16 iterations:
-    // its page, place in it, and what its scales give the scores.
+    // A lane looks up one of the 32 units (16 keys) of 16 iterations: its page and
+    // what its scales give the scores.  Page ids are asked for a batch of iterations
+    // before the scales, and these a batch before their use, so that no warp waits
+    // for one to ask for the other.
     struct Unit {
-        int id, off;
-        float mul, lvs, ivs;
+        int id;
+        float ks, vs;
     };
     const float mul0 = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : a.scale * kLog2e;
     bool bad = false;
-    float vref = 1.0f;
-    if (n_it > 0) {
-        const int64_t id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
-        if (id >= 0 && id < a.n_blocks)
-            vref = value_scale(a.vs[id * a.scb + h * a.sch]);
-    }
-    auto fetch = [&](int batch) {
-        Unit u = {0, 0, 0.0f, 0.0f, 0.0f};
-        const int it = i0 + batch * 16 + (lane >> 1);
-        if (it < i1) {
-            const int key = tiles.at(it) * kTile + warp * 32 + (lane & 1) * 16;
-            if (key < tiles.lim) {
-                const int j = static_cast<int>(a.div.div(key));
-                u.off = key - j * a.block;
-                u.id = a.table[r * a.table_stride + j];
-                if (u.id < 0 || u.id >= a.n_blocks) {
-                    bad = true;
-                    u.id = 0;
-                }
-                u.mul = a.ks[u.id * a.scb + h * a.sch] * mul0;
-                const float vs = value_scale(a.vs[u.id * a.scb + h * a.sch]);
-                u.lvs = lg2(vs);
-                u.ivs = share_of(vref, vs);
-            }
+    auto key_of = [&](int batch) { return tiles.at(i0 + batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
+    auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && key_of(batch) < tiles.lim; };
+    auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
+    auto ask_scales = [&](int batch, int id) {
+        Unit u = {0, 0.0f, 1.0f};
+        if (on(batch)) {
+            if (id < 0 || id >= a.n_blocks)
+                bad = true;
+            else
+                u.id = id;
+            u.ks = a.ks[u.id * a.scb + h * a.sch], u.vs = a.vs[u.id * a.scb + h * a.sch];
         }
         return u;
     };
-    Unit cur = fetch(0), nxt = fetch(1);
+    const int ref_id = n_it > 0 ? a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)] : -1;
+    int nid = ask(0), nnid = ask(1);
+    const float ref_vs = ref_id >= 0 && ref_id < a.n_blocks ? a.vs[ref_id * a.scb + h * a.sch] : 1.0f;
+    Unit cur = ask_scales(0, nid), nxt = ask_scales(1, nnid);
+    nid = ask(2);
     // keys of iteration `it` from the warp's first one on that are looked at
     auto first_key = [&](int it) { return tiles.at(i0 + it) * kTile + warp * 32; };
     auto issue = [&](int it, int batch) {
         const int nu = min(2, (tiles.lim - first_key(it) + 15) >> 4);
         const int from = (it & 15) * 2 + (lane & 1);
         const bool now = (it >> 4) == batch;
-        const int id = __shfl_sync(~0u, now ? cur.id : nxt.id, from), off = __shfl_sync(~0u, now ? cur.off : nxt.off, from);
+        const int id = __shfl_sync(~0u, now ? cur.id : nxt.id, from);
+        const int key = first_key(it) + (lane & 1) * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
         const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * STAGE;
         if (nu > 0) {
             if (lane == 0)
@@ -285,12 +280,23 @@ __global__ void __launch_bounds__(128, 3)
         l[n][0] = l[n][1] = 0.0f;
     }
 
+    // the scores' multiplier, the logarithm of V's scale, and the latter against the
+    // share's first page's
+    const float vref = n_it > 0 ? value_scale(ref_vs) : 1.0f;
+    float cur_mul, cur_lvs, cur_ivs;
+    auto finish = [&]() {
+        const float vs = value_scale(cur.vs);
+        cur_mul = cur.ks * mul0, cur_lvs = lg2(vs), cur_ivs = share_of(vref, vs);
+    };
+    finish();
     int batch = 0;
     for (int it = 0; it < n_it; ++it) {
         if ((it >> 4) != batch) {
             batch = it >> 4;
             cur = nxt;
-            nxt = fetch(batch + 1);
+            finish();
+            nxt = ask_scales(batch + 1, nid);
+            nid = ask(batch + 2);
         }
         if (it + ST - 1 < n_it)
             issue(it + ST - 1, batch);
@@ -361,8 +367,8 @@ __global__ void __launch_bounds__(128, 3)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int at = (it & 15) * 2 + u;
-            const float mul = __shfl_sync(~0u, cur.mul, at), lvs = __shfl_sync(~0u, cur.lvs, at);
-            ivs[u] = __shfl_sync(~0u, cur.ivs, at);
+            const float mul = __shfl_sync(~0u, cur_mul, at), lvs = __shfl_sync(~0u, cur_lvs, at);
+            ivs[u] = __shfl_sync(~0u, cur_ivs, at);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float x[4];
