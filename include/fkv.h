@@ -513,10 +513,10 @@ int fkv_page_plan(fkv_ctx *ctx, const fkv_plan *plan, void *stream);
 
 /* Quantise the K and V vectors of n_tok tokens (k and v: n_heads heads, the
  * same dtype) into the slots slots_dev[t] (int64; negative: the token is
- * skipped).  Tokens with consecutive slots form a run in each page; a page
- * takes one run a call, and its rows before the run's first one are those
- * written earlier (fkv_page_plan's slots are of this kind).  With amax the
- * run's largest finite magnitude, its wanted scale is
+ * skipped) of a pool of at most 2^32.  Tokens with consecutive slots form a run
+ * in each page; a page takes one run a call, and its rows before the run's first
+ * one are those written earlier (fkv_page_plan's slots are of this kind).  With
+ * amax the run's largest finite magnitude, its wanted scale is
  *     FKV_E4M3: the smallest power of two not below amax / 448,
  *     FKV_INT8: amax / 127 (rounded to float32),
  * at least 2^-100.  A page without earlier rows takes the wanted scale; another

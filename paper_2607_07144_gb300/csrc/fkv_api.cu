@@ -1173,6 +1173,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
         return fail(ctx, FKV_EINVAL, "K and V types differ");
     if ((n_tok / pages->block + 1) * 2 * pages->n_heads > INT32_MAX)
         return fail(ctx, FKV_EINVAL, "too many tokens for one launch");
+    if (pages->n_blocks * pages->block > int64_t(1) << 32)
+        return fail(ctx, FKV_EINVAL, "a pool of more than 2^32 slots");
     if (!slots_dev || misaligned(slots_dev, 8))
         return fail(ctx, FKV_EINVAL, "bad slot map");
     if (const char *why = check_device(ctx))

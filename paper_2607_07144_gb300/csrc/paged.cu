@@ -373,8 +373,9 @@ struct WriteArgs {
     const void *x[2];
     int64_t x_tok[2], x_head[2];
     const int64_t *slots;
-    int64_t T, sb, sh, st, scb, sch, n_blocks;
+    int64_t T, sb, sh, st, scb, sch, n_slots;              // n_slots: at most 2^32
     int block, stretch, heads;
+    FastDiv by_block, by_heads;
     unsigned *status;
 };
 
@@ -456,13 +457,12 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
     constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
     __shared__ uint32_t red[GT / 32];
     const int lane = threadIdx.x & 31, tid = GT == 32 ? lane : threadIdx.x, c = tid % C, row0 = tid / C;
-    int64_t t0, item = blockIdx.x;
+    unsigned item = blockIdx.x;
     if (GT == 32)
         item = item * 8 + (threadIdx.x >> 5);
-    const int h = static_cast<int>(item % a.heads);
-    item /= a.heads;
-    const int kv = item & 1;
-    t0 = (item >> 1) * a.stretch;
+    const unsigned both = a.by_heads.div(item);
+    const int h = static_cast<int>(item - both * a.heads), kv = both & 1;
+    const int64_t t0 = static_cast<int64_t>(both >> 1) * a.stretch;
     if (t0 >= a.T)
         return;
     const int64_t t1 = min(t0 + a.stretch, a.T);
@@ -476,17 +476,16 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
         if (mine < t1) {
             slot_l = a.slots[mine];
             const int64_t prev = mine > 0 ? a.slots[mine - 1] : -2;
-            lead = slot_l >= 0 && (prev != slot_l - 1 || slot_l % a.block == 0);
+            if (slot_l >= a.n_slots)
+                range = true;
+            else if (slot_l >= 0)
+                lead = prev != slot_l - 1 || slot_l == static_cast<int64_t>(a.by_block.div(static_cast<unsigned>(slot_l))) * a.block;
         }
         unsigned leads = __ballot_sync(~0u, lead);
         while (leads) {
             const int who = __ffs(leads) - 1;
             leads &= leads - 1;
-            const int64_t t = base + who, slot = __shfl_sync(~0u, slot_l, who), blk = slot / a.block;
-            if (blk >= a.n_blocks) {
-                range = true;
-                continue;
-            }
+            const int64_t t = base + who, slot = __shfl_sync(~0u, slot_l, who), blk = a.by_block.div(static_cast<unsigned>(slot));
             const int off = static_cast<int>(slot - blk * a.block);
             // the run's length: consecutive slots up to the page's end
             const int most = static_cast<int>(min(static_cast<int64_t>(a.block - off), a.T - t));
@@ -585,7 +584,7 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
     }
     if (nan)
         atomicOr(a.status, FKV_ST_CORRUPT);
-    if (range && tid == 0)
+    if (range)
         atomicOr(a.status, FKV_ST_RANGE);
 }
 
@@ -736,11 +735,12 @@ cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_
     a.slots = slots, a.T = T;
     a.sb = p->stride_block, a.sh = p->stride_head, a.st = p->stride_pos;
     a.scb = p->scale_stride_block, a.sch = p->scale_stride_head;
-    a.n_blocks = p->n_blocks, a.block = p->block;
+    a.n_slots = p->n_blocks * p->block, a.block = p->block;
     a.status = ctx->d_status;
     // a warp a token while that fills the device up to a few times over, else a
     // block for as many tokens as a page holds
     a.heads = p->n_heads;
+    a.by_block = FastDiv::make(static_cast<unsigned>(p->block)), a.by_heads = FastDiv::make(static_cast<unsigned>(p->n_heads));
     a.stretch = T * p->n_heads * 2 <= static_cast<int64_t>(ctx->sms) * 64 ? 1 : p->block;
     const bool i8 = p->format == FKV_INT8;
     switch (k->dtype) {

@@ -617,6 +617,21 @@ def test_refusals(fkv, ctx):
     assert ctx.sync_status() == 0
 
 
+def test_write_slots_are_32_bits(fkv, ctx):
+    """A pool of more than 2^32 slots is refused; in one of 2^32, slots from there on (their low 32 bits name
+    a slot of the pool) are skipped and reported."""
+    one = torch.zeros((1, 1, 1024, 64), dtype=torch.int8, device="cuda")
+    scale = torch.ones((1, 1), device="cuda")
+    x = torch.ones((2, 1, 64), dtype=torch.bfloat16, device="cuda")
+    pool = lambda n: fkv.Pages(*[one.expand(n, -1, -1, -1)] * 2, *[scale.expand(n, -1)] * 2)
+    with pytest.raises(fkv.FkvError) as e:
+        ctx.page_write(pool((1 << 22) + 1), x, x, torch.zeros(2, dtype=torch.int64, device="cuda"))
+    assert e.value.code == -1 and ctx.sync_status() == 0
+    ctx.page_write(pool(1 << 22), x, x, torch.tensor([1 << 32, (1 << 40) + 5], device="cuda"))
+    assert ctx.sync_status() == -2
+    assert not one.any() and (scale == 1).all()
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
