@@ -619,6 +619,8 @@ class Context:
             need = self._attend_need[key] = L.fkv_page_attend_workspace(self._h, buf)
         ws = nb = 0
         if workspace is not None:
+            if workspace.get_device() != dev or not workspace.is_contiguous():
+                raise ValueError("workspace must be a contiguous tensor on cuda:%d" % dev)
             ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         elif need:
             if stream is None:

@@ -632,6 +632,17 @@ def test_write_slots_are_32_bits(fkv, ctx):
     assert not one.any() and (scale == 1).all()
 
 
+def test_workspace_is_on_the_device(fkv, ctx):
+    """A workspace on the host, or one with gaps, is refused before its pointer goes anywhere."""
+    b = Batch(fkv, 30, [(600, 1)], 1, 4, 64, 16, "int8", "f16")
+    cu, ln, tab = _i32(b.cu), _i32(b.len), _i32(b.table)
+    size = 1 << 24
+    for ws in (torch.empty(size, dtype=torch.uint8), torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            ctx.page_attend(b.pages, b.q, cu, ln, tab, 1, 601, workspace=ws)
+    assert ctx.sync_status() == 0
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
