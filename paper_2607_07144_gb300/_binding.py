@@ -542,6 +542,14 @@ class Context:
             raise ValueError("the pages are on cuda:%d, the context on cuda:%d" % (pages.device, self._dev))
         return self._dev
 
+    def _empty(self, shape, dtype, stream) -> torch.Tensor:
+        """Memory for a call on `stream`: the allocator gives out what is free, and takes it back, in that
+        stream's order, not in the current one's."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self._dev)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self._dev)
+
     def page_plan(self, n_new: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free: torch.Tensor,
                   taken: torch.Tensor, block: int, cu: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor,
                   kv_len_out: torch.Tensor = None, taken_out: torch.Tensor = None, stream=None):
@@ -589,15 +597,16 @@ class Context:
         """Attention of q [tokens, query heads, dim] (rows cu[r] .. cu[r+1] the
         last tokens of request r's kv_len[r] positions) over the pages; scale
         defaults to dim ** -0.5.  max_new and max_len bound every request's new
-        tokens and positions.  lse: float32 [tokens, query heads] or None.  The
-        workspace is taken from torch's allocator unless given."""
+        tokens and positions.  lse: float32 [tokens, query heads] or None.  out and
+        the workspace are taken from torch's allocator, on the call's stream, unless
+        given."""
         dev = self._on(pages)
         n = kv_len.numel()
         dim = pages.dim
         qp, qd, shape, qt, qh = _vectors(q, dim, "q", dev)
         T, Hq = shape[0], shape[1]
         if out is None:
-            out = torch.empty((T, Hq, dim), dtype=q.dtype, device=q.device)
+            out = self._empty((T, Hq, dim), q.dtype, stream)
         op, od, oshape, ot, oh = _vectors(out, dim, "out", dev)
         if oshape != shape or od != qd:
             raise ValueError("out must have q's shape and type")
@@ -623,11 +632,7 @@ class Context:
                 raise ValueError("workspace must be a contiguous tensor on cuda:%d" % dev)
             ws, nb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         elif need:
-            if stream is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            else:
-                with torch.cuda.stream(stream):          # the allocator reuses it in that stream's order
-                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = self._empty((need,), torch.uint8, stream)
             ws, nb = workspace.data_ptr(), need
         rc = L.fkv_page_attend(self._h, buf, ws, nb, _stream(stream))
         if rc != OK:

@@ -643,6 +643,22 @@ def test_workspace_is_on_the_device(fkv, ctx):
     assert ctx.sync_status() == 0
 
 
+def test_memory_of_another_stream(fkv, ctx):
+    """What a call on another stream allocates is that stream's: memory freed in the current one's order may
+    still be read there when the call writes it."""
+    b = Batch(fkv, 31, [(600, 1)], 1, 4, 64, 16, "int8", "f16")
+    cu, ln, tab = _i32(b.cu), _i32(b.len), _i32(b.table)
+    want = ctx.page_attend(b.pages, b.q, cu, ln, tab, 1, 601)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out = ctx.page_attend(b.pages, b.q, cu, ln, tab, 1, 601, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    p = out.data_ptr()
+    seg = [s for s in torch.cuda.memory_snapshot() if s["address"] <= p < s["address"] + s["total_size"]]
+    assert len(seg) == 1 and seg[0]["stream"] == side.cuda_stream
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
