@@ -538,7 +538,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * or if (j <= p, unless causal is 0) and (there is no window, or j > p - window,
  * or j < sinks); a token at a negative position sees nothing.
  *     out = sum_j softmax_j(s_j) v_j,   s_j = f(scale q.k_j) + slope (j - p),
- *     f(s) = cap tanh(s / cap) if softcap = cap > 0, else s,
+ *     f(s) = cap tanh(s / cap) if softcap = cap > 0, else s
+ * (scale log2 e, and 2 scale log2 e / cap, finite in float32),
  * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse (float32
  * [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row that sees
  * nothing gets zeros and -infinity.  What masked positions and slots past a

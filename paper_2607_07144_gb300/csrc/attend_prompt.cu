@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const bool v_side = warp & 2;
         const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
         const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
-        const float mul0 = fabsf(a.scale) * (a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : kLog2e);
+        const float mul0 = a.softcap > 0.0f ? fabsf(a.scale) * (2.0f * kLog2e) / a.softcap : fabsf(a.scale) * kLog2e;
         const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
         // where the lane's first row's two 16-byte halves go in a tile
         const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;

@@ -1094,6 +1094,9 @@ const char *check_attend(const fkv_attend *a)
 {
     if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.0f)
         return "bad scale or softcap";
+    // what a product is multiplied by has to be a number: infinity times zero is none
+    if (!isfinite(a->scale * 1.4426951f) || (a->softcap > 0.0f && !isfinite(a->scale * 2.8853901f / a->softcap)))
+        return "scale too large, or too large for the softcap";
     if ((a->causal != 0 && a->causal != 1) || a->reserved != 0)
         return "bad mask";
     if (a->dtype != FKV_F16 && a->dtype != FKV_BF16)

@@ -659,6 +659,18 @@ def test_memory_of_another_stream(fkv, ctx):
     assert len(seg) == 1 and seg[0]["stream"] == side.cuda_stream
 
 
+def test_scale_within_float32(fkv, ctx):
+    """A scale whose multiplier is no float32 number would turn scores of zero into NaN: refused."""
+    b = Batch(fkv, 32, [(40, 1)], 1, 2, 64, 16, "e4m3", "bf16")
+    for opt in (dict(scale=3e38), dict(scale=-3e38), dict(softcap=1e-39), dict(scale=1e3, softcap=1e-36)):
+        with pytest.raises(fkv.FkvError) as e:
+            b.run(ctx, **opt)
+        assert e.value.code == -1
+    b.q.zero_()
+    out, lse = b.run(ctx, softcap=1e-30)[:2]
+    assert torch.isfinite(out).all() and torch.isfinite(torch.as_tensor(lse)).all()
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
