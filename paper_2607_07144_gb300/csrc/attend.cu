@@ -12,9 +12,8 @@
 // the second product is sum P_j c'_j with P rounded to fp16 (relative 2^-11, an
 // eighth of a bf16 result's own rounding; P spans 2^8 .. 2^-24, so nothing above
 // 2^-32 of the largest weight is lost), and the sum of the weights is
-// sum P_j / vs, from the unrounded P_j, in fp32 (as vref / vs, vref the share's first
-// page's scale, which stays in range).  So pages of any scales mix in
-// one accumulator without a rounding of V.
+// sum P_j / vs, from the unrounded P_j, in fp32 (share_of).  So pages of any
+// scales mix in one accumulator without a rounding of V.
 #include "attend.cuh"
 
 using namespace fkvd;
@@ -175,9 +174,7 @@ __global__ void __launch_bounds__(128, 3)
         }
         return u;
     };
-    const int ref_id = n_it > 0 ? a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)] : -1;
     int nid = ask(0), nnid = ask(1);
-    const float ref_vs = ref_id >= 0 && ref_id < a.n_blocks ? a.vs[ref_id * a.scb + h * a.sch] : 1.0f;
     Unit cur = ask_scales(0, nid), nxt = ask_scales(1, nnid);
     nid = ask(2);
     // keys of iteration `it` from the warp's first one on that are looked at
@@ -280,13 +277,11 @@ __global__ void __launch_bounds__(128, 3)
         l[n][0] = l[n][1] = 0.0f;
     }
 
-    // the scores' multiplier, the logarithm of V's scale, and the latter against the
-    // share's first page's
-    const float vref = n_it > 0 ? value_scale(ref_vs) : 1.0f;
+    // the scores' multiplier, the logarithm of V's scale, and what a weight counts
     float cur_mul, cur_lvs, cur_ivs;
     auto finish = [&]() {
         const float vs = value_scale(cur.vs);
-        cur_mul = cur.ks * mul0, cur_lvs = lg2(vs), cur_ivs = share_of(vref, vs);
+        cur_mul = cur.ks * mul0, cur_lvs = lg2(vs), cur_ivs = share_of(vs);
     };
     finish();
     int batch = 0;
@@ -406,7 +401,7 @@ __global__ void __launch_bounds__(128, 3)
             }
         }
         bool grown = false;
-        float mref[NT][2], alpha[NT][2];
+        float mref[NT][2], by[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -418,17 +413,20 @@ __global__ void __launch_bounds__(128, 3)
                 const float mn = fmaxf(m[n][c], x);
                 grown |= mn != m[n][c];
                 mref[n][c] = (mn == -INFINITY ? 0.0f : mn) - kPBits;
-                alpha[n][c] = ex2(m[n][c] - kPBits - mref[n][c]);
+                by[n][c] = m[n][c] - kPBits - mref[n][c];
                 m[n][c] = mn;
             }
         if (__any_sync(~0u, grown)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                l[n][0] *= alpha[n][0], l[n][1] *= alpha[n][1];
+                // a sum is scaled in two halves: counted up to 2^80 a weight (share_of), it
+                // outlasts factors below float32's least
+                const float h0 = ex2(0.5f * by[n][0]), h1 = ex2(0.5f * by[n][1]), f0 = h0 * h0, f1 = h1 * h1;
+                l[n][0] = l[n][0] * h0 * h0, l[n][1] = l[n][1] * h1 * h1;
 #pragma unroll
                 for (int d = 0; d < MO; ++d) {
-                    o[n][d][0] *= alpha[n][0], o[n][d][1] *= alpha[n][1];
-                    o[n][d][2] *= alpha[n][0], o[n][d][3] *= alpha[n][1];
+                    o[n][d][0] *= f0, o[n][d][1] *= f1;
+                    o[n][d][2] *= f0, o[n][d][3] *= f1;
                 }
             }
         }
@@ -532,11 +530,12 @@ __global__ void __launch_bounds__(128, 3)
     float lt = 0.0f, f[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        f[w] = ex2(ml[w][0][row] - mref);
-        lt += ml[w][1][row] * f[w];
+        const float half = ex2(0.5f * (ml[w][0][row] - mref));
+        f[w] = half * half;
+        lt += ml[w][1][row] * half * half;
     }
-    float inv = lt != 0.0f ? vref / lt : 0.0f;
-    float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - log2f(vref) : -INFINITY;
+    float inv = lt != 0.0f ? kRef / lt : 0.0f;
+    float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - kLog2Ref : -INFINITY;
     const int i = live ? static_cast<int>(a.gdiv.div(row0 + row)) : 0;
     const int64_t tok = q.tok0 + i, head = h * a.G + (live ? row0 + row - i * a.G : 0), flat = tok * (a.H * a.G) + head;
     float x[E];

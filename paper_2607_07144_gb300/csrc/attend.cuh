@@ -92,11 +92,13 @@ template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// The sum of weights counts each page's share as vref / vs, vref being the
-// scale of the share's first page, so that it stays in range whatever the
-// scales' size; the ratio is held below 2^100.
+// The sum of weights counts a page's at kRef / vs.  With scales from 2^-100 on
+// that is at most 2^80, and 2^30 weights of 2^15 add up to less than float32
+// holds; the share of a scale of 2^100 is 2^-120, so that one such page is not
+// lost either.
+constexpr float kRef = 0x1p-20f, kLog2Ref = -20.0f;
 __device__ __forceinline__ float value_scale(float vs) { return fmaxf(vs, FKV_PAGE_MIN_SCALE); }
-__device__ __forceinline__ float share_of(float vref, float vs) { return fminf(__fdividef(vref, vs), 0x1p100f); }
+__device__ __forceinline__ float share_of(float vs) { return __fdividef(kRef, vs); }
 
 }  // namespace fkvd
 

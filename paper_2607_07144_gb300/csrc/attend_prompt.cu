@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     using S = PromptShape<D>;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
-    // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and vref / vs
+    // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and share_of(vs)
     __shared__ float k_scales[4][8];
     __shared__ float2 v_scales[4][8];
     __shared__ uint32_t tmem_slot;
@@ -288,15 +288,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-
-    // the id of the share's first page, whose value scale the sums of weights are
-    // counted against (share_of); asked for early, used late
-    int first_id = -1;
-    if (n_it > 0 && group < 3)
-        first_id = a.table[r * a.table_stride + a.div.div(tiles.at(i0) * kTile)];
-    auto first_scale = [&]() {
-        return first_id >= 0 && first_id < a.n_blocks ? value_scale(a.vs[first_id * a.scb + h * a.sch]) : 1.0f;
-    };
 
     if (group == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -424,7 +415,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         nid = check(0, nid);
         load(0, nid);
         float scale = ask_scale(nid);
-        const float vref = first_scale();
         nid = check(1, nnid);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1
@@ -432,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (lane < 4) {
                 if (v_side) {
                     const float vs = value_scale(scale);
-                    v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vref, vs));
+                    v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vs));
                 } else {
                     k_scales[j & 3][4 * w + lane] = scale * mul0;
                 }
@@ -524,7 +514,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 fence_proxy_async_smem();
                 mbar_arrive(bar(Q_FULL));
             }
-            const float vref = first_scale();
             // the group's own range of positions, for tiles that need no mask
             const int ga = q.p0 + static_cast<int>(a.gdiv.div(row0 + 128 * w));
             const int gb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + 128 * w + 128, rows) - 1));
@@ -666,8 +655,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                             mx = fmaxf(mx, fmaf(s[e], mul[e / 16], off[e / 16]));
                         const float to = fmaxf(st.m, mx > -INFINITY ? ceilf(mx) - kPBits : st.m);
                         const float f = to == st.m ? 1.0f : ex2(st.m - to);
+                        // (the sum in two halves: counted up to 2^80 a weight, it outlasts
+                        // factors below float32's least)
+                        const float half = to == st.m ? 1.0f : ex2(0.5f * (st.m - to));
                         st.m = to;
-                        st.l *= f;
+                        st.l = st.l * half * half;
                         // the products so far are done: their commit came before this tile's scores'
                         if (j > 0) {
 #pragma unroll 1
@@ -737,8 +729,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (n_own > 0 && ok)
                 ok = mbar_park(bar(O_FULL + w), 0, a.status);
             tc_fence_after();
-            const float inv = st.l != 0.0f ? vref / st.l : 0.0f;
-            const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - log2f(vref) : -INFINITY;
+            const float inv = st.l != 0.0f ? kRef / st.l : 0.0f;
+            const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - kLog2Ref : -INFINITY;
             const int64_t flat = tok * (a.H * a.G) + head, at = split * a.T * (a.H * a.G) + flat;
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {

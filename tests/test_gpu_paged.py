@@ -135,6 +135,43 @@ def test_steps(fkv, ctx, D, fmt, dtype, block, G):
     Batch(fkv, 1, RAGGED, 2, G, D, block, fmt, dtype, by_token=G == 4, gap=2).check(ctx)
 
 
+@pytest.mark.parametrize("first,second", [(3, -100), (20, -100), (-100, 20), (60, -60), (100, -20), (-100, -100)])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("D,new", [(64, 1), (128, 7), (128, 40), (64, 300)])
+def test_value_scales_far_apart(fkv, ctx, D, new, fmt, first, second):
+    """Pages whose V scales differ by up to 2^120 (one of zeros has 2^-100) count alike in the sum of weights.
+    A weight is held as 2^(y - m + bits) in float32, y = log2 of weight x scale: what lies 2^126 under 2^-130
+    of the row's largest y (bits > 4, m at most the largest y rounded up) may be flushed to zero, in the sum
+    and in the product; `lost` is that part of the weights."""
+    b = Batch(fkv, 33, [(200, new), (64, new)], 2, 4, D, 32, fmt, "bf16")
+    for r in range(2):
+        for j in range(-(-b.len[r] // 32)):
+            b.scale[1][b.table[r, j]] = 2.0 ** (second if j % 2 else first)
+    b.pages.v_scale.copy_(torch.from_numpy(b.scale[1]))
+    out, lse = b.run(ctx)
+    assert ctx.sync_status() == 0
+    o, l, q = (t.double().cpu().numpy() for t in (out, lse, b.q))
+    for r, n in enumerate(b.new):
+        k, v = (paged.gather(c, s, b.table[r], b.len[r], fmt) for c, s in zip(b.codes, b.scale))
+        vs = b.scale[1][b.table[r, np.arange(b.len[r]) // 32]].astype(np.float64)       # [position, head]
+        rows = slice(b.cu[r], b.cu[r + 1])
+        want, wl, mass, size = paged.attend(q[rows], k, v, D ** -0.5, paged.visible(n, b.len[r], True, 0, 0, None))
+        for i in range(n):
+            end = b.before[r] + i + 1
+            for u in range(b.H * b.G):
+                x = D ** -0.5 * (k[u // b.G, :end] @ q[b.cu[r] + i, u])
+                y = x / np.log(2) + np.log2(vs[:end, u // b.G])
+                w = np.exp(x - wl[i, u])
+                low = y < y.max() - 130
+                lost, gone = w[low].sum(), w[low] @ np.abs(v[u // b.G, :end][low])
+                assert lost < 0.5
+                ds = 2.0 ** -20 * (size[i, u] + abs(wl[i, u]) + 16)
+                assert abs(l[b.cu[r] + i, u] - wl[i, u]) <= ds - np.log1p(-lost)
+                bound = (2.0 ** -8 * np.abs(want[i, u]) + (2.0 ** -11 + ds + end * 2.0 ** -30) * mass[i, u] * 1.01 +
+                         (lost * mass[i, u] + gone) / (1 - lost) * 1.01 + 1e-30)
+                assert (np.abs(o[b.cu[r] + i, u] - want[i, u]) <= bound).all()
+
+
 MASKS = [dict(causal=False), dict(window=1), dict(window=37, sinks=4), dict(window=300, sinks=130), dict(softcap=5.0),
          dict(slopes=True), dict(prefix=[3, 90, 200, 1000, 0, 17]), dict(window=20, sinks=2, prefix=[0, 140, 300, 7, 1, 1]),
          dict(causal=False, window=30, sinks=3, softcap=20.0, slopes=True), dict(scale=-0.3)]
