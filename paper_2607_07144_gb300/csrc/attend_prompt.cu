@@ -482,34 +482,56 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const RowMask mask(a, q, st.p, live);
             st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
             st.slope = a.slopes && live ? a.slopes[head] * kLog2e : 0.0f;
-            // the query row as fp16 (a negative scale turns its sign)
+            // The warp's 32 query rows as fp16 (a negative scale turns their sign), LR lanes
+            // a row: with a row a lane each access would touch 32 lines, 2000 cycles a
+            // block for 64 dimensions.
+            const int first = row0 + 128 * w + 32 * (warp & 3);
+            const uint32_t q_tile = sbase + S::off_q + w * S::tile + 32 * (warp & 3) * 128;
+            // 16-byte piece k of row r of the warp's in a tile of 128-byte rows
+            auto piece = [&](int r, int k) { return q_tile + (k >> 3) * S::half + r * 128 + (((k & 7) ^ (r & 7)) << 4); };
             {
-                const T *src = static_cast<const T *>(a.q) + tok * a.q_tok + head * a.q_head;
-                uint4 v[D / 8];
-                float amax = 0.0f;
+                constexpr int LR = D / 8, RI = 32 / LR;                  // rows at a time
+                const int c = lane % LR, rr = lane / LR;
+                uint4 v[LR];
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k) {
-                    v[k] = live ? reinterpret_cast<const uint4 *>(src)[k] : make_uint4(0, 0, 0, 0);
-                    const T *y = reinterpret_cast<const T *>(&v[k]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        amax = fmaxf(amax, fabsf(static_cast<float>(y[e])));
+                for (int k = 0; k < LR; ++k) {
+                    const int x = first + k * RI + rr;
+                    v[k] = make_uint4(0, 0, 0, 0);
+                    if (x < rows) {
+                        const int xi = static_cast<int>(a.gdiv.div(x));
+                        const T *src = static_cast<const T *>(a.q) + (q.tok0 + xi) * a.q_tok + (h * a.G + x - xi * a.G) * a.q_head;
+                        v[k] = reinterpret_cast<const uint4 *>(src)[c];
+                    }
                 }
-                float up = a.scale < 0.0f ? -1.0f : 1.0f;
-                if (!std::is_same<T, __half>::value) {
-                    const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
-                    up *= __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
-                    st.down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
-                }
-                const uint32_t at = sbase + S::off_q + w * S::tile + local * 128;
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k) {
-                    const T *y = reinterpret_cast<const T *>(&v[k]);
-                    uint32_t f[4];
+                for (int k = 0; k < LR; ++k) {
+                    uint32_t y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+                    if (std::is_same<T, __half>::value) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        f[e] = pack_half(static_cast<float>(y[2 * e]) * up, static_cast<float>(y[2 * e + 1]) * up);
-                    sts128(at + (k >> 3) * S::half + (((k & 7) ^ (local & 7)) << 4), f[0], f[1], f[2], f[3]);
+                        for (int e = 0; e < 4; ++e)
+                            y[e] ^= a.scale < 0.0f ? 0x80008000u : 0u;
+                    } else {
+                        // brought to [2^14, 2^15) by a power of two (see attend.cu)
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(y[e] & 0x7fff7fffu));
+                        m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+                        for (int o = 1; o < LR; o *= 2)
+                            m = max(m, __shfl_xor_sync(~0u, m, o));
+                        const int e2 = max(static_cast<int>(m >> 7) - 127, -100);
+                        float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e2) << 23);
+                        const float down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e2) << 23);
+                        const float mine = __shfl_sync(~0u, down, lane % RI * LR);
+                        if (lane / RI == k)
+                            st.down = mine;
+                        up = a.scale < 0.0f ? -up : up;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = pack_half(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
+                    }
+                    sts128(piece(k * RI + rr, c), y[0], y[1], y[2], y[3]);
                 }
                 fence_proxy_async_smem();
                 mbar_arrive(bar(Q_FULL));
@@ -732,32 +754,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const float inv = st.l != 0.0f ? kRef / st.l : 0.0f;
             const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - kLog2Ref : -INFINITY;
             const int64_t flat = tok * (a.H * a.G) + head, at = split * a.T * (a.H * a.G) + flat;
-#pragma unroll
+            // Rows meet in the group's query tile, which no product reads any more, 128
+            // bytes of each at a time, and eight lanes write a row's.
+            auto flush = [&](int chunk) {
+                __syncwarp();
+#pragma unroll 2
+                for (int k = 0; k < 8; ++k) {
+                    const int rl = 4 * k + (lane >> 3), x = first + rl;
+                    if (x >= rows)
+                        continue;
+                    const int xi = static_cast<int>(a.gdiv.div(x));
+                    const int64_t xt = q.tok0 + xi, xh = h * a.G + x - xi * a.G;
+                    uint8_t *dst = a.splits == 1
+                                       ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + xt * a.o_tok + xh * a.o_head)
+                                       : reinterpret_cast<uint8_t *>(a.ws_o + ((split * a.T + xt) * (a.H * a.G) + xh) * D);
+                    *reinterpret_cast<uint4 *>(dst + chunk * 128 + (lane & 7) * 16) =
+                        *reinterpret_cast<const uint4 *>(raw + (piece(rl, lane & 7) - smem_u32(raw)));
+                }
+                __syncwarp();
+            };
+#pragma unroll 1
             for (int k = 0; k < D / 32; ++k) {
                 float o[32];
                 tmem_ld32(o_t + 32 * k, o);
                 tmem_wait_ld(o);
-                if (!live)
-                    continue;
                 // a row that saw nothing has no products either: tensor memory holds anything
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                     o[e] = st.l != 0.0f ? o[e] * inv : 0.0f;
                 if (a.splits == 1) {
-                    T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + 32 * k;
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         T y[8];
 #pragma unroll
                         for (int f = 0; f < 8; ++f)
                             y[f] = from_float<T>(o[e + f]);
-                        *reinterpret_cast<uint4 *>(dst + e) = *reinterpret_cast<const uint4 *>(y);
+                        const uint4 z = *reinterpret_cast<const uint4 *>(y);
+                        sts128(piece(lane, 4 * (k & 1) + e / 8), z.x, z.y, z.z, z.w);
                     }
+                    if (k & 1)
+                        flush(k >> 1);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4 *>(a.ws_o + at * D + 32 * k + e) =
-                            make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        sts128(piece(lane, e / 4), __float_as_uint(o[e]), __float_as_uint(o[e + 1]), __float_as_uint(o[e + 2]),
+                               __float_as_uint(o[e + 3]));
+                    flush(k);
                 }
             }
             if (live) {
