@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kRows = 256, kThreads = 512;
 constexpr float kPBits = 6.0f;          // a reference gives its own score the weight 2^6
-constexpr float kMostSum = 32768.0f;    // of 16 weights: each then fits fp16
+constexpr float kMostSum = 32768.0f;    // of 64 weights: each then fits fp16
 
 template <int D> struct PromptShape {
     static constexpr int half = 128 * 128;                   // 64 dimensions of 128 rows in fp16
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             }
             return id;
         };
-        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 0.0f; };
+        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
         uint4 v[4][NL];
         auto load = [&](int j, int id) {
             // the unit's first row in the pool, from the lane that knows its page
@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const float *const km = k_scales[j & 3];
                 const float2 *const vm = v_scales[j & 3];
                 const bool full = all_see(a, q, ga, gb, key, key + kTile);
-                const bool plain = full && a.softcap == 0.0f && !a.slopes;
+                const bool simple = a.softcap == 0.0f && !a.slopes, plain = full && simple;
                 // before the scores are there: the pages' multipliers
                 float km_r[8], vo_r[8];
 #pragma unroll
@@ -561,11 +561,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 if (!ok)
                     break;
                 tc_fence_after();
-                // A tile that needs neither masks nor more than a multiplication, and
-                // whose rows have their reference: two halves of 64 columns, the second's
-                // products on their way while the first's weights are stored.
+                // the visible ones of 32 keys as bits: ranges meet as words, and a score's
+                // test is one bit (its three comparisons, short cuts and all, took 80
+                // cycles a score)
+                auto seen = [&](int j0) {
+                    return (below(st.hi - j0) & (~below(st.from - j0) | below(a.sinks - j0))) | below(st.pre - j0);
+                };
+                // A tile that needs no more than masks and a multiplication, and whose rows
+                // have their reference: two halves of 64 columns, the second's products on
+                // their way while the first's weights are stored.
                 int k = 0, again = j == 0;
-                if (plain && j > 0) {
+                if (simple && j > 0) {
                     float s[64], sum[4];
                     uint32_t p[32];
                     auto evaluate = [&](int half) {
@@ -584,13 +590,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                             sum[n] = sx + sy;
                         }
                         // (not <=: a sum that is no number is looked at as well)
-                        return __any_sync(~0u, !(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) <= kMostSum) ||
+                        return __any_sync(~0u, !((sum[0] + sum[1]) + (sum[2] + sum[3]) <= kMostSum) ||
                                                    st.m == -INFINITY);
+                    };
+                    // a masked product is -infinity (times a multiplier of zero no number,
+                    // which is looked at below)
+                    auto hide = [&](int half) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const uint32_t vis = seen(key + 64 * half + 32 * x);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                s[32 * x + e] = vis >> e & 1 ? s[32 * x + e] : -INFINITY;
+                        }
                     };
                     tmem_ld32(s_t, s);
                     tmem_ld32(s_t + 32, s + 32);
                     tmem_wait_ld(s);
                     tmem_wait_ld(s + 32);
+                    if (!full)
+                        hide(0);
                     again = evaluate(0);
                     if (!again) {
                         tmem_ld32(s_t + 64, s);
@@ -604,6 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         tmem_wait_ld(s);
                         tmem_wait_ld(s + 32);
                         k = 1;
+                        if (!full)
+                            hide(1);
                         again = evaluate(1);
                         if (!again) {
 #pragma unroll
@@ -651,13 +672,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                                 s[e] = fmaf(st.slope, at + static_cast<float>(e), s[e]);
                         }
                         if (!full) {
-                            // the visible keys as bits: ranges meet as words, and a
-                            // score's test is one bit (its three comparisons, short
-                            // cuts and all, took 80 cycles a score)
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                const int j0 = key + 64 * k + 32 * x;
-                                const uint32_t vis = (below(st.hi - j0) & (~below(st.from - j0) | below(a.sinks - j0))) | below(st.pre - j0);
+                                const uint32_t vis = seen(key + 64 * k + 32 * x);
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
                                     s[32 * x + e] = vis >> e & 1 ? s[32 * x + e] : -INFINITY;
@@ -728,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         sum[n] = sx + sy;
                     }
                     // (not <=: a sum that is no number is looked at as well)
-                    if (!again && __any_sync(~0u, !(fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) <= kMostSum) ||
+                    if (!again && __any_sync(~0u, !((sum[0] + sum[1]) + (sum[2] + sum[3]) <= kMostSum) ||
                                                       st.m == -INFINITY)) {
                         again = 1;
                         continue;

@@ -708,6 +708,15 @@ def test_scale_within_float32(fkv, ctx):
     assert torch.isfinite(out).all() and torch.isfinite(torch.as_tensor(lse)).all()
 
 
+@pytest.mark.parametrize("scale", [0.0, 1e-38])
+def test_masks_of_vanishing_scores(fkv, ctx, scale):
+    """Scores that are zero, or too small for float32, still have their masks."""
+    for D, dtype in ((64, "f16"), (128, "bf16")):
+        b = Batch(fkv, 34, [(130, 300), (5, 40), (0, 3), (400, 1)], 1, 2, D, 16, "int8", dtype)
+        b.check(ctx, scale=scale)
+        b.check(ctx, scale=scale, window=37, sinks=3, prefix=[20, 0, 3, 7])
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
