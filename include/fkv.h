@@ -556,8 +556,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * FKV_ERANGE in the status word.  Rows of no request are left as they are.
  * workspace: fkv_page_attend_workspace(ctx, a) bytes, 256-byte aligned (NULL
  * when that is 0), the caller's own until the call has run: calls that may
- * overlap need one each.  The bytes depend on the sizes alone, so a captured
- * call can be replayed with other lengths. */
+ * overlap need one each.  The bytes depend on the sizes (and whether there is a
+ * prefix) alone, so a captured call can be replayed with other lengths. */
 typedef struct {
     const fkv_pages *pages;      /* host struct, read by the call */
     const void *q;               /* vectors by (token, head) as fkv_rows: 16-byte */

@@ -620,7 +620,7 @@ class Context:
             window, sinks, qd, Hq, causal, dim ** -0.5 if scale is None else scale, softcap, 0)
         L = lib()
         # the workspace's size depends on these alone
-        key = (T, Hq, n, max_new, max_len, window, pages.heads, dim)
+        key = (T, Hq, n, max_new, max_len, window, sinks, prefix is None, pages.heads, dim)
         need = self._attend_need.get(key)
         if need is None:
             if len(self._attend_need) >= 4096:

@@ -716,9 +716,12 @@ Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
     const int64_t blocks = c.n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
+    // all that a block of rows may look at: with a window, that and the sinks (whose
+    // tiles end apart); a prefix may be of any length
     int64_t span = c.max_len;
-    if (window && window + c.max_new + 2 * kTile < span)
-        span = window + c.max_new + 2 * kTile;
+    const int64_t seen = c.window + c.max_new + 2 * kTile + (c.sinks > 0 ? c.sinks + kTile : 0);
+    if (window && !c.prefix && c.sinks < FKV_PAGE_MAX_LEN && seen < span)
+        span = seen;
     const int tiles = static_cast<int>((span + kTile - 1) / kTile);
     double best = 0.0;
     p.splits = 1;

@@ -717,6 +717,17 @@ def test_masks_of_vanishing_scores(fkv, ctx, scale):
         b.check(ctx, scale=scale, window=37, sinks=3, prefix=[20, 0, 3, 7])
 
 
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("D,fmt,dtype", [(64, "int8", "f16"), (128, "e4m3", "bf16")])
+def test_window_far_from_sinks_and_prefix(fkv, ctx, D, fmt, dtype, new):
+    """A window's keys and the first ones are both looked at, however many the latter are."""
+    b = Batch(fkv, 37, [(x, new) for x in (300, 2100, 5000)], 1, 4, D, 16, fmt, dtype)
+    rows = [0, new // 2, new - 1]
+    for opt in (dict(sinks=1500), dict(sinks=1 << 40), dict(prefix=[5, 600, 4100]), dict(sinks=700, prefix=[0, 1000, 300])):
+        b.check(ctx, rows=rows, window=100, **opt)
+    b.check(ctx, rows=rows, window=1, sinks=129)
+
+
 # --------------------------------------------------------------- together --
 def test_serving_loop_and_archive(fkv, oracle_mod):
     """Prompts, steps and a request that ends, all captured once and replayed; then the positions that leave
