@@ -70,7 +70,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
 // of what tcgen05 multiplies at least; its rate leaves the bytes the bound.
 // 8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, e4m3, 495 us, 6.6
 // TB/s; one of 131k, int8 with a cap, 52 us, 5.2 TB/s (the codes' conversion).  Up
-// to 28 rows, 24 sequences, a window of 4,096: 90 us, 2.2 TB/s (the chain of a
+// to 28 rows, 24 sequences, a window of 4,096, a bias: 87 us, 2.3 TB/s (the chain of a
 // warp's iteration, and two tiles of rows that read the keys each).
 template <int D, int NT> struct StepShape {
     static constexpr int stages = D == 128 ? 2 : 4, ring = 4 * stages * 64 * D;
@@ -144,7 +144,14 @@ __global__ void __launch_bounds__(128, 3)
     const int ia = static_cast<int>(a.gdiv.div(row0)), ib = static_cast<int>(a.gdiv.div(min(row0 + R - 1, rows - 1)));
     const int pa = q.p0 + ia, pb = q.p0 + ib;
     const Tiles tiles(a, q, pa, pb);
-    const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk), n_it = max(0, i1 - i0);
+    const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk);
+    // the last tile may end before this warp's keys
+    const int n_it = max(0, i1 - i0) - (i1 > i0 && tiles.at(i1 - 1) * kTile + warp * 32 >= tiles.lim);
+    // A bias by distance grows along the keys, and the maximum with it, so that the
+    // outputs are scaled at every iteration: biased scores are walked from the last
+    // tile back.
+    const bool back = a.slopes != nullptr;
+    auto tile_at = [&](int it) { return tiles.at(i0 + (back ? n_it - 1 - it : it)); };
 
     const uint32_t ring = sbase + warp * ST * STAGE, bar0 = smem_u32(bars) + warp * ST * 8;
     if (lane == 0) {
@@ -164,7 +171,7 @@ __global__ void __launch_bounds__(128, 3)
     };
     const float mul0 = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : a.scale * kLog2e;
     bool bad = false;
-    auto key_of = [&](int batch) { return tiles.at(i0 + batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
+    auto key_of = [&](int batch) { return tile_at(batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
     auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && key_of(batch) < tiles.lim; };
     auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
     auto ask_scales = [&](int batch, int id) {
@@ -182,7 +189,7 @@ __global__ void __launch_bounds__(128, 3)
     Unit cur = ask_scales(0, nid), nxt = ask_scales(1, nnid);
     nid = ask(2);
     // keys of iteration `it` from the warp's first one on that are looked at
-    auto first_key = [&](int it) { return tiles.at(i0 + it) * kTile + warp * 32; };
+    auto first_key = [&](int it) { return tile_at(it) * kTile + warp * 32; };
     auto issue = [&](int it, int batch) {
         const int nu = min(2, (tiles.lim - first_key(it) + 15) >> 4);
         const int from = (it & 15) * 2 + (lane & 1);
@@ -300,8 +307,6 @@ __global__ void __launch_bounds__(128, 3)
         if (it + ST - 1 < n_it)
             issue(it + ST - 1, batch);
         const int key = first_key(it), nu = min(2, (tiles.lim - key + 15) >> 4);
-        if (nu <= 0)
-            break;                      // the last tile's end
         if (!mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status)) {
             // give the loads in flight a while to land before the memory is used again
             for (int k = it + 1; k < min(n_it, it + ST); ++k)

@@ -719,6 +719,19 @@ def test_masks_of_vanishing_scores(fkv, ctx, scale):
 
 @pytest.mark.parametrize("new", [1, 5, 150])
 @pytest.mark.parametrize("D,fmt,dtype", [(64, "int8", "f16"), (128, "e4m3", "bf16")])
+def test_bias_at_every_end(fkv, ctx, D, fmt, dtype, new):
+    """Biased scores, walked from the last tile back: ends in each of a tile's quarters, shares of long ones."""
+    b = Batch(fkv, 35, [(x, new) for x in (0, 31, 32, 63, 64, 95, 96, 127, 128, 160, 300, 2100)], 1, 4, D, 16, fmt, dtype)
+    rows = [0, new // 2, new - 1]
+    slopes = [0.5, 0.25, 0.03, -0.02]
+    b.check(ctx, rows=rows, slopes=slopes)
+    b.check(ctx, rows=rows, slopes=slopes, window=100, sinks=40, prefix=[0, 10, 40, 0, 70, 1, 0, 128, 0, 5, 200, 600])
+    long = Batch(fkv, 36, [(20000, new)], 1, 4, D, 32, fmt, dtype)
+    long.check(ctx, rows=rows, slopes=slopes)
+
+
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("D,fmt,dtype", [(64, "int8", "f16"), (128, "e4m3", "bf16")])
 def test_window_far_from_sinks_and_prefix(fkv, ctx, D, fmt, dtype, new):
     """A window's keys and the first ones are both looked at, however many the latter are."""
     b = Batch(fkv, 37, [(x, new) for x in (300, 2100, 5000)], 1, 4, D, 16, fmt, dtype)
