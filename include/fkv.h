@@ -546,8 +546,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * request's end hold does not matter.  Sums, maxima and weights are held in
  * float32, a weight times V's scale as a normal number up to 2^15: one that lies
  * more than 2^130 below the row's largest counts as zero (which takes pages of
- * V scales that far apart, or nearly).  The weights are rounded to fp16 for the
- * product with V.
+ * V scales that far apart, or nearly).  For the product with V they are rounded
+ * to fp16, and to zero below 2^-30 of the largest.
  * table, table_stride and width as in fkv_page_plan.  max_new and max_len bound
  * n_new and kv_len of every request (they size the launch).  A request whose
  * numbers do not hold together (cu not increasing or past n_tok, a length past

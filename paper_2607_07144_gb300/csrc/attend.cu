@@ -70,7 +70,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
 // of what tcgen05 multiplies at least; its rate leaves the bytes the bound.
 // 8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, e4m3, 495 us, 6.6
 // TB/s; one of 131k, int8 with a cap, 52 us, 5.2 TB/s (the codes' conversion).  Up
-// to 28 rows, 24 sequences, a window of 4,096, a bias: 87 us, 2.3 TB/s (the chain of a
+// to 28 rows, 24 sequences, a window of 4,096, a bias: 88 us, 2.3 TB/s (the chain of a
 // warp's iteration, and two tiles of rows that read the keys each).
 template <int D, int NT> struct StepShape {
     static constexpr int stages = D == 128 ? 2 : 4, ring = 4 * stages * 64 * D;
