@@ -68,7 +68,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
 // takes 16 consecutive bytes of a key as four steps' operands, and 16 bytes of a
 // value row as 16 rows of the result.  mma.sync, as these shapes are a sixteenth
 // of what tcgen05 multiplies at least; its rate leaves the bytes the bound.
-// 8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, e4m3, 495 us, 6.6
+// 8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, e4m3, 497 us, 6.6
 // TB/s; one of 131k, int8 with a cap, 52 us, 5.2 TB/s (the codes' conversion).  Up
 // to 28 rows, 24 sequences, a window of 4,096, a bias: 88 us, 2.3 TB/s (the chain of a
 // warp's iteration, and two tiles of rows that read the keys each).
