@@ -12,7 +12,8 @@
 // descriptor.  A tile is read once, against the row's reference exponent from the
 // tiles before: only when weights come out above 2^15 does the reference move up
 // to the largest score seen (O and what has been written of P are then scaled by
-// the power of two between them, exactly), so no pass looks for the maximum.
+// the power of two between them, exactly but for weights that become subnormal in
+// fp16, 2^-20 of the largest and less), so no pass looks for the maximum.
 //
 // Two pieces of 4,096 tokens against 12-16k positions, 8 heads of 128 with 4 query
 // heads each: 1,386 us, 1.38 PFLOP/s, bound by a group's round of scores, softmax
@@ -734,15 +735,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                             }
                         }
                         if (k > 0) {
-                            const __half2 f2 = __float2half2_rn(f);
+                            // in fp32: a factor below fp16's least, 2^-24, still leaves weights
+                            // of up to 2^15 something
 #pragma unroll 1
                             for (int c = 0; c < 32; c += 16) {
                                 uint32_t o[16];
                                 tmem_ld16(s_t + c, o);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) {
-                                    const __half2 y = __hmul2(*reinterpret_cast<__half2 *>(&o[e]), f2);
-                                    o[e] = *reinterpret_cast<const uint32_t *>(&y);
+                                    const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&o[e]));
+                                    o[e] = pack_half(y.x * f, y.y * f);
                                 }
                                 tmem_st16(s_t + c, o);
                             }

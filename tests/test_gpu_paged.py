@@ -399,6 +399,30 @@ print("same")
     assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
 
 
+@pytest.mark.parametrize("slopes", [None, [0.0, 0.0]])
+@pytest.mark.parametrize("D,fmt,dtype", [(64, "int8", "f16"), (128, "e4m3", "bf16")])
+def test_weights_stored_before_a_larger_score_keep_their_share(fkv, ctx, D, fmt, dtype, slopes):
+    """A tile of many rows whose second half holds a score 2^18 times its first half's largest weight, and more
+    above what came before; its value is zero (a sink's), so that the output is the first half's alone: 2^-18 of
+    the largest weight times 100, far above the 2^-30 below which weights may be zero."""
+    b = Batch(fkv, 40, [(512, 64)], 1, 2, D, 16, fmt, dtype)
+    for c in b.codes:
+        c[:] = 0
+    k, v = (c[b.table[0]].transpose(1, 0, 2, 3).reshape(1, -1, D) for c in b.codes)
+    one = lambda x: paged.to_codes(np.array([x]), fmt)[0]
+    k[0, 138, 0], k[0, 228, 0], v[0, 138] = one(8.0), one(26.0), one(100.0)        # 138, 228: halves of 128 .. 255
+    for c, x, t in zip(b.codes, (k, v), (b.pages.k, b.pages.v)):
+        c[b.table[0]] = x.reshape(1, -1, 16, D).transpose(1, 0, 2, 3)
+        t.view(torch.uint8).copy_(torch.from_numpy(c))
+    for s, t in zip(b.scale, (b.pages.k_scale, b.pages.v_scale)):
+        s[:] = 1
+        t.fill_(1.0)
+    b.q.zero_()
+    b.q[:, :, 0] = 1.0
+    b.check(ctx, scale=float(np.log(2.0)), slopes=slopes)
+    assert (b.run(ctx, scale=float(np.log(2.0)))[0][:, :, 0] > 3e-4).all()
+
+
 # ------------------------------------------------------------------ plans --
 def _plan(ctx, new, ln, table, free, taken, block, rows, in_place=False):
     t = dict(new=_i32(new), ln=_i32(ln), table=_i32(table), free=_i32(free), taken=_i32([taken]),
