@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(128, 3)
         int id;
         float ks, vs;
     };
-    const float mul0 = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : a.scale * kLog2e;
+    const float mul0 = score_multiplier(a, a.scale);
     bool bad = false;
     auto key_of = [&](int batch) { return tile_at(batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
     auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && key_of(batch) < tiles.lim; };
@@ -376,14 +376,17 @@ __global__ void __launch_bounds__(128, 3)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float x[4];
-                if (a.softcap > 0.0f) {
-                    const float cap = a.softcap * kLog2e;
+                if (a.softcap > 0.0f && plain_cap(a)) {
+                    const float cap = a.cap2;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        // tanh y = 1 - 2 / (1 + e^2y): an absolute error of a few 2^-24
                         const float z = ex2(sc[u][n][e] * (mul * rowmul[n][e & 1]));
                         x[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + z), cap + lvs);
                     }
+                } else if (a.softcap > 0.0f) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = capped(a, sc[u][n][e] * (mul * rowmul[n][e & 1])) + lvs;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -819,6 +822,8 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws
     a.sinks = a.window ? static_cast<int>(c.sinks < FKV_PAGE_MAX_LEN ? c.sinks : FKV_PAGE_MAX_LEN) : 0;
     a.causal = c.causal;
     a.scale = c.scale, a.softcap = c.softcap;
+    // (a cap next to float32's largest has a reciprocal of zero: y is zero, f(s) is s)
+    a.cap2 = c.softcap * kLog2e, a.cap_inv = c.softcap > 0.0f ? 1.0f / a.cap2 : 0.0f;
     a.div = FastDiv::make(pg->block), a.gdiv = FastDiv::make(a.G);
     const Plan p = plan_of(ctx, c);
     a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk, a.cluster = p.cluster;

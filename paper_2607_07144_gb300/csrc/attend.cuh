@@ -26,6 +26,7 @@ struct AttendArgs {
     int splits, chunk, row_tiles;
     bool cluster;                // a row's splits are one cluster, which joins them
     float scale, softcap;
+    float cap2, cap_inv;         // cap log2 e and its reciprocal
     FastDiv div, gdiv;
 };
 
@@ -91,6 +92,42 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b)
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// f(s) = cap tanh(s / cap).  Up to this cap it is cap - 2 cap / (1 + e^2y), y = s / cap,
+// with 2 y log2 e straight from the product: wrong by cap 1.4 2^-22 at most, 2e-5
+// (weights are rounded to 2^-11).  The error grows with the cap, though, so that
+// larger ones take capped(), which is some dozen instructions more a score (two pieces
+// of 4,096 tokens against 12-16k positions, 8 x 4 heads of 128: 3,590 us with a cap of
+// 1,000, 2,590 with one of 30).
+constexpr float kPlainCap = 64.0f;
+__device__ __forceinline__ bool plain_cap(const AttendArgs &a) { return a.softcap <= kPlainCap; }
+
+// What a product is multiplied by: to 2 y log2 e for a plain cap, else to s log2 e.
+__device__ __forceinline__ float score_multiplier(const AttendArgs &a, float scale)
+{
+    return a.softcap > 0.0f && plain_cap(a) ? scale * (2.0f * kLog2e) / a.softcap : scale * kLog2e;
+}
+
+// f of s = score log2 e, right relative to s: where |y| < 1/2 by the Taylor series of
+// tanh y / y up to y^12 (the next term is below 2^-23), else as above, e^2y being away
+// from 1.
+__device__ __forceinline__ float capped_near(const AttendArgs &a, float s)
+{
+    const float y = s * a.cap_inv, w = y * y;
+    float t = 21844.0f / 6081075.0f;
+    t = fmaf(t, w, -1382.0f / 155925.0f);
+    t = fmaf(t, w, 62.0f / 2835.0f);
+    t = fmaf(t, w, -17.0f / 315.0f);
+    t = fmaf(t, w, 2.0f / 15.0f);
+    t = fmaf(t, w, -1.0f / 3.0f);
+    return fmaf(s * w, t, s);
+}
+__device__ __forceinline__ float capped(const AttendArgs &a, float s)
+{
+    const float y = s * a.cap_inv;
+    const float far = fmaf(-2.0f * a.cap2, __fdividef(1.0f, 1.0f + ex2(y * (2.0f * kLog2e))), a.cap2);
+    return fabsf(y) < 0.5f ? capped_near(a, s) : far;
+}
 
 // The sum of weights counts a page's at kRef / vs.  With scales from 2^-100 on
 // that is at most 2^80, and 2^30 weights of 2^15 add up to less than float32

@@ -229,11 +229,16 @@ struct Row {
     float slope;
 };
 
-// GEN: scores have a cap or a bias by distance.
-template <int D, int FMT, typename T, bool GEN>
+// What is done to a score: nothing; a cap that is plain (attend.cuh), a bias by
+// distance, or both; a larger cap, and a bias if there is one.  (Together in one
+// variant the larger caps' code costs the others 4 %.)
+enum { SCORES_PLAIN, SCORES_GENERAL, SCORES_LARGE_CAP };
+
+template <int D, int FMT, typename T, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs a)
 {
     using S = PromptShape<D>;
+    constexpr bool GEN = SCORES != SCORES_PLAIN;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and share_of(vs)
@@ -267,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int i0 = split * a.chunk, n_it = max(0, min(tiles.n, i0 + a.chunk) - i0);
     // A bias by distance grows along the keys, and the reference with it, tile by
     // tile: general scores are walked from the last tile back (two pieces of 4,096
-    // tokens against 12-16k positions, 8 heads of 128: 3,340 us forwards, 1,780 so; with a cap 2,630 either way).
+    // tokens against 12-16k positions, 8 heads of 128: 3,340 us forwards, 1,770 so; with a cap of 30 2,590 either way).
     auto tile_at = [&](int j) { return tiles.at(i0 + (GEN ? n_it - 1 - j : j)); };
     // the first group's rows end earlier: tiles at the share's end that none of
     // them sees are the second group's alone
@@ -379,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const bool v_side = warp & 2;
         const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
         const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
-        const float mul0 = a.softcap > 0.0f ? fabsf(a.scale) * (2.0f * kLog2e) / a.softcap : fabsf(a.scale) * kLog2e;
+        const float mul0 = score_multiplier(a, fabsf(a.scale));
         const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
         // where the lane's first row's two 16-byte halves go in a tile
         const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
@@ -580,9 +585,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 };
                 // products to scores in base 2 where a cap or a bias is between them
                 auto general = [&](float *s, int half, const float *mul, const float *off) {
-                    if (a.softcap > 0.0f) {
-                        const float cap = a.softcap * kLog2e;
-                        // tanh y = 1 - 2 / (1 + e^2y)
+                    if (SCORES == SCORES_LARGE_CAP) {
+                        // mostly no score is near the cap, and the series is all there is to do
+                        float most = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 64; ++e) {
+                            s[e] *= mul[e / 16];
+                            most = fmaxf(most, fabsf(s[e]));
+                        }
+                        if (__any_sync(~0u, !(most * a.cap_inv < 0.5f))) {
+#pragma unroll
+                            for (int e = 0; e < 64; ++e)
+                                s[e] = capped(a, s[e]) + off[e / 16];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 64; ++e)
+                                s[e] = capped_near(a, s[e]) + off[e / 16];
+                        }
+                    } else if (a.softcap > 0.0f) {
+                        const float cap = a.cap2;
 #pragma unroll
                         for (int e = 0; e < 64; ++e)
                             s[e] = fmaf(-2.0f * cap, __fdividef(1.0f, 1.0f + ex2(s[e] * mul[e / 16])), cap + off[e / 16]);
@@ -859,20 +880,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     }
 }
 
-template <int D, int FMT, typename T, bool GEN> cudaError_t prompt_as(const fkv_ctx *ctx, const AttendArgs &a, cudaStream_t st)
+template <int D, int FMT, typename T, int SCORES> cudaError_t prompt_as(const fkv_ctx *ctx, const AttendArgs &a, cudaStream_t st)
 {
-    const void *fn = reinterpret_cast<const void *>(k_attend_prompt<D, FMT, T, GEN>);
+    const void *fn = reinterpret_cast<const void *>(k_attend_prompt<D, FMT, T, SCORES>);
     const cudaError_t e = kernel_use(ctx, fn, kThreads, PromptShape<D>::smem, nullptr);
     if (e != cudaSuccess)
         return e;
     const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.row_tiles) * a.n_req * a.splits * a.H);
-    k_attend_prompt<D, FMT, T, GEN><<<grid, kThreads, PromptShape<D>::smem, st>>>(a);
+    k_attend_prompt<D, FMT, T, SCORES><<<grid, kThreads, PromptShape<D>::smem, st>>>(a);
     return cudaGetLastError();
 }
 
 template <int D, int FMT, typename T> cudaError_t prompt_t(const fkv_ctx *ctx, const AttendArgs &a, cudaStream_t st)
 {
-    return a.softcap > 0.0f || a.slopes ? prompt_as<D, FMT, T, true>(ctx, a, st) : prompt_as<D, FMT, T, false>(ctx, a, st);
+    if (a.softcap > kPlainCap)
+        return prompt_as<D, FMT, T, SCORES_LARGE_CAP>(ctx, a, st);
+    return a.softcap > 0.0f || a.slopes ? prompt_as<D, FMT, T, SCORES_GENERAL>(ctx, a, st)
+                                        : prompt_as<D, FMT, T, SCORES_PLAIN>(ctx, a, st);
 }
 
 template <int D, int FMT> cudaError_t prompt_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, cudaStream_t st)

@@ -63,7 +63,7 @@ struct fkv_ctx {
     int device = 0;
     int sms = 0;                   // SMs of the device
     // kernels this context has launched (calls on one context are serialised)
-    mutable fkv_kernel_use uses[64];
+    mutable fkv_kernel_use uses[96];
     mutable int n_uses = 0;
     double2 *d_V = nullptr;        // [N] vertices; first of one allocation with d_T, d_dec and d_status
     fkv_decconst *d_dec = nullptr; // decoder constants (device copy)

@@ -423,6 +423,38 @@ def test_weights_stored_before_a_larger_score_keep_their_share(fkv, ctx, D, fmt,
     assert (b.run(ctx, scale=float(np.log(2.0)))[0][:, :, 0] > 3e-4).all()
 
 
+def _compare(b, ctx, rel=2.0 ** -20, const=16.0, rows=None, **opt):
+    """Batch.check with an allowance of its own for the scores' error: rel (size + |lse|) + 2^-20 const;
+    and outputs below the type's smallest normal number, which step by eps times that (fp16: off by 2^-25)."""
+    out, lse = b.run(ctx, **opt)
+    assert ctx.sync_status() == 0
+    eps, tiny = torch.finfo(b.q.dtype).eps / 2, torch.finfo(b.q.dtype).tiny
+    o, l, q = (t.double().cpu().numpy() for t in (out, lse, b.q))
+    for r, (n, length) in enumerate(zip(b.new, b.len)):
+        k, v = (paged.gather(c, s, b.table[r], length, b.fmt) for c, s in zip(b.codes, b.scale))
+        seen = paged.visible(n, length, opt.get("causal", True), opt.get("window", 0), opt.get("sinks", 0), None)
+        for i in range(n) if rows is None else sorted({x % n for x in rows}):
+            at = b.cu[r] + i
+            want, wl, mass, size = paged.attend(q[at][None], k, v, opt.get("scale") or b.D ** -0.5, seen[i:i + 1],
+                                                opt.get("softcap", 0.0), None, b.before[r] + i)
+            ds = rel * (size[0] + np.abs(wl[0])) + 2.0 ** -20 * const
+            bound = eps * np.abs(want[0]) + (2.0 ** -11 + ds + length * 2.0 ** -30)[:, None] * mass[0] * (1 + eps) + eps * tiny
+            assert (np.abs(o[at] - want[0]) <= bound).all(), (r, i, np.max(np.abs(o[at] - want[0]) / bound))
+            assert (np.abs(l[at] - wl[0]) <= ds).all(), (r, i, np.max(np.abs(l[at] - wl[0]) / ds))
+
+
+@pytest.mark.parametrize("cap", [0.7, 30.0, 64.0, 65.0, 300.0, 1e3, 1e5, 1e8, 1e30, 3e38])
+@pytest.mark.parametrize("scale", [None, 5.0])
+@pytest.mark.parametrize("D,fmt,dtype,G", [(64, "int8", "f16", 1), (128, "e4m3", "bf16", 4)])
+def test_caps_of_any_size(fkv, ctx, D, fmt, dtype, G, scale, cap):
+    """cap tanh(s / cap) is s for a large cap: the allowance does not grow with the cap.  Up to 64 it is taken as
+    cap - 2 cap / (1 + e^2y): exponential and quotient of 2 ulp each and the sums' roundings err by
+    cap 1.4 2^-22 <= 23 2^-20.  Above, relative to s: e^2y >= e gives 2^-20.8, the series below it less, beside
+    the products' own error."""
+    b = Batch(fkv, 41, [(130, 3), (60, 40), (300, 1), (0, 2)], 2, G, D, 16, fmt, dtype)
+    _compare(b, ctx, 2.0 ** -19, 40.0, [0, -1], softcap=cap, scale=scale)
+
+
 # ------------------------------------------------------------------ plans --
 def _plan(ctx, new, ln, table, free, taken, block, rows, in_place=False):
     t = dict(new=_i32(new), ln=_i32(ln), table=_i32(table), free=_i32(free), taken=_i32([taken]),
