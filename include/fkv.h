@@ -543,7 +543,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse (float32
  * [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row that sees
  * nothing gets zeros and -infinity.  What masked positions and slots past a
- * request's end hold does not matter.  Sums, maxima and weights are held in
+ * request's end hold does not matter, nor does the table's entry of a page that
+ * none of the request's rows sees (one behind the window may be gone).  Sums, maxima and weights are held in
  * float32, a weight times V's scale as a normal number up to 2^15: one that lies
  * more than 2^130 below the row's largest counts as zero (which takes pages of
  * V scales that far apart, or nearly).  For the product with V they are rounded

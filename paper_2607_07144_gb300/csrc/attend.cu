@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(128, 3)
     constexpr int ST = StepShape<D, NT>::stages, NS = D / 64, UNIT = 16 * D, STAGE = 4 * UNIT, MO = D / 16, R = 8 * NT;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
+    __shared__ Seen rows_see[4];                 // a warp's own: registers are short
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     uint8_t *const base = raw + (sbase - smem_u32(raw));
@@ -155,28 +156,31 @@ __global__ void __launch_bounds__(128, 3)
 
     const uint32_t ring = sbase + warp * ST * STAGE, bar0 = smem_u32(bars) + warp * ST * 8;
     if (lane == 0) {
+        rows_see[warp] = tiles.seen;
         for (int s = 0; s < ST; ++s)
             mbar_init(bar0 + 8 * s, 1);
         fence_mbar_init();
     }
     __syncwarp();
 
-    // A lane looks up one of the 32 units (16 keys) of 16 iterations: its page and
-    // what its scales give the scores.  Page ids are asked for a batch of iterations
+    // A lane looks up one of the 32 units (16 keys) of 16 iterations, if any row sees
+    // one of its keys: its page and what its scales give the scores.  Page ids are asked for a batch of iterations
     // before the scales, and these a batch before their use, so that no warp waits
     // for one to ask for the other.
     struct Unit {
         int id;
         float ks, vs;
+        unsigned all;                  // which of the 32 units are looked at
     };
     const float mul0 = score_multiplier(a, a.scale);
     bool bad = false;
     auto key_of = [&](int batch) { return tile_at(batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
-    auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && key_of(batch) < tiles.lim; };
+    auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && rows_see[warp].of(key_of(batch)); };
     auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
     auto ask_scales = [&](int batch, int id) {
-        Unit u = {0, 0.0f, 1.0f};
-        if (on(batch)) {
+        const bool mine = on(batch);
+        Unit u = {0, 0.0f, 1.0f, __ballot_sync(~0u, mine)};
+        if (mine) {
             if (id < 0 || id >= a.n_blocks)
                 bad = true;
             else
@@ -188,23 +192,21 @@ __global__ void __launch_bounds__(128, 3)
     int nid = ask(0), nnid = ask(1);
     Unit cur = ask_scales(0, nid), nxt = ask_scales(1, nnid);
     nid = ask(2);
-    // keys of iteration `it` from the warp's first one on that are looked at
     auto first_key = [&](int it) { return tile_at(it) * kTile + warp * 32; };
     auto issue = [&](int it, int batch) {
-        const int nu = min(2, (tiles.lim - first_key(it) + 15) >> 4);
         const int from = (it & 15) * 2 + (lane & 1);
         const bool now = (it >> 4) == batch;
+        const unsigned units = (now ? cur.all : nxt.all) >> ((it & 15) * 2) & 3;
         const int id = __shfl_sync(~0u, now ? cur.id : nxt.id, from);
         const int key = first_key(it) + (lane & 1) * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
         const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * STAGE;
-        if (nu > 0) {
-            if (lane == 0)
-                mbar_arrive_expect_tx(bar, nu * 2 * UNIT);
-            __syncwarp();
-            // lanes 0 .. 3: units 0 and 1 of K, then of V
-            if (lane < 4 && (lane & 1) < nu)
-                tma_load_4d(dst + lane * UNIT, lane < 2 ? &mk : &mv, 0, off, h, id, bar);
-        }
+        // (without any the arrival alone completes the phase)
+        if (lane == 0)
+            mbar_arrive_expect_tx(bar, __popc(units) * 2 * UNIT);
+        __syncwarp();
+        // lanes 0 .. 3: units 0 and 1 of K, then of V
+        if (lane < 4 && (units >> (lane & 1) & 1))
+            tma_load_4d(dst + lane * UNIT, lane < 2 ? &mk : &mv, 0, off, h, id, bar);
         __syncwarp();
     };
     for (int it = 0; it < min(ST - 1, n_it); ++it)
@@ -306,13 +308,16 @@ __global__ void __launch_bounds__(128, 3)
         }
         if (it + ST - 1 < n_it)
             issue(it + ST - 1, batch);
-        const int key = first_key(it), nu = min(2, (tiles.lim - key + 15) >> 4);
+        const int key = first_key(it);
+        const unsigned units = cur.all >> ((it & 15) * 2) & 3;
         if (!mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status)) {
             // give the loads in flight a while to land before the memory is used again
             for (int k = it + 1; k < min(n_it, it + ST); ++k)
                 mbar_wait(bar0 + 8 * (k % ST), (k / ST) & 1, a.status, 2000000);
             break;
         }
+        if (units == 0)
+            continue;                  // keys between the first ones and the window
         const uint32_t kt = ring + (it % ST) * STAGE, vt = kt + 2 * UNIT;
 
         float sc[2][NT][4];
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(128, 3)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             mx[n][0] = mx[n][1] = -INFINITY;
-        const bool full = nu == 2 && all_see(a, q, pa, pb, key, key + 32);
+        const bool full = all_see(a, q, pa, pb, key, key + 32);
         float bias[NT][2];
         if (a.slopes) {
 #pragma unroll
@@ -402,7 +407,7 @@ __global__ void __launch_bounds__(128, 3)
                     for (int e = 0; e < 4; ++e) {
                         const int j = key + 16 * u + gid + 8 * (e >> 1), c = e & 1;
                         const bool see = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c];
-                        x[e] = see && u < nu ? x[e] : -INFINITY;
+                        x[e] = see ? x[e] : -INFINITY;
                     }
                 }
 #pragma unroll
@@ -444,8 +449,8 @@ __global__ void __launch_bounds__(128, 3)
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (u >= nu)
-                break;
+            if (!(units >> u & 1))
+                continue;
             uint32_t pf[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {

@@ -47,15 +47,25 @@ struct Request {
     }
 };
 
-// The tiles that rows at positions pa .. pb see: those of the first `lo`
-// positions (prefix, sinks), then those from the window's beginning on.
+// What some rows see: the first `lo` positions (prefix, sinks), and those from
+// `begin` to `end` (the window's).
+struct Seen {
+    int lo, begin, end;
+    // Whether any of the rows sees one of the 16 keys from k on.  Others of a tile are
+    // not looked up: their pages may be gone.
+    __device__ __forceinline__ bool of(int k) const { return k < lo || (k + 16 > begin && k < end); }
+};
+
+// The tiles that rows at positions pa .. pb see: the first positions', then the window's.
 struct Tiles {
+    Seen seen;
     int n_lo, hi0, n, lim;
     __device__ __forceinline__ Tiles(const AttendArgs &a, const Request &q, int pa, int pb)
     {
         const int end = pb < 0 ? 0 : (a.causal ? min(q.len, pb + 1) : q.len);
         const int lo = pb < 0 ? 0 : max(q.pre, a.window ? min(a.sinks, end) : 0);
         const int begin = a.window ? max(0, pa - a.window + 1) : 0;
+        seen = {lo, begin, end};
         lim = max(end, lo);
         n_lo = (lo + kTile - 1) / kTile;
         hi0 = max(n_lo, begin / kTile);

@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     __shared__ float k_scales[4][8];
     __shared__ float2 v_scales[4][8];
     __shared__ uint32_t tmem_slot;
+    __shared__ Seen rows_see;              // for the converters' look-ups: registers are short
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     auto bar = [&](int i) { return smem_u32(bars) + 8 * i; };
@@ -284,6 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     }
 
     if (tid == 0) {
+        rows_see = tiles.seen;
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(K_FULL + i), 2);
             mbar_init(bar(K_EMPTY + i), 1);
@@ -391,20 +393,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
         const int64_t row_step = RP * a.st;
         bool bad = false;
-        // Lane u < 4 looks after unit u: its page id (-1: no key of it is looked at)
+        // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
         // is asked for two tiles ahead and checked a tile later, its scale and the
         // codes one tile ahead, so that nothing here waits for memory.
         auto first = [&](int j) { return tile_at(j) * kTile + 64 * w; };
+        struct Page {
+            int id;
+            bool on;
+        };
         auto ask = [&](int j) {
             const int key = first(j) + 16 * lane;
-            return j < n_it && lane < 4 && key < tiles.lim ? a.table[r * a.table_stride + a.div.div(key)] : -1;
+            Page p = {-1, j < n_it && lane < 4 && rows_see.of(key)};
+            if (p.on)
+                p.id = a.table[r * a.table_stride + a.div.div(key)];
+            return p;
         };
-        auto check = [&](int j, int id) {
-            if (j < n_it && lane < 4 && first(j) + 16 * lane < tiles.lim && (id < 0 || id >= a.n_blocks)) {
+        auto check = [&](const Page &p) {
+            if (p.on && (p.id < 0 || p.id >= a.n_blocks)) {
                 bad = true;
                 return 0;
             }
-            return id;
+            return p.id;
         };
         auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
         uint4 v[4][NL];
@@ -428,14 +437,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     v[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
             }
         };
-        int nid = ask(0), nnid = ask(1);
-        nid = check(0, nid);
+        const Page start = ask(0);
+        Page after = ask(1);
+        int nid = check(start);
         load(0, nid);
         float scale = ask_scale(nid);
-        nid = check(1, nnid);
+        nid = check(after);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1
-            nnid = ask(j + 2);
+            after = ask(j + 2);
             if (lane < 4) {
                 if (v_side) {
                     const float vs = value_scale(scale);
@@ -481,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (lane == 0)
                 mbar_arrive(bar(full_bar + st));
             load(j + 1, nid);
-            nid = check(j + 2, nnid);
+            nid = check(after);
         }
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);

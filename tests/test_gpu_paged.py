@@ -455,6 +455,42 @@ def test_caps_of_any_size(fkv, ctx, D, fmt, dtype, G, scale, cap):
     _compare(b, ctx, 2.0 ** -19, 40.0, [0, -1], softcap=cap, scale=scale)
 
 
+@pytest.mark.parametrize("opt", [dict(), dict(softcap=20.0), dict(softcap=1e4), dict(slopes=True), dict(causal=False)])
+@pytest.mark.parametrize("window,sinks", [(20, 0), (20, 2), (300, 130)])
+@pytest.mark.parametrize("D,fmt,dtype,new", [(64, "e4m3", "f16", 1), (128, "e4m3", "bf16", 5), (64, "e4m3", "bf16", 60),
+                                             (128, "int8", "f16", 200), (128, "int8", "bf16", 1)])
+def test_pages_that_no_row_sees_are_not_looked_up(fkv, ctx, D, fmt, dtype, new, window, sinks, opt):
+    """Pages behind a window may be gone: their table entries lie outside the pool, or name a page of NaN codes
+    whose scales are NaN and infinite; page 0 is such a page too."""
+    b = Batch(fkv, 42, [(700, new), (333, new), (5, 1)], 2, 4, D, 16, fmt, dtype)
+    spare = sorted(set(range(b.codes[0].shape[0])) - set(b.table.ravel().tolist()))
+    if 0 not in spare:                                     # a spare page changes places with page 0
+        z = spare.pop()
+        b.table = np.where(b.table == 0, z, b.table)
+        for x in b.codes + b.scale:
+            x[[0, z]] = x[[z, 0]]
+    poison = [0] + [x for x in spare if x]
+    for c, s in zip(b.codes, b.scale):
+        c[poison] = 0x7F
+        s[poison] = np.nan
+        s[poison[1:], 0] = np.inf
+    for t, x in zip((b.pages.k.view(torch.uint8), b.pages.v.view(torch.uint8), b.pages.k_scale, b.pages.v_scale),
+                    b.codes + b.scale):
+        t.copy_(torch.from_numpy(x))
+    gone = 0
+    for r, (n, length) in enumerate(zip(b.new, b.len)):
+        seen = paged.visible(n, length, opt.get("causal", True), window, sinks, None).any(0)
+        for j in range(-(-length // 16)):
+            if not seen[16 * j:16 * j + 16].any():
+                b.table[r, j] = (-1, -2, poison[0], poison[-1])[j % 4]
+                gone += 1
+    assert gone > 3
+    opt = dict(opt)
+    if opt.get("slopes"):
+        opt["slopes"] = [0.5, 0.25, 0.03, -0.02] * 2
+    b.check(ctx, rows=[0, 1, new // 2, new - 1], window=window, sinks=sinks, **opt)
+
+
 # ------------------------------------------------------------------ plans --
 def _plan(ctx, new, ln, table, free, taken, block, rows, in_place=False):
     t = dict(new=_i32(new), ln=_i32(ln), table=_i32(table), free=_i32(free), taken=_i32([taken]),
