@@ -519,10 +519,10 @@ int fkv_page_plan(fkv_ctx *ctx, const fkv_plan *plan, void *stream);
  * amax the run's largest finite magnitude, its wanted scale is
  *     FKV_E4M3: the smallest power of two not below amax / 448,
  *     FKV_INT8: amax / 127 (rounded to float32),
- * at least 2^-100.  A page without earlier rows takes the wanted scale; another
- * keeps its own if that is as large, else its earlier rows' codes are rounded
- * again, code x (old scale x (1 / new scale)).  A value x is stored as
- * x x (1 / scale) rounded to the nearest code (ties to even), beyond the
+ * at least 2^-100 and at most 2^100.  A page without earlier rows takes the
+ * wanted scale; another keeps its own if that is as large, else its earlier rows'
+ * codes are rounded again, code x (old scale x (1 / new scale)).  A value x is
+ * stored as x x (1 / scale) rounded to the nearest code (ties to even), beyond the
  * largest as the largest.  A NaN is stored as zero and sets FKV_ECORRUPT in the
  * status word; a slot past the pool is skipped and sets FKV_ERANGE.  What two
  * runs of one page in a call leave there is not specified. */

@@ -7,7 +7,7 @@ import math
 import numpy as np
 
 E4M3, INT8 = "e4m3", "int8"
-FLOOR = 2.0 ** -100
+FLOOR, CEILING = 2.0 ** -100, 2.0 ** 100
 
 
 def _e4m3_table():
@@ -50,9 +50,9 @@ def scale_of(amax, fmt):
     if amax == 0:
         return np.float32(FLOOR)
     if fmt == INT8:
-        return np.float32(max(np.float32(np.float32(amax) / np.float32(127)), FLOOR))
+        return np.float32(min(max(np.float32(np.float32(amax) / np.float32(127)), FLOOR), CEILING))
     m, e = math.frexp(amax / 448.0)
-    return np.float32(max(math.ldexp(1.0, e - 1 if m == 0.5 else e), FLOOR))
+    return np.float32(min(max(math.ldexp(1.0, e - 1 if m == 0.5 else e), FLOOR), CEILING))
 
 
 def write(codes, scale, x, slots, fmt):

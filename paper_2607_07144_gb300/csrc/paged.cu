@@ -304,15 +304,16 @@ __device__ __forceinline__ float finite_abs(float v)
 
 // The scale that brings amax into the format's range (fkv.h): e4m3 the smallest
 // power of two, so that a later, larger scale rounds no stored code again but
-// in the lowest (subnormal) ones; int8 amax / 127, which uses all its codes.
+// in the lowest (subnormal) ones; int8 amax / 127, which uses all its codes.  Either
+// within [2^-100, 2^100].
 template <int FMT> __device__ __forceinline__ float scale_of(float amax)
 {
     if (FMT == FKV_INT8)
-        return fmaxf(__fdiv_rn(amax, 127.0f), FKV_PAGE_MIN_SCALE);
+        return fminf(fmaxf(__fdiv_rn(amax, 127.0f), FKV_PAGE_MIN_SCALE), FKV_PAGE_MAX_SCALE);
     const uint32_t u = __float_as_uint(amax);
     // amax = 1.m 2^E; 448 = 1.75 2^8
     const int e = static_cast<int>(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
-    return e < -100 ? FKV_PAGE_MIN_SCALE : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+    return __uint_as_float(static_cast<uint32_t>(min(max(e, -100), 100) + 127) << 23);
 }
 
 // 16 values times inv, rounded to codes.
@@ -539,7 +540,9 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
                 }
             };
             join();
-            const bool odd = amax_u >= 0x7f800000u;          // infinities or NaN among the values
+            // infinities or NaN among the values, or some beyond the largest code of the
+            // largest scale (of int8; e4m3's, 448, is larger)
+            const bool odd = amax_u > __float_as_uint(127.0f * FKV_PAGE_MAX_SCALE);
             if (odd) {
                 // rare: the largest finite magnitude
                 float amax = 0.0f;

@@ -6,6 +6,9 @@
 // Smallest scale of a page (2^-100): attention works with a value scale's
 // logarithm and reciprocal, and a page of zeros has to have both.
 #define FKV_PAGE_MIN_SCALE 7.888609052210118e-31f
+// And the largest, 2^100: its share of a sum of weights (attend.cuh) is one that
+// float32 holds.
+#define FKV_PAGE_MAX_SCALE 1.2676506002282294e30f
 
 #ifdef __CUDACC__
 // Launch `kernel` so that its blocks may be scheduled while the stream's

@@ -671,6 +671,40 @@ def test_slots_outside_the_pool_are_skipped_and_reported(fkv, ctx):
     _same(pages, codes, scale)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("T", [3, 200, 700])
+def test_write_keeps_scales_within_the_pools_range(fkv, ctx, T, fmt, dtype):
+    """A page's scale is at most 2^100, as attention wants it: values beyond its largest code are stored as that."""
+    H, D = 8, 64
+    rng = np.random.default_rng(43)
+    nb = max(T // 16, 3) + 1
+    codes, scale, pages = _pool(fkv, rng, nb, H, D, 16, fmt)
+    x = torch.from_numpy(rng.standard_normal((T, H, D)).astype(np.float32)).cuda() * 2.0 ** 118
+    x[0] *= 2.0 ** -60
+    x[1, 0, 3] = float("inf")
+    x = x.to(DT[dtype])
+    slots = np.arange(T) * (1 if T > 16 else 16)           # runs of a page, or a token a page
+    ctx.page_write(pages, x, x, torch.from_numpy(slots).cuda())
+    for c, s in zip(codes, scale):
+        paged.write(c, s, x.double().cpu().numpy(), slots, fmt)
+    _same(pages, codes, scale)
+    assert max(s.max() for s in scale) == 2.0 ** 100
+    # keys of the smallest scale, queries of zero: the mean of the values
+    pages.k_scale.fill_(2.0 ** -100)
+    q = torch.zeros((1, H, D), dtype=torch.bfloat16, device="cuda")
+    n = 16 if T > 16 else 1
+    table = _i32([[1]]) if T > 16 else _i32([[2]])
+    lse = torch.zeros((1, H), device="cuda")
+    out = ctx.page_attend(pages, q, _i32([0, 1]), _i32([n]), table, 1, n, lse=lse)
+    assert ctx.sync_status() == 0
+    v = paged.gather(codes[1], scale[1], [1 if T > 16 else 2], n, fmt)
+    want = v.mean(1)
+    bound = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * np.abs(v).mean(1)
+    assert (np.abs(out[0].double().cpu().numpy() - want) <= bound).all()
+    assert np.abs(lse[0].cpu().numpy() - np.log(n)).max() < 1e-4
+
+
 # ------------------------------------------------------------------ reads --
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("D,fmt,block", [(64, "int8", 16), (128, "e4m3", 48), (128, "int8", 128)])

@@ -33,6 +33,11 @@ def test_int8_scales():
     assert paged.scale_of(1.0, paged.INT8) == np.float32(1) / np.float32(127)
 
 
+def test_scales_stay_within_the_pools_range():
+    for fmt in (paged.E4M3, paged.INT8):
+        assert paged.scale_of(2.0 ** 120, fmt) == 2.0 ** 100 and paged.scale_of(2.0 ** -120, fmt) == 2.0 ** -100
+
+
 def test_a_grown_scale_rounds_earlier_rows_again():
     codes, scale = np.zeros((1, 1, 16, 1), np.uint8), np.zeros((1, 1), np.float32)
     paged.write(codes, scale, np.array([[[100.0]]]), np.array([3]), paged.INT8)   # rows 0..2 count as earlier ones
