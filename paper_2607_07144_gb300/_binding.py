@@ -619,13 +619,11 @@ class Context:
             0 if prefix is None else _array(prefix, _I32, n, "prefix", dev), qt, qh, ot, oh, T, n, ts, tw, max_new, max_len,
             window, sinks, qd, Hq, causal, dim ** -0.5 if scale is None else scale, softcap, 0)
         L = lib()
-        # the workspace's size depends on these alone
+        # the workspace's size depends on these alone, in a call that is not refused
         key = (T, Hq, n, max_new, max_len, window, sinks, prefix is None, pages.heads, dim)
         need = self._attend_need.get(key)
         if need is None:
-            if len(self._attend_need) >= 4096:
-                self._attend_need.clear()
-            need = self._attend_need[key] = L.fkv_page_attend_workspace(self._h, buf)
+            need = L.fkv_page_attend_workspace(self._h, buf)
         ws = nb = 0
         if workspace is not None:
             if workspace.get_device() != dev or not workspace.is_contiguous():
@@ -637,6 +635,10 @@ class Context:
         rc = L.fkv_page_attend(self._h, buf, ws, nb, _stream(stream))
         if rc != OK:
             self._check(rc)
+        if key not in self._attend_need:
+            if len(self._attend_need) >= 4096:
+                self._attend_need.clear()
+            self._attend_need[key] = need
         return out
 
     def page_read(self, pages: Pages, kv_len: torch.Tensor, block_table: torch.Tensor, t0: int, t1: int,

@@ -795,6 +795,16 @@ def test_write_slots_are_32_bits(fkv, ctx):
     assert not one.any() and (scale == 1).all()
 
 
+def test_a_refused_pool_leaves_the_next_call_its_workspace(fkv):
+    """A pool of pages of 24 is refused; a call of the same sizes on a good pool gets the workspace that it needs."""
+    ctx = fkv.Context(256)
+    b = Batch(fkv, 44, [(20000, 1)], 1, 4, 64, 16, "int8", "f16")
+    with pytest.raises(fkv.FkvError) as e:
+        ctx.page_attend(fkv.Pages.empty(900, 1, 24, 64, torch.int8), b.q, _i32(b.cu), _i32(b.len), _i32(b.table), 1, 20001)
+    assert e.value.code == -1
+    b.check(ctx)
+
+
 def test_workspace_is_on_the_device(fkv, ctx):
     """A workspace on the host, or one with gaps, is refused before its pointer goes anywhere."""
     b = Batch(fkv, 30, [(600, 1)], 1, 4, 64, 16, "int8", "f16")
