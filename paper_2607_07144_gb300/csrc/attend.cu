@@ -657,7 +657,14 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
             hi = mid;
     }
     Request q;
-    const bool mine = q.load(a, lo) && tok >= q.tok0 && tok < q.tok0 + q.nq;
+    bool mine = q.load(a, lo) && tok >= q.tok0 && tok < q.tok0 + q.nq;
+    if (!mine) {
+        // requests whose numbers do not hold together may have led the search astray
+        bool any = false;
+        for (int r = tid; r < a.n_req; r += 128)
+            any |= q.load(a, r) && tok >= q.tok0 && tok < q.tok0 + q.nq;
+        mine = __syncthreads_or(any);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");     // the partial results are written
     if (!mine)
         return;

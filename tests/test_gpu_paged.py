@@ -275,6 +275,20 @@ def test_padded_rows_and_skipped_requests_stay(fkv, ctx):
     assert (out[1:6] == 7).all() and torch.equal(out[:1], good[:1])
 
 
+def test_requests_after_one_that_does_not_hold_together_are_served(fkv, ctx):
+    """Row numbers of two requests that are out of order: the third, whose shares are joined by their own launch,
+    gets its row all the same."""
+    b = Batch(fkv, 45, [(10, 1), (10, 1), (20000, 1)], 1, 4, 64, 16, "int8", "f16", gap=2)
+    good, lse = b.run(ctx)
+    assert ctx.sync_status() == 0
+    b.cu = np.array([0, 9, 2, 3])
+    out, lse2 = b.run(ctx)
+    assert ctx.sync_status() == -2
+    assert torch.equal(out[2], good[2]) and torch.equal(lse2[2], lse[2])
+    keep = [0, 1, 3, 4]
+    assert (out[keep] == 7).all() and (lse2[keep] == 7).all()
+
+
 def test_a_page_outside_the_pool_is_reported(fkv, ctx):
     b = Batch(fkv, 10, [(40, 1), (60, 5)], 1, 2, 64, 16, "e4m3", "bf16")
     good, _ = b.run(ctx)
