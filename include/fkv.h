@@ -300,8 +300,9 @@ int fkv_measure_fp64_rate(double *ops_per_s, void *stream);
  * the same barrier, under the library's full 2 s limit, must leave on that
  * flag.  Waits for the kernel and writes to result[0..5] (host):
  * [0] the first waiter's result (0 = gave up), [1] the second's, [2] 1 if
- * the second left within 2 x limit_ns, [3] a bounded wait on a completed
- * phase (1), [4] one on an open phase (0), [5] 1 once the teardown ran.
+ * the second left within 2 x limit_ns, [3] bounded waits, polling and suspended,
+ * on a completed phase (1), [4] on an open phase (0; 1 also if one gave up before
+ * its limit), [5] 1 once the teardown ran.
  * The timeouts set FKV_ETIMEOUT in ctx's status word: fkv_sync_status()
  * reports and clears it, and the context stays usable. */
 int fkv_check_bounded_wait(fkv_ctx *ctx, int64_t limit_ns, int32_t *result, void *stream);

@@ -310,10 +310,12 @@ __global__ void __launch_bounds__(128, 3)
             issue(it + ST - 1, batch);
         const int key = first_key(it);
         const unsigned units = cur.all >> ((it & 15) * 2) & 3;
-        if (!mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status)) {
+        // (a lane that gives up takes its warp along: the others would meet it nowhere)
+        if (!__all_sync(~0u, mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status))) {
             // give the loads in flight a while to land before the memory is used again
             for (int k = it + 1; k < min(n_it, it + ST); ++k)
                 mbar_wait(bar0 + 8 * (k % ST), (k / ST) & 1, a.status, 2000000);
+            __syncwarp();
             break;
         }
         if (units == 0)

@@ -77,28 +77,6 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// mbar_wait for warps that share their schedulers with working ones: the
-// hardware suspends a waiting thread for up to 10 ms a try instead of polling
-// (polls took a fifth of the instruction issue), 200 tries being the 2 s limit.
-__device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, unsigned *status)
-{
-#pragma unroll 1
-    for (int i = 0; i < 200; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(10000000u)
-            : "memory");
-        if (ok)
-            return true;
-    }
-    atomicOr(status, FKV_ST_TIMEOUT);
-    return false;
-}
-
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t r;
@@ -331,21 +309,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     umma_commit(bar(b));
                 __syncwarp();
             };
-            auto wait = [&](int b, int parity) { return __all_sync(~0u, mbar_park(bar(b), parity, a.status)); };
-            bool ok = wait(Q_FULL, 0) && wait(K_FULL, 0);
-            if (ok) {
-                tc_fence_after();
-                for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
-                    scores(w, 0);
-                commit(K_EMPTY);
-            }
-            for (int j = 0; j < n_it && ok; ++j) {
+            bool ok = true;                    // (see the softmax's)
+            auto wait = [&](int b, int parity) { ok = ok && mbar_park(bar(b), parity, a.status); };
+            wait(Q_FULL, 0);
+            wait(K_FULL, 0);
+            tc_fence_after();
+            for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
+                scores(w, 0);
+            commit(K_EMPTY);
+            for (int j = 0; j < n_it; ++j) {
                 bool have_v = false, have_k = false;
                 for (int w = j < n_first ? 0 : 1; w < groups; ++w) {
-                    ok = wait(P_FULL + w, j & 1) && (have_v || wait(V_FULL + (j & 1), (j >> 1) & 1));
+                    wait(P_FULL + w, j & 1);
+                    if (!have_v)
+                        wait(V_FULL + (j & 1), (j >> 1) & 1);
                     have_v = true;
-                    if (!ok)
-                        break;
                     tc_fence_after();
                     if (elect_one()) {
                         umma_tile_ts(tmem + 256 + 128 * w, tmem + 128 * w, v_d + (j & 1) * step, id_o, j > 0, v_hi);
@@ -357,10 +335,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     __syncwarp();
                     if (j + 1 == (w ? n_it : n_first))
                         continue;
-                    ok = have_k || wait(K_FULL + ((j + 1) & 1), ((j + 1) >> 1) & 1);
+                    if (!have_k)
+                        wait(K_FULL + ((j + 1) & 1), ((j + 1) >> 1) & 1);
                     have_k = true;
-                    if (!ok)
-                        break;
                     tc_fence_after();
                     scores(w, j + 1);
                     if (w == groups - 1)
@@ -392,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
         const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
         const int64_t row_step = RP * a.st;
-        bool bad = false;
+        bool bad = false, ok = true;           // (ok: see the softmax's)
         // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
         // is asked for two tiles ahead and checked a tile later, its scale and the
         // codes one tile ahead, so that nothing here waits for memory.
@@ -459,8 +436,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (lane == 0)
                 mbar_arrive(bar(SC_FULL + (j & 3)));
             const int st = j & 1;
-            if (j >= 2 && !mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status))
-                break;
+            if (j >= 2 && ok)
+                ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
+            __syncwarp();
             const int first_key = first(j);
             if (v_side && first_key + 64 > q.len) {
                 // rows behind the request's end hold any bytes, NaN codes among them
@@ -568,12 +546,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int gb = q.p0 + static_cast<int>(a.gdiv.div(min(row0 + 128 * w + 128, rows) - 1));
             const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
             const uint32_t s_t = tmem + 128 * w + lanes, o_t = tmem + 256 + 128 * w + lanes;
+            // A thread that gives up waits no more but goes on with what it finds, to the
+            // loop's end (the call has failed and says so): one that left would be waited
+            // for by its warp, whose next step is for all its threads, for ever.
             bool ok = true;
             const int n_own = w ? n_it : n_first;
             for (int j = 0; j < n_own; ++j) {
-                ok = mbar_park(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status);
-                if (!ok)
-                    break;
+                ok = ok && mbar_park(bar(SC_FULL + (j & 3)), (j >> 2) & 1, a.status);
                 const int key = tile_at(j) * kTile;
                 const float *const km = k_scales[j & 3];
                 const float2 *const vm = v_scales[j & 3];
@@ -583,9 +562,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
                     km_r[n] = km[n] * st.down, vo_r[n] = vm[n].x;
-                ok = mbar_park(bar(S_FULL + w), j & 1, a.status);
-                if (!ok)
-                    break;
+                ok = ok && mbar_park(bar(S_FULL + w), j & 1, a.status);
+                __syncwarp();          // tensor memory is read by whole warps
                 tc_fence_after();
                 // the visible ones of 32 keys as bits: ranges meet as words, and a score's
                 // test is one bit (its three comparisons, short cuts and all, took 80
@@ -821,7 +799,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     mbar_arrive(bar(P_FULL + w));
             }
             if (n_own > 0 && ok)
-                ok = mbar_park(bar(O_FULL + w), 0, a.status);
+                mbar_park(bar(O_FULL + w), 0, a.status);
+            __syncwarp();
             tc_fence_after();
             const float inv = st.l != 0.0f ? kRef / st.l : 0.0f;
             const float lse2 = st.l != 0.0f ? st.m + log2f(st.l) - kLog2Ref : -INFINITY;

@@ -247,6 +247,13 @@ __device__ __forceinline__ uint32_t smem_u32(const void *p)
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+__device__ __forceinline__ unsigned globaltimer_lo()
+{
+    unsigned t;
+    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+    return t;
+}
+
 __device__ __forceinline__ uint64_t globaltimer_ns()
 {
     uint64_t t;
@@ -302,6 +309,36 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigne
             return false;
         }
     }
+}
+
+// mbar_wait for warps that share their schedulers with working ones: the hardware
+// may suspend a waiting thread for up to 10 ms a try instead of polling (polls
+// took a fifth of the prompt attention's instruction issue).  A try may also come
+// back early, so that the limit (below 4 s) is one of time here too; half the clock
+// is enough for it, and the shorter loop is 2 % of that kernel.
+__device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, unsigned *status,
+                                          uint64_t limit_ns = kWaitLimitNs)
+{
+    auto done = [&]() {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(10000000u)
+            : "memory");
+        return ok != 0;
+    };
+    if (done())
+        return true;
+    const unsigned t0 = globaltimer_lo();
+    do {
+        if (done())
+            return true;
+    } while (globaltimer_lo() - t0 <= limit_ns);
+    atomicOr(status, FKV_ST_TIMEOUT);
+    return false;
 }
 
 __device__ __forceinline__ void fence_proxy_async_smem()

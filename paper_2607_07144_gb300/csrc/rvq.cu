@@ -2460,11 +2460,12 @@ k_rvq128_pair(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ 
 // which nothing arrives on, gives up after limit_ns and raises the abort
 // flag; warp 1's lane 0 waits on the same barrier with the library's full
 // limit and must leave on the flag, well before its own timer.  Warp 2 checks
-// that a plain bounded wait passes a completed phase and times out on an
-// open one.  All warps then meet and TMEM is released, as in the kernels'
-// teardown.  out: [0] warp 0's wait result, [1] warp 1's, [2] 1 if warp 1
-// left within 2 x limit_ns (on the flag), [3] the completed phase's wait,
-// [4] the open phase's wait, [5] 1 after the teardown.
+// that the other bounded waits, a polling and a suspended one, pass a completed
+// phase and time out on an open one, not before their limit.  All warps then meet
+// and TMEM is released, as in the kernels' teardown.  out: [0] warp 0's wait
+// result, [1] warp 1's, [2] 1 if warp 1 left within 2 x limit_ns (on the flag),
+// [3] the completed phase's waits, [4] the open phase's (1 also if one gave up
+// early), [5] 1 after the teardown.
 __global__ void __launch_bounds__(96, 1) k_wait_check(unsigned *status, uint64_t limit_ns, int *out)
 {
     __shared__ __align__(8) uint64_t bars[3];
@@ -2494,8 +2495,12 @@ __global__ void __launch_bounds__(96, 1) k_wait_check(unsigned *status, uint64_t
             out[2] = globaltimer_ns() - t0 < 2 * limit_ns ? 1 : 0;
         } else {
             mbar_arrive(bar(1));
-            out[3] = mbar_wait(bar(1), 0, status, limit_ns) ? 1 : 0;
-            out[4] = mbar_wait(bar(2), 0, status, limit_ns) ? 1 : 0;
+            out[3] = mbar_wait(bar(1), 0, status, limit_ns) && mbar_park(bar(1), 0, status, limit_ns) ? 1 : 0;
+            const uint64_t t0 = globaltimer_ns();
+            bool over = mbar_wait(bar(2), 0, status, limit_ns);
+            const uint64_t t1 = globaltimer_ns();
+            over |= mbar_park(bar(2), 0, status, limit_ns);
+            out[4] = over || t1 - t0 < limit_ns || globaltimer_ns() - t1 < limit_ns ? 1 : 0;
         }
     }
     tc_fence_before();
