@@ -289,7 +289,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     if (group == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ---------------------------------------------------- MMA issuer
-        // The whole warp follows the loop and one elected thread issues.
+        // One elected thread follows the loop: what it waits for, it waits for alone.
+        // (K's next tile is asked for before the weights: asked for after the product it
+        // costs 1 to 5 %.)
         if (warp == 12 && n_it > 0) {
             constexpr uint32_t id_s = idesc_f16_f32(128, 128), id_o = idesc_f16_f32(128, D) | 1u << 16;
             constexpr uint32_t step = S::tile >> 4;
@@ -297,56 +299,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const uint32_t k_d = static_cast<uint32_t>(sdesc_sw128(sbase + S::off_k));
             const uint32_t v_d = static_cast<uint32_t>(sdesc_mn_sw128(sbase + S::off_v, S::half));
             const uint32_t v_hi = static_cast<uint32_t>(sdesc_mn_sw128(0, S::half) >> 32);
-            auto scores = [&](int w, int j) {
-                if (elect_one()) {
-                    umma_tile_ss<D>(tmem + 128 * w, q_d + w * step, k_d + (j & 1) * step, id_s);
-                    umma_commit(bar(S_FULL + w));
-                }
-                __syncwarp();
-            };
-            auto commit = [&](int b) {
-                if (elect_one())
-                    umma_commit(bar(b));
-                __syncwarp();
-            };
             bool ok = true;                    // (see the softmax's)
             auto wait = [&](int b, int parity) { ok = ok && mbar_park(bar(b), parity, a.status); };
-            wait(Q_FULL, 0);
-            wait(K_FULL, 0);
-            tc_fence_after();
-            for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
-                scores(w, 0);
-            commit(K_EMPTY);
-            for (int j = 0; j < n_it; ++j) {
-                bool have_v = false, have_k = false;
-                for (int w = j < n_first ? 0 : 1; w < groups; ++w) {
-                    wait(P_FULL + w, j & 1);
-                    if (!have_v)
-                        wait(V_FULL + (j & 1), (j >> 1) & 1);
-                    have_v = true;
-                    tc_fence_after();
-                    if (elect_one()) {
+            auto scores = [&](int w, int j) {
+                umma_tile_ss<D>(tmem + 128 * w, q_d + w * step, k_d + (j & 1) * step, id_s);
+                umma_commit(bar(S_FULL + w));
+            };
+            if (elect_one()) {
+                wait(Q_FULL, 0);
+                wait(K_FULL, 0);
+                tc_fence_after();
+                for (int w = n_first > 0 ? 0 : 1; w < groups; ++w)
+                    scores(w, 0);
+                umma_commit(bar(K_EMPTY));
+                for (int j = 0; j < n_it; ++j) {
+                    wait(V_FULL + (j & 1), (j >> 1) & 1);
+                    if (j + 1 < n_it)
+                        wait(K_FULL + ((j + 1) & 1), ((j + 1) >> 1) & 1);
+                    for (int w = j < n_first ? 0 : 1; w < groups; ++w) {
+                        wait(P_FULL + w, j & 1);
+                        tc_fence_after();
                         umma_tile_ts(tmem + 256 + 128 * w, tmem + 128 * w, v_d + (j & 1) * step, id_o, j > 0, v_hi);
                         if (w == groups - 1)
                             umma_commit(bar(V_EMPTY + (j & 1)));
-                        if (j + 1 == (w ? n_it : n_first))
+                        if (j + 1 == (w ? n_it : n_first)) {
                             umma_commit(bar(O_FULL + w));
+                            continue;
+                        }
+                        scores(w, j + 1);
+                        if (w == groups - 1)
+                            umma_commit(bar(K_EMPTY + ((j + 1) & 1)));
                     }
-                    __syncwarp();
-                    if (j + 1 == (w ? n_it : n_first))
-                        continue;
-                    if (!have_k)
-                        wait(K_FULL + ((j + 1) & 1), ((j + 1) >> 1) & 1);
-                    have_k = true;
-                    tc_fence_after();
-                    scores(w, j + 1);
-                    if (w == groups - 1)
-                        commit(K_EMPTY + ((j + 1) & 1));
                 }
+                // every MMA has completed before tensor memory is released
+                umma_commit(bar(DRAIN));
+                mbar_park(bar(DRAIN), 0, a.status);
             }
-            // every MMA has completed before tensor memory is released
-            commit(DRAIN);
-            mbar_park(bar(DRAIN), 0, a.status);
+            __syncwarp();
         }
     } else if (group == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
@@ -438,7 +427,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int st = j & 1;
             if (j >= 2 && ok)
                 ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
-            __syncwarp();
             const int first_key = first(j);
             if (v_side && first_key + 64 > q.len) {
                 // rows behind the request's end hold any bytes, NaN codes among them
@@ -563,7 +551,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 for (int n = 0; n < 8; ++n)
                     km_r[n] = km[n] * st.down, vo_r[n] = vm[n].x;
                 ok = ok && mbar_park(bar(S_FULL + w), j & 1, a.status);
-                __syncwarp();          // tensor memory is read by whole warps
                 tc_fence_after();
                 // the visible ones of 32 keys as bits: ranges meet as words, and a score's
                 // test is one bit (its three comparisons, short cuts and all, took 80
