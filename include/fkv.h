@@ -485,12 +485,18 @@ typedef struct {
  *   slots   [rows]: page id x block + position in the page of each token's
  *           place, -1 from row cu[n_req] on
  *   pos     [rows]: its position in the request, -1 likewise
- * A page belongs to one request.  A call that does not fit is not carried out:
- * a negative length, one that is or becomes more than FKV_PAGE_MAX_LEN, more
- * than `width` pages, more tokens than rows, more pages than are free, or more
- * given back than were taken.  It sets FKV_ERANGE in the status word, copies
- * lengths and count, sets every cu to 0 and every slot and position to -1, and
- * changes nothing else. */
+ * A page belongs to one request, whose kv_len says how many it has: the first
+ * ceil(kv_len / block) entries of its row.  Single pages are not taken back.  A
+ * caller who lowers kv_len past a page's beginning (drafts that were not accepted)
+ * puts the pages behind it on the stack itself, before entry *taken, and counts
+ * *taken down: a later call knows nothing of them, gives fresh ones out, and the
+ * pool runs dry.  The same goes for pages behind a window, and then for the rest
+ * of such a request when it ends, as the call gives all its entries back.
+ * A call that does not fit is not carried out: a negative length, one that is or
+ * becomes more than FKV_PAGE_MAX_LEN, more than `width` pages, more tokens than
+ * rows, more pages than are free, or more given back than were taken.  It sets
+ * FKV_ERANGE in the status word, copies lengths and count, sets every cu to 0 and
+ * every slot and position to -1, and changes nothing else. */
 typedef struct {
     const int32_t *n_new;
     const int32_t *kv_len;
@@ -549,13 +555,17 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * float32, a weight times V's scale as a normal number up to 2^15: one that lies
  * more than 2^130 below the row's largest counts as zero (which takes pages of
  * V scales that far apart, or nearly).  For the product with V they are rounded
- * to fp16, and to zero below 2^-30 of the largest.
+ * to fp16, and to zero below 2^-30 of the largest.  Elements of a bfloat16 query
+ * below 2^-31 of its largest are rounded to 2^-39 of that.  A score, and a query's
+ * largest element times K's scale and `scale`, have to be float32 numbers, else
+ * the row's values are unspecified.
  * table, table_stride and width as in fkv_page_plan.  max_new and max_len bound
  * n_new and kv_len of every request (they size the launch).  A request whose
  * numbers do not hold together (cu not increasing or past n_tok, a length past
  * max_new, max_len or the table) is skipped, its rows left as they are, a page
  * id outside the pool gives the row unspecified values, and either sets
- * FKV_ERANGE in the status word.  Rows of no request are left as they are.
+ * FKV_ERANGE in the status word.  Rows of no request are left as they are, and
+ * with max_new, n_tok or n_req 0 nothing is done.  `out` may be q itself.
  * workspace: fkv_page_attend_workspace(ctx, a) bytes, 256-byte aligned (NULL
  * when that is 0), the caller's own until the call has run: calls that may
  * overlap need one each.  The bytes depend on the sizes (and whether there is a

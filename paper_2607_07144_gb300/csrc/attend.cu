@@ -5,9 +5,10 @@
 //     x_j = f(scale ks q.c_j) + slope (j - p),   f(s) = cap tanh(s / cap) or s
 //     o   = sum_j exp(x_j) vs c'_j / sum_j exp(x_j)   over the visible j.
 // Codes are exact in fp16, and so is a query row brought to [2^14, 2^15) by a
-// power of two (fp16 queries as they are): the products are exact and summed in
-// fp32 on the tensor cores, and the scale of a page multiplies afterwards, once
-// for each score.  The value scale goes into the softmax instead: with
+// power of two (fp16 queries as they are), but for a bf16 row's elements below
+// 2^-31 of its largest, which fp16's subnormals round to 2^-39 of that: the products
+// are exact and summed in fp32 on the tensor cores, and the scale of a page
+// multiplies afterwards, once for each score.  The value scale goes into the softmax instead: with
 //     y_j = x_j log2 e + log2 vs,    P_j = 2^(y_j - m + 8),   m = max y_j
 // the second product is sum P_j c'_j with P rounded to fp16 (relative 2^-11, an
 // eighth of a bf16 result's own rounding; P spans 2^8 .. 2^-24, so nothing above

@@ -328,6 +328,29 @@ def test_views_with_strides(fkv, ctx, new):
     assert torch.equal(res[:, 2:8], want) and (res[:, :2] == 7).all() and (res[:, 8:] == 7).all()
 
 
+@pytest.mark.parametrize("lens", [[(40, 1)], [(300, 1), (5, 2)], [(900, 5)], [(20000, 1)], [(100, 60)], [(3000, 40)], [(90, 700)]])
+def test_output_over_the_queries(fkv, ctx, lens):
+    """out may be q itself: one share, shares joined in their cluster or by a launch, few rows and many."""
+    b = Batch(fkv, 46, lens, 2, 4, 128, 16, "e4m3", "bf16", gap=1)
+    want, _ = b.run(ctx)
+    q = b.q.clone()
+    ctx.page_attend(b.pages, q, _i32(b.cu), _i32(b.len), _i32(b.table), max(b.new), max(b.len), out=q)
+    assert ctx.sync_status() == 0
+    assert torch.equal(q[:-1], want[:-1]) and torch.equal(q[-1], b.q[-1])
+
+
+def test_calls_of_nothing(fkv, ctx):
+    """No tokens, no requests, or a bound of no new tokens: nothing is done."""
+    b = Batch(fkv, 47, [(40, 1), (60, 5)], 2, 2, 64, 16, "int8", "f16")
+    out, lse = b.run(ctx, max_new=0)
+    assert (out == 7).all() and (lse == 7).all()
+    cu, none = _i32([0]), _i32([])
+    out = torch.full_like(b.q, 7.0)
+    ctx.page_attend(b.pages, b.q, cu, none, _i32(b.table), 5, 65, out=out)
+    ctx.page_attend(b.pages, b.q[:0], _i32([0, 0, 0]), _i32(b.len), _i32(b.table), 5, 65, out=out[:0])
+    assert (out == 7).all() and ctx.sync_status() == 0
+
+
 @pytest.mark.parametrize("by_token", [False, True])
 def test_pages_past_four_gigabytes(fkv, ctx, by_token):
     """Byte offsets that do not fit 32 bits: a pool of 5 GiB whose last pages are written, read and attended to."""
