@@ -721,11 +721,11 @@ struct Plan {
 // Which kernel serves the call, and how many shares the keys are split into.
 // Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step
 // kernel, more to the tensor-memory one (nt = 0): for 24 sequences of 3-16k
-// positions and 8 heads of 128, 63 rows take 377 us against 252; 28 rows 260
-// against 244, but 88 against 117 with a window of 4,096 and 281 against 391 with
-// a cap.  A block's time is its keys plus a fixed part (its launch, the first loads' latency and its end: about that
-// of 384 keys); the blocks run in waves of `slots`.  The split with the least
-// waves x time wins.  Up to eight shares of the step kernel are joined in their
+// positions and 8 heads of 128, 63 rows take 384 us against 236; 28 rows 265
+// against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
+// 4,096 and 283 against 364 with a cap.  A block's time is its keys plus a fixed
+// part (its launch, the first loads' latency and its end: about that of 384 keys);
+// the blocks run in waves of `slots`.  The split with the least waves x time wins.  Up to eight shares of the step kernel are joined in their
 // cluster (about 100 keys' time) if all blocks run at once: where blocks queue,
 // those of a cluster hold their places until its last one is done (64 ragged
 // sequences of 16-32k positions: 561 us, and 499 with the shares joined by

@@ -107,8 +107,8 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 // with 2 y log2 e straight from the product: wrong by cap 1.4 2^-22 at most, 2e-5
 // (weights are rounded to 2^-11).  The error grows with the cap, though, so that
 // larger ones take capped(), which is some dozen instructions more a score (two pieces
-// of 4,096 tokens against 12-16k positions, 8 x 4 heads of 128: 3,590 us with a cap of
-// 1,000, 2,590 with one of 30).
+// of 4,096 tokens against 12-16k positions, 8 x 4 heads of 128: 3,550 us with a cap of
+// 1,000, 2,610 with one of 30).
 constexpr float kPlainCap = 64.0f;
 __device__ __forceinline__ bool plain_cap(const AttendArgs &a) { return a.softcap <= kPlainCap; }
 

@@ -16,9 +16,9 @@
 // fp16, 2^-20 of the largest and less), so no pass looks for the maximum.
 //
 // Two pieces of 4,096 tokens against 12-16k positions, 8 heads of 128 with 4 query
-// heads each: 1,386 us, 1.38 PFLOP/s, bound by a group's round of scores, softmax
+// heads each: 1,383 us, 1.38 PFLOP/s, bound by a group's round of scores, softmax
 // and product (3.5k cycles a tile, of which the products of both groups are 2.1k).
-// 13 prompts of 1 to 1,000 tokens, 12 heads of 64: 40 us, bound by the start and
+// 13 prompts of 1 to 1,000 tokens, 12 heads of 64: 39 us, bound by the start and
 // the end of a block.
 #include "attend.cuh"
 
@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int i0 = split * a.chunk, n_it = max(0, min(tiles.n, i0 + a.chunk) - i0);
     // A bias by distance grows along the keys, and the reference with it, tile by
     // tile: general scores are walked from the last tile back (two pieces of 4,096
-    // tokens against 12-16k positions, 8 heads of 128: 3,340 us forwards, 1,770 so; with a cap of 30 2,590 either way).
+    // tokens against 12-16k positions, 8 heads of 128: 3,360 us forwards, 1,670 so; with
+    // a cap of 30 2,580 and 2,610).
     auto tile_at = [&](int j) { return tiles.at(i0 + (GEN ? n_it - 1 - j : j)); };
     // the first group's rows end earlier: tiles at the share's end that none of
     // them sees are the second group's alone
@@ -290,8 +291,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ---------------------------------------------------- MMA issuer
         // One elected thread follows the loop: what it waits for, it waits for alone.
-        // (K's next tile is asked for before the weights: asked for after the product it
-        // costs 1 to 5 %.)
+        // (K's next tile is waited for before the weights; after the product with V it
+        // cost 1 to 3 %.)
         if (warp == 12 && n_it > 0) {
             constexpr uint32_t id_s = idesc_f16_f32(128, 128), id_o = idesc_f16_f32(128, D) | 1u << 16;
             constexpr uint32_t step = S::tile >> 4;
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         // ---------------------------------------------------- softmax
-        const int w = group, row = row0 + 128 * w + (tid & 127), local = tid & 127;
+        const int w = group, row = row0 + 128 * w + (tid & 127);
         const bool live = row < rows;
         if (w < groups) {
             const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;

@@ -314,8 +314,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigne
 // mbar_wait for warps that share their schedulers with working ones: the hardware
 // may suspend a waiting thread for up to 10 ms a try instead of polling (polls
 // took a fifth of the prompt attention's instruction issue).  A try may also come
-// back early, so that the limit (below 4 s) is one of time here too; half the clock
-// is enough for it, and the shorter loop is 2 % of that kernel.
+// back early, so that the limit is one of time here too (below 4 s: the timer's low
+// word is enough, and less in a loop that many warps share).
 __device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, unsigned *status,
                                           uint64_t limit_ns = kWaitLimitNs)
 {

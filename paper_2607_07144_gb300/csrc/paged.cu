@@ -455,8 +455,8 @@ template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *
 // which keeps up to four rows a thread in registers between the search for the
 // largest magnitude and the rounding (longer runs are read again).  Bytes bound
 // long calls, the chain slot, page, store a step's.  9 prompts of 1,000 to 8,192
-// tokens, 8 heads of 128, bf16 to int8: 59 us, 5.2 TB/s; 64 tokens, one a page:
-// 5.7 us, the host's.
+// tokens, 8 heads of 128, bf16 to int8: 59 us, 5.2 TB/s, from float32 150 us, 3.4
+// TB/s (fewer warps, for its registers); 64 tokens, one a page: 5.7 us, the host's.
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(GT == 32 ? 256 : GT, GT == 32 || sizeof(T) == 4 ? 1 : 8) k_page_write(WriteArgs a)
 {
     constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
@@ -747,8 +747,8 @@ cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_
     a.status = ctx->d_status;
     // a warp a token while that fills the device up to a few times over, else a
     // block for as many tokens as a page holds (8 heads of 128: 64 tokens one a page
-    // 8 us against 41 as blocks, 1,200 such 25 against 45; 600 of two prompts 16
-    // against 10, 1,200 of them 21 against 12: large calls are prompts mostly)
+    // 6 us against 32 as blocks, 600 such 10 against 33, 1,200 17 against 35; 600 of two
+    // prompts 12 against 6, 1,200 of them 16 against 6.5: large calls are prompts mostly)
     a.heads = p->n_heads;
     a.by_block = FastDiv::make(static_cast<unsigned>(p->block)), a.by_heads = FastDiv::make(static_cast<unsigned>(p->n_heads));
     a.stretch = T * p->n_heads * 2 <= static_cast<int64_t>(ctx->sms) * 64 ? 1 : p->block;
