@@ -293,7 +293,7 @@ int fkv_ac_decode(fkv_ctx *ctx, const uint32_t *words_dev, int64_t word_stride, 
 int fkv_measure_fp64_rate(double *ops_per_s, void *stream);
 
 /* Failure-path check (no counterpart in the paper): runs, in one CTA on
- * `stream`, the bounded device waits of the RVQ kernels against mbarriers
+ * `stream`, the bounded device waits of the kernels against mbarriers
  * that nothing completes, with their teardown (TMEM held and released as the
  * MMA warp does).  The first waiter gives up after limit_ns (1e5..1e9 ns,
  * else FKV_EINVAL) and raises the kernel's abort flag; a second waiter on

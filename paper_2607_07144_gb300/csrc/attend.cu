@@ -8,7 +8,8 @@
 // power of two (fp16 queries as they are), but for a bf16 row's elements below
 // 2^-31 of its largest, which fp16's subnormals round to 2^-39 of that: the products
 // are exact and summed in fp32 on the tensor cores, and the scale of a page
-// multiplies afterwards, once for each score.  The value scale goes into the softmax instead: with
+// multiplies afterwards, once for each score.  The value scale goes into the
+// softmax instead: with
 //     y_j = x_j log2 e + log2 vs,    P_j = 2^(y_j - m + 8),   m = max y_j
 // the second product is sum P_j c'_j with P rounded to fp16 (relative 2^-11, an
 // eighth of a bf16 result's own rounding; P spans 2^8 .. 2^-24, so nothing above
@@ -165,9 +166,9 @@ __global__ void __launch_bounds__(128, 3)
     __syncwarp();
 
     // A lane looks up one of the 32 units (16 keys) of 16 iterations, if any row sees
-    // one of its keys: its page and what its scales give the scores.  Page ids are asked for a batch of iterations
-    // before the scales, and these a batch before their use, so that no warp waits
-    // for one to ask for the other.
+    // one of its keys: its page and what its scales give the scores.  Page ids are
+    // asked for a batch of iterations before the scales, and these a batch before
+    // their use, so that no warp waits for one to ask for the other.
     struct Unit {
         int id;
         float ks, vs;
@@ -725,8 +726,9 @@ struct Plan {
 // against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
 // 4,096 and 283 against 364 with a cap.  A block's time is its keys plus a fixed
 // part (its launch, the first loads' latency and its end: about that of 384 keys);
-// the blocks run in waves of `slots`.  The split with the least waves x time wins.  Up to eight shares of the step kernel are joined in their
-// cluster (about 100 keys' time) if all blocks run at once: where blocks queue,
+// the blocks run in waves of `slots`.  The split with the least waves x time wins.
+// Up to eight shares of the step kernel are joined in their cluster (about 100
+// keys' time) if all blocks run at once: where blocks queue,
 // those of a cluster hold their places until its last one is done (64 ragged
 // sequences of 16-32k positions: 561 us, and 499 with the shares joined by
 // another launch, which costs 512 keys' time and 8 a share).
