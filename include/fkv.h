@@ -415,32 +415,41 @@ int fkv_read_kv(fkv_ctx *ctx, const double *pts_dev, int64_t n_streams, int64_t 
                 int64_t pt_stride, const int64_t *req_dev, int64_t n_req, void *out_dev,
                 int dtype, void *stream);
 
-/* ------------------------------------------------ paged 8-bit cache ----- */
+/* ------------------------------------------ paged 8- and 4-bit cache ----- */
 
-/* The positions that are still attended to, held in 8 bits until they are
+/* The positions that are still attended to, held in 8 or 4 bits until they are
  * archived (the paper keeps its exact window in the cache's own type and has
  * no counterpart).  A page is `block` consecutive positions of one request;
- * its codes for one head share a float32 scale, a value being code x scale.
+ * its 8-bit codes for one head share a float32 scale, a value being code x scale,
+ * its 4-bit codes have a step and a middle for each head and position.
  * Requests reach their pages through a block table.  fkv_page_plan gives pages
- * to new tokens, fkv_page_write quantises them, fkv_page_attend attends over
+ * to new tokens, fkv_page_write quantises them, fkv_page_append does that with
+ * keys turned to their positions on the way, fkv_page_attend attends over
  * them, and fkv_page_read rebuilds positions into the K/V cache that
  * fkv_rvq_encode archives. */
 
 /* Formats of a code: FKV_E4M3, 1-4-3 bits, finite values up to 448 (the two
  * NaN codes are never written, and a page that holds one in a written slot is
- * not valid); FKV_INT8, -127 .. 127. */
+ * not valid); FKV_INT8, -127 .. 127; FKV_UINT4, 0 .. 15, two a byte, the even
+ * dimension in the low half.  A 4-bit row (one position of one head) has two
+ * bfloat16 numbers of its own, and a code c stands for middle + (c - 7.5) step. */
 #define FKV_E4M3 0
 #define FKV_INT8 1
+#define FKV_UINT4 2
 
 #define FKV_PAGE_MAX_REQ 16384         /* requests a call */
 #define FKV_PAGE_MAX_LEN (1 << 30)     /* positions a request */
 
 /* A pool of pages on the device, caller-owned: K and V code tensors indexed by
- * (page, head, position in the page) with `dim` contiguous bytes each and the
- * same byte strides (multiples of 16, data 16-byte aligned), and their scales,
- * indexed by (page, head).  dim is 64 or 128, block a multiple of 16 up to
- * 1024.  Any order of the strides will do: [page][head][position][dim] and
- * [page][position][head][dim] alike.  Scales lie in [2^-100, 2^100]. */
+ * (page, head, position in the page) with `dim` contiguous bytes each (FKV_UINT4:
+ * dim / 2) and the same byte strides (multiples of 16, data 16-byte aligned), and
+ * their scales, indexed by (page, head).  dim is 64 or 128, block a multiple of 16
+ * up to 1024.  Any order of the strides will do: [page][head][position][dim] and
+ * [page][position][head][dim] alike.  Scales lie in [2^-100, 2^100].
+ * FKV_UINT4: k_scale and v_scale hold the rows' numbers instead, `block` pairs
+ * (step, middle) of bfloat16 one behind the other for each (page, head), 16-byte
+ * aligned, the strides multiples of 4 floats (a pair takes the place of one).
+ * Steps lie in [2^-100, 2^100] and are at least 2^-16 of the middle's magnitude. */
 typedef struct {
     void *k;
     void *v;
@@ -532,9 +541,62 @@ int fkv_page_plan(fkv_ctx *ctx, const fkv_plan *plan, void *stream);
  * stored as x x (1 / scale) rounded to the nearest code (ties to even), beyond the
  * largest as the largest.  A NaN is stored as zero and sets FKV_ECORRUPT in the
  * status word; a slot past the pool is skipped and sets FKV_ERANGE.  What two
- * runs of one page in a call leave there is not specified. */
+ * runs of one page in a call leave there is not specified.
+ * FKV_UINT4: every row by itself, in any order of the slots (of a slot that is named
+ * twice the row is one of the two, or a mixture).  With its values limited to 2^102
+ * either way, lo and hi the least and the greatest, in float32 operations rounded
+ * one by one:
+ *     middle = bfloat16(lo / 2 + hi / 2), to nearest (ties to even),
+ *     step   = max(hi - middle, middle - lo) x (2 / 15), up to bfloat16, at least
+ *              2^-100 and 2^-16 |middle|,
+ *     code   = (x - middle) x (1 / step) + 7.5 to nearest (ties to even),
+ * so that a stored value is off by half a step at most (and float32's rounding). */
 int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, const fkv_rows *v,
                    const int64_t *slots_dev, int64_t n_tok, void *stream);
+
+/* fkv_page_write with rotary positions: the keys' first `rot` dimensions are turned
+ * by their tokens' angles before they are quantised, and so are the queries', into
+ * q_out.  Dimensions (a, b) become
+ *     (a cos - b sin, b cos + a sin),
+ * products and sums rounded to float32 one by one: dimensions i and i + rot / 2, i <
+ * rot / 2, or with `interleaved` 2 i and 2 i + 1.  cos and sin: float32 tables of
+ * n_pos positions, rot / 2 values each at pos x table_stride (the halves of one
+ * [n_pos][rot] table will do); angles of far positions are best computed in 64
+ * bits.  Keys are not rounded to their type between turning and quantising; a
+ * query's dimensions are rounded to it once, those from rot on are copied.  V goes
+ * into the pages as it is.
+ * slots and pos as fkv_page_plan gives them, slots as in fkv_page_write.  A token
+ * of a negative position is left out: nothing of it is stored, its row of q_out left
+ * as it is; one of a position past the tables too, and FKV_ERANGE is set.  A token of
+ * a negative slot has its query turned all the same.  q_out may be q itself; its
+ * rows overlap nothing else of the call.  q and q_out may be NULL. */
+typedef struct {
+    const void *q;               /* vectors by (token, head) as fkv_rows, all of `dtype`: */
+    void *q_out;                 /*   16-byte boundaries, element strides below */
+    const void *k;
+    const void *v;
+    const int64_t *slots;        /* device, [n_tok] */
+    const int32_t *pos;          /* device, [n_tok] */
+    const float *cos;            /* device, 16-byte aligned */
+    const float *sin;
+    int64_t q_stride_tok;
+    int64_t q_stride_head;
+    int64_t out_stride_tok;
+    int64_t out_stride_head;
+    int64_t k_stride_tok;
+    int64_t k_stride_head;
+    int64_t v_stride_tok;
+    int64_t v_stride_head;
+    int64_t table_stride;        /* floats between positions, a multiple of 4 */
+    int64_t n_pos;
+    int64_t n_tok;
+    int32_t dtype;               /* FKV_F32, FKV_F16 or FKV_BF16 */
+    int32_t n_q_heads;           /* of q and q_out (any number, 0 without them) */
+    int32_t rot;                 /* a multiple of 16 up to dim */
+    int32_t interleaved;         /* 0 or 1 */
+} fkv_rotary;
+
+int fkv_page_append(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rotary *a, void *stream);
 
 /* Attention of a batch's query rows over the pages.  q: n_tok tokens of
  * n_q_heads heads (FKV_F16 or FKV_BF16), n_q_heads a multiple of
@@ -607,7 +669,8 @@ int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t 
 /* Rebuild positions [t0, min(t1, kv_len_dev[r])) of every request r < n_req
  * into layer `layer`, sequence r of k_out and v_out (either may be NULL; views
  * of n_req sequences and the pages' heads and dim that hold t1 positions):
- * code x scale, rounded to nearest-even into the view's dtype.  Other
+ * code x scale, or middle + (code - 7.5) step rounded to float32, rounded to
+ * nearest-even into the view's dtype.  Other
  * positions are left as they are.  A page id outside the pool, or a length
  * past the table, leaves its positions as they are and sets FKV_ERANGE. */
 int fkv_page_read(fkv_ctx *ctx, const fkv_pages *pages, const int32_t *kv_len_dev, int64_t n_req,

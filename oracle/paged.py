@@ -1,4 +1,4 @@
-"""Float64 oracle of the paged 8-bit K/V cache, written from the definitions in
+"""Float64 oracle of the paged 8- and 4-bit K/V cache, written from the definitions in
 include/fkv.h: plain numpy, one request, page and row at a time."""
 from __future__ import annotations
 
@@ -83,6 +83,72 @@ def write(codes, scale, x, slots, fmt):
             codes[blk, h, off:off + n] = to_codes(np.clip(y, -1e30, 1e30), fmt)
             scale[blk, h] = now
         t += n
+
+
+# ------------------------------------------------------- 4-bit rows, turning --
+MOST4 = np.float32(2.0 ** 102)
+
+
+def to_bf16(x, up=False):
+    """float32 -> the nearest bfloat16 (ties to even), or the next one not below a non-negative x, as float32."""
+    u = np.ascontiguousarray(x, np.float32).view(np.uint32).astype(np.uint64)
+    u = u + 0xffff if up else u + 0x7fff + (u >> 16 & 1)
+    return (u & 0xffff0000).astype(np.uint32).view(np.float32)
+
+
+def rows4(x):
+    """(codes uint8 [..., D], step, middle float32 [...]) of rows x; the rounding steps that fkv.h names are float32."""
+    with np.errstate(over="ignore", invalid="ignore"):
+        x = np.asarray(x).astype(np.float32)
+    x = np.clip(np.where(np.isnan(x), np.float32(0), x), -MOST4, MOST4)
+    lo, hi, f = x.min(-1), x.max(-1), np.float32
+    mid = to_bf16(lo * f(0.5) + hi * f(0.5))
+    step = to_bf16(np.maximum(hi - mid, mid - lo) * f(2.0 / 15.0), up=True)
+    step = np.maximum(np.maximum(step, np.abs(mid) * f(2.0 ** -16)), f(FLOOR))
+    y = (x - mid[..., None]) * (f(1) / step)[..., None] + f(7.5)
+    return np.rint(y).astype(np.uint8), step, mid
+
+
+def pack4(c):
+    return c[..., ::2] | c[..., 1::2] << 4
+
+
+def write4(codes, numbers, x, slots):
+    """codes uint8 [n_blocks, H, B, D / 2] and numbers float32 [n_blocks, H, B, 2] (step, middle) updated in place."""
+    B = codes.shape[2]
+    c, step, mid = rows4(x)
+    for t, s in enumerate(int(s) for s in slots):
+        if 0 <= s < codes.shape[0] * B:
+            codes[s // B, :, s % B] = pack4(c[t])
+            numbers[s // B, :, s % B] = np.stack([step[t], mid[t]], -1)
+
+
+def values4(codes, numbers):
+    """float64 values of packed rows: middle + (code - 7.5) step."""
+    c = np.stack([codes & 15, codes >> 4], -1).reshape(codes.shape[:-1] + (-1,)).astype(np.float64)
+    n = np.asarray(numbers, np.float64)
+    return n[..., 1:] + (c - 7.5) * n[..., :1]
+
+
+def gather4(codes, numbers, table_row, tokens):
+    """float64 values [H, tokens, D] of one request's first positions."""
+    ids = [int(i) for i in table_row[:-(-tokens // codes.shape[2])]]
+    if not ids:
+        return np.zeros((codes.shape[1], 0, 2 * codes.shape[3]))
+    return np.concatenate([values4(codes[i], numbers[i]) for i in ids], 1)[:, :tokens]
+
+
+def turn(x, pos, cos, sin, rot, interleaved=False):
+    """float32 [T, heads, D]: the first rot dimensions turned by the tokens' angles, products and sums rounded one by one."""
+    x = np.asarray(x, np.float32).copy()
+    p = np.clip(np.asarray(pos), 0, len(cos) - 1)
+    c, s = (np.asarray(y, np.float32)[p][:, None] for y in (cos, sin))
+    i = np.arange(rot // 2)
+    i, j = (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+    with np.errstate(over="ignore", invalid="ignore"):
+        a, b = x[..., i], x[..., j]
+        x[..., i], x[..., j] = a * c - b * s, b * c + a * s
+    return x
 
 
 def plan(n_new, kv_len, table, free, taken, block, rows):

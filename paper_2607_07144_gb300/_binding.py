@@ -16,8 +16,8 @@ LIB_PATH = os.path.join(_PKG, "libfkv.so")
 
 OK, EINVAL, ERANGE, ENOMEM, ECUDA, ECORRUPT, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
 F32, F16, BF16 = 0, 1, 2
-E4M3, INT8 = 0, 1
-_FORMAT = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
+E4M3, INT8, UINT4 = 0, 1, 2
+_FORMAT = {torch.float8_e4m3fn: E4M3, torch.int8: INT8, torch.uint8: UINT4}
 _DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _ERRNAME = {EINVAL: "EINVAL", ERANGE: "ERANGE", ENOMEM: "ENOMEM", ECUDA: "ECUDA",
             ECORRUPT: "ECORRUPT", ETIMEOUT: "ETIMEOUT"}
@@ -60,6 +60,7 @@ _CACHE = struct.Struct("@Pi6q")
 _ROWS = struct.Struct("@Piqq")
 _PLAN = struct.Struct("@10P6q")
 _ATTEND = struct.Struct("@9P12q3i2fi")
+_ROTARY = struct.Struct("@8P11q4i")
 
 
 # name -> (restype, argtypes)
@@ -98,6 +99,7 @@ SIGNATURES = {
     "fkv_cache_upload": (_I, [_P, _P, _P, _I64, _I64, _P]),
     "fkv_page_plan": (_I, [_P, _P, _P]),
     "fkv_page_write": (_I, [_P, _P, _P, _P, _P, _I64, _P]),
+    "fkv_page_append": (_I, [_P, _P, _P, _P]),
     "fkv_page_attend_workspace": (_I64, [_P, _P]),
     "fkv_page_attend": (_I, [_P, _P, _P, _I64, _P]),
     "fkv_page_read": (_I, [_P, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _P, _P, _P]),
@@ -207,23 +209,40 @@ def _table(t: torch.Tensor, n_req: int, dev: int):
 
 
 class Pages:
-    """A pool of 8-bit K/V pages (fkv_pages): codes k and v [n_blocks, heads,
+    """A pool of 8- or 4-bit K/V pages (fkv_pages): codes k and v [n_blocks, heads,
     block, dim], torch.float8_e4m3fn or torch.int8, of the same strides (any,
     with a contiguous dim: [n_blocks, block, heads, dim] permuted will do), and
-    float32 scales [n_blocks, heads].  The tensors stay the caller's."""
+    float32 scales [n_blocks, heads].  torch.uint8: 4-bit codes, two a byte (the
+    even dimension in the low half), [n_blocks, heads, block, dim / 2], and in place
+    of the scales (step, middle) of every row, bfloat16 [n_blocks, heads, block, 2]
+    with the last two dimensions contiguous.  The tensors stay the caller's."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         if (k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1 or
                 k.dtype not in _FORMAT or not k.is_cuda or any(t.device != k.device for t in (v, k_scale, v_scale))):
-            raise ValueError("k and v must be float8_e4m3fn or int8 tensors [blocks, heads, block, dim] of one shape "
-                             "and strides, with contiguous dim, and all four on one CUDA device")
-        if (k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:2] or
+            raise ValueError("k and v must be float8_e4m3fn, int8 or uint8 tensors [blocks, heads, block, dim] of one "
+                             "shape and strides, with contiguous dim, and all four on one CUDA device")
+        four = k.dtype == torch.uint8
+        if four:
+            ss = k_scale.stride()
+            if (k_scale.dtype != torch.bfloat16 or v_scale.dtype != torch.bfloat16 or k_scale.shape != k.shape[:3] + (2,) or
+                    v_scale.shape != k_scale.shape or ss != v_scale.stride() or ss[3] != 1 or ss[2] != 2):
+                raise ValueError("k_scale and v_scale of uint8 codes must be bfloat16 tensors [blocks, heads, block, 2] of "
+                                 "the same strides, the last two dimensions contiguous")
+            # in pairs; the stride of a dimension of one is never used, but has to be a valid one
+            if any(x % 2 for x, n in zip(ss[:2], k.shape) if n > 1):
+                raise ValueError("k_scale and v_scale must have even strides")
+            ss = [x // 2 if n > 1 else 0 for x, n in zip(ss[:2], k.shape)]
+        elif (k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:2] or
                 v_scale.shape != k.shape[:2] or k_scale.stride() != v_scale.stride()):
             raise ValueError("k_scale and v_scale must be float32 tensors [blocks, heads] of the same strides")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_blocks, self.heads, self.block, self.dim = k.shape
+        if four:
+            self.dim *= 2
+        else:
+            ss = k_scale.stride()
         self.device = k.get_device()
-        ss = k_scale.stride()
         # the stride of a dimension of one is never used, but has to be a valid one
         st = [x if n > 1 else self.dim for x, n in zip(k.stride(), k.shape)]
         self._c = _Pages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _FORMAT[k.dtype],
@@ -233,10 +252,12 @@ class Pages:
 
     @classmethod
     def empty(cls, n_blocks: int, heads: int, block: int, dim: int, dtype=torch.float8_e4m3fn, device="cuda"):
-        shape = (n_blocks, heads, block, dim)
+        """Pages of `dtype`: torch.float8_e4m3fn, torch.int8, or torch.uint8 for 4-bit codes."""
+        four = dtype == torch.uint8
+        shape = (n_blocks, heads, block, dim // 2 if four else dim)
+        scale, st = (shape[:3] + (2,), torch.bfloat16) if four else (shape[:2], torch.float32)
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
-                   torch.empty(shape[:2], dtype=torch.float32, device=device),
-                   torch.empty(shape[:2], dtype=torch.float32, device=device))
+                   torch.empty(scale, dtype=st, device=device), torch.empty(scale, dtype=st, device=device))
 
 
 class Context:
@@ -278,6 +299,7 @@ class Context:
         self._plan = ctypes.create_string_buffer(_PLAN.size)
         self._rows = [ctypes.create_string_buffer(_ROWS.size) for _ in range(2)]
         self._attend = ctypes.create_string_buffer(_ATTEND.size)
+        self._rotary = ctypes.create_string_buffer(_ROTARY.size)
         self._caches = [ctypes.create_string_buffer(_CACHE.size) for _ in range(2)]
         self._attend_need = {}
         # symbols are uint8 up to N = 256, uint16 above; torch.int16 holds the
@@ -588,6 +610,46 @@ class Context:
                                   _array(slots, _INT64, n, "slots", dev), n, _stream(stream))
         if rc != OK:
             self._check(rc)
+
+    def page_append(self, pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor,
+                    cos: torch.Tensor, sin: torch.Tensor, q: torch.Tensor = None, q_out: torch.Tensor = None,
+                    interleaved: bool = False, stream=None) -> torch.Tensor:
+        """page_write with rotary positions: k's, and q's [tokens, query heads, dim], first 2 * cos.shape[1]
+        dimensions are turned by row positions[t] (int32; negative: the token is left out) of cos and sin
+        (float32 [positions, dimensions / 2], halves of one table will do), dimension i together with i + half,
+        or interleaved 2 i with 2 i + 1.  Returns the turned queries: q_out (which may be q), by default new
+        memory on the call's stream, whose rows of tokens left out hold anything; None without q."""
+        dev = self._on(pages)
+        dim = pages.dim
+        kp, dt, shape, kt, kh = _vectors(k, dim, "k", dev)
+        vp, vd, vshape, vt, vh = _vectors(v, dim, "v", dev)
+        n = shape[0]
+        if vshape != shape or vd != dt or shape[1] != pages.heads:
+            raise ValueError("k and v must be [tokens, %d, %d] of one type" % (pages.heads, dim))
+        cs, ss, st = cos.shape, sin.shape, cos.stride()
+        if (len(cs) != 2 or cs != ss or st != sin.stride() or (st[1] != 1 and cs[1] > 1) or cos.dtype is not _FLOAT or
+                sin.dtype is not _FLOAT or cos.get_device() != dev or sin.get_device() != dev):
+            raise ValueError("cos and sin must be float32 tensors [positions, turned dimensions / 2] of the same strides, "
+                             "contiguous in the second, on cuda:%d" % dev)
+        qp = op = qt = qh = ot = oh = heads = 0
+        if q is not None:
+            qp, qd, qshape, qt, qh = _vectors(q, dim, "q", dev)
+            if q_out is None:
+                q_out = self._empty(tuple(qshape), q.dtype, stream)
+            op, od, oshape, ot, oh = _vectors(q_out, dim, "q_out", dev)
+            heads = qshape[1]
+            if qshape[0] != n or qd != dt or od != dt or oshape != qshape:
+                raise ValueError("q and q_out must be [%d, query heads, %d] of k's type" % (n, dim))
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        buf = self._rotary
+        _ROTARY.pack_into(buf, 0, qp, op, kp, vp, _array(slots, _INT64, n, "slots", dev),
+                          _array(positions, _I32, n, "positions", dev), cos.data_ptr(), sin.data_ptr(), qt, qh, ot, oh, kt, kh,
+                          vt, vh, st[0] if cs[0] > 1 else cs[1], cs[0], n, dt, heads, 2 * cs[1], 1 if interleaved else 0)
+        rc = lib().fkv_page_append(self._h, pages._addr, buf, _stream(stream))
+        if rc != OK:
+            self._check(rc)
+        return q_out
 
     def page_attend(self, pages: Pages, q: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor,
                     block_table: torch.Tensor, max_new: int, max_len: int, out: torch.Tensor = None,

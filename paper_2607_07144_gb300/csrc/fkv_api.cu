@@ -1031,7 +1031,7 @@ const char *check_pages(const fkv_pages *p)
 {
     if (!p || !p->k || !p->v || !p->k_scale || !p->v_scale)
         return "null page pool";
-    if (p->format != FKV_E4M3 && p->format != FKV_INT8)
+    if (p->format != FKV_E4M3 && p->format != FKV_INT8 && p->format != FKV_UINT4)
         return "unknown page format";
     if (p->dim != 64 && p->dim != 128)
         return "pages hold heads of 64 or 128 dimensions";
@@ -1045,7 +1045,11 @@ const char *check_pages(const fkv_pages *p)
             return "bad page stride";
     if (p->scale_stride_block < 0 || p->scale_stride_head < 0)
         return "bad scale stride";
-    if (misaligned(p->k, 16) || misaligned(p->v, 16) || misaligned(p->k_scale, 4) || misaligned(p->v_scale, 4))
+    // the numbers of 16 positions of 4-bit rows are copied together
+    const size_t to = p->format == FKV_UINT4 ? 16 : 4;
+    if (to == 16 && (p->scale_stride_block % 4 || p->scale_stride_head % 4))
+        return "bad scale stride";
+    if (misaligned(p->k, 16) || misaligned(p->v, 16) || misaligned(p->k_scale, to) || misaligned(p->v_scale, to))
         return "misaligned page pool";
     return nullptr;
 }
@@ -1082,6 +1086,8 @@ const char *check_attend_sizes(const fkv_attend *a)
     if (a->n_tok < 0 || a->n_tok > INT32_MAX || a->n_req < 0 || a->n_req > FKV_PAGE_MAX_REQ || a->max_new < 0 ||
         a->max_new > FKV_PAGE_MAX_LEN || a->max_len < 0 || a->max_len > FKV_PAGE_MAX_LEN || a->window < 0 || a->sinks < 0)
         return "size out of range";
+    if (a->pages->format == FKV_UINT4)
+        return "no attention over 4-bit pages";
     const int H = a->pages->n_heads;
     if (a->n_q_heads < H || a->n_q_heads % H || a->n_q_heads > 65535)
         return "query heads must be a multiple of the pages' heads";
@@ -1174,7 +1180,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
         return fail(ctx, FKV_EINVAL, why);
     if (k->dtype != v->dtype)
         return fail(ctx, FKV_EINVAL, "K and V types differ");
-    if ((n_tok / pages->block + 1) * 2 * pages->n_heads > INT32_MAX)
+    // (of 4-bit pages rows, a block of threads for four at least)
+    if ((pages->format == FKV_UINT4 ? n_tok / 4 + 1 : n_tok / pages->block + 1) * 2 * pages->n_heads > INT32_MAX)
         return fail(ctx, FKV_EINVAL, "too many tokens for one launch");
     if (pages->n_blocks * pages->block > int64_t(1) << 32)
         return fail(ctx, FKV_EINVAL, "a pool of more than 2^32 slots");
@@ -1183,6 +1190,45 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
     if (const char *why = check_device(ctx))
         return fail(ctx, FKV_EINVAL, why);
     CK(launch_page_write(ctx, pages, k, v, slots_dev, n_tok, as_stream(stream)), "page write launch");
+    return FKV_OK;
+}
+
+int fkv_page_append(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rotary *a, void *stream)
+{
+    if (!ctx)
+        return FKV_EINVAL;
+    if (!a)
+        return fail(ctx, FKV_EINVAL, "null arguments");
+    if (a->n_tok < 0 || a->n_tok > INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "size out of range");
+    if (const char *why = check_pages(pages))
+        return fail(ctx, FKV_EINVAL, why);
+    if (a->n_tok == 0)
+        return FKV_OK;
+    const fkv_rows rows[4] = {{const_cast<void *>(a->k), a->dtype, a->k_stride_tok, a->k_stride_head},
+                              {const_cast<void *>(a->v), a->dtype, a->v_stride_tok, a->v_stride_head},
+                              {const_cast<void *>(a->q), a->dtype, a->q_stride_tok, a->q_stride_head},
+                              {a->q_out, a->dtype, a->out_stride_tok, a->out_stride_head}};
+    const bool queries = a->q || a->q_out;
+    for (int i = 0; i < (queries ? 4 : 2); ++i)
+        if (const char *why = check_rows(&rows[i]))
+            return fail(ctx, FKV_EINVAL, why);
+    if (a->n_q_heads < (queries ? 1 : 0) || a->n_q_heads > 65535 || (!queries && a->n_q_heads))
+        return fail(ctx, FKV_EINVAL, "bad number of query heads");
+    if (a->rot < 16 || a->rot > pages->dim || a->rot % 16 || (a->interleaved != 0 && a->interleaved != 1))
+        return fail(ctx, FKV_EINVAL, "turned dimensions must be a multiple of 16 up to the heads'");
+    if (!a->cos || !a->sin || misaligned(a->cos, 16) || misaligned(a->sin, 16) || a->n_pos < 1 || a->n_pos > FKV_PAGE_MAX_LEN ||
+        a->table_stride < 0 || a->table_stride % 4)
+        return fail(ctx, FKV_EINVAL, "bad table of cosines or sines");
+    if (page_append_blocks(pages, *a) > INT32_MAX)
+        return fail(ctx, FKV_EINVAL, "too many tokens for one launch");
+    if (pages->n_blocks * pages->block > int64_t(1) << 32)
+        return fail(ctx, FKV_EINVAL, "a pool of more than 2^32 slots");
+    if (!a->slots || misaligned(a->slots, 8) || !a->pos || misaligned(a->pos, 4))
+        return fail(ctx, FKV_EINVAL, "bad slot or position map");
+    if (const char *why = check_device(ctx))
+        return fail(ctx, FKV_EINVAL, why);
+    CK(launch_page_append(ctx, pages, *a, as_stream(stream)), "page append launch");
     return FKV_OK;
 }
 

@@ -63,7 +63,7 @@ struct fkv_ctx {
     int device = 0;
     int sms = 0;                   // SMs of the device
     // kernels this context has launched (calls on one context are serialised)
-    mutable fkv_kernel_use uses[96];
+    mutable fkv_kernel_use uses[160];
     mutable int n_uses = 0;
     double2 *d_V = nullptr;        // [N] vertices; first of one allocation with d_T, d_dec and d_status
     fkv_decconst *d_dec = nullptr; // decoder constants (device copy)
@@ -203,6 +203,9 @@ int64_t read_order_ints(const fkv_ctx *c, int64_t n_req);
 cudaError_t launch_page_plan(const fkv_ctx *c, const fkv_plan &p, cudaStream_t st);
 cudaError_t launch_page_write(const fkv_ctx *c, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
                               const int64_t *slots, int64_t n_tok, cudaStream_t st);
+cudaError_t launch_page_append(const fkv_ctx *c, const fkv_pages *p, const fkv_rotary &r, cudaStream_t st);
+// More blocks than a call of these sizes launches.
+int64_t page_append_blocks(const fkv_pages *p, const fkv_rotary &r);
 cudaError_t launch_page_read(const fkv_ctx *c, const fkv_pages *p, const int32_t *kv_len, int64_t n_req,
                              const int32_t *table, int64_t table_stride, int64_t width, int64_t t0, int64_t t1,
                              int64_t layer, const fkv_cache *k_out, const fkv_cache *v_out, cudaStream_t st);

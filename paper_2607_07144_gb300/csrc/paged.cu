@@ -1,9 +1,8 @@
-// The paged 8-bit K/V cache: block tables and slot maps from request lengths
-// (k_page_plan), quantising writes (k_page_write) and the way back to a K/V
-// cache (k_page_read).  Attention over the pages is in attend.cu.
-#include <type_traits>
-
-#include "paged.cuh"
+// The paged 8- and 4-bit K/V cache: block tables and slot maps from request lengths
+// (k_page_plan), quantising writes of 8-bit pages (k_page_write) and the way back to a
+// K/V cache (k_page_read).  Writes of 4-bit rows and of turned keys are in append.cu,
+// attention over the pages in attend.cu.
+#include "quant.cuh"
 
 using namespace fkvd;
 
@@ -260,116 +259,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan_finish(PlanArgs a)
 }
 
 // ----------------------------------------------------------------- write --
-template <typename T> __device__ __forceinline__ void load16(const T *p, float *x);
-template <> __device__ __forceinline__ void load16<float>(const float *p, float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float4 v = reinterpret_cast<const float4 *>(p)[i];
-        x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
-    }
-}
-template <> __device__ __forceinline__ void load16<__half>(const __half *p, float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-        const __half2 *h = reinterpret_cast<const __half2 *>(&v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 f = __half22float2(h[k]);
-            x[8 * i + 2 * k] = f.x, x[8 * i + 2 * k + 1] = f.y;
-        }
-    }
-}
-template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16 *p, float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
-            x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-        }
-    }
-}
-
-__device__ __forceinline__ float finite_abs(float v)
-{
-    const float a = fabsf(v);
-    return a <= 3.402823466e38f ? a : 0.0f;      // false for infinities and NaN
-}
-
-// The scale that brings amax into the format's range (fkv.h): e4m3 the smallest
-// power of two, so that a later, larger scale rounds no stored code again but
-// in the lowest (subnormal) ones; int8 amax / 127, which uses all its codes.  Either
-// within [2^-100, 2^100].
-template <int FMT> __device__ __forceinline__ float scale_of(float amax)
-{
-    if (FMT == FKV_INT8)
-        return fminf(fmaxf(__fdiv_rn(amax, 127.0f), FKV_PAGE_MIN_SCALE), FKV_PAGE_MAX_SCALE);
-    const uint32_t u = __float_as_uint(amax);
-    // amax = 1.m 2^E; 448 = 1.75 2^8
-    const int e = static_cast<int>(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
-    return __uint_as_float(static_cast<uint32_t>(min(max(e, -100), 100) + 127) << 23);
-}
-
-// 16 values times inv, rounded to codes.
-template <int FMT> __device__ __forceinline__ uint4 codes16(const float *x, float inv)
-{
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = x[4 * i] * inv, b = x[4 * i + 1] * inv, c = x[4 * i + 2] * inv, d = x[4 * i + 3] * inv;
-        if (FMT == FKV_INT8) {
-            int q[4];
-            const float y[4] = {a, b, c, d};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)       // NaN: 0 (the conversion's), infinities: +-127
-                q[k] = max(-127, min(127, __float2int_rn(y[k])));
-            w[i] = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | static_cast<uint32_t>(q[3]) << 24;
-        } else {
-            uint16_t lo, hi;
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-            w[i] = static_cast<uint32_t>(hi) << 16 | lo;
-        }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// A NaN has no code a reader could take as one: it is stored as zero.
-__device__ __forceinline__ bool drop_nan(float *x)
-{
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (x[i] != x[i])
-            x[i] = 0.0f, any = true;
-    return any;
-}
-
-template <int FMT> __device__ __forceinline__ void values16(const uint4 &v, float *x)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (FMT == FKV_INT8) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                x[4 * i + k] = static_cast<float>(static_cast<int8_t>(w[i] >> (8 * k)));
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float2 f = __half22float2(e4m3x2_half2(static_cast<uint16_t>(w[i] >> (16 * k))));
-                x[4 * i + 2 * k] = f.x, x[4 * i + 2 * k + 1] = f.y;
-            }
-        }
-    }
-}
-
 struct WriteArgs {
     uint8_t *pool[2];
     float *scale[2];
@@ -381,71 +270,6 @@ struct WriteArgs {
     FastDiv by_block, by_heads;
     unsigned *status;
 };
-
-// 16 elements as they lie in memory.
-template <typename T> struct Raw {
-    uint4 v[sizeof(T)];
-};
-
-template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *p)
-{
-    Raw<T> r;
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)); ++i)
-        r.v[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
-    return r;
-}
-
-// The largest magnitude of some elements, two at a time for 16-bit types; a NaN
-// makes it NaN.
-template <typename T> struct Largest {
-    uint32_t m = 0;
-    __device__ __forceinline__ void take(const Raw<T> &r)
-    {
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(&r);
-#pragma unroll
-        for (int i = 0; i < 4 * static_cast<int>(sizeof(T)); ++i) {
-            if (std::is_same<T, float>::value)
-                // magnitudes compare as integers do, NaN above infinity
-                m = max(m, w[i] & 0x7fffffffu);
-            else if (std::is_same<T, __half>::value)
-                asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
-            else
-                asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
-        }
-    }
-    __device__ __forceinline__ float value() const
-    {
-        if (std::is_same<T, float>::value)
-            return __uint_as_float(m);
-        if (std::is_same<T, __half>::value) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&m));
-            return f.x != f.x || f.y != f.y ? __uint_as_float(0x7fffffffu) : fmaxf(f.x, f.y);
-        }
-        const uint32_t b = max(m & 0xffffu, m >> 16);
-        return __uint_as_float(b << 16);
-    }
-};
-
-// codes16 of values of at most the scale's range: no limits to look at, and an
-// int8's rounding is an addition of 1.5 2^23, whose sum's low byte is the code.
-template <int FMT> __device__ __forceinline__ uint4 codes16_inside(const float *x, float inv)
-{
-    if (FMT == FKV_E4M3) {
-        return codes16<FMT>(x, inv);
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t q[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                q[k] = __float_as_uint(__fadd_rn(__fmul_rn(x[4 * i + k], inv), 12582912.0f));
-            w[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
 
 // A run of tokens with consecutive slots inside one page belongs to the group of
 // GT threads whose stretch of tokens holds its first one, for one head and K or
@@ -596,32 +420,6 @@ template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(
 }
 
 // ------------------------------------------------------------------ read --
-template <typename T> __device__ __forceinline__ void store16(T *p, const float *x);
-template <> __device__ __forceinline__ void store16<float>(float *p, const float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        reinterpret_cast<float4 *>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-}
-template <> __device__ __forceinline__ void store16<__half>(__half *p, const float *x)
-{
-    __half2 h[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-    reinterpret_cast<uint4 *>(p)[0] = *reinterpret_cast<uint4 *>(&h[0]);
-    reinterpret_cast<uint4 *>(p)[1] = *reinterpret_cast<uint4 *>(&h[4]);
-}
-template <> __device__ __forceinline__ void store16<__nv_bfloat16>(__nv_bfloat16 *p, const float *x)
-{
-    __nv_bfloat162 h[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    reinterpret_cast<uint4 *>(p)[0] = *reinterpret_cast<uint4 *>(&h[0]);
-    reinterpret_cast<uint4 *>(p)[1] = *reinterpret_cast<uint4 *>(&h[4]);
-}
-
 struct ReadArgs {
     const uint8_t *pool[2];
     const float *scale[2];
@@ -634,8 +432,8 @@ struct ReadArgs {
     unsigned *status;
 };
 
-// A warp per 16 positions of one page, head and K or V: 16 bytes of codes a
-// lane and step, their 16 values out.  A call moves D + 1 .. 4 D bytes a
+// A warp per 16 positions of one page, head and K or V: 16 codes a lane and step,
+// their 16 values out.  A call moves D + 1 .. 4 D bytes a
 // vector and computes next to nothing: the bytes bound it (4 sequences of 9-33k
 // positions, 8 heads of 128, e4m3 to bf16: 93 us, 6.2 TB/s).
 template <int D, int FMT, typename T> __global__ void __launch_bounds__(256) k_page_read(ReadArgs a)
@@ -661,18 +459,25 @@ template <int D, int FMT, typename T> __global__ void __launch_bounds__(256) k_p
             atomicOr(a.status, FKV_ST_RANGE);
         return;
     }
-    const float s = a.scale[kv][id * a.scb + h * a.sch];
-    const uint8_t *page = a.pool[kv] + id * a.sb + h * a.sh + (p0 - static_cast<int64_t>(j) * a.block) * a.st + c * 16;
+    const int off = static_cast<int>(p0 - static_cast<int64_t>(j) * a.block);
+    // 4-bit rows have numbers of their own
+    const float *const sp = a.scale[kv] + id * a.scb + h * a.sch + (FMT == FKV_UINT4 ? off : 0);
+    const float s = FMT == FKV_UINT4 ? 0.0f : *sp;
+    const uint8_t *page = a.pool[kv] + id * a.sb + h * a.sh + off * a.st + c * (FMT == FKV_UINT4 ? 8 : 16);
     T *out = static_cast<T *>(a.out[kv]) + r * a.o_batch[kv] + h * a.o_head[kv] + p0 * a.o_pos[kv] + c * 16;
 #pragma unroll
     for (int i = lane / C; i < 16; i += R) {
         if (p0 + i < a.t0 || p0 + i >= to)
             continue;
         float v[16];
-        values16<FMT>(*reinterpret_cast<const uint4 *>(page + i * a.st), v);
+        if (FMT == FKV_UINT4) {
+            values16_4bit(*reinterpret_cast<const uint2 *>(page + i * a.st), __float_as_uint(sp[i]), v);
+        } else {
+            values16<FMT>(*reinterpret_cast<const uint4 *>(page + i * a.st), v);
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-            v[k] *= s;
+            for (int k = 0; k < 16; ++k)
+                v[k] *= s;
+        }
         store16<T>(out + i * a.o_pos[kv], v);
     }
 }
@@ -699,6 +504,13 @@ template <int FMT, typename T> cudaError_t read_as(const ReadArgs &a, int dim, d
     else
         k_page_read<128, FMT, T><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
+}
+
+template <int FMT> cudaError_t read_type(const ReadArgs &a, int dim, int dtype, dim3 grid, cudaStream_t st)
+{
+    return dtype == FKV_F32   ? read_as<FMT, float>(a, dim, grid, st)
+           : dtype == FKV_F16 ? read_as<FMT, __half>(a, dim, grid, st)
+                              : read_as<FMT, __nv_bfloat16>(a, dim, grid, st);
 }
 
 }  // namespace
@@ -731,6 +543,14 @@ cudaError_t launch_page_plan(const fkv_ctx *ctx, const fkv_plan &p, cudaStream_t
 cudaError_t launch_page_write(const fkv_ctx *ctx, const fkv_pages *p, const fkv_rows *k, const fkv_rows *v,
                               const int64_t *slots, int64_t T, cudaStream_t st)
 {
+    if (p->format == FKV_UINT4) {
+        // rows by themselves: append.cu's, which turns nothing here
+        fkv_rotary r = {};
+        r.k = k->data, r.v = v->data, r.slots = slots, r.n_tok = T, r.dtype = k->dtype;
+        r.k_stride_tok = k->stride_tok, r.k_stride_head = k->stride_head;
+        r.v_stride_tok = v->stride_tok, r.v_stride_head = v->stride_head;
+        return launch_page_append(ctx, p, r, st);
+    }
     WriteArgs a;
     const fkv_rows *x[2] = {k, v};
     for (int i = 0; i < 2; ++i) {
@@ -790,14 +610,7 @@ cudaError_t launch_page_read(const fkv_ctx *ctx, const fkv_pages *p, const int32
     a.units = static_cast<int>((t1 + 15) / 16 - t0 / 16);
     a.kv0 = k_out ? 0 : 1;
     const dim3 grid(static_cast<unsigned>((n_req * a.units + 7) / 8), p->n_heads, k_out && v_out ? 2 : 1);
-    const bool i8 = p->format == FKV_INT8;
-    switch (dtype) {
-    case FKV_F32:
-        return i8 ? read_as<FKV_INT8, float>(a, p->dim, grid, st) : read_as<FKV_E4M3, float>(a, p->dim, grid, st);
-    case FKV_F16:
-        return i8 ? read_as<FKV_INT8, __half>(a, p->dim, grid, st) : read_as<FKV_E4M3, __half>(a, p->dim, grid, st);
-    default:
-        return i8 ? read_as<FKV_INT8, __nv_bfloat16>(a, p->dim, grid, st)
-                  : read_as<FKV_E4M3, __nv_bfloat16>(a, p->dim, grid, st);
-    }
+    return p->format == FKV_UINT4  ? read_type<FKV_UINT4>(a, p->dim, dtype, grid, st)
+           : p->format == FKV_INT8 ? read_type<FKV_INT8>(a, p->dim, dtype, grid, st)
+                                   : read_type<FKV_E4M3>(a, p->dim, dtype, grid, st);
 }
