@@ -238,6 +238,7 @@ class Pages:
             raise ValueError("k_scale and v_scale must be float32 tensors [blocks, heads] of the same strides")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_blocks, self.heads, self.block, self.dim = k.shape
+        self.four = four                         # 4-bit codes
         if four:
             self.dim *= 2
         else:
@@ -682,7 +683,7 @@ class Context:
             window, sinks, qd, Hq, causal, dim ** -0.5 if scale is None else scale, softcap, 0)
         L = lib()
         # the workspace's size depends on these alone, in a call that is not refused
-        key = (T, Hq, n, max_new, max_len, window, sinks, prefix is None, pages.heads, dim)
+        key = (T, Hq, n, max_new, max_len, window, sinks, prefix is None, pages.heads, dim, pages.four)
         need = self._attend_need.get(key)
         if need is None:
             need = L.fkv_page_attend_workspace(self._h, buf)

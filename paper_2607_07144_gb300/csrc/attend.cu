@@ -16,45 +16,11 @@
 // 2^-32 of the largest weight is lost), and the sum of the weights is
 // sum P_j / vs, from the unrounded P_j, in fp32 (share_of).  So pages of any
 // scales mix in one accumulator without a rounding of V.
-#include "attend.cuh"
+#include "attend_step.cuh"
 
 using namespace fkvd;
 
 namespace {
-
-constexpr float kPBits = 8.0f;     // P is at most 2^8
-constexpr int kMaxCluster = 8;     // blocks of a portable cluster
-
-__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3,
-                                            uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-    return v;
-}
-
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-    return v;
-}
 
 // ------------------------------------------------------------------ steps --
 // Up to 8 NT rows (the query heads of a KV head, times the new tokens) against a
@@ -80,42 +46,6 @@ template <int D, int NT> struct StepShape {
     static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0, ml = 4 * 2 * 8 * NT * 4;
     static constexpr int smem = ring + q + ml + 1024;
 };
-
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// The same place in the shared memory of the cluster's block `rank`.
-__device__ __forceinline__ uint32_t in_cluster(const float *p, int rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ float ld_cluster(const float *p, int rank)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cluster(p, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 ld_cluster4(const float *p, int rank)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(in_cluster(p, rank))
-                 : "memory");
-    return v;
-}
-
-__device__ __forceinline__ uint32_t transpose8(uint32_t x)
-{
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
 
 template <int D, int FMT, typename T, int NT>
 __global__ void __launch_bounds__(128, 3)
@@ -509,131 +439,7 @@ __global__ void __launch_bounds__(128, 3)
         __syncwarp();                  // the stage is free: the next issue may overwrite it
     }
 
-    // merge the warps: a row's largest m, then sums and outputs against it
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float x = l[n][c];
-            x += __shfl_xor_sync(~0u, x, 4);
-            x += __shfl_xor_sync(~0u, x, 8);
-            x += __shfl_xor_sync(~0u, x, 16);
-            if (gid == 0) {
-                ml[warp][0][8 * n + 2 * t + c] = m[n][c];
-                ml[warp][1][8 * n + 2 * t + c] = x;
-            }
-        }
-    if (bad)
-        atomicOr(a.status, FKV_ST_RANGE);
-    __syncthreads();                   // every ring is read: its memory takes the outputs
-    float *mo = reinterpret_cast<float *>(base);
-    constexpr int LD = D + 4;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float *dst = mo + (warp * R + 8 * n + 2 * t + c) * LD + gid * (D / 8);
-#pragma unroll
-            for (int d = 0; d < MO; ++d)
-                *reinterpret_cast<float2 *>(dst + 2 * d) = make_float2(o[n][d][c], o[n][d][2 + c]);
-        }
-    __syncthreads();
-    constexpr int TPR = 128 / R, E = D / TPR;      // threads a row, dimensions a thread
-    const int row = tid / TPR, c = (tid % TPR) * E;
-    const bool live = row0 + row < rows;
-    if (!live && !a.cluster)
-        return;
-    float mt = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-        mt = fmaxf(mt, ml[w][0][row]);
-    const float mref = mt == -INFINITY ? 0.0f : mt;
-    float lt = 0.0f, f[4];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float half = ex2(0.5f * (ml[w][0][row] - mref));
-        f[w] = half * half;
-        lt += ml[w][1][row] * half * half;
-    }
-    float inv = lt != 0.0f ? kRef / lt : 0.0f;
-    float lse2 = lt != 0.0f ? mref - kPBits + log2f(lt) - kLog2Ref : -INFINITY;
-    const int i = live ? static_cast<int>(a.gdiv.div(row0 + row)) : 0;
-    const int64_t tok = q.tok0 + i, head = h * a.G + (live ? row0 + row - i * a.G : 0), flat = tok * (a.H * a.G) + head;
-    float x[E];
-#pragma unroll
-    for (int k = 0; k < E; ++k)
-        x[k] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int k = 0; k < E; k += 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(mo + (w * R + row) * LD + c + k);
-            x[k] = fmaf(v.x, f[w], x[k]), x[k + 1] = fmaf(v.y, f[w], x[k + 1]);
-            x[k + 2] = fmaf(v.z, f[w], x[k + 2]), x[k + 3] = fmaf(v.w, f[w], x[k + 3]);
-        }
-    if (a.cluster) {
-        // the shares of a row meet in their cluster's shared memory: every block
-        // leaves its rows there, and the blocks take every splits-th row
-        float *const part = mo + 4 * R * LD, *const part_lse = part + R * D;
-#pragma unroll
-        for (int k = 0; k < E; k += 4)
-            *reinterpret_cast<float4 *>(part + row * D + c + k) = make_float4(x[k] * inv, x[k + 1] * inv, x[k + 2] * inv, x[k + 3] * inv);
-        if (c == 0)
-            part_lse[row] = lse2;
-        cluster_sync();
-        const bool mine = live && row % a.splits == split;
-        if (mine) {
-            float most = -INFINITY, sum = 0.0f, l_s[kMaxCluster];
-#pragma unroll
-            for (int s = 0; s < kMaxCluster; ++s) {
-                l_s[s] = s < a.splits ? ld_cluster(part_lse + row, s) : -INFINITY;
-                most = fmaxf(most, l_s[s]);
-            }
-            const float ref = most == -INFINITY ? 0.0f : most;
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-                x[k] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < kMaxCluster; ++s) {
-                if (s >= a.splits)
-                    break;
-                const float w = ex2(l_s[s] - ref);
-                sum += w;
-#pragma unroll
-                for (int k = 0; k < E; k += 4) {
-                    const float4 v = ld_cluster4(part + row * D + c + k, s);
-                    x[k] = fmaf(v.x, w, x[k]), x[k + 1] = fmaf(v.y, w, x[k + 1]);
-                    x[k + 2] = fmaf(v.z, w, x[k + 2]), x[k + 3] = fmaf(v.w, w, x[k + 3]);
-                }
-            }
-            inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-            lse2 = sum != 0.0f ? ref + log2f(sum) : -INFINITY;
-        }
-        cluster_sync();                // no block's memory goes before the others have read it
-        if (!mine)
-            return;
-    }
-    if (a.splits == 1 || a.cluster) {
-        T *dst = static_cast<T *>(a.out) + tok * a.o_tok + head * a.o_head + c;
-#pragma unroll
-        for (int k = 0; k < E; k += 4) {
-            T y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                y[e] = from_float<T>(x[k + e] * inv);
-            *reinterpret_cast<uint2 *>(dst + k) = *reinterpret_cast<const uint2 *>(y);
-        }
-        if (a.lse && c == 0)
-            a.lse[flat] = lse2 / kLog2e;
-    } else {
-        const int64_t at = split * a.T * (a.H * a.G) + flat;
-#pragma unroll
-        for (int k = 0; k < E; k += 4)
-            *reinterpret_cast<float4 *>(a.ws_o + at * D + c + k) =
-                make_float4(x[k] * inv, x[k + 1] * inv, x[k + 2] * inv, x[k + 3] * inv);
-        if (c == 0)
-            a.ws_lse[at] = lse2;
-    }
+    finish_rows<D, T, NT>(a, q, base, ml, m, l, o, h, split, row0, rows, bad);
 }
 
 // --------------------------------------------------------------- combine --
@@ -737,7 +543,7 @@ Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
     Plan p;
     const int H = c.pages->n_heads, G = c.n_q_heads / H, window = window_of(c);
     const int64_t most = c.max_new * G;
-    p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
+    p.nt = most <= 8 ? 1 : most <= 32 || c.pages->format == FKV_UINT4 ? 2 : 0;
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
     const int64_t blocks = c.n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
@@ -800,6 +606,15 @@ cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUten
     return launch_after(k_attend_combine<D, T>, static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st, a);
 }
 
+template <int D, typename T>
+cudaError_t step4_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+{
+    const cudaError_t e = launch_attend_step4(ctx, a, D, std::is_same<T, __half>::value ? FKV_F16 : FKV_BF16, nt, mk, mv, st);
+    if (e != cudaSuccess || a.splits == 1 || a.cluster)
+        return e;
+    return launch_after(k_attend_combine<D, T>, static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st, a);
+}
+
 template <int D, int FMT>
 cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, const CUtensorMap &mk, const CUtensorMap &mv,
                     cudaStream_t st)
@@ -846,6 +661,11 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws
     a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk, a.cluster = p.cluster;
     a.ws_o = static_cast<float *>(ws);
     a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * pg->dim : nullptr;
+    if (pg->format == FKV_UINT4) {
+        if (pg->dim == 64)
+            return c.dtype == FKV_F16 ? step4_as<64, __half>(ctx, a, p.nt, mk, mv, st) : step4_as<64, __nv_bfloat16>(ctx, a, p.nt, mk, mv, st);
+        return c.dtype == FKV_F16 ? step4_as<128, __half>(ctx, a, p.nt, mk, mv, st) : step4_as<128, __nv_bfloat16>(ctx, a, p.nt, mk, mv, st);
+    }
     const bool i8 = pg->format == FKV_INT8;
     if (pg->dim == 64)
         return i8 ? step_dt<64, FKV_INT8>(ctx, a, c.dtype, p.nt, mk, mv, st) : step_dt<64, FKV_E4M3>(ctx, a, c.dtype, p.nt, mk, mv, st);

@@ -149,6 +149,9 @@ __device__ __forceinline__ float share_of(float vs) { return __fdividef(kRef, vs
 
 }  // namespace fkvd
 
+// Over 4-bit pages (attend4.cu): nt tiles of 8 rows a block.
+cudaError_t launch_attend_step4(const fkv_ctx *ctx, const fkvd::AttendArgs &a, int dim, int dtype, int nt, const CUtensorMap &mk,
+                                const CUtensorMap &mv, cudaStream_t st);
 // Rows of 256 (attend_prompt.cu): a.row_tiles, splits and chunk as for the steps.
 int prompt_rows();
 cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const fkvd::AttendArgs &a, int dim, int format, int dtype,

@@ -1,0 +1,505 @@
+// Attention over 4-bit pages for a few rows a KV head (attend.cu has the mathematics
+// of the 8-bit ones and the plan).
+//
+// Key j is mid_j + (c_j - 7.5) step_j and value j mid'_j + (c'_j - 7.5) step'_j, with
+// numbers of their own for every row of a page.  So
+//     q.k_j = step_j (q.c_j - 7.5 sum q) + mid_j sum q,
+// one multiplication and two additions a score behind the product of the query with
+// whole numbers, and with
+//     y_j = x_j log2 e + log2 step'_j,   P_j = 2^(y_j - m + 8),   m = max y_j
+// the row's output is
+//     (sum P_j (c'_j - 7.5) + sum P_j mid'_j / step'_j) / sum P_j / step'_j,
+// the first sum on the tensor cores with P rounded to fp16 (as for 8-bit pages), the
+// others of unrounded weights in fp32.  sum P_j 7.5, of the rounded weights as the
+// product with c' has them, is one more row of that product, of ones.
+//
+// A code needs no conversion: as the low four bits of an fp16 number it is the
+// subnormal c 2^-24, and one place to the left c 2^-20.  A word of eight codes is four
+// operands of two after four masks and a shift; the factor 16 between neighbours is
+// taken out of the query for K and of the output for V, both exactly but for elements
+// of a query below 2^-25 of its largest (rounded to 2^-35 of that).
+#include "attend_step.cuh"
+
+using namespace fkvd;
+
+namespace {
+
+// As k_attend_step: four warps, each with every fourth group of 32 keys, a ring of
+// its own filled by TMA and a softmax of its own; keys are the rows of the first
+// product, dimensions those of the second, query rows their 8 columns.
+template <int D, int NT> struct Step4Shape {
+    static constexpr int stages = D == 128 ? 3 : 4;
+    static constexpr int unit = 8 * D;                          // 16 keys' codes
+    static constexpr int numbers = 4 * unit, stage = (4 * unit + 4 * 64 + 511) / 512 * 512;
+    static constexpr int ring = 4 * stages * stage;
+    static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0;  // the query operands, [column tile][step][lane]
+    static constexpr int keys = 4 * 32 * 16;                    // a warp's keys' numbers
+    static constexpr int ml = 4 * 2 * 8 * NT * 4;
+    static constexpr int smem = ring + q + keys + ml + 1024;
+};
+
+// Contiguous bytes into shared memory, 16-byte aligned and a multiple of 16 of them.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, int bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Eight codes as four fp16 pairs: (c0, c4) and (c2, c6) times 2^-24, (c1, c5) and
+// (c3, c7) times 2^-20.
+__device__ __forceinline__ void codes8_pairs(uint32_t w, uint32_t *f)
+{
+    const uint32_t x = w >> 8;
+    f[0] = w & 0x000f000fu, f[1] = w & 0x00f000f0u;
+    f[2] = x & 0x000f000fu, f[3] = x & 0x00f000f0u;
+}
+
+template <int D, typename T, int NT>
+__global__ void __launch_bounds__(128, 3)
+    k_attend_step4(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
+{
+    using S = Step4Shape<D, NT>;
+    constexpr int ST = S::stages, W = D / 32, MO = D / 16, R = 8 * NT;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[4 * ST];
+    __shared__ Seen rows_see[4];                 // a warp's own: registers are short
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
+    const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
+    uint8_t *const base = raw + (sbase - smem_u32(raw));
+    uint2 *const q_s = reinterpret_cast<uint2 *>(base + S::ring);
+    float4 *const keys_s = reinterpret_cast<float4 *>(base + S::ring + S::q) + 32 * warp;
+    typedef float RowPair[2][R];                 // a warp's maxima and sums
+    RowPair *const ml = reinterpret_cast<RowPair *>(base + S::ring + S::q + S::keys);
+
+    const int h = blockIdx.y;
+    const int split = blockIdx.x % a.splits, rr = blockIdx.x / a.splits;
+    const int rt = rr % a.row_tiles, r = rr / a.row_tiles;
+    Request q;
+    if (!q.load(a, r)) {
+        if (tid == 0)
+            atomicOr(a.status, FKV_ST_RANGE);
+        return;
+    }
+    const int rows = q.nq * a.G, row0 = rt * R;
+    if (row0 >= rows)
+        return;
+    const int ia = static_cast<int>(a.gdiv.div(row0)), ib = static_cast<int>(a.gdiv.div(min(row0 + R - 1, rows - 1)));
+    const int pa = q.p0 + ia, pb = q.p0 + ib;
+    const Tiles tiles(a, q, pa, pb);
+    const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk);
+    // the last tile may end before this warp's keys
+    const int n_it = max(0, i1 - i0) - (i1 > i0 && tiles.at(i1 - 1) * kTile + warp * 32 >= tiles.lim);
+    const bool back = a.slopes != nullptr;       // (see k_attend_step)
+    auto tile_at = [&](int it) { return tiles.at(i0 + (back ? n_it - 1 - it : it)); };
+
+    const uint32_t ring = sbase + warp * ST * S::stage, bar0 = smem_u32(bars) + warp * ST * 8;
+    if (lane == 0) {
+        rows_see[warp] = tiles.seen;
+        for (int s = 0; s < ST; ++s)
+            mbar_init(bar0 + 8 * s, 1);
+        fence_mbar_init();
+    }
+    __syncwarp();
+
+    // A lane looks up the page of one of the 32 units (16 keys) of 16 iterations, a
+    // batch of iterations ahead, if any row sees one of its keys.
+    bool bad = false;
+    struct Unit {
+        int id;
+        unsigned all;                  // which of the 32 units are looked at
+    };
+    auto key_of = [&](int batch) { return tile_at(batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
+    auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && rows_see[warp].of(key_of(batch)); };
+    auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
+    auto check = [&](int batch, int id) {
+        const bool mine = on(batch);
+        Unit u = {0, __ballot_sync(~0u, mine)};
+        if (mine) {
+            if (id < 0 || id >= a.n_blocks)
+                bad = true;
+            else
+                u.id = id;
+        }
+        return u;
+    };
+    Unit cur = check(0, ask(0)), nxt = check(1, ask(1));
+    int nid = ask(2);
+    auto first_key = [&](int it) { return tile_at(it) * kTile + warp * 32; };
+    auto issue = [&](int it, int batch) {
+        const int from = (it & 15) * 2 + (lane & 1);
+        const bool now = (it >> 4) == batch;
+        const unsigned units = (now ? cur.all : nxt.all) >> ((it & 15) * 2) & 3;
+        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, from);
+        const int key = first_key(it) + (lane & 1) * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
+        const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * S::stage;
+        // (without any the arrival alone completes the phase)
+        if (lane == 0)
+            mbar_arrive_expect_tx(bar, __popc(units) * 2 * (S::unit + 64));
+        __syncwarp();
+        // lanes 0 .. 3: codes of units 0 and 1 of K, then of V; 4 .. 7: their numbers
+        if (lane < 8 && (units >> (lane & 1) & 1)) {
+            if (lane < 4)
+                tma_load_4d(dst + lane * S::unit, lane < 2 ? &mk : &mv, 0, off, h, static_cast<int>(id), bar);
+            else
+                bulk_load(dst + S::numbers + (lane - 4) * 64, (lane < 6 ? a.ks : a.vs) + id * a.scb + h * a.sch + off, 64, bar);
+        }
+        __syncwarp();
+    };
+    for (int it = 0; it < min(ST - 1, n_it); ++it)
+        issue(it, 0);
+
+    // The query rows as fp16 operands: lane t's steps take D / 4 consecutive dimensions
+    // of row gid, brought to [2^14, 2^15) by a power of two, eight at a time in the order
+    // of codes8_pairs.
+    const float mul0 = score_multiplier(a, a.scale);
+    uint32_t qf[NT > 1 ? 1 : 2 * W][2];
+    float rowmul[NT][2], rowsum[NT][2], start[NT][2], slope[NT][2];
+    int prow[NT][2], hi[NT][2], from[NT][2], pre[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + 8 * n + gid;
+        const bool live = row < rows;
+        const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
+        const T *src = static_cast<const T *>(a.q) + (q.tok0 + i) * a.q_tok + (h * a.G + u) * a.q_head + t * (D / 4);
+        float x[W][8];
+        float amax = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (live)
+                v = reinterpret_cast<const uint4 *>(src)[w];
+            const T *y = reinterpret_cast<const T *>(&v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                x[w][k] = static_cast<float>(y[k]);
+                amax = fmaxf(amax, fabsf(x[w][k]));
+            }
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
+        const int e = max(static_cast<int>(__float_as_uint(amax) >> 23) - 127, -100);
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e) << 23);
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e) << 23);
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                x[w][k] *= up;
+                sum += x[w][k];
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t f0 = pack_half(x[w][2 * s], x[w][2 * s + 4]);
+                const uint32_t f1 = pack_half(x[w][2 * s + 1] * 0.0625f, x[w][2 * s + 5] * 0.0625f);
+                if (NT > 1) {
+                    if (warp == n % 4)
+                        q_s[(n * 2 * W + 2 * w + s) * 32 + lane] = make_uint2(f0, f1);
+                } else {
+                    qf[2 * w + s][0] = f0, qf[2 * w + s][1] = f1;
+                }
+            }
+        }
+        sum += __shfl_xor_sync(~0u, sum, 1);
+        sum += __shfl_xor_sync(~0u, sum, 2);
+        // a lane's scores are of rows 2t and 2t + 1: what a product (in 2^-24) and the sum of
+        // the query are multiplied by beside step and middle, and where a product starts
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const float by = __shfl_sync(~0u, down, (2 * t + c) * 4) * mul0, all = __shfl_sync(~0u, sum, (2 * t + c) * 4);
+            rowmul[n][c] = by * 0x1p24f, rowsum[n][c] = by * all, start[n][c] = -7.5f * 0x1p-24f * all;
+            const int rw = row0 + 8 * n + 2 * t + c;
+            const bool live_c = rw < rows;
+            const int ii = live_c ? static_cast<int>(a.gdiv.div(rw)) : 0;
+            prow[n][c] = q.p0 + ii;
+            slope[n][c] = a.slopes && live_c ? a.slopes[h * a.G + rw - ii * a.G] * kLog2e : 0.0f;
+            const RowMask m(a, q, prow[n][c], live_c);
+            hi[n][c] = m.hi, from[n][c] = m.from, pre[n][c] = m.pre;
+        }
+    }
+
+    if (NT > 1)
+        __syncthreads();
+
+    // outputs (even dimensions in 2^-24, odd ones in 2^-20); the sums of the rounded weights
+    // in p (all four of its values), of weights over steps and of weights' middles
+    float o[NT][MO][4], p_sum[NT][4];
+    float m[NT][2], l[NT][2], mid[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int d = 0; d < MO; ++d)
+            o[n][d][0] = o[n][d][1] = o[n][d][2] = o[n][d][3] = 0.0f;
+        p_sum[n][0] = p_sum[n][1] = p_sum[n][2] = p_sum[n][3] = 0.0f;
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = mid[n][0] = mid[n][1] = 0.0f;
+    }
+    const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+
+    int batch = 0;
+    for (int it = 0; it < n_it; ++it) {
+        if ((it >> 4) != batch) {
+            batch = it >> 4;
+            cur = nxt;
+            nxt = check(batch + 1, nid);
+            nid = ask(batch + 2);
+        }
+        if (it + ST - 1 < n_it)
+            issue(it + ST - 1, batch);
+        const int key = first_key(it);
+        const unsigned units = cur.all >> ((it & 15) * 2) & 3;
+        // (a lane that gives up takes its warp along: the others would meet it nowhere)
+        if (!__all_sync(~0u, mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status))) {
+            // give the loads in flight a while to land before the memory is used again
+            for (int k = it + 1; k < min(n_it, it + ST); ++k)
+                mbar_wait(bar0 + 8 * (k % ST), (k / ST) & 1, a.status, 2000000);
+            __syncwarp();
+            break;
+        }
+        if (units == 0)
+            continue;                  // keys between the first ones and the window
+        const uint32_t kt = ring + (it % ST) * S::stage, vt = kt + 2 * S::unit;
+
+        // a lane a key: its numbers, and what its value's step gives its weights.  Those of
+        // keys behind the request's end, or that were not loaded, may be anything.
+        {
+            const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (kt - sbase) + S::numbers) + lane;
+            uint32_t kn = num[0], vn = num[32];
+            if (!(units >> (lane >> 4) & 1) || key + lane >= q.len)
+                kn = vn = 0;
+            const float vs = value_scale(__uint_as_float(vn << 16));
+            keys_s[lane] = make_float4(__uint_as_float(kn), __uint_as_float(vn), lg2(vs), share_of(vs));
+        }
+
+        float sc[2][NT][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                sc[u][n][0] = sc[u][n][2] = start[n][0], sc[u][n][1] = sc[u][n][3] = start[n][1];
+        // both units' keys gid and gid + 8; a unit that was not loaded gives
+        // products of any codes, which no row sees
+        uint32_t kw[2][2][W];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int kr = 16 * u + gid + 8 * x;
+                if (D == 128) {
+                    const uint4 v = lds128(kt + kr * 64 + ((t ^ ((kr >> 1) & 3)) << 4));
+                    kw[u][x][0] = v.x, kw[u][x][1] = v.y;
+                    kw[u][x][W - 2] = v.z, kw[u][x][W - 1] = v.w;
+                } else {
+                    const uint2 v = lds64(kt + kr * 32 + t * 8);
+                    kw[u][x][0] = v.x, kw[u][x][1] = v.y;
+                }
+            }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            uint32_t f[2][2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    codes8_pairs(kw[u][x][w], f[u][x]);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint2 qv;
+                    if (NT > 1)
+                        qv = q_s[(n * 2 * W + 2 * w + s) * 32 + lane];
+                    else
+                        qv = make_uint2(qf[2 * w + s][0], qf[2 * w + s][1]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t g[4] = {f[u][0][2 * s], f[u][1][2 * s], f[u][0][2 * s + 1], f[u][1][2 * s + 1]};
+                        mma16816(sc[u][n], g, qv.x, qv.y);
+                    }
+                }
+        }
+
+        // scores in base 2 with the logarithms of the values' steps
+        __syncwarp();                  // keys_s
+        float mx[NT][2], share[2][2], vmid[2][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            mx[n][0] = mx[n][1] = -INFINITY;
+        const bool full = all_see(a, q, pa, pb, key, key + 32);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float4 num = keys_s[16 * u + gid + 8 * x];
+                const float step = __uint_as_float(__float_as_uint(num.x) << 16), kmid = __uint_as_float(__float_as_uint(num.x) & 0xffff0000u);
+                vmid[u][x] = __uint_as_float(__float_as_uint(num.y) & 0xffff0000u);
+                const float lvs = num.z;
+                share[u][x] = num.w;
+                const int j = key + 16 * u + gid + 8 * x;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float &s = sc[u][n][2 * x + c];
+                        const float mul = step * rowmul[n][c];
+                        float y;
+                        if (a.softcap > 0.0f) {
+                            y = fmaf(s, mul, kmid * rowsum[n][c]);
+                            if (plain_cap(a))
+                                y = fmaf(-2.0f * a.cap2, __fdividef(1.0f, 1.0f + ex2(y)), a.cap2 + lvs);
+                            else
+                                y = capped(a, y) + lvs;
+                        } else {
+                            y = fmaf(s, mul, fmaf(kmid, rowsum[n][c], lvs));
+                        }
+                        if (a.slopes)
+                            y = fmaf(slope[n][c], static_cast<float>(j - prow[n][c]), y);
+                        if (!full) {
+                            const bool see = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c];
+                            y = see ? y : -INFINITY;
+                        }
+                        s = y;
+                        mx[n][c] = fmaxf(mx[n][c], y);
+                    }
+            }
+        bool grown = false;
+        float mref[NT][2], by[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float x = mx[n][c];
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                const float mn = fmaxf(m[n][c], x);
+                grown |= mn != m[n][c];
+                mref[n][c] = (mn == -INFINITY ? 0.0f : mn) - kPBits;
+                by[n][c] = m[n][c] - kPBits - mref[n][c];
+                m[n][c] = mn;
+            }
+        if (__any_sync(~0u, grown)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    // sums of weights over steps are scaled in two halves: counted up to 2^80 a
+                    // weight (share_of), they outlast factors below float32's least
+                    const float half = ex2(0.5f * by[n][c]), f = half * half;
+                    l[n][c] = l[n][c] * half * half, mid[n][c] = mid[n][c] * half * half;
+                    p_sum[n][c] *= f, p_sum[n][2 + c] *= f;
+#pragma unroll
+                    for (int d = 0; d < MO; ++d)
+                        o[n][d][c] *= f, o[n][d][2 + c] *= f;
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (!(units >> u & 1))
+                continue;
+            uint32_t pf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    float p[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        p[c] = ex2(sc[u][n][2 * x + c] - mref[n][c]);
+                        const float w = p[c] * share[u][x];
+                        l[n][c] += w;
+                        mid[n][c] = fmaf(w, vmid[u][x], mid[n][c]);
+                    }
+                    pf[n][x] = transpose8(pack_half(p[0], p[1]));
+                }
+                mma16816(p_sum[n], ones, pf[n][0], pf[n][1]);
+            }
+            // value rows 2t, 2t + 1, 2t + 8, 2t + 9 of the unit, D / 8 dimensions each
+            uint32_t w[4][D / 64];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int row = 16 * u + 2 * t + (x & 1) + 8 * (x >> 1);
+                if (D == 128) {
+                    const uint2 v = lds64(vt + row * 64 + ((((gid >> 1) ^ ((row >> 1) & 3)) << 4) | (gid & 1) << 3));
+                    w[x][0] = v.x, w[x][D / 64 - 1] = v.y;
+                } else {
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[x][0]) : "r"(vt + row * 32 + gid * 4));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < D / 64; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // rows gid and gid + 8 of two tiles: dimensions 8k + 4e and the next, and the two behind
+                    const int sel = e ? 0x7632 : 0x5410;
+                    uint32_t f0[4], f1[4];
+                    codes8_pairs(__byte_perm(w[0][k], w[1][k], sel), f0);
+                    codes8_pairs(__byte_perm(w[2][k], w[3][k], sel), f1);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t f[4] = {f0[2 * y], f0[2 * y + 1], f1[2 * y], f1[2 * y + 1]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma16816(o[n][4 * k + 2 * e + y], f, pf[n][0], pf[n][1]);
+                    }
+                }
+        }
+        __syncwarp();                  // the stage is free: the next issue may overwrite it
+    }
+
+    // outputs in units of one, with the middles
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float x = mid[n][c];
+            x += __shfl_xor_sync(~0u, x, 4);
+            x += __shfl_xor_sync(~0u, x, 8);
+            x += __shfl_xor_sync(~0u, x, 16);
+            // (middles count as weights do, by kRef)
+            const float add = fmaf(-7.5f, p_sum[n][c], x * (1.0f / kRef));
+#pragma unroll
+            for (int d = 0; d < MO; ++d) {
+                o[n][d][c] = fmaf(o[n][d][c], 0x1p24f, add);
+                o[n][d][2 + c] = fmaf(o[n][d][2 + c], 0x1p20f, add);
+            }
+        }
+    finish_rows<D, T, NT>(a, q, base, ml, m, l, o, h, split, row0, rows, bad);
+}
+
+template <int D, typename T, int NT>
+cudaError_t step4_rows(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+{
+    constexpr int smem = Step4Shape<D, NT>::smem;
+    // the block's end takes the rings' place: the warps' outputs, and a cluster's shares
+    static_assert(4 * 8 * NT * (D + 4) * 4 + 8 * NT * (D + 1) * 4 <= Step4Shape<D, NT>::ring, "the ring holds the outputs");
+    const void *fn = reinterpret_cast<const void *>(k_attend_step4<D, T, NT>);
+    const cudaError_t e = kernel_use(ctx, fn, 128, smem, nullptr);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = a.cluster ? a.splits : 1, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_req * a.row_tiles * a.splits), a.H), cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = smem, cfg.stream = st;
+    cfg.attrs = &at, cfg.numAttrs = a.cluster ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, k_attend_step4<D, T, NT>, a, mk, mv);
+}
+
+template <int D, typename T>
+cudaError_t step4_nt(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
+{
+    return nt == 1 ? step4_rows<D, T, 1>(ctx, a, mk, mv, st) : step4_rows<D, T, 2>(ctx, a, mk, mv, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_step4(const fkv_ctx *ctx, const AttendArgs &a, int dim, int dtype, int nt, const CUtensorMap &mk,
+                                const CUtensorMap &mv, cudaStream_t st)
+{
+    if (dim == 64)
+        return dtype == FKV_F16 ? step4_nt<64, __half>(ctx, a, nt, mk, mv, st) : step4_nt<64, __nv_bfloat16>(ctx, a, nt, mk, mv, st);
+    return dtype == FKV_F16 ? step4_nt<128, __half>(ctx, a, nt, mk, mv, st) : step4_nt<128, __nv_bfloat16>(ctx, a, nt, mk, mv, st);
+}

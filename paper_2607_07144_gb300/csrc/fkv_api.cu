@@ -1086,8 +1086,6 @@ const char *check_attend_sizes(const fkv_attend *a)
     if (a->n_tok < 0 || a->n_tok > INT32_MAX || a->n_req < 0 || a->n_req > FKV_PAGE_MAX_REQ || a->max_new < 0 ||
         a->max_new > FKV_PAGE_MAX_LEN || a->max_len < 0 || a->max_len > FKV_PAGE_MAX_LEN || a->window < 0 || a->sinks < 0)
         return "size out of range";
-    if (a->pages->format == FKV_UINT4)
-        return "no attention over 4-bit pages";
     const int H = a->pages->n_heads;
     if (a->n_q_heads < H || a->n_q_heads % H || a->n_q_heads > 65535)
         return "query heads must be a multiple of the pages' heads";
@@ -1119,11 +1117,11 @@ const char *check_attend(const fkv_attend *a)
     return check_table(a->n_req, a->table, a->table_stride, a->width);
 }
 
-// The pool as [page][head][position][dim] bytes, in boxes of 16 positions of
-// one head whose rows are swizzled by their own width.
+// The pool as [page][head][position][row] bytes, in boxes of 16 positions of one
+// head whose rows are swizzled by their own width (those of 32 bytes are not).
 bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *map)
 {
-    const cuuint64_t D = static_cast<cuuint64_t>(p->dim);
+    const cuuint64_t D = static_cast<cuuint64_t>(p->format == FKV_UINT4 ? p->dim / 2 : p->dim);
     const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(p->block), static_cast<cuuint64_t>(p->n_heads),
                                 static_cast<cuuint64_t>(p->n_blocks)};
     // the stride of a dimension of one is never used, but has to be a valid one
@@ -1132,7 +1130,9 @@ bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *ma
                                    p->n_blocks > 1 ? static_cast<cuuint64_t>(p->stride_block) : D};
     const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), 16, 1, 1}, estr[4] = {1, 1, 1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               p->dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+               D == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+               : D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                         : CU_TENSOR_MAP_SWIZZLE_NONE,
                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
