@@ -18,7 +18,10 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfkv.so")
 INCLUDE = os.path.join(ROOT, "include")
-SOURCES = ["fkv_api.cu", "codec.cu", "rvq.cu", "gather.cu", "decode_static.cu", "ac.cu", "paged.cu", "append.cu", "attend.cu", "attend4.cu", "attend_prompt.cu"]
+SOURCES = ["fkv_api.cu", "codec.cu", "rvq.cu", "gather.cu", "decode_static.cu", "ac.cu", "paged.cu", "append.cu", "attend.cu",
+           "attend4.cu", "attend_prompt.cu"]
+# sources compiled once more, with a macro, to an object of their own
+VARIANTS = [("attend_prompt.cu", "FKV_PAGES_4BIT", "attend_prompt4.o")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -47,22 +50,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
     headers.append(os.path.join(INCLUDE, "fkv.h"))
     objs = []
     jobs = []
-    for src in SOURCES:
+    for src, macro, obj in [(src, None, src.replace(".cu", ".o")) for src in SOURCES] + VARIANTS:
         s = os.path.join(CSRC, src)
-        o = os.path.join(BUILD, src.replace(".cu", ".o"))
+        o = os.path.join(BUILD, obj)
         objs.append(o)
         if force or _stale(o, [s] + headers):
-            jobs.append((s, o))
+            jobs.append((s, o, ["-D" + macro] if macro else []))
 
     def compile_one(job):
-        s, o = job
-        cmd = [nvcc()] + _flags() + ["-c", s, "-o", o]
+        s, o, more = job
+        cmd = [nvcc()] + _flags() + more + ["-c", s, "-o", o]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("nvcc failed for %s:\n%s%s" % (s, r.stdout, r.stderr))
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(VARIANTS)) as ex:
         for log in ex.map(compile_one, jobs):
             if verbose and log:
                 sys.stderr.write(log)

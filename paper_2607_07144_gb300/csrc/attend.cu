@@ -543,7 +543,7 @@ Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
     Plan p;
     const int H = c.pages->n_heads, G = c.n_q_heads / H, window = window_of(c);
     const int64_t most = c.max_new * G;
-    p.nt = most <= 8 ? 1 : most <= 32 || c.pages->format == FKV_UINT4 ? 2 : 0;
+    p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
     const int64_t blocks = c.n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
@@ -609,7 +609,8 @@ cudaError_t step_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUten
 template <int D, typename T>
 cudaError_t step4_as(const fkv_ctx *ctx, const AttendArgs &a, int nt, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
-    const cudaError_t e = launch_attend_step4(ctx, a, D, std::is_same<T, __half>::value ? FKV_F16 : FKV_BF16, nt, mk, mv, st);
+    const int dtype = std::is_same<T, __half>::value ? FKV_F16 : FKV_BF16;
+    const cudaError_t e = nt == 0 ? launch_attend_prompt4(ctx, a, D, dtype, st) : launch_attend_step4(ctx, a, D, dtype, nt, mk, mv, st);
     if (e != cudaSuccess || a.splits == 1 || a.cluster)
         return e;
     return launch_after(k_attend_combine<D, T>, static_cast<unsigned>(a.T * a.H * a.G), 128, 0, st, a);

@@ -156,3 +156,4 @@ cudaError_t launch_attend_step4(const fkv_ctx *ctx, const fkvd::AttendArgs &a, i
 int prompt_rows();
 cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const fkvd::AttendArgs &a, int dim, int format, int dtype,
                                  cudaStream_t st);
+cudaError_t launch_attend_prompt4(const fkv_ctx *ctx, const fkvd::AttendArgs &a, int dim, int dtype, cudaStream_t st);

@@ -1,5 +1,5 @@
-// Attention over the paged 8-bit cache for many rows a KV head (attend.cu has the
-// mathematics): both products on the 5th-generation tensor cores.
+// Attention over the paged 8- and 4-bit cache for many rows a KV head (attend.cu has
+// the mathematics): both products on the 5th-generation tensor cores.
 //
 // A block takes 256 rows of one KV head (its query heads, times new tokens) and
 // walks its share of the keys in tiles of 128.  Four warps load the pages' codes
@@ -20,6 +20,15 @@
 // and product (3.5k cycles a tile, of which the products of both groups are 2.1k).
 // 13 prompts of 1 to 1,000 tokens, 12 heads of 64: 39 us, bound by the start and
 // the end of a block.
+//
+// 4-bit pages: a code less 7.5 is exact in fp16 and is what K's tile holds; the key's
+// own step and middle come to the product in fp32, two fused operations a score on
+// numbers of the keys in shared memory (attend4.cu has the formula).  V's tile holds
+// values, middle + (c - 7.5) step, over the power of two that brings the largest of 16
+// keys' to [2^14, 2^15): rounded to fp16 once, half a step (2^-11) of the value down to
+// 2^-29 of the largest, what the weights are rounded to as well; that power is the unit's
+// value scale.  Eight codes of a word lie in a tile in the order 0 4 1 5 2 6 3 7, as masks
+// give them two at a time; so do the queries' elements, and the outputs' are put back.
 #include "attend.cuh"
 
 using namespace fkvd;
@@ -33,7 +42,9 @@ constexpr float kMostSum = 32768.0f;    // of 64 weights: each then fits fp16
 template <int D> struct PromptShape {
     static constexpr int half = 128 * 128;                   // 64 dimensions of 128 rows in fp16
     static constexpr int tile = half * (D / 64);             // 128 rows
-    static constexpr int off_q = 0, off_k = 2 * tile, off_v = 4 * tile, smem = 6 * tile + 1024;
+    static constexpr int off_q = 0, off_k = 2 * tile, off_v = 4 * tile, off_n = 6 * tile;
+    static constexpr int numbers(int format) { return format == FKV_UINT4 ? 2 * 4 * 128 * 4 : 0; }   // of four tiles' 4-bit keys
+    static constexpr int smem(int format) { return off_n + numbers(format) + 1024; }
 };
 
 enum { K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_EMPTY = 6, SC_FULL = 8, S_FULL = 12, P_FULL = 14, O_FULL = 16, Q_FULL = 18,
@@ -193,6 +204,35 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b)
         : "f"(a), "f"(b));
 }
 
+// Two products of two, and two fused multiply-adds with an own factor each.
+__device__ __forceinline__ void mul2(float &x, float &y, float m)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\t"
+        "mul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(m));
+}
+__device__ __forceinline__ void fma2_each(float &x, float &y, float a, float b, float m, float n, float c, float d)
+{
+    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %5};\n\tmov.b64 u, {%6, %7};\n\t"
+        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "f"(a), "f"(b), "f"(m), "f"(n), "f"(c), "f"(d));
+}
+
+// Eight 4-bit codes less 7.5 as fp16 pairs (0, 4), (1, 5), (2, 6) and (3, 7): with the
+// code at bits 4 to 7 of a number of exponent 6, 64 + code is exact, less 71.5 as well.
+__device__ __forceinline__ void codes8_centred(uint32_t w, __half2 *f)
+{
+    const uint32_t x[4] = {w << 4, w, w >> 4, w >> 8};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t y = (x[i] & 0x00f000f0u) | 0x54005400u;
+        f[i] = __hsub2(*reinterpret_cast<const __half2 *>(&y), __half2half2(__ushort_as_half(0x5478)));
+    }
+}
+__device__ __forceinline__ uint32_t half2_bits(const __half2 &h) { return *reinterpret_cast<const uint32_t *>(&h); }
+
 // The word whose first n bits are set (none for n <= 0, all for n >= 32).
 __device__ __forceinline__ uint32_t below(int n)
 {
@@ -205,6 +245,7 @@ struct Row {
     float down;                 // what a score is multiplied by for the row's power of two
     int p, hi, from, pre;       // position and visible keys
     float slope;
+    float qs;                   // 4-bit pages: the query's sum, times down
 };
 
 // What is done to a score: nothing; a cap that is plain (attend.cuh), a bias by
@@ -216,7 +257,7 @@ template <int D, int FMT, typename T, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs a)
 {
     using S = PromptShape<D>;
-    constexpr bool GEN = SCORES != SCORES_PLAIN;
+    constexpr bool GEN = SCORES != SCORES_PLAIN, FOUR = FMT == FKV_UINT4;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and share_of(vs)
@@ -227,6 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     auto bar = [&](int i) { return smem_u32(bars) + 8 * i; };
+    // 4-bit pages: of the last four tiles' keys their two numbers times the scores' multiplier
+    float *const k_step = reinterpret_cast<float *>(raw + (sbase - smem_u32(raw)) + S::off_n), *const k_mid = k_step + 4 * 128;
 
     // the last rows of a causal prompt see the most keys: they go first
     int x = blockIdx.x;
@@ -346,18 +389,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         // A lane moves 16-byte piece c of rows r0, r0 + RP, ...; eight lanes that
         // store together hold four pieces of two rows of different parity, which
         // the swizzle puts on different banks.
-        constexpr int RP = 512 / D, NL = 16 / RP;                 // rows at a time, loads a unit
+        // (4-bit rows: eight lanes that store together hold the same piece of eight rows)
+        constexpr int RP = (FOUR ? 1024 : 512) / D, NL = 16 / RP; // rows at a time, loads a unit
         const int w = warp & 1;
-        const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
-        const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+        const int c = FOUR ? lane / RP : D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+        const int r0 = FOUR ? lane % RP : D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
         const bool v_side = warp & 2;
         const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
         const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
         const float mul0 = score_multiplier(a, fabsf(a.scale));
         const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
         // where the lane's first row's two 16-byte halves go in a tile
-        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
-        const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
+        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> (FOUR ? 1 : 2)) * S::half + (64 * w + r0) * 128;
+        const uint32_t sw = static_cast<uint32_t>((FOUR ? 4 * (c & 1) : 2 * (c & 3)) ^ (r0 & 7)) * 16;
         const int64_t row_step = RP * a.st;
         bool bad = false, ok = true;           // (ok: see the softmax's)
         // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
@@ -382,7 +426,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             }
             return p.id;
         };
-        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
+        auto ask_scale = [&](int id) { return !FOUR && id >= 0 ? scale_of[id * a.scb] : 1.0f; };
+        // 4-bit rows: the numbers of the lane's keys l and l + 32 (0: not one of the request's
+        // or not looked at)
+        uint32_t num[2];
+        auto ask_numbers = [&](int j, int id) {
+            int64_t from = -1;
+            if (id >= 0) {
+                const int key = first(j) + 16 * lane;
+                from = id * a.scb + key - static_cast<int>(a.div.div(key)) * a.block;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int64_t at = __shfl_sync(~0u, from, 2 * x + (lane >> 4));
+                num[x] = 0;
+                if (at >= 0 && first(j) + 32 * x + lane < q.len)
+                    num[x] = __ldg(reinterpret_cast<const uint32_t *>(scale_of) + at + (lane & 15));
+            }
+        };
         uint4 v[4][NL];
         auto load = [&](int j, int id) {
             // the unit's first row in the pool, from the lane that knows its page
@@ -409,11 +470,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         int nid = check(start);
         load(0, nid);
         float scale = ask_scale(nid);
+        if (FOUR)
+            ask_numbers(0, nid);
         nid = check(after);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1
             after = ask(j + 2);
-            if (lane < 4) {
+            uint32_t by[2] = {0, 0};           // 4-bit values: step and middle as they go into the tile
+            if (FOUR && !v_side) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    k_step[(j & 3) * 128 + 64 * w + 32 * x + lane] = num[x] ? __uint_as_float(num[x] << 16) * mul0 : 1.0f;
+                    k_mid[(j & 3) * 128 + 64 * w + 32 * x + lane] = __uint_as_float(num[x] & 0xffff0000u) * mul0;
+                }
+            } else if (FOUR) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float step = __uint_as_float(num[x] << 16), mid = __uint_as_float(num[x] & 0xffff0000u);
+                    float most = fmaf(7.5f, step, fabsf(mid));
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1)
+                        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                    // 2^e, at most 2^-14 of the largest
+                    const int e = max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 14, -100);
+                    const float unit = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+                    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+                    by[x] = pack_half(step * inv, mid * inv);
+                    if ((lane & 15) == 0)
+                        v_scales[j & 3][4 * w + 2 * x + (lane >> 4)] = make_float2(static_cast<float>(e), share_of(unit));
+                }
+            } else if (lane < 4) {
                 if (v_side) {
                     const float vs = value_scale(scale);
                     v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vs));
@@ -422,6 +508,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 }
             }
             scale = ask_scale(nid);
+            if (FOUR)
+                ask_numbers(j + 1, nid);
             __syncwarp();
             if (lane == 0)
                 mbar_arrive(bar(SC_FULL + (j & 3)));
@@ -429,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (j >= 2 && ok)
                 ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
             const int first_key = first(j);
-            if (v_side && first_key + 64 > q.len) {
+            if (!FOUR && v_side && first_key + 64 > q.len) {
                 // rows behind the request's end hold any bytes, NaN codes among them
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -443,11 +531,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
+                    if (FOUR) {
+                        __half2 step, mid;
+                        if (v_side) {
+                            const uint32_t n = __shfl_sync(~0u, by[u >> 1], 16 * (u & 1) + i * RP + r0);
+                            const __half2 both = *reinterpret_cast<const __half2 *>(&n);
+                            step = __low2half2(both), mid = __high2half2(both);
+                        }
+                        const uint32_t word[4] = {v[u][i].x, v[u][i].y, v[u][i].z, v[u][i].w};
+                        const uint32_t at = tile + (16 * u + i * RP) * 128;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            __half2 f[4];
+                            codes8_centred(word[k], f);
+                            if (v_side) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    f[e] = __hfma2(f[e], step, mid);
+                            }
+                            sts128(at + (sw ^ (16 * k)), half2_bits(f[0]), half2_bits(f[1]), half2_bits(f[2]), half2_bits(f[3]));
+                        }
+                        continue;
+                    }
                     uint32_t f[8];
-                    codes4_half<FMT>(v[u][i].x, f[0], f[1]);
-                    codes4_half<FMT>(v[u][i].y, f[2], f[3]);
-                    codes4_half<FMT>(v[u][i].z, f[4], f[5]);
-                    codes4_half<FMT>(v[u][i].w, f[6], f[7]);
+                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].x, f[0], f[1]);
+                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].y, f[2], f[3]);
+                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].z, f[4], f[5]);
+                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].w, f[6], f[7]);
                     // the row's place in its group of eight turns with i for RP = 4
                     const uint32_t at = tile + (16 * u + i * RP) * 128, x = RP == 4 && (i & 1) ? sw ^ 64 : sw;
                     sts128(at + x, f[0], f[1], f[2], f[3]);
@@ -471,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
             const int64_t tok = q.tok0 + i, head = h * a.G + u;
             Row st;
-            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f;
+            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f, st.qs = 0.0f;
             st.p = q.p0 + i;
             const RowMask mask(a, q, st.p, live);
             st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
@@ -525,8 +635,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         for (int e = 0; e < 4; ++e)
                             y[e] = pack_half(__uint_as_float(y[e] << 16) * up, __uint_as_float(y[e] & 0xffff0000u) * up);
                     }
-                    sts128(piece(k * RI + rr, c), y[0], y[1], y[2], y[3]);
+                    if (FOUR) {
+                        // the row's sum, and the order of the codes
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&y[e]));
+                            sum += z.x + z.y;
+                        }
+#pragma unroll
+                        for (int o = 1; o < LR; o *= 2)
+                            sum += __shfl_xor_sync(~0u, sum, o);
+                        const float mine = __shfl_sync(~0u, sum, lane % RI * LR);
+                        if (lane / RI == k)
+                            st.qs = mine;
+                        sts128(piece(k * RI + rr, c), __byte_perm(y[0], y[2], 0x5410), __byte_perm(y[0], y[2], 0x7632),
+                               __byte_perm(y[1], y[3], 0x5410), __byte_perm(y[1], y[3], 0x7632));
+                    } else {
+                        sts128(piece(k * RI + rr, c), y[0], y[1], y[2], y[3]);
+                    }
                 }
+                st.qs *= st.down;
                 fence_proxy_async_smem();
                 mbar_arrive(bar(Q_FULL));
             }
@@ -550,7 +679,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 float km_r[8], vo_r[8];
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
-                    km_r[n] = km[n] * st.down, vo_r[n] = vm[n].x;
+                    km_r[n] = FOUR ? 1.0f : km[n] * st.down, vo_r[n] = vm[n].x;
+                // 4-bit keys: products to scores, steps and middles four keys at a time
+                const float4 *const ks4 = reinterpret_cast<const float4 *>(k_step + (j & 3) * 128);
+                const float4 *const km4 = reinterpret_cast<const float4 *>(k_mid + (j & 3) * 128);
+                auto own_numbers = [&](float *s, int at, float off) {
+                    const float4 step = ks4[at >> 2], mid = km4[at >> 2];
+                    float u0, u1, u2, u3;
+                    fma2(u0, u1, mid.x, mid.y, st.qs, off);
+                    fma2(u2, u3, mid.z, mid.w, st.qs, off);
+                    mul2(s[0], s[1], st.down);
+                    mul2(s[2], s[3], st.down);
+                    fma2_each(s[0], s[1], s[0], s[1], step.x, step.y, u0, u1);
+                    fma2_each(s[2], s[3], s[2], s[3], step.z, step.w, u2, u3);
+                };
                 ok = ok && mbar_park(bar(S_FULL + w), j & 1, a.status);
                 tc_fence_after();
                 // the visible ones of 32 keys as bits: ranges meet as words, and a score's
@@ -561,6 +703,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 };
                 // products to scores in base 2 where a cap or a bias is between them
                 auto general = [&](float *s, int half, const float *mul, const float *off) {
+                    if (FOUR) {
+#pragma unroll
+                        for (int e = 0; e < 64; e += 4)
+                            own_numbers(s + e, 64 * half + e, 0.0f);
+                    }
                     if (SCORES == SCORES_LARGE_CAP) {
                         // mostly no score is near the cap, and the series is all there is to do
                         float most = 0.0f;
@@ -609,7 +756,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                             for (int e = 16 * n; e < 16 * n + 16; e += 2) {
                                 float y0, y1;
-                                fma2(y0, y1, s[e], s[e + 1], mul, o);
+                                if (FOUR && !GEN) {
+                                    if (e % 4 == 0)
+                                        own_numbers(s + e, 64 * half + e, o);
+                                    y0 = s[e], y1 = s[e + 1];
+                                } else {
+                                    fma2(y0, y1, s[e], s[e + 1], mul, o);
+                                }
                                 y0 = ex2(y0), y1 = ex2(y1);
                                 add2(sx, sy, y0, y1);
                                 p[e >> 1] = pack_half(y0, y1);
@@ -680,11 +833,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     float mul[4], off[4];
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
-                        mul[n] = km[4 * k + n] * st.down;
+                        mul[n] = FOUR ? 1.0f : km[4 * k + n] * st.down;
                         off[n] = vm[4 * k + n].x;
                     }
-                    if (GEN || !full) {
-                        if (GEN) {
+                    if (GEN || FOUR || !full) {
+                        if (GEN || FOUR) {
                             general(s, k, mul, off);
                         } else {
 #pragma unroll
@@ -821,13 +974,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                     o[e] = st.l != 0.0f ? o[e] * inv : 0.0f;
+                // dimension e of the 32 (4-bit pages: see the codes' order)
+                auto dim = [&](int e) { return FOUR ? o[(e & ~7) | (e << 1 & 6) | (e >> 2 & 1)] : o[e]; };
                 if (a.splits == 1) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         T y[8];
 #pragma unroll
                         for (int f = 0; f < 8; ++f)
-                            y[f] = from_float<T>(o[e + f]);
+                            y[f] = from_float<T>(dim(e + f));
                         const uint4 z = *reinterpret_cast<const uint4 *>(y);
                         sts128(piece(lane, 4 * (k & 1) + e / 8), z.x, z.y, z.z, z.w);
                     }
@@ -836,8 +991,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        sts128(piece(lane, e / 4), __float_as_uint(o[e]), __float_as_uint(o[e + 1]), __float_as_uint(o[e + 2]),
-                               __float_as_uint(o[e + 3]));
+                        sts128(piece(lane, e / 4), __float_as_uint(dim(e)), __float_as_uint(dim(e + 1)), __float_as_uint(dim(e + 2)),
+                               __float_as_uint(dim(e + 3)));
                     flush(k);
                 }
             }
@@ -859,12 +1014,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 
 template <int D, int FMT, typename T, int SCORES> cudaError_t prompt_as(const fkv_ctx *ctx, const AttendArgs &a, cudaStream_t st)
 {
+    constexpr int smem = PromptShape<D>::smem(FMT);
     const void *fn = reinterpret_cast<const void *>(k_attend_prompt<D, FMT, T, SCORES>);
-    const cudaError_t e = kernel_use(ctx, fn, kThreads, PromptShape<D>::smem, nullptr);
+    const cudaError_t e = kernel_use(ctx, fn, kThreads, smem, nullptr);
     if (e != cudaSuccess)
         return e;
     const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(a.row_tiles) * a.n_req * a.splits * a.H);
-    k_attend_prompt<D, FMT, T, SCORES><<<grid, kThreads, PromptShape<D>::smem, st>>>(a);
+    k_attend_prompt<D, FMT, T, SCORES><<<grid, kThreads, smem, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -883,6 +1039,8 @@ template <int D, int FMT> cudaError_t prompt_dt(const fkv_ctx *ctx, const Attend
 
 }  // namespace
 
+// The build compiles this file twice, for 8-bit and for 4-bit pages.
+#ifndef FKV_PAGES_4BIT
 int prompt_rows() { return kRows; }
 
 cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const AttendArgs &a, int dim, int format, int dtype, cudaStream_t st)
@@ -891,3 +1049,9 @@ cudaError_t launch_attend_prompt(const fkv_ctx *ctx, const AttendArgs &a, int di
         return format == FKV_INT8 ? prompt_dt<64, FKV_INT8>(ctx, a, dtype, st) : prompt_dt<64, FKV_E4M3>(ctx, a, dtype, st);
     return format == FKV_INT8 ? prompt_dt<128, FKV_INT8>(ctx, a, dtype, st) : prompt_dt<128, FKV_E4M3>(ctx, a, dtype, st);
 }
+#else
+cudaError_t launch_attend_prompt4(const fkv_ctx *ctx, const AttendArgs &a, int dim, int dtype, cudaStream_t st)
+{
+    return dim == 64 ? prompt_dt<64, FKV_UINT4>(ctx, a, dtype, st) : prompt_dt<128, FKV_UINT4>(ctx, a, dtype, st);
+}
+#endif
