@@ -24,18 +24,20 @@ using namespace fkvd;
 
 namespace {
 
-// As k_attend_step: four warps, each with every fourth group of 32 keys, a ring of
-// its own filled by TMA and a softmax of its own; keys are the rows of the first
-// product, dimensions those of the second, query rows their 8 columns.
+// As k_attend_step: four warps, each with every fourth group of keys, a ring of its
+// own filled by TMA and a softmax of its own; keys are the rows of the first
+// product, dimensions those of the second, query rows their 8 columns.  A group is 64
+// keys for 8 rows, 32 for more (registers).
 template <int D, int NT> struct Step4Shape {
-    static constexpr int stages = D == 128 ? 3 : 4;
+    static constexpr int units = NT == 1 ? 4 : 2, keys = 16 * units;
+    static constexpr int stages = D == 128 ? (NT == 1 ? 2 : 3) : NT == 1 ? 3 : 4;
     static constexpr int unit = 8 * D;                          // 16 keys' codes
-    static constexpr int numbers = 4 * unit, stage = (4 * unit + 4 * 64 + 511) / 512 * 512;
+    static constexpr int numbers = 2 * units * unit, stage = (2 * units * (unit + 64) + 511) / 512 * 512;
     static constexpr int ring = 4 * stages * stage;
     static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0;  // the query operands, [column tile][step][lane]
-    static constexpr int keys = 4 * 32 * 16;                    // a warp's keys' numbers
+    static constexpr int nums = 4 * keys * 20;                  // a warp's keys' numbers
     static constexpr int ml = 4 * 2 * 8 * NT * 4;
-    static constexpr int smem = ring + q + keys + ml + 1024;
+    static constexpr int smem = ring + q + nums + ml + 1024;
 };
 
 // Contiguous bytes into shared memory, 16-byte aligned and a multiple of 16 of them.
@@ -60,7 +62,7 @@ __global__ void __launch_bounds__(128, 3)
     k_attend_step4(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
 {
     using S = Step4Shape<D, NT>;
-    constexpr int ST = S::stages, W = D / 32, MO = D / 16, R = 8 * NT;
+    constexpr int ST = S::stages, U = S::units, KW = S::keys, PT = kTile / KW, W = D / 32, MO = D / 16, R = 8 * NT;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
     __shared__ Seen rows_see[4];                 // a warp's own: registers are short
@@ -68,9 +70,11 @@ __global__ void __launch_bounds__(128, 3)
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     uint8_t *const base = raw + (sbase - smem_u32(raw));
     uint2 *const q_s = reinterpret_cast<uint2 *>(base + S::ring);
-    float4 *const keys_s = reinterpret_cast<float4 *>(base + S::ring + S::q) + 32 * warp;
+    // a warp's keys: K's step and middle, log2 of V's step; what a weight counts, and times V's middle
+    float4 *const keys_s = reinterpret_cast<float4 *>(base + S::ring + S::q) + KW * warp;
+    float *const mids_s = reinterpret_cast<float *>(base + S::ring + S::q + 4 * KW * 16) + KW * warp;
     typedef float RowPair[2][R];                 // a warp's maxima and sums
-    RowPair *const ml = reinterpret_cast<RowPair *>(base + S::ring + S::q + S::keys);
+    RowPair *const ml = reinterpret_cast<RowPair *>(base + S::ring + S::q + S::nums);
 
     const int h = blockIdx.y;
     const int split = blockIdx.x % a.splits, rr = blockIdx.x / a.splits;
@@ -88,10 +92,15 @@ __global__ void __launch_bounds__(128, 3)
     const int pa = q.p0 + ia, pb = q.p0 + ib;
     const Tiles tiles(a, q, pa, pb);
     const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk);
-    // the last tile may end before this warp's keys
-    const int n_it = max(0, i1 - i0) - (i1 > i0 && tiles.at(i1 - 1) * kTile + warp * 32 >= tiles.lim);
-    const bool back = a.slopes != nullptr;       // (see k_attend_step)
-    auto tile_at = [&](int it) { return tiles.at(i0 + (back ? n_it - 1 - it : it)); };
+    // the share's groups of keys, but for those behind all that any row sees; a warp's are
+    // every fourth (a bias: from the last one back, see k_attend_step)
+    auto group_at = [&](int g) { return tiles.at(i0 + g / PT) * kTile + g % PT * KW; };
+    int groups = max(0, i1 - i0) * PT;
+    while (groups > 0 && group_at(groups - 1) >= tiles.lim)
+        --groups;
+    const int n_it = (groups - warp + 3) >> 2;   // 0 or less: none
+    const bool back = a.slopes != nullptr;
+    auto first_key = [&](int it) { return group_at(back ? groups - 1 - 4 * it - warp : 4 * it + warp); };
 
     const uint32_t ring = sbase + warp * ST * S::stage, bar0 = smem_u32(bars) + warp * ST * 8;
     if (lane == 0) {
@@ -102,15 +111,16 @@ __global__ void __launch_bounds__(128, 3)
     }
     __syncwarp();
 
-    // A lane looks up the page of one of the 32 units (16 keys) of 16 iterations, a
+    // A lane looks up the page of one of the 32 units (16 keys) of 32 / U iterations, a
     // batch of iterations ahead, if any row sees one of its keys.
+    constexpr int BI = 32 / U;
     bool bad = false;
     struct Unit {
         int id;
         unsigned all;                  // which of the 32 units are looked at
     };
-    auto key_of = [&](int batch) { return tile_at(batch * 16 + (lane >> 1)) * kTile + warp * 32 + (lane & 1) * 16; };
-    auto on = [&](int batch) { return batch * 16 + (lane >> 1) < n_it && rows_see[warp].of(key_of(batch)); };
+    auto key_of = [&](int batch) { return first_key(batch * BI + lane / U) + lane % U * 16; };
+    auto on = [&](int batch) { return batch * BI + lane / U < n_it && rows_see[warp].of(key_of(batch)); };
     auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
     auto check = [&](int batch, int id) {
         const bool mine = on(batch);
@@ -125,24 +135,24 @@ __global__ void __launch_bounds__(128, 3)
     };
     Unit cur = check(0, ask(0)), nxt = check(1, ask(1));
     int nid = ask(2);
-    auto first_key = [&](int it) { return tile_at(it) * kTile + warp * 32; };
+    auto units_of = [&](const Unit &u, int it) { return u.all >> (it % BI * U) & ((1u << U) - 1); };
     auto issue = [&](int it, int batch) {
-        const int from = (it & 15) * 2 + (lane & 1);
-        const bool now = (it >> 4) == batch;
-        const unsigned units = (now ? cur.all : nxt.all) >> ((it & 15) * 2) & 3;
-        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, from);
-        const int key = first_key(it) + (lane & 1) * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
+        const bool now = it / BI == batch;
+        const unsigned units = units_of(now ? cur : nxt, it);
+        const int u = lane % U;
+        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, it % BI * U + u);
+        const int key = first_key(it) + u * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
         const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * S::stage;
         // (without any the arrival alone completes the phase)
         if (lane == 0)
             mbar_arrive_expect_tx(bar, __popc(units) * 2 * (S::unit + 64));
         __syncwarp();
-        // lanes 0 .. 3: codes of units 0 and 1 of K, then of V; 4 .. 7: their numbers
-        if (lane < 8 && (units >> (lane & 1) & 1)) {
-            if (lane < 4)
-                tma_load_4d(dst + lane * S::unit, lane < 2 ? &mk : &mv, 0, off, h, static_cast<int>(id), bar);
+        // U lanes each: codes of K's units, of V's, their numbers
+        if (lane < 4 * U && (units >> u & 1)) {
+            if (lane < 2 * U)
+                tma_load_4d(dst + lane * S::unit, lane < U ? &mk : &mv, 0, off, h, static_cast<int>(id), bar);
             else
-                bulk_load(dst + S::numbers + (lane - 4) * 64, (lane < 6 ? a.ks : a.vs) + id * a.scb + h * a.sch + off, 64, bar);
+                bulk_load(dst + S::numbers + (lane - 2 * U) * 64, (lane < 3 * U ? a.ks : a.vs) + id * a.scb + h * a.sch + off, 64, bar);
         }
         __syncwarp();
     };
@@ -239,8 +249,8 @@ __global__ void __launch_bounds__(128, 3)
 
     int batch = 0;
     for (int it = 0; it < n_it; ++it) {
-        if ((it >> 4) != batch) {
-            batch = it >> 4;
+        if (it / BI != batch) {
+            batch = it / BI;
             cur = nxt;
             nxt = check(batch + 1, nid);
             nid = ask(batch + 2);
@@ -248,7 +258,7 @@ __global__ void __launch_bounds__(128, 3)
         if (it + ST - 1 < n_it)
             issue(it + ST - 1, batch);
         const int key = first_key(it);
-        const unsigned units = cur.all >> ((it & 15) * 2) & 3;
+        const unsigned units = units_of(cur, it);
         // (a lane that gives up takes its warp along: the others would meet it nowhere)
         if (!__all_sync(~0u, mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status))) {
             // give the loads in flight a while to land before the memory is used again
@@ -259,110 +269,118 @@ __global__ void __launch_bounds__(128, 3)
         }
         if (units == 0)
             continue;                  // keys between the first ones and the window
-        const uint32_t kt = ring + (it % ST) * S::stage, vt = kt + 2 * S::unit;
+        const uint32_t kt = ring + (it % ST) * S::stage, vt = kt + U * S::unit;
 
         // a lane a key: its numbers, and what its value's step gives its weights.  Those of
         // keys behind the request's end, or that were not loaded, may be anything.
-        {
-            const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (kt - sbase) + S::numbers) + lane;
-            uint32_t kn = num[0], vn = num[32];
-            if (!(units >> (lane >> 4) & 1) || key + lane >= q.len)
+        const bool all_loaded = units == (1u << U) - 1 && key + KW <= q.len;
+#pragma unroll
+        for (int x = 0; x < KW; x += 32) {
+            const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (kt - sbase) + S::numbers) + x + lane;
+            uint32_t kn = num[0], vn = num[KW];
+            if (!all_loaded && (!(units >> ((x + lane) >> 4) & 1) || key + x + lane >= q.len))
                 kn = vn = 0;
-            const float vs = value_scale(__uint_as_float(vn << 16));
-            keys_s[lane] = make_float4(__uint_as_float(kn), __uint_as_float(vn), lg2(vs), share_of(vs));
+            const float vs = value_scale(__uint_as_float(vn << 16)), share = share_of(vs);
+            keys_s[x + lane] = make_float4(__uint_as_float(kn << 16), __uint_as_float(kn & 0xffff0000u), lg2(vs), share);
+            mids_s[x + lane] = share * __uint_as_float(vn & 0xffff0000u);
         }
 
-        float sc[2][NT][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                sc[u][n][0] = sc[u][n][2] = start[n][0], sc[u][n][1] = sc[u][n][3] = start[n][1];
-        // both units' keys gid and gid + 8; a unit that was not loaded gives
+        // the units' keys gid and gid + 8; a unit that was not loaded gives
         // products of any codes, which no row sees
-        uint32_t kw[2][2][W];
+        float sc[U][NT][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; u += 2) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int kr = 16 * u + gid + 8 * x;
-                if (D == 128) {
-                    const uint4 v = lds128(kt + kr * 64 + ((t ^ ((kr >> 1) & 3)) << 4));
-                    kw[u][x][0] = v.x, kw[u][x][1] = v.y;
-                    kw[u][x][W - 2] = v.z, kw[u][x][W - 1] = v.w;
-                } else {
-                    const uint2 v = lds64(kt + kr * 32 + t * 8);
-                    kw[u][x][0] = v.x, kw[u][x][1] = v.y;
-                }
-            }
+            for (int v = u; v < u + 2; ++v)
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            uint32_t f[2][2][4];
+                for (int n = 0; n < NT; ++n)
+                    sc[v][n][0] = sc[v][n][2] = start[n][0], sc[v][n][1] = sc[v][n][3] = start[n][1];
+            uint32_t kw[2][2][W];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int v = 0; v < 2; ++v)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    codes8_pairs(kw[u][x][w], f[u][x]);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint2 qv;
-                    if (NT > 1)
-                        qv = q_s[(n * 2 * W + 2 * w + s) * 32 + lane];
-                    else
-                        qv = make_uint2(qf[2 * w + s][0], qf[2 * w + s][1]);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t g[4] = {f[u][0][2 * s], f[u][1][2 * s], f[u][0][2 * s + 1], f[u][1][2 * s + 1]};
-                        mma16816(sc[u][n], g, qv.x, qv.y);
+                for (int x = 0; x < 2; ++x) {
+                    const int kr = 16 * (u + v) + gid + 8 * x;
+                    if (D == 128) {
+                        const uint4 z = lds128(kt + kr * 64 + ((t ^ ((kr >> 1) & 3)) << 4));
+                        kw[v][x][0] = z.x, kw[v][x][1] = z.y;
+                        kw[v][x][W - 2] = z.z, kw[v][x][W - 1] = z.w;
+                    } else {
+                        const uint2 z = lds64(kt + kr * 32 + t * 8);
+                        kw[v][x][0] = z.x, kw[v][x][1] = z.y;
                     }
                 }
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                uint32_t f[2][2][4];
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        codes8_pairs(kw[v][x][w], f[v][x]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint2 qv;
+                        if (NT > 1)
+                            qv = q_s[(n * 2 * W + 2 * w + s) * 32 + lane];
+                        else
+                            qv = make_uint2(qf[2 * w + s][0], qf[2 * w + s][1]);
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            const uint32_t g[4] = {f[v][0][2 * s], f[v][1][2 * s], f[v][0][2 * s + 1], f[v][1][2 * s + 1]};
+                            mma16816(sc[u + v][n], g, qv.x, qv.y);
+                        }
+                    }
+            }
         }
 
         // scores in base 2 with the logarithms of the values' steps
         __syncwarp();                  // keys_s
-        float mx[NT][2], share[2][2], vmid[2][2];
+        const bool caps = a.softcap > 0.0f;
+        float share[U][2], lvs[U][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-            mx[n][0] = mx[n][1] = -INFINITY;
-        const bool full = all_see(a, q, pa, pb, key, key + 32);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const float4 num = keys_s[16 * u + gid + 8 * x];
-                const float step = __uint_as_float(__float_as_uint(num.x) << 16), kmid = __uint_as_float(__float_as_uint(num.x) & 0xffff0000u);
-                vmid[u][x] = __uint_as_float(__float_as_uint(num.y) & 0xffff0000u);
-                const float lvs = num.z;
-                share[u][x] = num.w;
-                const int j = key + 16 * u + gid + 8 * x;
+                lvs[u][x] = num.z, share[u][x] = num.w;
+                const float off = caps ? 0.0f : num.z;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float &s = sc[u][n][2 * x + c];
-                        const float mul = step * rowmul[n][c];
-                        float y;
-                        if (a.softcap > 0.0f) {
-                            y = fmaf(s, mul, kmid * rowsum[n][c]);
-                            if (plain_cap(a))
-                                y = fmaf(-2.0f * a.cap2, __fdividef(1.0f, 1.0f + ex2(y)), a.cap2 + lvs);
-                            else
-                                y = capped(a, y) + lvs;
-                        } else {
-                            y = fmaf(s, mul, fmaf(kmid, rowsum[n][c], lvs));
-                        }
-                        if (a.slopes)
-                            y = fmaf(slope[n][c], static_cast<float>(j - prow[n][c]), y);
-                        if (!full) {
-                            const bool see = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c];
-                            y = see ? y : -INFINITY;
-                        }
-                        s = y;
-                        mx[n][c] = fmaxf(mx[n][c], y);
-                    }
+                    for (int c = 0; c < 2; ++c)
+                        sc[u][n][2 * x + c] = fmaf(sc[u][n][2 * x + c], num.x * rowmul[n][c], fmaf(num.y, rowsum[n][c], off));
             }
+        auto each = [&](auto &&f) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        f(sc[u][n][e], n, e & 1, lvs[u][e >> 1], key + 16 * u + gid + 8 * (e >> 1));
+        };
+        if (caps) {
+            if (plain_cap(a))
+                each([&](float &y, int, int, float lv, int) {
+                    y = fmaf(-2.0f * a.cap2, __fdividef(1.0f, 1.0f + ex2(y)), a.cap2 + lv);
+                });
+            else
+                each([&](float &y, int, int, float lv, int) { y = capped(a, y) + lv; });
+        }
+        if (a.slopes)
+            each([&](float &y, int n, int c, float, int j) { y = fmaf(slope[n][c], static_cast<float>(j - prow[n][c]), y); });
+        if (!all_see(a, q, pa, pb, key, key + KW))
+            each([&](float &y, int n, int c, float, int j) {
+                y = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c] ? y : -INFINITY;
+            });
+        float mx[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            mx[n][0] = mx[n][1] = -INFINITY;
+        each([&](float &y, int n, int c, float, int) { mx[n][c] = fmaxf(mx[n][c], y); });
         bool grown = false;
         float mref[NT][2], by[NT][2];
 #pragma unroll
@@ -395,10 +413,11 @@ __global__ void __launch_bounds__(128, 3)
                 }
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
             if (!(units >> u & 1))
                 continue;
             uint32_t pf[NT][2];
+            const float vmid[2] = {mids_s[16 * u + gid], mids_s[16 * u + gid + 8]};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -407,9 +426,8 @@ __global__ void __launch_bounds__(128, 3)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         p[c] = ex2(sc[u][n][2 * x + c] - mref[n][c]);
-                        const float w = p[c] * share[u][x];
-                        l[n][c] += w;
-                        mid[n][c] = fmaf(w, vmid[u][x], mid[n][c]);
+                        l[n][c] = fmaf(p[c], share[u][x], l[n][c]);
+                        mid[n][c] = fmaf(p[c], vmid[x], mid[n][c]);
                     }
                     pf[n][x] = transpose8(pack_half(p[0], p[1]));
                 }
