@@ -626,6 +626,16 @@ cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, 
 
 }  // namespace
 
+// A load takes as many units of 16 positions as lie in a page, up to a warp's group
+// (attend4.cu); of 8-bit pages one.
+int page_attend_box(const fkv_ctx *ctx, const fkv_attend &c)
+{
+    if (c.pages->format != FKV_UINT4)
+        return 16;
+    const int most = plan_of(ctx, c).nt == 1 ? 64 : 32;
+    return c.pages->block % 64 == 0 ? most : c.pages->block % 32 == 0 ? 32 : 16;
+}
+
 int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_attend &c)
 {
     const Plan p = plan_of(ctx, c);
@@ -659,6 +669,7 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws
     a.cap2 = c.softcap * kLog2e, a.cap_inv = c.softcap > 0.0f ? 1.0f / a.cap2 : 0.0f;
     a.div = FastDiv::make(pg->block), a.gdiv = FastDiv::make(a.G);
     const Plan p = plan_of(ctx, c);
+    a.box = __builtin_ctz(static_cast<unsigned>(page_attend_box(ctx, c))) - 4;
     a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk, a.cluster = p.cluster;
     a.ws_o = static_cast<float *>(ws);
     a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * pg->dim : nullptr;

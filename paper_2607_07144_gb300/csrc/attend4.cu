@@ -136,23 +136,30 @@ __global__ void __launch_bounds__(128, 3)
     Unit cur = check(0, ask(0)), nxt = check(1, ask(1));
     int nid = ask(2);
     auto units_of = [&](const Unit &u, int it) { return u.all >> (it % BI * U) & ((1u << U) - 1); };
+    // Units are loaded as many together as pages hold whole ones of (2^box): a load takes some
+    // 15 instructions, as its operands are the warp's.
+    const int pieces = U >> a.box;
     auto issue = [&](int it, int batch) {
         const bool now = it / BI == batch;
         const unsigned units = units_of(now ? cur : nxt, it);
-        const int u = lane % U;
-        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, it % BI * U + u);
+        const int x = lane & (pieces - 1), u = x << a.box, what = lane >> (31 - __clz(pieces));
+        // (whichever of a piece's units any row sees has its page)
+        const unsigned mine = units >> u & ((1u << (1 << a.box)) - 1);
+        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, it % BI * U + u + (mine ? __ffs(mine) - 1 : 0));
         const int key = first_key(it) + u * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
         const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * S::stage;
+        const unsigned heads = __ballot_sync(~0u, lane < pieces && mine);
         // (without any the arrival alone completes the phase)
         if (lane == 0)
-            mbar_arrive_expect_tx(bar, __popc(units) * 2 * (S::unit + 64));
+            mbar_arrive_expect_tx(bar, __popc(heads) * 2 * (S::unit + 64) << a.box);
         __syncwarp();
-        // U lanes each: codes of K's units, of V's, their numbers
-        if (lane < 4 * U && (units >> u & 1)) {
-            if (lane < 2 * U)
-                tma_load_4d(dst + lane * S::unit, lane < U ? &mk : &mv, 0, off, h, static_cast<int>(id), bar);
+        // `pieces` lanes each: codes of K, of V, their numbers
+        if (what < 4 && mine) {
+            if (what < 2)
+                tma_load_4d(dst + (what * U + u) * S::unit, what ? &mv : &mk, 0, off, h, static_cast<int>(id), bar);
             else
-                bulk_load(dst + S::numbers + (lane - 2 * U) * 64, (lane < 3 * U ? a.ks : a.vs) + id * a.scb + h * a.sch + off, 64, bar);
+                bulk_load(dst + S::numbers + ((what - 2) * U + u) * 64, (what < 3 ? a.ks : a.vs) + id * a.scb + h * a.sch + off,
+                          64 << a.box, bar);
         }
         __syncwarp();
     };

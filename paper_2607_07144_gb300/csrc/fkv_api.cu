@@ -1117,9 +1117,9 @@ const char *check_attend(const fkv_attend *a)
     return check_table(a->n_req, a->table, a->table_stride, a->width);
 }
 
-// The pool as [page][head][position][row] bytes, in boxes of 16 positions of one
+// The pool as [page][head][position][row] bytes, in boxes of some positions of one
 // head whose rows are swizzled by their own width (those of 32 bytes are not).
-bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *map)
+bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, int positions, CUtensorMap *map)
 {
     const cuuint64_t D = static_cast<cuuint64_t>(p->format == FKV_UINT4 ? p->dim / 2 : p->dim);
     const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(p->block), static_cast<cuuint64_t>(p->n_heads),
@@ -1128,7 +1128,7 @@ bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, CUtensorMap *ma
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(p->stride_pos),
                                    p->n_heads > 1 ? static_cast<cuuint64_t>(p->stride_head) : D,
                                    p->n_blocks > 1 ? static_cast<cuuint64_t>(p->stride_block) : D};
-    const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), 16, 1, 1}, estr[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), static_cast<cuuint32_t>(positions), 1, 1}, estr[4] = {1, 1, 1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                D == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
                : D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
@@ -1259,7 +1259,8 @@ int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t 
         return fail(ctx, FKV_EINVAL, why);
     EncodeTiledFn enc = encode_tiled();
     CUtensorMap mk, mv;
-    if (!enc || !page_map(enc, a->pages, a->pages->k, &mk) || !page_map(enc, a->pages, a->pages->v, &mv))
+    const int box = page_attend_box(ctx, *a);
+    if (!enc || !page_map(enc, a->pages, a->pages->k, box, &mk) || !page_map(enc, a->pages, a->pages->v, box, &mv))
         return fail(ctx, FKV_ECUDA, "cuTensorMapEncodeTiled failed");
     CK(launch_page_attend(ctx, *a, need ? workspace : nullptr, mk, mv, as_stream(stream)), "page attention launch");
     return FKV_OK;

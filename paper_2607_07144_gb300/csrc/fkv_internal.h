@@ -212,6 +212,7 @@ cudaError_t launch_page_read(const fkv_ctx *c, const fkv_pages *p, const int32_t
 // mk, mv: TMA maps over the pools as [page][head][position][dim] bytes, 16 positions a box
 // bytes, or -1: too many blocks for one launch
 int64_t page_attend_workspace(const fkv_ctx *c, const fkv_attend &a);
+int page_attend_box(const fkv_ctx *c, const fkv_attend &a);      // positions a load takes of a page
 cudaError_t launch_page_attend(const fkv_ctx *c, const fkv_attend &a, void *ws, const CUtensorMap &mk,
                                const CUtensorMap &mv, cudaStream_t st);
 
