@@ -632,8 +632,11 @@ int page_attend_box(const fkv_ctx *ctx, const fkv_attend &c)
 {
     if (c.pages->format != FKV_UINT4)
         return 16;
-    const int most = plan_of(ctx, c).nt == 1 ? 64 : 32;
-    return c.pages->block % 64 == 0 ? most : c.pages->block % 32 == 0 ? 32 : 16;
+    const int nt = plan_of(ctx, c).nt, most = nt ? step4_keys(nt) : 16;
+    int box = 16;
+    while (box < most && c.pages->block % (2 * box) == 0)
+        box *= 2;
+    return box;
 }
 
 int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_attend &c)

@@ -148,6 +148,9 @@ constexpr float kRef = 0x1p-20f, kLog2Ref = -20.0f;
 __device__ __forceinline__ float value_scale(float vs) { return fmaxf(vs, FKV_PAGE_MIN_SCALE); }
 __device__ __forceinline__ float share_of(float vs) { return __fdividef(kRef, vs); }
 
+// Keys that a warp of the kernel for a few rows over 4-bit pages takes at a time (attend4.cu).
+constexpr int step4_keys(int nt) { return nt == 1 ? 64 : 32; }
+
 }  // namespace fkvd
 
 // Over 4-bit pages (attend4.cu): nt tiles of 8 rows a block.

@@ -16,8 +16,8 @@
 // A code needs no conversion: as the low four bits of an fp16 number it is the
 // subnormal c 2^-24, and one place to the left c 2^-20.  A word of eight codes is four
 // operands of two after four masks and a shift; the factor 16 between neighbours is
-// taken out of the query for K and of the output for V, both exactly but for elements
-// of a query below 2^-25 of its largest (rounded to 2^-35 of that).
+// taken out of the query for K, exactly but for elements of it below 2^-25 of its largest
+// (rounded to 2^-35 of that), and of the output for V.
 #include "attend_step.cuh"
 
 using namespace fkvd;
@@ -29,11 +29,10 @@ namespace {
 // product, dimensions those of the second, query rows their 8 columns.  A group is 64
 // keys for 8 rows, 32 for more (registers).
 template <int D, int NT> struct Step4Shape {
-    static constexpr int units = NT == 1 ? 4 : 2, keys = 16 * units;
+    static constexpr int keys = step4_keys(NT), units = keys / 16;
     static constexpr int stages = D == 128 ? (NT == 1 ? 2 : 3) : NT == 1 ? 3 : 4;
-    static constexpr int unit = 8 * D;                          // 16 keys' codes
-    static constexpr int numbers = 2 * units * unit, stage = (2 * units * (unit + 64) + 511) / 512 * 512;
-    static constexpr int ring = 4 * stages * stage;
+    static constexpr int unit = 8 * D, stage = 2 * units * unit;                // 16 keys' codes; a group's
+    static constexpr int codes = 4 * stages * stage, ring = codes + 4 * stages * 2 * units * 64;   // with their numbers
     static constexpr int q = NT > 1 ? NT * (D / 16) * 256 : 0;  // the query operands, [column tile][step][lane]
     static constexpr int nums = 4 * keys * 20;                  // a warp's keys' numbers
     static constexpr int ml = 4 * 2 * 8 * NT * 4;
@@ -57,6 +56,24 @@ __device__ __forceinline__ void codes8_pairs(uint32_t w, uint32_t *f)
     f[2] = x & 0x000f000fu, f[3] = x & 0x00f000f0u;
 }
 
+// The same of two values' codes 0 .. 3 (of the words' halves `sel` takes): (c0, c0'),
+// (c2, c2') times 2^-24, and (c0 + 16 c1, ..), (c2 + 16 c3, ..): an operation less, and
+// what the even dimension adds to the odd one's sum is taken off at the end.
+__device__ __forceinline__ void codes4_pairs(uint32_t w0, uint32_t w1, int sel, uint32_t *f)
+{
+    const uint32_t x = __byte_perm(w0, w1, sel), y = __byte_perm(x, 0, 0x4341);
+    f[0] = x & 0x000f000fu, f[1] = x & 0x00ff00ffu;
+    f[2] = y & 0x000f000fu, f[3] = y;
+}
+
+// D = A B + C.
+__device__ __forceinline__ void mma16816_from(float *d, const uint32_t *a, uint32_t b0, uint32_t b1, float c0, float c1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+
 template <int D, typename T, int NT>
 __global__ void __launch_bounds__(128, 3)
     k_attend_step4(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
@@ -66,7 +83,9 @@ __global__ void __launch_bounds__(128, 3)
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
     __shared__ Seen rows_see[4];                 // a warp's own: registers are short
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
+    // (the same for all of a warp as far as the compiler can see: addresses and loop bounds
+    // are uniform then)
+    const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31, gid = lane >> 2, t = lane & 3;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     uint8_t *const base = raw + (sbase - smem_u32(raw));
     uint2 *const q_s = reinterpret_cast<uint2 *>(base + S::ring);
@@ -100,9 +119,12 @@ __global__ void __launch_bounds__(128, 3)
         --groups;
     const int n_it = (groups - warp + 3) >> 2;   // 0 or less: none
     const bool back = a.slopes != nullptr;
+    // what every row sees: positions up to first_end, and from begin to last_end
+    const int last_end = pa < 0 ? 0 : a.causal ? min(q.len, pa + 1) : q.len, begin = a.window ? pb - a.window + 1 : 0;
+    const int first_end = pa < 0 ? 0 : max(q.pre, a.window ? min(a.sinks, last_end) : 0);
     auto first_key = [&](int it) { return group_at(back ? groups - 1 - 4 * it - warp : 4 * it + warp); };
 
-    const uint32_t ring = sbase + warp * ST * S::stage, bar0 = smem_u32(bars) + warp * ST * 8;
+    const uint32_t ring = sbase + warp * ST * S::stage, nums = sbase + S::codes + warp * ST * (2 * U * 64), bar0 = smem_u32(bars) + warp * ST * 8;
     if (lane == 0) {
         rows_see[warp] = tiles.seen;
         for (int s = 0; s < ST; ++s)
@@ -147,7 +169,7 @@ __global__ void __launch_bounds__(128, 3)
         const unsigned mine = units >> u & ((1u << (1 << a.box)) - 1);
         const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, it % BI * U + u + (mine ? __ffs(mine) - 1 : 0));
         const int key = first_key(it) + u * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
-        const uint32_t bar = bar0 + 8 * (it % ST), dst = ring + (it % ST) * S::stage;
+        const uint32_t bar = bar0 + 8 * (it % ST), slot = it % ST;
         const unsigned heads = __ballot_sync(~0u, lane < pieces && mine);
         // (without any the arrival alone completes the phase)
         if (lane == 0)
@@ -156,9 +178,9 @@ __global__ void __launch_bounds__(128, 3)
         // `pieces` lanes each: codes of K, of V, their numbers
         if (what < 4 && mine) {
             if (what < 2)
-                tma_load_4d(dst + (what * U + u) * S::unit, what ? &mv : &mk, 0, off, h, static_cast<int>(id), bar);
+                tma_load_4d(ring + slot * S::stage + (what * U + u) * S::unit, what ? &mv : &mk, 0, off, h, static_cast<int>(id), bar);
             else
-                bulk_load(dst + S::numbers + ((what - 2) * U + u) * 64, (what < 3 ? a.ks : a.vs) + id * a.scb + h * a.sch + off,
+                bulk_load(nums + slot * (2 * U * 64) + ((what - 2) * U + u) * 64, (what < 3 ? a.ks : a.vs) + id * a.scb + h * a.sch + off,
                           64 << a.box, bar);
         }
         __syncwarp();
@@ -239,7 +261,7 @@ __global__ void __launch_bounds__(128, 3)
     if (NT > 1)
         __syncthreads();
 
-    // outputs (even dimensions in 2^-24, odd ones in 2^-20); the sums of the rounded weights
+    // outputs (in 2^-24; odd dimensions 16 times themselves plus the even one before); the sums of the rounded weights
     // in p (all four of its values), of weights over steps and of weights' middles
     float o[NT][MO][4], p_sum[NT][4];
     float m[NT][2], l[NT][2], mid[NT][2];
@@ -277,14 +299,14 @@ __global__ void __launch_bounds__(128, 3)
         if (units == 0)
             continue;                  // keys between the first ones and the window
         const uint32_t kt = ring + (it % ST) * S::stage, vt = kt + U * S::unit;
+        const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (nums - sbase)) + it % ST * (2 * KW) + lane;
 
         // a lane a key: its numbers, and what its value's step gives its weights.  Those of
         // keys behind the request's end, or that were not loaded, may be anything.
         const bool all_loaded = units == (1u << U) - 1 && key + KW <= q.len;
 #pragma unroll
         for (int x = 0; x < KW; x += 32) {
-            const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (kt - sbase) + S::numbers) + x + lane;
-            uint32_t kn = num[0], vn = num[KW];
+            uint32_t kn = num[x], vn = num[KW + x];
             if (!all_loaded && (!(units >> ((x + lane) >> 4) & 1) || key + x + lane >= q.len))
                 kn = vn = 0;
             const float vs = value_scale(__uint_as_float(vn << 16)), share = share_of(vs);
@@ -297,11 +319,6 @@ __global__ void __launch_bounds__(128, 3)
         float sc[U][NT][4];
 #pragma unroll
         for (int u = 0; u < U; u += 2) {
-#pragma unroll
-            for (int v = u; v < u + 2; ++v)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    sc[v][n][0] = sc[v][n][2] = start[n][0], sc[v][n][1] = sc[v][n][3] = start[n][1];
             uint32_t kw[2][2][W];
 #pragma unroll
             for (int v = 0; v < 2; ++v)
@@ -337,7 +354,10 @@ __global__ void __launch_bounds__(128, 3)
 #pragma unroll
                         for (int v = 0; v < 2; ++v) {
                             const uint32_t g[4] = {f[v][0][2 * s], f[v][1][2 * s], f[v][0][2 * s + 1], f[v][1][2 * s + 1]};
-                            mma16816(sc[u + v][n], g, qv.x, qv.y);
+                            if (w == 0 && s == 0)
+                                mma16816_from(sc[u + v][n], g, qv.x, qv.y, start[n][0], start[n][1]);
+                            else
+                                mma16816(sc[u + v][n], g, qv.x, qv.y);
                         }
                     }
             }
@@ -379,7 +399,8 @@ __global__ void __launch_bounds__(128, 3)
         }
         if (a.slopes)
             each([&](float &y, int n, int c, float, int j) { y = fmaf(slope[n][c], static_cast<float>(j - prow[n][c]), y); });
-        if (!all_see(a, q, pa, pb, key, key + KW))
+        // whether every row sees all of them (as all_see)
+        if (!(key + KW <= first_end || (key + KW <= last_end && key >= begin)))
             each([&](float &y, int n, int c, float, int j) {
                 y = (j < hi[n][c] && (j >= from[n][c] || j < a.sinks)) || j < pre[n][c] ? y : -INFINITY;
             });
@@ -421,8 +442,7 @@ __global__ void __launch_bounds__(128, 3)
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!(units >> u & 1))
-                continue;
+            // (a unit that was not loaded has weights of zero, and codes of any bytes)
             uint32_t pf[NT][2];
             const float vmid[2] = {mids_s[16 * u + gid], mids_s[16 * u + gid + 8]};
 #pragma unroll
@@ -459,8 +479,8 @@ __global__ void __launch_bounds__(128, 3)
                     // rows gid and gid + 8 of two tiles: dimensions 8k + 4e and the next, and the two behind
                     const int sel = e ? 0x7632 : 0x5410;
                     uint32_t f0[4], f1[4];
-                    codes8_pairs(__byte_perm(w[0][k], w[1][k], sel), f0);
-                    codes8_pairs(__byte_perm(w[2][k], w[3][k], sel), f1);
+                    codes4_pairs(w[0][k], w[1][k], sel, f0);
+                    codes4_pairs(w[2][k], w[3][k], sel, f1);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const uint32_t f[4] = {f0[2 * y], f0[2 * y + 1], f1[2 * y], f1[2 * y + 1]};
@@ -486,8 +506,8 @@ __global__ void __launch_bounds__(128, 3)
             const float add = fmaf(-7.5f, p_sum[n][c], x * (1.0f / kRef));
 #pragma unroll
             for (int d = 0; d < MO; ++d) {
+                o[n][d][2 + c] = fmaf(o[n][d][2 + c] - o[n][d][c], 0x1p20f, add);
                 o[n][d][c] = fmaf(o[n][d][c], 0x1p24f, add);
-                o[n][d][2 + c] = fmaf(o[n][d][2 + c], 0x1p20f, add);
             }
         }
     finish_rows<D, T, NT>(a, q, base, ml, m, l, o, h, split, row0, rows, bad);
