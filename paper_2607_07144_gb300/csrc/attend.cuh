@@ -148,6 +148,47 @@ constexpr float kRef = 0x1p-20f, kLog2Ref = -20.0f;
 __device__ __forceinline__ float value_scale(float vs) { return fmaxf(vs, FKV_PAGE_MIN_SCALE); }
 __device__ __forceinline__ float share_of(float vs) { return __fdividef(kRef, vs); }
 
+// Two fp32 fused multiply-adds, or additions, in one instruction.
+__device__ __forceinline__ void fma2(float &x, float &y, float a, float b, float m, float c)
+{
+    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %4};\n\tmov.b64 u, {%5, %5};\n\t"
+        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "f"(a), "f"(b), "f"(m), "f"(c));
+}
+__device__ __forceinline__ void add2(float &x, float &y, float a, float b)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\t"
+        "add.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+
+// Two products of two, and two fused multiply-adds with an own factor each.
+__device__ __forceinline__ void mul2(float &x, float &y, float m)
+{
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\t"
+        "mul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(m));
+}
+__device__ __forceinline__ void fma2_each(float &x, float &y, float a, float b, float m, float n, float c, float d)
+{
+    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %5};\n\tmov.b64 u, {%6, %7};\n\t"
+        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(x), "=f"(y)
+        : "f"(a), "f"(b), "f"(m), "f"(n), "f"(c), "f"(d));
+}
+
+// x += a m, y += b m.
+__device__ __forceinline__ void acc2(float &x, float &y, float a, float b, float m)
+{
+    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %4};\n\t"
+        "fma.rn.f32x2 u, v, w, u;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b), "f"(m));
+}
+
 // Keys that a warp of the kernel for a few rows over 4-bit pages takes at a time (attend4.cu).
 constexpr int step4_keys(int nt) { return nt == 1 ? 64 : 32; }
 

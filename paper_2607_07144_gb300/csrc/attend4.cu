@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(128, 3)
     k_attend_step4(const AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
 {
     using S = Step4Shape<D, NT>;
-    constexpr int ST = S::stages, U = S::units, KW = S::keys, PT = kTile / KW, W = D / 32, MO = D / 16, R = 8 * NT;
+    constexpr int ST = S::stages, U = S::units, KW = S::keys, PT = kTile / KW /* 2 or 4 */, W = D / 32, MO = D / 16, R = 8 * NT;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[4 * ST];
     __shared__ Seen rows_see[4];                 // a warp's own: registers are short
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(128, 3)
     const int i0 = split * a.chunk, i1 = min(tiles.n, i0 + a.chunk);
     // the share's groups of keys, but for those behind all that any row sees; a warp's are
     // every fourth (a bias: from the last one back, see k_attend_step)
-    auto group_at = [&](int g) { return tiles.at(i0 + g / PT) * kTile + g % PT * KW; };
+    auto group_at = [&](int g) { return tiles.at(i0 + (g >> PT / 2)) * kTile + (g & (PT - 1)) * KW; };
     int groups = max(0, i1 - i0) * PT;
     while (groups > 0 && group_at(groups - 1) >= tiles.lim)
         --groups;
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(128, 3)
         int id;
         unsigned all;                  // which of the 32 units are looked at
     };
-    auto key_of = [&](int batch) { return first_key(batch * BI + lane / U) + lane % U * 16; };
+    auto key_of = [&](int batch) { return first_key(batch * BI + lane / U) + (lane & (U - 1)) * 16; };
     auto on = [&](int batch) { return batch * BI + lane / U < n_it && rows_see[warp].of(key_of(batch)); };
     auto ask = [&](int batch) { return on(batch) ? a.table[r * a.table_stride + a.div.div(key_of(batch))] : 0; };
     auto check = [&](int batch, int id) {
@@ -157,17 +157,17 @@ __global__ void __launch_bounds__(128, 3)
     };
     Unit cur = check(0, ask(0)), nxt = check(1, ask(1));
     int nid = ask(2);
-    auto units_of = [&](const Unit &u, int it) { return u.all >> (it % BI * U) & ((1u << U) - 1); };
+    auto units_of = [&](const Unit &u, unsigned it) { return u.all >> ((it & (BI - 1)) * U) & ((1u << U) - 1); };
     // Units are loaded as many together as pages hold whole ones of (2^box): a load takes some
     // 15 instructions, as its operands are the warp's.
     const int pieces = U >> a.box;
-    auto issue = [&](int it, int batch) {
+    auto issue = [&](unsigned it, unsigned batch) {
         const bool now = it / BI == batch;
         const unsigned units = units_of(now ? cur : nxt, it);
         const int x = lane & (pieces - 1), u = x << a.box, what = lane >> (31 - __clz(pieces));
         // (whichever of a piece's units any row sees has its page)
         const unsigned mine = units >> u & ((1u << (1 << a.box)) - 1);
-        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, it % BI * U + u + (mine ? __ffs(mine) - 1 : 0));
+        const int64_t id = __shfl_sync(~0u, now ? cur.id : nxt.id, (it & (BI - 1)) * U + u + (mine ? __ffs(mine) - 1 : 0));
         const int key = first_key(it) + u * 16, off = key - static_cast<int>(a.div.div(key)) * a.block;
         const uint32_t bar = bar0 + 8 * (it % ST), slot = it % ST;
         const unsigned heads = __ballot_sync(~0u, lane < pieces && mine);
@@ -274,24 +274,27 @@ __global__ void __launch_bounds__(128, 3)
         m[n][0] = m[n][1] = -INFINITY;
         l[n][0] = l[n][1] = mid[n][0] = mid[n][1] = 0.0f;
     }
+    // where a lane's codes lie among a unit's: K's of key gid, V's of key 2t
+    const uint32_t k_at = D == 128 ? gid * 64 + ((t ^ (gid >> 1 & 3)) << 4) : gid * 32 + t * 8;
+    const uint32_t v_at = D == 128 ? 2 * t * 64 + (((gid >> 1) ^ t) << 4 | (gid & 1) << 3) : 2 * t * 32 + gid * 4;
     const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 
-    int batch = 0;
-    for (int it = 0; it < n_it; ++it) {
+    unsigned batch = 0;
+    for (unsigned it = 0; static_cast<int>(it) < n_it; ++it) {
         if (it / BI != batch) {
             batch = it / BI;
             cur = nxt;
             nxt = check(batch + 1, nid);
             nid = ask(batch + 2);
         }
-        if (it + ST - 1 < n_it)
+        if (static_cast<int>(it) + ST - 1 < n_it)
             issue(it + ST - 1, batch);
         const int key = first_key(it);
         const unsigned units = units_of(cur, it);
         // (a lane that gives up takes its warp along: the others would meet it nowhere)
         if (!__all_sync(~0u, mbar_wait(bar0 + 8 * (it % ST), (it / ST) & 1, a.status))) {
             // give the loads in flight a while to land before the memory is used again
-            for (int k = it + 1; k < min(n_it, it + ST); ++k)
+            for (unsigned k = it + 1; k < min(static_cast<unsigned>(n_it), it + ST); ++k)
                 mbar_wait(bar0 + 8 * (k % ST), (k / ST) & 1, a.status, 2000000);
             __syncwarp();
             break;
@@ -324,13 +327,13 @@ __global__ void __launch_bounds__(128, 3)
             for (int v = 0; v < 2; ++v)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int kr = 16 * (u + v) + gid + 8 * x;
+                    const uint32_t at = kt + (16 * (u + v) + 8 * x) * (D / 2) + k_at;
                     if (D == 128) {
-                        const uint4 z = lds128(kt + kr * 64 + ((t ^ ((kr >> 1) & 3)) << 4));
+                        const uint4 z = lds128(at);
                         kw[v][x][0] = z.x, kw[v][x][1] = z.y;
                         kw[v][x][W - 2] = z.z, kw[v][x][W - 1] = z.w;
                     } else {
-                        const uint2 z = lds64(kt + kr * 32 + t * 8);
+                        const uint2 z = lds64(at);
                         kw[v][x][0] = z.x, kw[v][x][1] = z.y;
                     }
                 }
@@ -375,10 +378,13 @@ __global__ void __launch_bounds__(128, 3)
                 lvs[u][x] = num.z, share[u][x] = num.w;
                 const float off = caps ? 0.0f : num.z;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        sc[u][n][2 * x + c] = fmaf(sc[u][n][2 * x + c], num.x * rowmul[n][c], fmaf(num.y, rowsum[n][c], off));
+                for (int n = 0; n < NT; ++n) {
+                    float *const y = sc[u][n] + 2 * x;
+                    float m0 = rowmul[n][0], m1 = rowmul[n][1], b0, b1;
+                    mul2(m0, m1, num.x);
+                    fma2(b0, b1, rowsum[n][0], rowsum[n][1], num.y, off);
+                    fma2_each(y[0], y[1], y[0], y[1], m0, m1, b0, b1);
+                }
             }
         auto each = [&](auto &&f) {
 #pragma unroll
@@ -449,13 +455,11 @@ __global__ void __launch_bounds__(128, 3)
             for (int n = 0; n < NT; ++n) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    float p[2];
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        p[c] = ex2(sc[u][n][2 * x + c] - mref[n][c]);
-                        l[n][c] = fmaf(p[c], share[u][x], l[n][c]);
-                        mid[n][c] = fmaf(p[c], vmid[x], mid[n][c]);
-                    }
+                    float p[2] = {sc[u][n][2 * x], sc[u][n][2 * x + 1]};
+                    add2(p[0], p[1], -mref[n][0], -mref[n][1]);
+                    p[0] = ex2(p[0]), p[1] = ex2(p[1]);
+                    acc2(l[n][0], l[n][1], p[0], p[1], share[u][x]);
+                    acc2(mid[n][0], mid[n][1], p[0], p[1], vmid[x]);
                     pf[n][x] = transpose8(pack_half(p[0], p[1]));
                 }
                 mma16816(p_sum[n], ones, pf[n][0], pf[n][1]);
@@ -464,12 +468,12 @@ __global__ void __launch_bounds__(128, 3)
             uint32_t w[4][D / 64];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int row = 16 * u + 2 * t + (x & 1) + 8 * (x >> 1);
+                const uint32_t at = vt + (16 * u + (x & 1) + 8 * (x >> 1)) * (D / 2) + v_at;
                 if (D == 128) {
-                    const uint2 v = lds64(vt + row * 64 + ((((gid >> 1) ^ ((row >> 1) & 3)) << 4) | (gid & 1) << 3));
+                    const uint2 v = lds64(at);
                     w[x][0] = v.x, w[x][D / 64 - 1] = v.y;
                 } else {
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[x][0]) : "r"(vt + row * 32 + gid * 4));
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[x][0]) : "r"(at));
                 }
             }
 #pragma unroll

@@ -188,38 +188,6 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// Two fp32 fused multiply-adds, or additions, in one instruction.
-__device__ __forceinline__ void fma2(float &x, float &y, float a, float b, float m, float c)
-{
-    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %4};\n\tmov.b64 u, {%5, %5};\n\t"
-        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
-        : "=f"(x), "=f"(y)
-        : "f"(a), "f"(b), "f"(m), "f"(c));
-}
-__device__ __forceinline__ void add2(float &x, float &y, float a, float b)
-{
-    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\t"
-        "add.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
-        : "+f"(x), "+f"(y)
-        : "f"(a), "f"(b));
-}
-
-// Two products of two, and two fused multiply-adds with an own factor each.
-__device__ __forceinline__ void mul2(float &x, float &y, float m)
-{
-    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %2};\n\t"
-        "mul.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
-        : "+f"(x), "+f"(y)
-        : "f"(m));
-}
-__device__ __forceinline__ void fma2_each(float &x, float &y, float a, float b, float m, float n, float c, float d)
-{
-    asm("{\n\t.reg .b64 v, w, u;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %5};\n\tmov.b64 u, {%6, %7};\n\t"
-        "fma.rn.f32x2 v, v, w, u;\n\tmov.b64 {%0, %1}, v;\n\t}"
-        : "=f"(x), "=f"(y)
-        : "f"(a), "f"(b), "f"(m), "f"(n), "f"(c), "f"(d));
-}
-
 // Eight 4-bit codes less 7.5 as fp16 pairs (0, 4), (1, 5), (2, 6) and (3, 7): with the
 // code at bits 4 to 7 of a number of exponent 6, 64 + code is exact, less 71.5 as well.
 __device__ __forceinline__ void codes8_centred(uint32_t w, __half2 *f)
