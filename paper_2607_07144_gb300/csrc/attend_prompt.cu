@@ -21,14 +21,17 @@
 // 13 prompts of 1 to 1,000 tokens, 12 heads of 64: 39 us, bound by the start and
 // the end of a block.
 //
-// 4-bit pages: a code less 7.5 is exact in fp16 and is what K's tile holds; the key's
-// own step and middle come to the product in fp32, two fused operations a score on
-// numbers of the keys in shared memory (attend4.cu has the formula).  V's tile holds
-// values, middle + (c - 7.5) step, over the power of two that brings the largest of 16
-// keys' to [2^14, 2^15): rounded to fp16 once, half a step (2^-11) of the value down to
-// 2^-29 of the largest, what the weights are rounded to as well; that power is the unit's
-// value scale.  Eight codes of a word lie in a tile in the order 0 4 1 5 2 6 3 7, as masks
-// give them two at a time; so do the queries' elements, and the outputs' are put back.
+// 4-bit pages: a key, middle + (c - 7.5) step, is (c - 8) step, whose 11 bits fp16 holds,
+// and middle + step / 2 in every dimension.  K's tile holds the former over the power of
+// two that brings the largest of 16 keys' 8 steps to [2^14, 2^15), the unit's scale (where
+// one is below 2^-28 of that, to 2^-40); the latter times the query's sum is a step of 16
+// more dimensions: middle, middle, step / 2, step / 2 against the sum's upper and lower
+// half, twice.  So scores come out exactly as
+// over 8-bit pages.  V's tile holds whole values over such a power of two: rounded to fp16
+// once, half a step (2^-11) of the value down to 2^-29 of the unit's largest, what the
+// weights are rounded to as well.  Eight codes of a word lie in a tile in the order
+// 0 4 1 5 2 6 3 7, as masks give them two at a time; so do the queries' elements, and the
+// outputs' are put back.
 #include "attend.cuh"
 
 using namespace fkvd;
@@ -43,8 +46,8 @@ template <int D> struct PromptShape {
     static constexpr int half = 128 * 128;                   // 64 dimensions of 128 rows in fp16
     static constexpr int tile = half * (D / 64);             // 128 rows
     static constexpr int off_q = 0, off_k = 2 * tile, off_v = 4 * tile, off_n = 6 * tile;
-    static constexpr int numbers(int format) { return format == FKV_UINT4 ? 2 * 4 * 128 * 4 : 0; }   // of four tiles' 4-bit keys
-    static constexpr int smem(int format) { return off_n + numbers(format) + 1024; }
+    // 4-bit pages: 16 more dimensions of two tiles of keys, then of the groups' queries, 32 bytes each of 128-byte rows
+    static constexpr int smem(int format) { return off_n + (format == FKV_UINT4 ? half : 0) + 1024; }
 };
 
 enum { K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_EMPTY = 6, SC_FULL = 8, S_FULL = 12, P_FULL = 14, O_FULL = 16, Q_FULL = 18,
@@ -188,15 +191,17 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// Eight 4-bit codes less 7.5 as fp16 pairs (0, 4), (1, 5), (2, 6) and (3, 7): with the
-// code at bits 4 to 7 of a number of exponent 6, 64 + code is exact, less 71.5 as well.
-__device__ __forceinline__ void codes8_centred(uint32_t w, __half2 *f)
+// Eight 4-bit codes of a word as values, fp16 pairs (0, 4), (1, 5), (2, 6) and (3, 7), rounded
+// once: (c - less) step + add.  A code at bits 4 to 7 of an fp16 number with an exponent of 6
+// is 64 + c, exactly, and less 64 and 7.5 or 8 as well.
+__device__ __forceinline__ void codes8_half(uint32_t w, __half2 less, __half2 step, __half2 add, uint32_t *f)
 {
     const uint32_t x[4] = {w << 4, w, w >> 4, w >> 8};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t y = (x[i] & 0x00f000f0u) | 0x54005400u;
-        f[i] = __hsub2(*reinterpret_cast<const __half2 *>(&y), __half2half2(__ushort_as_half(0x5478)));
+        const __half2 z = __hfma2(__hsub2(*reinterpret_cast<const __half2 *>(&y), less), step, add);
+        f[i] = *reinterpret_cast<const uint32_t *>(&z);
     }
 }
 __device__ __forceinline__ uint32_t half2_bits(const __half2 &h) { return *reinterpret_cast<const uint32_t *>(&h); }
@@ -213,7 +218,6 @@ struct Row {
     float down;                 // what a score is multiplied by for the row's power of two
     int p, hi, from, pre;       // position and visible keys
     float slope;
-    float qs;                   // 4-bit pages: the query's sum, times down
 };
 
 // What is done to a score: nothing; a cap that is plain (attend.cuh), a bias by
@@ -236,9 +240,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     auto bar = [&](int i) { return smem_u32(bars) + 8 * i; };
-    // 4-bit pages: of the last four tiles' keys their two numbers times the scores' multiplier
-    float *const k_step = reinterpret_cast<float *>(raw + (sbase - smem_u32(raw)) + S::off_n), *const k_mid = k_step + 4 * 128;
-
     // the last rows of a causal prompt see the most keys: they go first
     int x = blockIdx.x;
     const int h = x % a.H;
@@ -277,29 +278,186 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     if (tid == 0) {
         rows_see = tiles.seen;
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(K_FULL + i), 2);
+            mbar_init(bar(K_FULL + i), FOUR ? 3 : 2);
             mbar_init(bar(K_EMPTY + i), 1);
-            mbar_init(bar(V_FULL + i), 2);
+            mbar_init(bar(V_FULL + i), FOUR ? 4 : 2);
             mbar_init(bar(V_EMPTY + i), 1);
             mbar_init(bar(S_FULL + i), 1);
             mbar_init(bar(P_FULL + i), 4);
             mbar_init(bar(O_FULL + i), 1);
         }
         for (int i = 0; i < 4; ++i)
-            mbar_init(bar(SC_FULL + i), 4);
+            mbar_init(bar(SC_FULL + i), FOUR ? 7 : 4);
         mbar_init(bar(Q_FULL), 128 * groups);
         mbar_init(bar(DRAIN), 1);
         fence_mbar_init();
     }
     if (warp == 12)
         tmem_alloc(smem_u32(&tmem_slot), 512);
+    if (FOUR) {
+        // (most of the 16 dimensions are no one's)
+        for (int i = tid; i < S::half / 16; i += kThreads)
+            sts128(sbase + S::off_n + 16 * i, 0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
-    if (group == 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // 4-bit codes to fp16 tiles: a warp's n (2 or 3) units of 16 keys from u0 on, of K or V.
+    // What 16 keys share, and every row's numbers, are one lane's a key; ids, codes and numbers
+    // are asked for as 8-bit pages' are below.
+    auto convert4 = [&](bool v_side, int u0, int n) {
+        constexpr int C = D / 32, RP = 32 / C, NL = 16 / RP;       // 16-byte pieces of a row, rows at a time, loads a unit
+        // eight lanes that store together hold the same piece of eight rows: other banks each
+        const int c = lane / RP, r0 = lane % RP;
+        const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
+        const uint32_t *const numbers = reinterpret_cast<const uint32_t *>(v_side ? a.vs : a.ks) + h * a.sch;
+        const float mul0 = score_multiplier(a, fabsf(a.scale));
+        const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
+        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 1) * S::half + (16 * u0 + r0) * 128;
+        const uint32_t sw = static_cast<uint32_t>((4 * (c & 1)) ^ (r0 & 7)) * 16;
+        const __half2 less = __half2half2(__ushort_as_half(v_side ? 0x5478 : 0x5480));        // 71.5, 72
+        bool bad = false, ok = true;           // (ok: see the softmax's)
+        auto first = [&](int j) { return tile_at(j) * kTile + 16 * u0; };
+        struct Page {
+            int id;
+            bool on;
+        };
+        auto ask = [&](int j) {
+            const int key = first(j) + 16 * lane;
+            Page p = {-1, j < n_it && lane < n && rows_see.of(key)};
+            if (p.on)
+                p.id = a.table[r * a.table_stride + a.div.div(key)];
+            return p;
+        };
+        auto check = [&](const Page &p) {
+            if (p.on && (p.id < 0 || p.id >= a.n_blocks)) {
+                bad = true;
+                return 0;
+            }
+            return p.id;
+        };
+        uint4 v[3][NL];
+        uint32_t num[2];                       // of keys lane and 32 + lane % 16; 0: not the request's, or not looked at
+        auto load = [&](uint4 (&x)[3][NL], int j, int id) {
+            int64_t from = -1, from_n = -1;
+            if (id >= 0) {
+                const int key = first(j) + 16 * lane, off = key - static_cast<int>(a.div.div(key)) * a.block;
+                from = id * a.sb + off * a.st, from_n = id * a.scb + off;
+            }
+            // all of them before the first load: a shuffle behind one waits for it as well
+            int64_t at[3], at_n[2];
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+                at[u] = __shfl_sync(~0u, from, u);
+            at_n[0] = __shfl_sync(~0u, from_n, lane >> 4), at_n[1] = __shfl_sync(~0u, from_n, 2);
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    x[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(pool + at[u] + i * RP * a.st)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                num[y] = at_n[y] >= 0 && first(j) + (y ? 32 + (lane & 15) : lane) < q.len ? __ldg(numbers + at_n[y] + (lane & 15)) : 0;
+        };
+        const Page start = ask(0);
+        Page after = ask(1);
+        load(v, 0, check(start));
+        int nid = check(after);
+        for (int j = 0; j < n_it; ++j) {
+            // nid: checked ids of tile j + 1.  All shuffles of an iteration come before its loads.
+            uint32_t by[2];                    // step and middle as they go into the tile
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const float step = __uint_as_float(num[y] << 16), mid = __uint_as_float(num[y] & 0xffff0000u);
+                float most = fmaf(8.0f, step, fabsf(mid));
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1)
+                    most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                // 2^e: the largest, no less than any value or 8 of any step, in [2^14, 2^15)
+                const int e = max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 14, -100);
+                const float unit = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+                const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+                by[y] = pack_half(step * inv, mid * inv);
+                if ((lane & 15) == 0 && (y == 0 || (lane == 0 && n == 3))) {
+                    const int at = u0 + (y ? 2 : lane >> 4);
+                    if (v_side)
+                        v_scales[j & 3][at] = make_float2(static_cast<float>(e), share_of(unit));
+                    else
+                        k_scales[j & 3][at] = unit * mul0;
+                }
+            }
+            uint32_t row_by[3][NL];            // and those of the lane's rows
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    row_by[u][i] = __shfl_sync(~0u, by[u >> 1], 16 * (u & 1) + i * RP + r0);
+            uint4 next[3][NL];
+            load(next, j + 1, nid);
+            after = ask(j + 2);
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(SC_FULL + (j & 3)));
+            const int st = j & 1;
+            if (j >= 2 && ok)
+                ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
+            if (!v_side) {
+                // the 16 more dimensions of the lane's keys
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const __half2 both = *reinterpret_cast<const __half2 *>(&by[y]);
+                    const int row = 16 * u0 + (y ? 32 + lane : lane);
+                    if (y == 0 || (n == 3 && lane < 16))
+                        sts128(sbase + S::off_n + row * 128 + (((2 * st) ^ (row & 7)) << 4), half2_bits(__high2half2(both)),
+                               half2_bits(__hmul2(__low2half2(both), __float2half2_rn(0.5f))), 0, 0);
+                }
+            }
+            const uint32_t tile = at0 + st * S::tile;
+#pragma unroll
+            for (int u = 0; u < 3; ++u) {
+                if (u == 2 && n == 2)
+                    break;
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const __half2 both = *reinterpret_cast<const __half2 *>(&row_by[u][i]), step = __low2half2(both);
+                    const __half2 add = v_side ? __high2half2(both) : __float2half2_rn(-0.0f);
+                    const uint32_t word[4] = {v[u][i].x, v[u][i].y, v[u][i].z, v[u][i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t f[4];
+                        codes8_half(word[k], less, step, add, f);
+                        sts128(tile + (16 * u + i * RP) * 128 + (sw ^ (16 * k)), f[0], f[1], f[2], f[3]);
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar(full_bar + st));
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                    v[u][i] = next[u][i];
+            nid = check(after);
+        }
+        if (bad)
+            atomicOr(a.status, FKV_ST_RANGE);
+    };
+
+    if (FOUR && group >= 2)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");       // (all warps of a group by the same instruction)
+    if (FOUR && group >= 2 && warp != 12) {
+        // 4-bit codes take more instructions: V's are four warps', K's three of the issuer's
+        // group's (units 0 to 2, 3 to 5, 6 and 7 of a tile).  (One place for both: what every
+        // warp executes competes for the instruction cache.)
+        convert4(group == 2, group == 2 ? 2 * (warp & 3) : 3 * (warp - 13), warp < 15 && group == 3 ? 3 : 2);
+    } else if (group == 3) {
+        if (!FOUR)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ---------------------------------------------------- MMA issuer
         // One elected thread follows the loop: what it waits for, it waits for alone.
         // (K's next tile is waited for before the weights; after the product with V it
@@ -315,6 +473,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             auto wait = [&](int b, int parity) { ok = ok && mbar_park(bar(b), parity, a.status); };
             auto scores = [&](int w, int j) {
                 umma_tile_ss<D>(tmem + 128 * w, q_d + w * step, k_d + (j & 1) * step, id_s);
+                if (FOUR)
+                    umma_f16(tmem + 128 * w, sdesc_sw128(sbase + S::off_n + 64 + 32 * w), sdesc_sw128(sbase + S::off_n + 32 * (j & 1)), id_s, 1);
                 umma_commit(bar(S_FULL + w));
             };
             if (elect_one()) {
@@ -350,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             __syncwarp();
         }
     } else if (group == 2) {
+        if constexpr (!FOUR) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         // ---------------------------------------------------- codes to fp16 tiles
         // warps 0 and 1 take K's keys 0 .. 63 and 64 .. 127 of a tile, 2 and 3 V's:
@@ -357,19 +518,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         // A lane moves 16-byte piece c of rows r0, r0 + RP, ...; eight lanes that
         // store together hold four pieces of two rows of different parity, which
         // the swizzle puts on different banks.
-        // (4-bit rows: eight lanes that store together hold the same piece of eight rows)
-        constexpr int RP = (FOUR ? 1024 : 512) / D, NL = 16 / RP; // rows at a time, loads a unit
+        constexpr int RP = 512 / D, NL = 16 / RP;                 // rows at a time, loads a unit
         const int w = warp & 1;
-        const int c = FOUR ? lane / RP : D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
-        const int r0 = FOUR ? lane % RP : D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+        const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+        const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
         const bool v_side = warp & 2;
         const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
         const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
         const float mul0 = score_multiplier(a, fabsf(a.scale));
         const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
         // where the lane's first row's two 16-byte halves go in a tile
-        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> (FOUR ? 1 : 2)) * S::half + (64 * w + r0) * 128;
-        const uint32_t sw = static_cast<uint32_t>((FOUR ? 4 * (c & 1) : 2 * (c & 3)) ^ (r0 & 7)) * 16;
+        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
+        const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
         const int64_t row_step = RP * a.st;
         bool bad = false, ok = true;           // (ok: see the softmax's)
         // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
@@ -394,24 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             }
             return p.id;
         };
-        auto ask_scale = [&](int id) { return !FOUR && id >= 0 ? scale_of[id * a.scb] : 1.0f; };
-        // 4-bit rows: the numbers of the lane's keys l and l + 32 (0: not one of the request's
-        // or not looked at)
-        uint32_t num[2];
-        auto ask_numbers = [&](int j, int id) {
-            int64_t from = -1;
-            if (id >= 0) {
-                const int key = first(j) + 16 * lane;
-                from = id * a.scb + key - static_cast<int>(a.div.div(key)) * a.block;
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int64_t at = __shfl_sync(~0u, from, 2 * x + (lane >> 4));
-                num[x] = 0;
-                if (at >= 0 && first(j) + 32 * x + lane < q.len)
-                    num[x] = __ldg(reinterpret_cast<const uint32_t *>(scale_of) + at + (lane & 15));
-            }
-        };
+        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
         uint4 v[4][NL];
         auto load = [&](int j, int id) {
             // the unit's first row in the pool, from the lane that knows its page
@@ -438,36 +581,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         int nid = check(start);
         load(0, nid);
         float scale = ask_scale(nid);
-        if (FOUR)
-            ask_numbers(0, nid);
         nid = check(after);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1
             after = ask(j + 2);
-            uint32_t by[2] = {0, 0};           // 4-bit values: step and middle as they go into the tile
-            if (FOUR && !v_side) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    k_step[(j & 3) * 128 + 64 * w + 32 * x + lane] = num[x] ? __uint_as_float(num[x] << 16) * mul0 : 1.0f;
-                    k_mid[(j & 3) * 128 + 64 * w + 32 * x + lane] = __uint_as_float(num[x] & 0xffff0000u) * mul0;
-                }
-            } else if (FOUR) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float step = __uint_as_float(num[x] << 16), mid = __uint_as_float(num[x] & 0xffff0000u);
-                    float most = fmaf(7.5f, step, fabsf(mid));
-#pragma unroll
-                    for (int o = 1; o < 16; o <<= 1)
-                        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-                    // 2^e, at most 2^-14 of the largest
-                    const int e = max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 14, -100);
-                    const float unit = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-                    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-                    by[x] = pack_half(step * inv, mid * inv);
-                    if ((lane & 15) == 0)
-                        v_scales[j & 3][4 * w + 2 * x + (lane >> 4)] = make_float2(static_cast<float>(e), share_of(unit));
-                }
-            } else if (lane < 4) {
+            if (lane < 4) {
                 if (v_side) {
                     const float vs = value_scale(scale);
                     v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vs));
@@ -476,8 +594,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 }
             }
             scale = ask_scale(nid);
-            if (FOUR)
-                ask_numbers(j + 1, nid);
             __syncwarp();
             if (lane == 0)
                 mbar_arrive(bar(SC_FULL + (j & 3)));
@@ -485,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             if (j >= 2 && ok)
                 ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
             const int first_key = first(j);
-            if (!FOUR && v_side && first_key + 64 > q.len) {
+            if (v_side && first_key + 64 > q.len) {
                 // rows behind the request's end hold any bytes, NaN codes among them
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -499,28 +615,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
-                    if (FOUR) {
-                        __half2 step, mid;
-                        if (v_side) {
-                            const uint32_t n = __shfl_sync(~0u, by[u >> 1], 16 * (u & 1) + i * RP + r0);
-                            const __half2 both = *reinterpret_cast<const __half2 *>(&n);
-                            step = __low2half2(both), mid = __high2half2(both);
-                        }
-                        const uint32_t word[4] = {v[u][i].x, v[u][i].y, v[u][i].z, v[u][i].w};
-                        const uint32_t at = tile + (16 * u + i * RP) * 128;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            __half2 f[4];
-                            codes8_centred(word[k], f);
-                            if (v_side) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    f[e] = __hfma2(f[e], step, mid);
-                            }
-                            sts128(at + (sw ^ (16 * k)), half2_bits(f[0]), half2_bits(f[1]), half2_bits(f[2]), half2_bits(f[3]));
-                        }
-                        continue;
-                    }
                     uint32_t f[8];
                     codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].x, f[0], f[1]);
                     codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].y, f[2], f[3]);
@@ -540,6 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         }
         if (bad)
             atomicOr(a.status, FKV_ST_RANGE);
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         // ---------------------------------------------------- softmax
@@ -549,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
             const int64_t tok = q.tok0 + i, head = h * a.G + u;
             Row st;
-            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f, st.qs = 0.0f;
+            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f;
             st.p = q.p0 + i;
             const RowMask mask(a, q, st.p, live);
             st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
@@ -563,6 +658,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             auto piece = [&](int r, int k) { return q_tile + (k >> 3) * S::half + r * 128 + (((k & 7) ^ (r & 7)) << 4); };
             {
                 constexpr int LR = D / 8, RI = 32 / LR;                  // rows at a time
+                // (with 4-bit keys rows of either type are scaled, and to less, so that fp16
+                // holds their sums: elements below 2^-22 of the largest are rounded to 2^-33 of it)
+                constexpr int TOP = FOUR ? 7 : 14;
+                float all = 0.0f;                                        // the lane's row's sum
                 const int c = lane % LR, rr = lane / LR;
                 uint4 v[LR];
 #pragma unroll
@@ -578,10 +677,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                 for (int k = 0; k < LR; ++k) {
                     uint32_t y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-                    if (std::is_same<T, __half>::value) {
+                    if (!FOUR && std::is_same<T, __half>::value) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             y[e] ^= a.scale < 0.0f ? 0x80008000u : 0u;
+                    } else if (std::is_same<T, __half>::value) {
+                        float m = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&y[e]));
+                            m = fmaxf(m, fmaxf(fabsf(z.x), fabsf(z.y)));
+                        }
+#pragma unroll
+                        for (int o = 1; o < LR; o *= 2)
+                            m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+                        const int e2 = max(static_cast<int>(__float_as_uint(m) >> 23) - 127, -100);
+                        float up = __uint_as_float(static_cast<uint32_t>(127 + TOP - e2) << 23);
+                        const float down = __uint_as_float(static_cast<uint32_t>(127 - TOP + e2) << 23);
+                        const float mine = __shfl_sync(~0u, down, lane % RI * LR);
+                        if (lane / RI == k)
+                            st.down = mine;
+                        up = a.scale < 0.0f ? -up : up;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&y[e]));
+                            y[e] = pack_half(z.x * up, z.y * up);
+                        }
                     } else {
                         // brought to [2^14, 2^15) by a power of two (see attend.cu)
                         uint32_t m = 0;
@@ -593,8 +714,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         for (int o = 1; o < LR; o *= 2)
                             m = max(m, __shfl_xor_sync(~0u, m, o));
                         const int e2 = max(static_cast<int>(m >> 7) - 127, -100);
-                        float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - e2) << 23);
-                        const float down = __uint_as_float(static_cast<uint32_t>(127 - 14 + e2) << 23);
+                        float up = __uint_as_float(static_cast<uint32_t>(127 + TOP - e2) << 23);
+                        const float down = __uint_as_float(static_cast<uint32_t>(127 - TOP + e2) << 23);
                         const float mine = __shfl_sync(~0u, down, lane % RI * LR);
                         if (lane / RI == k)
                             st.down = mine;
@@ -616,14 +737,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                             sum += __shfl_xor_sync(~0u, sum, o);
                         const float mine = __shfl_sync(~0u, sum, lane % RI * LR);
                         if (lane / RI == k)
-                            st.qs = mine;
+                            all = mine;
                         sts128(piece(k * RI + rr, c), __byte_perm(y[0], y[2], 0x5410), __byte_perm(y[0], y[2], 0x7632),
                                __byte_perm(y[1], y[3], 0x5410), __byte_perm(y[1], y[3], 0x7632));
                     } else {
                         sts128(piece(k * RI + rr, c), y[0], y[1], y[2], y[3]);
                     }
                 }
-                st.qs *= st.down;
+                if (FOUR) {
+                    const float hi = __half2float(__float2half_rn(all));
+                    const uint32_t both = pack_half(hi, all - hi);
+                    const int rl = 32 * (warp & 3) + lane;
+                    sts128(sbase + S::off_n + rl * 128 + (((4 + 2 * w) ^ (rl & 7)) << 4), both, both, 0, 0);
+                }
                 fence_proxy_async_smem();
                 mbar_arrive(bar(Q_FULL));
             }
@@ -647,20 +773,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 float km_r[8], vo_r[8];
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
-                    km_r[n] = FOUR ? 1.0f : km[n] * st.down, vo_r[n] = vm[n].x;
-                // 4-bit keys: products to scores, steps and middles four keys at a time
-                const float4 *const ks4 = reinterpret_cast<const float4 *>(k_step + (j & 3) * 128);
-                const float4 *const km4 = reinterpret_cast<const float4 *>(k_mid + (j & 3) * 128);
-                auto own_numbers = [&](float *s, int at, float off) {
-                    const float4 step = ks4[at >> 2], mid = km4[at >> 2];
-                    float u0, u1, u2, u3;
-                    fma2(u0, u1, mid.x, mid.y, st.qs, off);
-                    fma2(u2, u3, mid.z, mid.w, st.qs, off);
-                    mul2(s[0], s[1], st.down);
-                    mul2(s[2], s[3], st.down);
-                    fma2_each(s[0], s[1], s[0], s[1], step.x, step.y, u0, u1);
-                    fma2_each(s[2], s[3], s[2], s[3], step.z, step.w, u2, u3);
-                };
+                    km_r[n] = km[n] * st.down, vo_r[n] = vm[n].x;
                 ok = ok && mbar_park(bar(S_FULL + w), j & 1, a.status);
                 tc_fence_after();
                 // the visible ones of 32 keys as bits: ranges meet as words, and a score's
@@ -671,11 +784,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 };
                 // products to scores in base 2 where a cap or a bias is between them
                 auto general = [&](float *s, int half, const float *mul, const float *off) {
-                    if (FOUR) {
-#pragma unroll
-                        for (int e = 0; e < 64; e += 4)
-                            own_numbers(s + e, 64 * half + e, 0.0f);
-                    }
                     if (SCORES == SCORES_LARGE_CAP) {
                         // mostly no score is near the cap, and the series is all there is to do
                         float most = 0.0f;
@@ -724,13 +832,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                             for (int e = 16 * n; e < 16 * n + 16; e += 2) {
                                 float y0, y1;
-                                if (FOUR && !GEN) {
-                                    if (e % 4 == 0)
-                                        own_numbers(s + e, 64 * half + e, o);
-                                    y0 = s[e], y1 = s[e + 1];
-                                } else {
-                                    fma2(y0, y1, s[e], s[e + 1], mul, o);
-                                }
+                                fma2(y0, y1, s[e], s[e + 1], mul, o);
                                 y0 = ex2(y0), y1 = ex2(y1);
                                 add2(sx, sy, y0, y1);
                                 p[e >> 1] = pack_half(y0, y1);
@@ -801,11 +903,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     float mul[4], off[4];
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
-                        mul[n] = FOUR ? 1.0f : km[4 * k + n] * st.down;
+                        mul[n] = km[4 * k + n] * st.down;
                         off[n] = vm[4 * k + n].x;
                     }
-                    if (GEN || FOUR || !full) {
-                        if (GEN || FOUR) {
+                    if (GEN || !full) {
+                        if (GEN) {
                             general(s, k, mul, off);
                         } else {
 #pragma unroll
