@@ -179,7 +179,7 @@ template <int LANES> __device__ __forceinline__ bool put4(float *x, const Groups
 // (D / 16 threads each) and `per` heads of them, several at a time.
 template <int D, int FMT, typename T> __device__ __forceinline__ void append_rows(const AppendArgs &a, unsigned task)
 {
-    constexpr int C = D / 16, R = 32 / C, B = sizeof(T) == 4 ? 2 : 4;
+    constexpr int C = D / 16, R = 32 / C, B = sizeof(T) == 4 ? 2 : 4;       // B heads in flight
     const int lane = threadIdx.x & 31, c = lane % C;
     const unsigned group = a.by_chunks.div(task);
     const int u0 = static_cast<int>(task - group * a.chunks) * a.per, u1 = min(u0 + a.per, a.row_heads);
@@ -248,7 +248,7 @@ template <int D, int FMT, typename T> __device__ __forceinline__ void append_row
 // run, one head, K or V.
 template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void append_runs(const AppendArgs &a, unsigned item)
 {
-    constexpr int C = D / 16, R = GT / C, KEEP = 4;        // 16-element pieces a row, rows at a time, kept of them
+    constexpr int C = D / 16, R = GT / C, KEEP = sizeof(T) == 4 ? 2 : 4;        // 16-element pieces a row, rows at a time, kept of them
     __shared__ uint32_t red[GT / 32];
     const int lane = threadIdx.x & 31, tid = GT == 32 ? lane : threadIdx.x, c = tid % C, row0 = tid / C;
     const unsigned both = a.by_heads.div(item);
@@ -267,17 +267,18 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
         const int64_t s = a.slots[t];
         return p < 0 || p >= a.n_pos ? -1 : s;
     };
-    // the thread's elements of a token's row, turned (rows behind a run are loaded
-    // before its length is known: their positions may be any)
-    auto row_of = [&](int64_t t, float *v) {
-        const Raw<T> r = load_groups<T>(x + t * x_tok, g);
+    // the thread's elements of a token's row, and what they are turned (twice, for the largest
+    // magnitude and the codes: kept turned they would take twice the registers)
+    auto raw_of = [&](int64_t t) { return load_groups<T>(x + t * x_tok, g); };
+    auto turned = [&](const Raw<T> &r, int64_t t, float *v) {
         load16<T>(reinterpret_cast<const T *>(&r), v);
         if (g.f >= 0) {
             Turn turn;
-            turn.load(a, min(max(static_cast<int64_t>(a.pos[t]), int64_t(0)), a.n_pos - 1), g.f);
+            turn.load(a, a.pos[t], g.f);
             turn.apply(v, a.pairs);
         }
     };
+    auto row_of = [&](int64_t t, float *v) { turned(raw_of(t), t, v); };
     auto most_of = [](const float *v, uint32_t m) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -306,11 +307,11 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
             const int64_t t = base + who, slot = __shfl_sync(~0u, slot_l, who), blk = a.by_block.div(static_cast<unsigned>(slot));
             const int off = static_cast<int>(slot - blk * a.block);
             const int most = static_cast<int>(min(static_cast<int64_t>(a.block - off), a.T - t));
-            float keep[KEEP][16];
+            Raw<T> keep[KEEP];
 #pragma unroll
             for (int k = 0; k < KEEP; ++k)
                 if ((GT > 32 || k == 0) && row0 + k * R < most)
-                    row_of(t + row0 + k * R, keep[k]);
+                    keep[k] = raw_of(t + row0 + k * R);
             int len = most;
             for (int i = 0; i < most; i += 32) {
                 const unsigned off_run = __ballot_sync(~0u, i + lane < most && slot_of(t + i + lane) != slot + i + lane);
@@ -326,13 +327,16 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
 #pragma unroll
                 for (int k = 1; k < KEEP; ++k)
                     if (row0 + k * R < len)
-                        row_of(t + row0 + k * R, keep[k]);
+                        keep[k] = raw_of(t + row0 + k * R);
             }
             uint32_t amax_u = 0;
 #pragma unroll
             for (int k = 0; k < KEEP; ++k)
-                if (row0 + k * R < len)
-                    amax_u = most_of(keep[k], amax_u);
+                if (row0 + k * R < len) {
+                    float v[16];
+                    turned(keep[k], t + row0 + k * R, v);
+                    amax_u = most_of(v, amax_u);
+                }
             for (int i = row0 + KEEP * R; i < len; i += R) {
                 float v[16];
                 row_of(t + i, v);
@@ -379,8 +383,11 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
             if (!odd) {
 #pragma unroll
                 for (int k = 0; k < KEEP; ++k)
-                    if (row0 + k * R < len)
-                        put(off + row0 + k * R, codes16_inside<FMT>(keep[k], inv));
+                    if (row0 + k * R < len) {
+                        float v[16];
+                        turned(keep[k], t + row0 + k * R, v);
+                        put(off + row0 + k * R, codes16_inside<FMT>(v, inv));
+                    }
             }
             for (int i = odd ? row0 : row0 + KEEP * R; i < len; i += R) {
                 float v[16];
@@ -408,7 +415,11 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
         atomicOr(a.status, FKV_ST_RANGE);
 }
 
-template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads) k_page_append(const AppendArgs a)
+// Bytes bound long calls, and a few blocks an SM more or less what is in flight of them: 9
+// prompts of 1,000 to 8,192 tokens (32 query and 8 KV heads of 128, bf16) into 4-bit pages
+// 193 us, 5.6 TB/s, with six blocks an SM, 216 without the limit, 252 with eight (spills); into
+// e4m3 pages 242 us with five, 277 with six, 335 with turned rows kept in fp32.
+template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads, FMT == FKV_UINT4 ? 6 : 5) k_page_append(const AppendArgs a)
 {
     if (FMT == FKV_UINT4 || blockIdx.x < a.row_blocks)
         append_rows<D, FMT, T>(a, blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5));
@@ -432,7 +443,9 @@ template <int D, int FMT, typename T> cudaError_t append_as(const AppendArgs &a,
         return cudaGetLastError();
     }
     const int64_t items = (a.T + a.stretch - 1) / a.stretch * 2 * a.heads;
-    if (a.stretch == 1)
+    // a warp a run where it takes four rows a lane at most: a block's other threads had none
+    // (13 GPT-2-shaped prompts, pages of 16: 31 us against 52)
+    if (a.stretch == 1 || a.block * (D / 16) <= 32 * 4)
         k_page_append<D, FMT, T, 32><<<a.row_blocks + static_cast<unsigned>((items + 3) / 4), kAppendThreads, 0, st>>>(a);
     else
         k_page_append<D, FMT, T, FMT == FKV_UINT4 ? 32 : kAppendThreads>
