@@ -16,6 +16,8 @@
 // 2^-32 of the largest weight is lost), and the sum of the weights is
 // sum P_j / vs, from the unrounded P_j, in fp32 (share_of).  So pages of any
 // scales mix in one accumulator without a rounding of V.
+#include <algorithm>
+
 #include "attend_step.cuh"
 
 using namespace fkvd;
@@ -528,7 +530,7 @@ struct Plan {
 // Which kernel serves the call, and how many shares the keys are split into.
 // Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step
 // kernel, more to the tensor-memory one (nt = 0): for 24 sequences of 3-16k
-// positions and 8 heads of 128, 63 rows take 384 us against 236; 28 rows 265
+// positions and 8 heads of 128 in 8-bit pages, 63 rows take 384 us against 236; 28 rows 265
 // against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
 // 4,096 and 283 against 364 with a cap.  A block's time is its keys plus a fixed
 // part (its launch, the first loads' latency and its end: about that of 384 keys);
@@ -546,7 +548,15 @@ Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
     p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
     const int per = p.nt ? 8 * p.nt : prompt_rows();
     p.row_tiles = static_cast<int>((most + per - 1) / per);
-    const int64_t blocks = c.n_req * H * p.row_tiles, slots = p.nt ? ctx->sms * 3 : ctx->sms;
+    const int64_t blocks = c.n_req * H * p.row_tiles, slots = ctx->sms * (p.nt == 0 ? 1 : c.pages->format == FKV_UINT4 ? step4_blocks(p.nt) : 3);
+    // Of 4-bit pages, the blocks that will have rows, as far as the number of tokens tells:
+    // others end at once, and no wave has to be saved for them (24 requests of 2 to 7 tokens,
+    // 4 query heads each: 66 us, 83 with all their second tiles counted).
+    int64_t busy = blocks;
+    if (c.pages->format == FKV_UINT4) {
+        const int64_t tiles = std::max(std::min(c.n_req, c.n_tok), (c.n_tok * G + per - 1) / per + c.n_req / 3);
+        busy = H * std::min(tiles, c.n_req * p.row_tiles);
+    }
     // all that a block of rows may look at: with a window, that and the sinks (whose
     // tiles end apart); a prefix may be of any length
     int64_t span = c.max_len;
@@ -563,7 +573,7 @@ Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
     const int most_splits = c.n_tok * c.n_q_heads > INT32_MAX ? 1 : static_cast<int>(room < kMaxSplits ? room : kMaxSplits);
     for (int s = 1; s <= most_splits && s <= tiles; ++s) {
         const int chunk = (tiles + s - 1) / s;
-        const int64_t waves = (blocks * s + slots - 1) / slots;
+        const int64_t waves = (busy * s + slots - 1) / slots;
         const bool in_cluster = p.nt && s > 1 && s <= kMaxCluster && blocks * s <= slots;
         const double join = s == 1 ? 0.0 : in_cluster ? 100.0 : 512.0 + 8.0 * s;
         const double cost = waves * (chunk * kTile + 384.0) + join;
@@ -632,7 +642,7 @@ int page_attend_box(const fkv_ctx *ctx, const fkv_attend &c)
 {
     if (c.pages->format != FKV_UINT4)
         return 16;
-    const int nt = plan_of(ctx, c).nt, most = nt ? step4_keys(nt) : 16;
+    const int most = plan_of(ctx, c).nt ? kStep4Keys : 16;
     int box = 16;
     while (box < most && c.pages->block % (2 * box) == 0)
         box *= 2;

@@ -190,7 +190,9 @@ __device__ __forceinline__ void acc2(float &x, float &y, float a, float b, float
 }
 
 // Keys that a warp of the kernel for a few rows over 4-bit pages takes at a time (attend4.cu).
-constexpr int step4_keys(int nt) { return nt == 1 ? 64 : 32; }
+constexpr int kStep4Keys = 64;
+// And its blocks an SM, for one or two tiles of 8 rows (registers).
+constexpr int step4_blocks(int nt) { return nt == 1 ? 3 : 2; }
 
 }  // namespace fkvd
 
