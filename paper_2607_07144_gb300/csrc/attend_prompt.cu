@@ -29,7 +29,7 @@
 // half, twice.  So scores come out exactly as
 // over 8-bit pages.  V's tile holds whole values over such a power of two: rounded to fp16
 // once, half a step (2^-11) of the value down to 2^-29 of the unit's largest, what the
-// weights are rounded to as well.  Eight codes of a word lie in a tile in the order
+// weights are rounded to as well (for bfloat16 outputs; see EXACT).  Eight codes of a word lie in a tile in the order
 // 0 4 1 5 2 6 3 7, as masks give them two at a time; so do the queries' elements, and the
 // outputs' are put back.
 #include "attend.cuh"
@@ -47,7 +47,9 @@ template <int D> struct PromptShape {
     static constexpr int tile = half * (D / 64);             // 128 rows
     static constexpr int off_q = 0, off_k = 2 * tile, off_v = 4 * tile, off_n = 6 * tile;
     // 4-bit pages: 16 more dimensions of two tiles of keys, then of the groups' queries, 32 bytes each of 128-byte rows
-    static constexpr int smem(int format) { return off_n + (format == FKV_UINT4 ? half : 0) + 1024; }
+    // (and of four tiles' values what all dimensions of a key have, see EXACT)
+    static constexpr int off_h = off_n + half;
+    static constexpr int smem(int format) { return (format == FKV_UINT4 ? off_h + 4 * 128 * 4 : off_n) + 1024; }
 };
 
 enum { K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_EMPTY = 6, SC_FULL = 8, S_FULL = 12, P_FULL = 14, O_FULL = 16, Q_FULL = 18,
@@ -218,6 +220,7 @@ struct Row {
     float down;                 // what a score is multiplied by for the row's power of two
     int p, hi, from, pre;       // position and visible keys
     float slope;
+    float mid;                  // EXACT: the weighted sum of what all dimensions of a value have
 };
 
 // What is done to a score: nothing; a cap that is plain (attend.cuh), a bias by
@@ -230,6 +233,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 {
     using S = PromptShape<D>;
     constexpr bool GEN = SCORES != SCORES_PLAIN, FOUR = FMT == FKV_UINT4;
+    // Outputs of 11 bits show a rounding of V as much as that of the weights: for them V's
+    // tile, too, holds (c - 8) step, exactly, and the weighted sum of middle + step / 2 is
+    // kept in fp32 beside the sum of weights.
+    constexpr bool EXACT = FOUR && std::is_same<T, __half>::value;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     // of the last four tiles' units of 16 keys: the scores' multiplier; log2 vs and share_of(vs)
@@ -305,6 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
 
+    float *const v_mids = reinterpret_cast<float *>(raw + (sbase - smem_u32(raw)) + S::off_h);
     // 4-bit codes to fp16 tiles: a warp's n (2 or 3) units of 16 keys from u0 on, of K or V.
     // What 16 keys share, and every row's numbers, are one lane's a key; ids, codes and numbers
     // are asked for as 8-bit pages' are below.
@@ -318,7 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
         const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 1) * S::half + (16 * u0 + r0) * 128;
         const uint32_t sw = static_cast<uint32_t>((4 * (c & 1)) ^ (r0 & 7)) * 16;
-        const __half2 less = __half2half2(__ushort_as_half(v_side ? 0x5478 : 0x5480));        // 71.5, 72
+        const bool whole = v_side && !EXACT;   // values, middle and all
+        const __half2 less = __half2half2(__ushort_as_half(whole ? 0x5478 : 0x5480));         // 71.5, 72
         bool bad = false, ok = true;           // (ok: see the softmax's)
         auto first = [&](int j) { return tile_at(j) * kTile + 16 * u0; };
         struct Page {
@@ -381,6 +390,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const float unit = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
                 const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
                 by[y] = pack_half(step * inv, mid * inv);
+                if (EXACT && v_side && (y == 0 || (n == 3 && lane < 16)))
+                    v_mids[(j & 3) * 128 + 16 * u0 + (y ? 32 : 0) + lane] = fmaf(0.5f, step, mid) * inv;
                 if ((lane & 15) == 0 && (y == 0 || (lane == 0 && n == 3))) {
                     const int at = u0 + (y ? 2 : lane >> 4);
                     if (v_side)
@@ -423,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
                     const __half2 both = *reinterpret_cast<const __half2 *>(&row_by[u][i]), step = __low2half2(both);
-                    const __half2 add = v_side ? __high2half2(both) : __float2half2_rn(-0.0f);
+                    const __half2 add = whole ? __high2half2(both) : __float2half2_rn(-0.0f);
                     const uint32_t word[4] = {v[u][i].x, v[u][i].y, v[u][i].z, v[u][i].w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -644,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int i = live ? static_cast<int>(a.gdiv.div(row)) : 0, u = live ? row - i * a.G : 0;
             const int64_t tok = q.tok0 + i, head = h * a.G + u;
             Row st;
-            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f;
+            st.m = live ? -INFINITY : 0.0f, st.l = 0.0f, st.down = 1.0f, st.mid = 0.0f;
             st.p = q.p0 + i;
             const RowMask mask(a, q, st.p, live);
             st.hi = mask.hi, st.from = mask.from, st.pre = mask.pre;
@@ -768,6 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const int key = tile_at(j) * kTile;
                 const float *const km = k_scales[j & 3];
                 const float2 *const vm = v_scales[j & 3];
+                const float4 *const mids = reinterpret_cast<const float4 *>(v_mids + (j & 3) * 128);
                 const bool full = all_see(a, q, ga, gb, key, key + kTile);
                 // before the scores are there: the pages' multipliers
                 float km_r[8], vo_r[8];
@@ -822,9 +834,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 // second's products on their way while the first's weights are stored.
                 int k = 0, again = j == 0;
                 if (j > 0) {
-                    float s[64], sum[4];
+                    float s[64], sum[4], mid[2];
                     uint32_t p[32];
                     auto evaluate = [&](int half) {
+                        mid[0] = mid[1] = 0.0f;
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
                             float sx = 0.0f, sy = 0.0f;
@@ -835,6 +848,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                                 fma2(y0, y1, s[e], s[e + 1], mul, o);
                                 y0 = ex2(y0), y1 = ex2(y1);
                                 add2(sx, sy, y0, y1);
+                                if (EXACT) {
+                                    const float4 h = mids[16 * half + e / 4];
+                                    fma2_each(mid[0], mid[1], y0, y1, e % 4 ? h.z : h.x, e % 4 ? h.w : h.y, mid[0], mid[1]);
+                                }
                                 p[e >> 1] = pack_half(y0, y1);
                             }
                             sum[n] = sx + sy;
@@ -869,6 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                         for (int n = 0; n < 4; ++n)
                             st.l = fmaf(sum[n], vm[n].y, st.l);
+                        st.mid += mid[0] + mid[1];
                         // fp16 pairs in the tile's first columns, which have been read
                         tmem_st16(s_t, p);
                         tmem_st16(s_t + 16, p + 16);
@@ -884,6 +902,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                             for (int n = 0; n < 4; ++n)
                                 st.l = fmaf(sum[n], vm[4 + n].y, st.l);
+                            st.mid += mid[0] + mid[1];
                             tmem_st16(s_t + 32, p);
                             tmem_st16(s_t + 48, p + 16);
                             k = 2;
@@ -942,6 +961,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                         const float half = to == st.m ? 1.0f : ex2(0.5f * (st.m - to));
                         st.m = to;
                         st.l = st.l * half * half;
+                        st.mid *= f;
                         // the products so far are done: their commit came before this tile's scores'
                         if (j > 0) {
 #pragma unroll 1
@@ -973,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     }
                     const float base = again && st.m == -INFINITY ? 0.0f : st.m;
                     uint32_t p[32];
-                    float sum[4];
+                    float sum[4], mid[2] = {0.0f, 0.0f};
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
                         float sx = 0.0f, sy = 0.0f;
@@ -984,6 +1004,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                             fma2(y0, y1, s[e], s[e + 1], mul[n], o);
                             y0 = ex2(y0), y1 = ex2(y1);
                             add2(sx, sy, y0, y1);
+                            if (EXACT) {
+                                const float4 h = mids[16 * k + e / 4];
+                                fma2_each(mid[0], mid[1], y0, y1, e % 4 ? h.z : h.x, e % 4 ? h.w : h.y, mid[0], mid[1]);
+                            }
                             p[e >> 1] = pack_half(y0, y1);
                         }
                         sum[n] = sx + sy;
@@ -997,6 +1021,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
                         st.l = fmaf(sum[n], vm[4 * k + n].y, st.l);
+                    st.mid += mid[0] + mid[1];
                     // fp16 pairs in the tile's first columns, which have been read
                     tmem_st16(s_t + 32 * k, p);
                     tmem_st16(s_t + 32 * k + 16, p + 16);
@@ -1043,7 +1068,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 // a row that saw nothing has no products either: tensor memory holds anything
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                    o[e] = st.l != 0.0f ? o[e] * inv : 0.0f;
+                    o[e] = st.l != 0.0f ? (EXACT ? o[e] + st.mid : o[e]) * inv : 0.0f;
                 // dimension e of the 32 (4-bit pages: see the codes' order)
                 auto dim = [&](int e) { return FOUR ? o[(e & ~7) | (e << 1 & 6) | (e >> 2 & 1)] : o[e]; };
                 if (a.splits == 1) {
