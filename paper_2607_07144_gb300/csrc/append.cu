@@ -418,20 +418,23 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
 // Bytes bound long calls, and a few blocks an SM more or less what is in flight of them: 9
 // prompts of 1,000 to 8,192 tokens (32 query and 8 KV heads of 128, bf16) into 4-bit pages
 // 193 us, 5.6 TB/s, with six blocks an SM, 216 without the limit, 252 with eight (spills); into
-// e4m3 pages 242 us with five, 277 with six, 335 with turned rows kept in fp32.
+// e4m3 pages 242 us with five, 277 with six, 335 with turned rows kept in fp32 (238 in this order).
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads, FMT == FKV_UINT4 ? 6 : 5) k_page_append(const AppendArgs a)
 {
-    if (FMT == FKV_UINT4 || blockIdx.x < a.row_blocks)
-        append_rows<D, FMT, T>(a, blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5));
+    // the runs, whose chains are longer, first (238 us against 242)
+    const unsigned runs = gridDim.x - a.row_blocks, block = blockIdx.x < runs ? blockIdx.x + a.row_blocks : blockIdx.x - runs;
+    if (FMT == FKV_UINT4 || block < a.row_blocks)
+        append_rows<D, FMT, T>(a, block * (kAppendThreads / 32) + (threadIdx.x >> 5));
     else if (FMT != FKV_UINT4)
         append_runs<D, FMT == FKV_UINT4 ? FKV_E4M3 : FMT, T, GT>(
-            a, GT == 32 ? (blockIdx.x - a.row_blocks) * (kAppendThreads / 32) + (threadIdx.x >> 5) : blockIdx.x - a.row_blocks);
+            a, GT == 32 ? (block - a.row_blocks) * (kAppendThreads / 32) + (threadIdx.x >> 5) : block - a.row_blocks);
 }
 
-// Heads a warp takes: as many as leave every SM its warps a few times over.
+// Heads a warp takes, with one look at the tables: as many as leave every SM 16 warps (with
+// 64, small heads looked at them twice as often: 23 us against 19 for 13 GPT-2-shaped prompts).
 int append_heads(const fkv_ctx *ctx, int64_t groups, int heads)
 {
-    const int64_t tasks = groups * heads, most = static_cast<int64_t>(ctx->sms) * 64;
+    const int64_t tasks = groups * heads, most = static_cast<int64_t>(ctx->sms) * 16;
     const int64_t per = tasks / most;
     return static_cast<int>(per < 1 ? 1 : per > 16 ? 16 : per);
 }
