@@ -421,13 +421,16 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
 // e4m3 pages 242 us with five, 277 with six, 335 with turned rows kept in fp32 (238 in this order).
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads, FMT == FKV_UINT4 ? 6 : 5) k_page_append(const AppendArgs a)
 {
-    // the runs, whose chains are longer, first (238 us against 242)
-    const unsigned runs = gridDim.x - a.row_blocks, block = blockIdx.x < runs ? blockIdx.x + a.row_blocks : blockIdx.x - runs;
-    if (FMT == FKV_UINT4 || block < a.row_blocks)
-        append_rows<D, FMT, T>(a, block * (kAppendThreads / 32) + (threadIdx.x >> 5));
-    else if (FMT != FKV_UINT4)
-        append_runs<D, FMT == FKV_UINT4 ? FKV_E4M3 : FMT, T, GT>(
-            a, GT == 32 ? (block - a.row_blocks) * (kAppendThreads / 32) + (threadIdx.x >> 5) : block - a.row_blocks);
+    if constexpr (FMT == FKV_UINT4) {
+        append_rows<D, FMT, T>(a, blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5));
+    } else {
+        // the runs, whose chains are longer, first (238 us against 242)
+        const unsigned runs = gridDim.x - a.row_blocks;
+        if (blockIdx.x >= runs)
+            append_rows<D, FMT, T>(a, (blockIdx.x - runs) * (kAppendThreads / 32) + (threadIdx.x >> 5));
+        else
+            append_runs<D, FMT, T, GT>(a, GT == 32 ? blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5) : blockIdx.x);
+    }
 }
 
 // Heads a warp takes, with one look at the tables: as many as leave every SM 16 warps (with
