@@ -567,8 +567,9 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * into the pages as it is.
  * slots and pos as fkv_page_plan gives them, slots as in fkv_page_write.  A token
  * of a negative position is left out: nothing of it is stored, its row of q_out left
- * as it is; one of a position past the tables too, and FKV_ERANGE is set.  A token of
- * a negative slot has its query turned all the same.  q_out may be q itself; its
+ * as it is; one of a position past the tables too, and FKV_ERANGE is set (in 8-bit
+ * pages either ends its run).  A token of a negative slot has its query turned all the
+ * same.  q_out may be q itself; its
  * rows overlap nothing else of the call.  q and q_out may be NULL. */
 typedef struct {
     const void *q;               /* vectors by (token, head) as fkv_rows, all of `dtype`: */
@@ -621,6 +622,13 @@ int fkv_page_append(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rotary *a, v
  * below 2^-31 of its largest are rounded to 2^-39 of that.  A score, and a query's
  * largest element times K's scale and `scale`, have to be float32 numbers, else
  * the row's values are unspecified.
+ * FKV_UINT4: k_j and v_j are middle + (c - 7.5) step.  Elements of a query below
+ * 2^-22 of its largest are rounded to 2^-33 of that, and that largest times a step
+ * of K and `scale` has to be below 2^100.  What is said above of a weight times V's
+ * scale holds for it times V's step, and for more than 32 rows a KV head (max_new x
+ * query heads a KV head) times a power of two near the largest value of 16
+ * positions; a bfloat16 q of that many rows has V's values rounded to fp16 as well
+ * (those below 2^-29 of that largest to 2^-40 of it).
  * table, table_stride and width as in fkv_page_plan.  max_new and max_len bound
  * n_new and kv_len of every request (they size the launch).  A request whose
  * numbers do not hold together (cu not increasing or past n_tok, a length past

@@ -4,8 +4,8 @@
 // Key j is mid_j + (c_j - 7.5) step_j and value j mid'_j + (c'_j - 7.5) step'_j, with
 // numbers of their own for every row of a page.  So
 //     q.k_j = step_j (q.c_j - 7.5 sum q) + mid_j sum q,
-// one multiplication and two additions a score behind the product of the query with
-// whole numbers, and with
+// two multiplications and additions a score behind the product of the query with whole
+// numbers, which starts from -7.5 sum q; and with
 //     y_j = x_j log2 e + log2 step'_j,   P_j = 2^(y_j - m + 8),   m = max y_j
 // the row's output is
 //     (sum P_j (c'_j - 7.5) + sum P_j mid'_j / step'_j) / sum P_j / step'_j,
@@ -18,6 +18,16 @@
 // operands of two after four masks and a shift; the factor 16 between neighbours is
 // taken out of the query for K, exactly but for elements of it below 2^-25 of its largest
 // (rounded to 2^-35 of that), and of the output for V.
+//
+// Half of the bytes of 8-bit pages bring the same work: what bounds these kernels is no longer
+// bytes alone.  8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, 336 us, 5.2 TB/s
+// (78 % of a copy's; 363 us without both products where all of it took 457, at equal lengths).
+// Steps: 481 us; 64 keys an iteration, scores without branches in their loop 404; loads of
+// whole pages' units together 380; a warp's number uniform 369; four operations a half word of
+// V, no branch a unit 349; two-wide arithmetic 344 (as timed one at a time).  One sequence of
+// 131k with a cap 39 us, 3.7 TB/s (two launches' starts and ends, 12 us of it); up to 28 rows, 24
+// sequences, a window of 4,096 and a bias 63 us.  Not kept: w >> 8 on the multipliers (403 against
+// 369); four blocks of 128 threads an SM with 32 keys an iteration (425).
 #include "attend_step.cuh"
 
 using namespace fkvd;

@@ -23,15 +23,21 @@
 //
 // 4-bit pages: a key, middle + (c - 7.5) step, is (c - 8) step, whose 11 bits fp16 holds,
 // and middle + step / 2 in every dimension.  K's tile holds the former over the power of
-// two that brings the largest of 16 keys' 8 steps to [2^14, 2^15), the unit's scale (where
-// one is below 2^-28 of that, to 2^-40); the latter times the query's sum is a step of 16
-// more dimensions: middle, middle, step / 2, step / 2 against the sum's upper and lower
-// half, twice.  So scores come out exactly as
-// over 8-bit pages.  V's tile holds whole values over such a power of two: rounded to fp16
-// once, half a step (2^-11) of the value down to 2^-29 of the unit's largest, what the
-// weights are rounded to as well (for bfloat16 outputs; see EXACT).  Eight codes of a word lie in a tile in the order
-// 0 4 1 5 2 6 3 7, as masks give them two at a time; so do the queries' elements, and the
-// outputs' are put back.
+// two that brings the largest of 16 keys' 8 step + |middle| to [2^14, 2^15), the unit's
+// scale (where a step is below 2^-28 of that, to 2^-40); the latter times the query's sum is
+// a step of 16 more dimensions: middle, middle, step / 2, step / 2 against the sum's upper
+// and lower half, twice.  So scores come out exactly as over 8-bit pages, without a number
+// of the key's in the softmax (with two there, 8 bytes of shared memory a score: 2,334 us
+// against 1,678).  V's tile holds whole values over such a power of two, rounded to fp16
+// once, as the weights are (for bfloat16 outputs; see EXACT).  Eight codes of a word lie in a
+// tile in the order 0 4 1 5 2 6 3 7, as masks give them two at a time; so do the queries'
+// elements, and the outputs' are put back.
+//
+// The pieces above: 1,678 us, 1.14 PFLOP/s (float16 1,848), GPT-2-shaped prompts 47 us (float16).
+// Without the codes' loads 1,471: a shuffle behind a load in flight waits for it, so that an
+// iteration's come before its loads (1,682 against 2,138); with the table's look-up left for the
+// iteration after 2,134.  Seven warps convert instead of four, all with the same statements:
+// those for K and V apart compete for the instruction cache.
 #include "attend.cuh"
 
 using namespace fkvd;
@@ -522,129 +528,129 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         }
     } else if (group == 2) {
         if constexpr (!FOUR) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
-        // ---------------------------------------------------- codes to fp16 tiles
-        // warps 0 and 1 take K's keys 0 .. 63 and 64 .. 127 of a tile, 2 and 3 V's:
-        // four units of 16 keys, each of one page
-        // A lane moves 16-byte piece c of rows r0, r0 + RP, ...; eight lanes that
-        // store together hold four pieces of two rows of different parity, which
-        // the swizzle puts on different banks.
-        constexpr int RP = 512 / D, NL = 16 / RP;                 // rows at a time, loads a unit
-        const int w = warp & 1;
-        const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
-        const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
-        const bool v_side = warp & 2;
-        const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
-        const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
-        const float mul0 = score_multiplier(a, fabsf(a.scale));
-        const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
-        // where the lane's first row's two 16-byte halves go in a tile
-        const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
-        const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
-        const int64_t row_step = RP * a.st;
-        bool bad = false, ok = true;           // (ok: see the softmax's)
-        // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
-        // is asked for two tiles ahead and checked a tile later, its scale and the
-        // codes one tile ahead, so that nothing here waits for memory.
-        auto first = [&](int j) { return tile_at(j) * kTile + 64 * w; };
-        struct Page {
-            int id;
-            bool on;
-        };
-        auto ask = [&](int j) {
-            const int key = first(j) + 16 * lane;
-            Page p = {-1, j < n_it && lane < 4 && rows_see.of(key)};
-            if (p.on)
-                p.id = a.table[r * a.table_stride + a.div.div(key)];
-            return p;
-        };
-        auto check = [&](const Page &p) {
-            if (p.on && (p.id < 0 || p.id >= a.n_blocks)) {
-                bad = true;
-                return 0;
-            }
-            return p.id;
-        };
-        auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
-        uint4 v[4][NL];
-        auto load = [&](int j, int id) {
-            // the unit's first row in the pool, from the lane that knows its page
-            int64_t from = -1;
-            if (id >= 0) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+            // ---------------------------------------------------- codes to fp16 tiles
+            // warps 0 and 1 take K's keys 0 .. 63 and 64 .. 127 of a tile, 2 and 3 V's:
+            // four units of 16 keys, each of one page
+            // A lane moves 16-byte piece c of rows r0, r0 + RP, ...; eight lanes that
+            // store together hold four pieces of two rows of different parity, which
+            // the swizzle puts on different banks.
+            constexpr int RP = 512 / D, NL = 16 / RP;                 // rows at a time, loads a unit
+            const int w = warp & 1;
+            const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+            const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+            const bool v_side = warp & 2;
+            const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
+            const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
+            const float mul0 = score_multiplier(a, fabsf(a.scale));
+            const int full_bar = v_side ? V_FULL : K_FULL, empty_bar = v_side ? V_EMPTY : K_EMPTY;
+            // where the lane's first row's two 16-byte halves go in a tile
+            const uint32_t at0 = sbase + (v_side ? S::off_v : S::off_k) + (c >> 2) * S::half + (64 * w + r0) * 128;
+            const uint32_t sw = static_cast<uint32_t>((2 * (c & 3)) ^ (r0 & 7)) * 16;
+            const int64_t row_step = RP * a.st;
+            bool bad = false, ok = true;           // (ok: see the softmax's)
+            // Lane u < 4 looks after unit u: its page id (-1: no row sees a key of it)
+            // is asked for two tiles ahead and checked a tile later, its scale and the
+            // codes one tile ahead, so that nothing here waits for memory.
+            auto first = [&](int j) { return tile_at(j) * kTile + 64 * w; };
+            struct Page {
+                int id;
+                bool on;
+            };
+            auto ask = [&](int j) {
                 const int key = first(j) + 16 * lane;
-                from = id * a.sb + (key - static_cast<int>(a.div.div(key)) * a.block) * a.st;
-            }
-            // all of them before the first load: a shuffle behind one waits for it as well
-            int64_t at[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                at[u] = __shfl_sync(~0u, from, u);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint8_t *p = pool + at[u];
-#pragma unroll
-                for (int i = 0; i < NL; ++i, p += row_step)
-                    v[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        const Page start = ask(0);
-        Page after = ask(1);
-        int nid = check(start);
-        load(0, nid);
-        float scale = ask_scale(nid);
-        nid = check(after);
-        for (int j = 0; j < n_it; ++j) {
-            // nid: checked ids of tile j + 1
-            after = ask(j + 2);
-            if (lane < 4) {
-                if (v_side) {
-                    const float vs = value_scale(scale);
-                    v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vs));
-                } else {
-                    k_scales[j & 3][4 * w + lane] = scale * mul0;
+                Page p = {-1, j < n_it && lane < 4 && rows_see.of(key)};
+                if (p.on)
+                    p.id = a.table[r * a.table_stride + a.div.div(key)];
+                return p;
+            };
+            auto check = [&](const Page &p) {
+                if (p.on && (p.id < 0 || p.id >= a.n_blocks)) {
+                    bad = true;
+                    return 0;
                 }
-            }
-            scale = ask_scale(nid);
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(bar(SC_FULL + (j & 3)));
-            const int st = j & 1;
-            if (j >= 2 && ok)
-                ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
-            const int first_key = first(j);
-            if (v_side && first_key + 64 > q.len) {
-                // rows behind the request's end hold any bytes, NaN codes among them
+                return p.id;
+            };
+            auto ask_scale = [&](int id) { return id >= 0 ? scale_of[id * a.scb] : 1.0f; };
+            uint4 v[4][NL];
+            auto load = [&](int j, int id) {
+                // the unit's first row in the pool, from the lane that knows its page
+                int64_t from = -1;
+                if (id >= 0) {
+                    const int key = first(j) + 16 * lane;
+                    from = id * a.sb + (key - static_cast<int>(a.div.div(key)) * a.block) * a.st;
+                }
+                // all of them before the first load: a shuffle behind one waits for it as well
+                int64_t at[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    at[u] = __shfl_sync(~0u, from, u);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint8_t *p = pool + at[u];
+#pragma unroll
+                    for (int i = 0; i < NL; ++i, p += row_step)
+                        v[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+                }
+            };
+            const Page start = ask(0);
+            Page after = ask(1);
+            int nid = check(start);
+            load(0, nid);
+            float scale = ask_scale(nid);
+            nid = check(after);
+            for (int j = 0; j < n_it; ++j) {
+                // nid: checked ids of tile j + 1
+                after = ask(j + 2);
+                if (lane < 4) {
+                    if (v_side) {
+                        const float vs = value_scale(scale);
+                        v_scales[j & 3][4 * w + lane] = make_float2(lg2(vs), share_of(vs));
+                    } else {
+                        k_scales[j & 3][4 * w + lane] = scale * mul0;
+                    }
+                }
+                scale = ask_scale(nid);
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(bar(SC_FULL + (j & 3)));
+                const int st = j & 1;
+                if (j >= 2 && ok)
+                    ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
+                const int first_key = first(j);
+                if (v_side && first_key + 64 > q.len) {
+                    // rows behind the request's end hold any bytes, NaN codes among them
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int i = 0; i < NL; ++i)
+                            if (first_key + 16 * u + r0 + i * RP >= q.len)
+                                v[u][i] = make_uint4(0, 0, 0, 0);
+                }
+                const uint32_t tile = at0 + st * S::tile;
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
-                    for (int i = 0; i < NL; ++i)
-                        if (first_key + 16 * u + r0 + i * RP >= q.len)
-                            v[u][i] = make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < NL; ++i) {
+                        uint32_t f[8];
+                        codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].x, f[0], f[1]);
+                        codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].y, f[2], f[3]);
+                        codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].z, f[4], f[5]);
+                        codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].w, f[6], f[7]);
+                        // the row's place in its group of eight turns with i for RP = 4
+                        const uint32_t at = tile + (16 * u + i * RP) * 128, x = RP == 4 && (i & 1) ? sw ^ 64 : sw;
+                        sts128(at + x, f[0], f[1], f[2], f[3]);
+                        sts128(at + (x ^ 16), f[4], f[5], f[6], f[7]);
+                    }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(bar(full_bar + st));
+                load(j + 1, nid);
+                nid = check(after);
             }
-            const uint32_t tile = at0 + st * S::tile;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < NL; ++i) {
-                    uint32_t f[8];
-                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].x, f[0], f[1]);
-                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].y, f[2], f[3]);
-                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].z, f[4], f[5]);
-                    codes4_half<FOUR ? FKV_E4M3 : FMT>(v[u][i].w, f[6], f[7]);
-                    // the row's place in its group of eight turns with i for RP = 4
-                    const uint32_t at = tile + (16 * u + i * RP) * 128, x = RP == 4 && (i & 1) ? sw ^ 64 : sw;
-                    sts128(at + x, f[0], f[1], f[2], f[3]);
-                    sts128(at + (x ^ 16), f[4], f[5], f[6], f[7]);
-                }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(bar(full_bar + st));
-            load(j + 1, nid);
-            nid = check(after);
-        }
-        if (bad)
-            atomicOr(a.status, FKV_ST_RANGE);
+            if (bad)
+                atomicOr(a.status, FKV_ST_RANGE);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
