@@ -67,14 +67,23 @@ __device__ __forceinline__ void codes8_pairs(uint32_t w, uint32_t *f)
     f[2] = x & 0x000f000fu, f[3] = x & 0x00f000f0u;
 }
 
-// The same of two values' codes 0 .. 3 (of the words' halves `sel` takes): (c0, c0'),
-// (c2, c2') times 2^-24, and (c0 + 16 c1, ..), (c2 + 16 c3, ..): an operation less, and
-// what the even dimension adds to the odd one's sum is taken off at the end.
-__device__ __forceinline__ void codes4_pairs(uint32_t w0, uint32_t w1, int sel, uint32_t *f)
+// Four codes each of two values, x = (c0 c1 c2 c3, c0' ..): (c0, c0'), (c2, c2') times 2^-24,
+// and (c0 + 16 c1, ..), (c2 + 16 c3, ..): an operation less, and what the even dimension
+// adds to the odd one's sum is taken off at the end.
+__device__ __forceinline__ void codes4_pairs(uint32_t x, uint32_t *f)
 {
-    const uint32_t x = __byte_perm(w0, w1, sel), y = __byte_perm(x, 0, 0x4341);
+    const uint32_t y = __byte_perm(x, 0, 0x4341);
     f[0] = x & 0x000f000fu, f[1] = x & 0x00ff00ffu;
     f[2] = y & 0x000f000fu, f[3] = y;
+}
+
+// Four 8 x 8 matrices of 16-bit elements from rows of 16 bytes (a lane's address is one of
+// eight rows of one of them), transposed: a lane has elements (2t, gid) and (2t + 1, gid).
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t *r, uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr));
 }
 
 // D = A B + C.
@@ -285,9 +294,14 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
         m[n][0] = m[n][1] = -INFINITY;
         l[n][0] = l[n][1] = mid[n][0] = mid[n][1] = 0.0f;
     }
-    // where a lane's codes lie among a unit's: K's of key gid, V's of key 2t
-    const uint32_t k_at = D == 128 ? gid * 64 + ((t ^ (gid >> 1 & 3)) << 4) : gid * 32 + t * 8;
-    const uint32_t v_at = D == 128 ? 2 * t * 64 + (((gid >> 1) ^ t) << 4 | (gid & 1) << 3) : 2 * t * 32 + gid * 4;
+    // where a lane's codes lie among a unit's: K's of key gid; V's row lane % 16, whose first 16
+    // bytes are lanes 0 to 15's, the next the others' (16-byte pieces are swizzled by the row)
+    const uint32_t k_at = D == 128 ? gid * 64 + ((t ^ (gid >> 1 & 3)) << 4) : gid * 32 + (((t >> 1) ^ (gid >> 2)) << 4 | (t & 1) << 3);
+    const int v_turn = D == 128 ? lane >> 1 & 3 : lane >> 2 & 1;
+    uint32_t v_at[D / 64];
+#pragma unroll
+    for (int g = 0; g < D / 64; ++g)
+        v_at[g] = (lane & 15) * (D / 2) + (((2 * g + (lane >> 4)) ^ v_turn) << 4);
     const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 
     unsigned batch = 0;
@@ -475,35 +489,27 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
                 }
                 mma16816(p_sum[n], ones, pf[n][0], pf[n][1]);
             }
-            // value rows 2t, 2t + 1, 2t + 8, 2t + 9 of the unit, D / 8 dimensions each
-            uint32_t w[4][D / 64];
+            // Value rows 2t and 2t + 1, and 2t + 8 and 2t + 9, of the unit: four codes of either as
+            // one 16-bit element each, dimensions 4 gid to 4 gid + 3 of every 32.
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t at = vt + (16 * u + (x & 1) + 8 * (x >> 1)) * (D / 2) + v_at;
-                if (D == 128) {
-                    const uint2 v = lds64(at);
-                    w[x][0] = v.x, w[x][D / 64 - 1] = v.y;
-                } else {
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[x][0]) : "r"(at));
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < D / 64; ++k)
+            for (int g = 0; g < D / 64; ++g) {
+                uint32_t x[4];
+                ldmatrix4_trans(x, vt + u * S::unit + v_at[g]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    // rows gid and gid + 8 of two tiles: dimensions 8k + 4e and the next, and the two behind
-                    const int sel = e ? 0x7632 : 0x5410;
+                    // rows gid and gid + 8 of two tiles: a dimension and the next, and the two behind
                     uint32_t f0[4], f1[4];
-                    codes4_pairs(w[0][k], w[1][k], sel, f0);
-                    codes4_pairs(w[2][k], w[3][k], sel, f1);
+                    codes4_pairs(x[2 * e], f0);
+                    codes4_pairs(x[2 * e + 1], f1);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const uint32_t f[4] = {f0[2 * y], f0[2 * y + 1], f1[2 * y], f1[2 * y + 1]};
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            mma16816(o[n][4 * k + 2 * e + y], f, pf[n][0], pf[n][1]);
+                            mma16816(o[n][4 * g + 2 * e + y], f, pf[n][0], pf[n][1]);
                     }
                 }
+            }
         }
         __syncwarp();                  // the stage is free: the next issue may overwrite it
     }
@@ -525,7 +531,7 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
                 o[n][d][c] = fmaf(o[n][d][c], 0x1p24f, add);
             }
         }
-    finish_rows<D, T, NT>(a, q, base, ml, m, l, o, h, split, row0, rows, bad);
+    finish_rows<D, T, NT, true>(a, q, base, ml, m, l, o, h, split, row0, rows, bad);
 }
 
 template <int D, typename T, int NT>

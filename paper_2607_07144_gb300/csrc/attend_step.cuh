@@ -78,9 +78,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 
 // The end of a block of four warps and 8 NT rows: a row's maxima m, sums l (a lane's
 // own keys of rows 2t, 2t + 1) and outputs o (dimensions 2d and 2d + 1 of the lane's
-// D / 8) meet in shared memory, which takes them from `base` on, and the shares of
+// D / 8; QUADS: of its fours, one in every 32) meet in shared memory, which takes them from `base` on, and the shares of
 // a row's keys in their cluster or in the workspace.
-template <int D, typename T, int NT>
+template <int D, typename T, int NT, bool QUADS = false>
 __device__ __forceinline__ void finish_rows(const AttendArgs &a, const Request &q, uint8_t *base, float (*ml)[2][8 * NT],
                                             const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[NT][D / 16][4],
                                             int h, int split, int row0, int rows, bool bad)
@@ -110,10 +110,10 @@ __device__ __forceinline__ void finish_rows(const AttendArgs &a, const Request &
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            float *dst = mo + (warp * R + 8 * n + 2 * t + c) * LD + gid * (D / 8);
+            float *dst = mo + (warp * R + 8 * n + 2 * t + c) * LD + gid * (QUADS ? 4 : D / 8);
 #pragma unroll
             for (int d = 0; d < MO; ++d)
-                *reinterpret_cast<float2 *>(dst + 2 * d) = make_float2(o[n][d][c], o[n][d][2 + c]);
+                *reinterpret_cast<float2 *>(dst + (QUADS ? 32 * (d >> 1) + 2 * (d & 1) : 2 * d)) = make_float2(o[n][d][c], o[n][d][2 + c]);
         }
     __syncthreads();
     constexpr int TPR = 128 / R, E = D / TPR;      // threads a row, dimensions a thread

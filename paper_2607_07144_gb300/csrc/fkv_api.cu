@@ -1118,7 +1118,7 @@ const char *check_attend(const fkv_attend *a)
 }
 
 // The pool as [page][head][position][row] bytes, in boxes of some positions of one
-// head whose rows are swizzled by their own width (those of 32 bytes are not).
+// head whose rows are swizzled by their own width.
 bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, int positions, CUtensorMap *map)
 {
     const cuuint64_t D = static_cast<cuuint64_t>(p->format == FKV_UINT4 ? p->dim / 2 : p->dim);
@@ -1132,7 +1132,7 @@ bool page_map(EncodeTiledFn enc, const fkv_pages *p, void *pool, int positions, 
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                D == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
                : D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
-                         : CU_TENSOR_MAP_SWIZZLE_NONE,
+                         : CU_TENSOR_MAP_SWIZZLE_32B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
