@@ -6,7 +6,7 @@
 //     q.k_j = step_j (q.c_j - 7.5 sum q) + mid_j sum q,
 // two multiplications and additions a score behind the product of the query with whole
 // numbers, which starts from -7.5 sum q; and with
-//     y_j = x_j log2 e + log2 step'_j,   P_j = 2^(y_j - m + 8),   m = max y_j
+//     y_j = x_j log2 e + log2 step'_j,   P_j = 2^(y_j - m + 8),   m >= max y_j - 7
 // the row's output is
 //     (sum P_j (c'_j - 7.5) + sum P_j mid'_j / step'_j) / sum P_j / step'_j,
 // the first sum on the tensor cores with P rounded to fp16 (as for 8-bit pages), the
@@ -440,30 +440,26 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
         for (int n = 0; n < NT; ++n)
             mx[n][0] = mx[n][1] = -INFINITY;
         each([&](float &y, int n, int c, float, int) { mx[n][c] = fmaxf(mx[n][c], y); });
-        bool grown = false;
-        float mref[NT][2], by[NT][2];
+        // The reference moves, to the largest score so far, only when a weight would come out
+        // above 2^15: mostly no maximum has to be joined over the lanes.
+        bool up = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float x = mx[n][c];
-                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                const float mn = fmaxf(m[n][c], x);
-                grown |= mn != m[n][c];
-                mref[n][c] = (mn == -INFINITY ? 0.0f : mn) - kPBits;
-                by[n][c] = m[n][c] - kPBits - mref[n][c];
-                m[n][c] = mn;
-            }
-        if (__any_sync(~0u, grown)) {
+            up |= mx[n][0] > m[n][0] + (15.0f - kPBits) || mx[n][1] > m[n][1] + (15.0f - kPBits);
+        if (__any_sync(~0u, up)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    float x = mx[n][c];
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                    const float mn = fmaxf(m[n][c], x), by = m[n][c] == mn ? 0.0f : m[n][c] - mn;
+                    m[n][c] = mn;
                     // sums of weights over steps are scaled in two halves: counted up to 2^80 a
                     // weight (share_of), they outlast factors below float32's least
-                    const float half = ex2(0.5f * by[n][c]), f = half * half;
+                    const float half = ex2(0.5f * by), f = half * half;
                     l[n][c] = l[n][c] * half * half, mid[n][c] = mid[n][c] * half * half;
                     p_sum[n][c] *= f, p_sum[n][2 + c] *= f;
 #pragma unroll
@@ -471,6 +467,12 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
                         o[n][d][c] *= f, o[n][d][2 + c] *= f;
                 }
         }
+        float mref[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                mref[n][c] = (m[n][c] == -INFINITY ? 0.0f : m[n][c]) - kPBits;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             // (a unit that was not loaded has weights of zero, and codes of any bytes)
