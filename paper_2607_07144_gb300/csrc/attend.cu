@@ -532,7 +532,8 @@ struct Plan {
 // kernel, more to the tensor-memory one (nt = 0): for 24 sequences of 3-16k
 // positions and 8 heads of 128 in 8-bit pages, 63 rows take 384 us against 236; 28 rows 265
 // against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
-// 4,096 and 283 against 364 with a cap.  A block's time is its keys plus a fixed
+// 4,096 and 283 against 364 with a cap.  (4-bit pages: 28 rows 205 us, 32 rows 217,
+// 36 by the tensor-memory kernel 324.)  A block's time is its keys plus a fixed
 // part (its launch, the first loads' latency and its end: about that of 384 keys);
 // the blocks run in waves of `slots`.  The split with the least waves x time wins.
 // Up to eight shares of the step kernel are joined in their cluster (about 100

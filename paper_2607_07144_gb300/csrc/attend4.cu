@@ -20,14 +20,15 @@
 // (rounded to 2^-35 of that), and of the output for V.
 //
 // Half of the bytes of 8-bit pages bring the same work: what bounds these kernels is no longer
-// bytes alone.  8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, 336 us, 5.2 TB/s
-// (78 % of a copy's; 363 us without both products where all of it took 457, at equal lengths).
-// Steps: 481 us; 64 keys an iteration, scores without branches in their loop 404; loads of
-// whole pages' units together 380; a warp's number uniform 369; four operations a half word of
-// V, no branch a unit 349; two-wide arithmetic 344 (as timed one at a time).  One sequence of
-// 131k with a cap 39 us, 3.7 TB/s (two launches' starts and ends, 12 us of it); up to 28 rows, 24
-// sequences, a window of 4,096 and a bias 63 us.  Not kept: w >> 8 on the multipliers (403 against
-// 369); four blocks of 128 threads an SM with 32 keys an iteration (425).
+// bytes alone.  8 heads of 128, 4 rows each: 64 sequences of 16-32k positions, 311 us, 5.6 TB/s,
+// 84 % of a copy's.  Steps (each call timed by itself, 10 us more): 481 us; 64 keys an
+// iteration, scores without branches in their loop 404; loads of whole pages' units together
+// 380; a warp's number uniform 369; four operations a half word of V, no branch a unit 349;
+// two-wide arithmetic 344; V by transposed loads 328; the reference moved only where a weight
+// asks for it 321.  One sequence of 131k with a cap 36 us, 3.9 TB/s (two launches' starts and
+// ends, 12 us of it); up to 28 rows, 24 sequences, a window of 4,096 and a bias 61 us.  Not
+// kept: w >> 8 on the multipliers (403 against 369); four blocks of 128 threads an SM with 32
+// keys an iteration (425).
 #include "attend_step.cuh"
 
 using namespace fkvd;
