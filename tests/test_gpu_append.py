@@ -333,6 +333,51 @@ def test_captured_and_replayed_on_another_stream(fkv, ctx):
             pool.same()
 
 
+@pytest.mark.parametrize("fmt", ["int8", "uint4"])
+def test_one_head_one_token_and_gaps(fkv, ctx, fmt):
+    """Dimensions of one (whose strides mean nothing), queries and outputs with gaps, tables with a gap, pages of 1024."""
+    rng = np.random.default_rng(10)
+    cos, sin = _table(2000, 32)
+    wide = torch.zeros((2000, 80), device="cuda")
+    wide[:, 4:36], wide[:, 40:72] = _cuda(cos), _cuda(sin)
+    for T, Hq in ((1, 1), (1, 7), (33, 1)):
+        pool = Pool(fkv, rng, 3, 1, 64, 1024, fmt)
+        x = torch.from_numpy(rng.standard_normal((T, 2 * Hq + 3, 64)).astype(np.float32)).half().cuda()
+        q, k, v = x[:, :2 * Hq:2], x[:, -2:-1], x[:, -1:]
+        big = torch.full((T, 2, Hq, 128), 7.0, dtype=torch.float16, device="cuda")
+        slots, pos = 1024 + 990 + np.arange(T), (1990 - T + np.arange(T)).astype(np.int32)
+        ctx.page_append(pool.pages, k, v, _cuda(slots), _cuda(pos), wide[:, 4:36], wide[:, 40:72], q=q, q_out=big[:, 1, :, 64:])
+        assert ctx.sync_status() == 0
+        h = x.float().cpu().numpy()
+        want = torch.from_numpy(paged.turn(h[:, :2 * Hq:2], pos, cos, sin, 64)).half()
+        assert torch.equal(big[:, 1, :, 64:].cpu(), want) and (big[:, 0] == 7).all() and (big[:, 1, :, :64] == 7).all()
+        pool.write(paged.turn(h[:, -2:-1], pos, cos, sin, 64), h[:, -1:], slots)
+        pool.same()
+
+
+def test_values_that_are_no_numbers_are_reported_where_they_are_stored(fkv, ctx):
+    rng = np.random.default_rng(11)
+    cos, sin = _table(100, 64)
+    for fmt in ("e4m3", "uint4"):
+        pool = Pool(fkv, rng, 8, 2, 128, 16, fmt)
+        x = torch.from_numpy(rng.standard_normal((5, 8, 128)).astype(np.float32)).bfloat16().cuda()
+        x[0, 1, 3], x[2, 4, 5], x[4, 7, 127] = float("nan"), float("nan"), float("inf")       # a query, a key, a value
+        slots = np.arange(5) * 16
+        slots[2] = -1
+        go = lambda s: ctx.page_append(pool.pages, x[:, 4:6], x[:, 6:], _cuda(s), _cuda(np.arange(5, dtype=np.int32)), _cuda(cos),
+                                       _cuda(sin), q=x[:, :4])
+        out = go(slots)
+        assert ctx.sync_status() == 0 and out[0, 1, 3].isnan() and out[0, 1, 67].isnan() and not out[1:].isnan().any()
+        h = x.float().cpu().numpy()
+        pool.write(paged.turn(h[:, 4:6], np.arange(5), cos, sin, 128), h[:, 6:], slots)
+        pool.same()
+        slots[2] = 32
+        go(slots)
+        assert ctx.sync_status() == -5
+        pool.write(paged.turn(h[:, 4:6], np.arange(5), cos, sin, 128), h[:, 6:], slots)
+        pool.same()
+
+
 def test_append_refusals(fkv, ctx):
     pages = fkv.Pages.empty(4, 2, 16, 64, torch.uint8)
     x = torch.zeros((3, 2, 64), device="cuda")

@@ -240,6 +240,90 @@ def test_queries_of_any_size(fkv, ctx, dtype, new):
     b.check(ctx)
 
 
+@pytest.mark.parametrize("G", [8, 9, 16, 17, 32, 33, 71])
+@pytest.mark.parametrize("D,block,dtype", [(64, 80, "bf16"), (128, 96, "f16"), (128, 1024, "bf16")])
+def test_many_query_heads_a_kv_head(fkv, ctx, D, block, dtype, G):
+    """Rows around what one and two tiles, and the other kernel, take; pages of which 16, 32 and 64 rows are loaded together."""
+    b = Batch(fkv, 20, [(300, 1), (0, 1), (64, 1), (1100, 1)], 1, G, D, block, dtype, gap=3)
+    b.check(ctx)
+    b.check(ctx, window=70, sinks=3)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-38, -0.1])
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "bf16")])
+def test_vanishing_and_negative_scores_of_prompts(fkv, ctx, D, dtype, scale):
+    b = Batch(fkv, 21, [(130, 300), (5, 40), (0, 3), (400, 1)], 1, 2, D, 16, dtype)
+    b.check(ctx, scale=scale, rows=[0, 1, 39, 150, 299])
+    b.check(ctx, scale=scale, rows=[0, 39, 299], window=37, sinks=3, prefix=[20, 0, 3, 7])
+
+
+@pytest.mark.parametrize("new", [1, 5, 60])
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "bf16"), (128, "f16")])
+def test_middles_far_above_steps(fkv, ctx, D, dtype, new):
+    """Rows that are nearly constant, up to middles of 2^16 steps, beside others that are not."""
+    b = Batch(fkv, 22, [(150, new), (17, new)], 1, 2, D, 16, dtype)
+    rng = np.random.default_rng(70)
+    for kv in (0, 1):
+        n = b.numbers[kv]
+        far = np.exp2(-rng.integers(0, 17, n.shape[:3]) * rng.integers(0, 2, n.shape[:3])).astype(np.float32)
+        big = paged.to_bf16((rng.standard_normal(n.shape[:3]) * (0.2 if kv == 0 else 3)).astype(np.float32))
+        with np.errstate(invalid="ignore"):
+            step = np.maximum(np.abs(big) * far, np.float32(2.0 ** -100))
+            n[..., 0] = np.where(far < 1, np.where(np.isfinite(n[..., 0]), step, n[..., 0]), n[..., 0])
+            n[..., 1] = np.where(far < 1, np.where(np.isfinite(n[..., 1]), big, n[..., 1]), n[..., 1])
+    p = b.pages
+    b.pages = fkv.Pages(p.k, p.v, *(torch.from_numpy(s).bfloat16().cuda() for s in b.numbers))
+    b.check(ctx, rows=[0, new // 2, new - 1])
+
+
+@pytest.mark.parametrize("new", [1, 9, 70])
+def test_large_float16_queries(fkv, ctx, new):
+    b = Batch(fkv, 23, [(100, new)], 1, 4, 128, 32, "f16")
+    b.q = (b.q.float() * 2.0 ** 13).clamp(-65504, 65504).half()
+    b.check(ctx, scale=2.0 ** -17)
+
+
+def test_bounds_far_above_the_lengths(fkv, ctx):
+    """max_len of 2^30 sizes the launch, not the work."""
+    for new in (1, 3, 50):
+        b = Batch(fkv, 24, [(70, new), (0, new), (500, new)], 2, 2, 64, 16, "bf16")
+        want, lse = b.run(ctx)
+        width = 1 << 20                                        # a table row that could hold 2^24 positions
+        tab = torch.zeros((3, width), dtype=torch.int32, device="cuda")
+        tab[:, :b.table.shape[1]] = _i32(b.table)
+        out = torch.full_like(b.q, 7.0)
+        ctx.page_attend(b.pages, b.q, _i32(b.cu), _i32(b.len), tab, 64, 1 << 30, out=out)
+        assert ctx.sync_status() == 0
+        eps = torch.finfo(b.q.dtype).eps
+        # other shares of the keys, other sums: each of the two is as near to the exact result as check() asks
+        v = np.nanmax(np.abs(paged.values4(b.codes[1], np.nan_to_num(b.numbers[1], posinf=0.0))))
+        assert (out.double() - want.double()).abs().max().item() <= eps * want.double().abs().max().item() + 2 * 2.0 ** -10 * 2 * v
+
+
+def test_prompts_captured_and_replayed_with_other_lengths(fkv, ctx):
+    for dtype, D in (("f16", 64), ("bf16", 128)):
+        b = Batch(fkv, 25, [(700, 90), (20, 64)], 2, 2, D, 16, dtype)
+        d = dict(ln=_i32(b.len), out=torch.zeros_like(b.q))
+        run = lambda: ctx.page_attend(b.pages, b.q, _c, d["ln"], _t, 90, max(b.len), out=d["out"])
+        _c, _t = _i32(b.cu), _i32(b.table)
+        run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        for cut in (0, 5, 80):
+            d["ln"].copy_(_i32([max(0, x - cut) for x in b.len]))
+            run()
+            want = d["out"].clone()
+            d["out"].zero_()
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                g.replay()
+            s.synchronize()
+            assert torch.equal(d["out"], want)
+        assert ctx.sync_status() == 0
+
+
 @pytest.mark.parametrize("new", [1, 6, 90])
 def test_requests_that_do_not_hold_together(fkv, ctx, new):
     b = Batch(fkv, 9, [(60, new), (40, new), (90, new)], 2, 2, 64, 16, "bf16")
