@@ -32,7 +32,7 @@ struct AppendArgs {
     const int *pos;                          // or null: nothing is turned
     const float *cos, *sin;
     int64_t T, sb, sh, st, scb, sch, n_slots, n_pos, table_stride;    // n_slots: at most 2^32
-    int q_heads, row_heads, heads, per, chunks, block, stretch, rot, pairs;
+    int q_heads, row_heads, heads, per, chunks, run_heads, run_chunks, block, stretch, rot, pairs;
     unsigned row_blocks;                     // blocks that take rows; others take runs of 8-bit pages
     FastDiv by_block, by_heads, by_chunks;
     unsigned *status;
@@ -245,20 +245,21 @@ template <int D, int FMT, typename T> __device__ __forceinline__ void append_row
 }
 
 // Runs of slots of 8-bit pages, as k_page_write takes them (paged.cu): GT threads a
-// run, one head, K or V.
+// run, some heads, K or V.
 template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void append_runs(const AppendArgs &a, unsigned item)
 {
     constexpr int C = D / 16, R = GT / C, KEEP = sizeof(T) == 4 ? 2 : 4;        // 16-element pieces a row, rows at a time, kept of them
     __shared__ uint32_t red[GT / 32];
     const int lane = threadIdx.x & 31, tid = GT == 32 ? lane : threadIdx.x, c = tid % C, row0 = tid / C;
     const unsigned both = a.by_heads.div(item);
-    const int h = static_cast<int>(item - both * a.heads), kv = both & 1;
+    const int h0 = static_cast<int>(item - both * a.run_chunks) * a.run_heads, h1 = min(h0 + a.run_heads, a.heads), kv = both & 1;
     const int64_t t0 = static_cast<int64_t>(both >> 1) * a.stretch;
     if (t0 >= a.T)
         return;
     const int64_t t1 = min(t0 + a.stretch, a.T);
-    const T *const x = static_cast<const T *>(a.x[1 + kv]) + h * a.x_head[1 + kv];
-    const int64_t x_tok = a.x_tok[1 + kv];
+    const T *x = static_cast<const T *>(a.x[1 + kv]);
+    const int64_t x_tok = a.x_tok[1 + kv], x_head = a.x_head[1 + kv];
+    x += h0 * x_head;
     Groups g(a, c);
     if (kv)                                  // values stay as they are
         g.d0 = 16 * c, g.d1 = 16 * c + 8, g.f = -1;
@@ -320,93 +321,95 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
                     break;
                 }
             }
-            float *const sp = a.scale[kv] + blk * a.scb + h * a.sch;
-            const float was = off > 0 ? *sp : 0.0f;
-            uint8_t *const page = a.pool[kv] + blk * a.sb + h * a.sh;
-            if (GT == 32) {
+            // the run's heads, one after the other
+            for (int h = h0; h < h1; ++h, x += x_head) {
+                float *const sp = a.scale[kv] + blk * a.scb + h * a.sch;
+                const float was = off > 0 ? *sp : 0.0f;
+                uint8_t *const page = a.pool[kv] + blk * a.sb + h * a.sh;
 #pragma unroll
-                for (int k = 1; k < KEEP; ++k)
-                    if (row0 + k * R < len)
+                for (int k = 0; k < KEEP; ++k)
+                    if (((GT == 32 && k > 0) || h > h0) && row0 + k * R < len)
                         keep[k] = raw_of(t + row0 + k * R);
-            }
-            uint32_t amax_u = 0;
-#pragma unroll
-            for (int k = 0; k < KEEP; ++k)
-                if (row0 + k * R < len) {
-                    float v[16];
-                    turned(keep[k], t + row0 + k * R, v);
-                    amax_u = most_of(v, amax_u);
-                }
-            for (int i = row0 + KEEP * R; i < len; i += R) {
-                float v[16];
-                row_of(t + i, v);
-                amax_u = most_of(v, amax_u);
-            }
-            auto join = [&]() {
-                amax_u = __reduce_max_sync(~0u, amax_u);
-                if (GT > 32) {
-                    __syncthreads();       // red is free (also: every thread has read the page's old scale)
-                    if (lane == 0)
-                        red[threadIdx.x >> 5] = amax_u;
-                    __syncthreads();
-#pragma unroll
-                    for (int w = 0; w < GT / 32; ++w)
-                        amax_u = max(amax_u, red[w]);
-                }
-            };
-            join();
-            // infinities or NaN among the values, or some beyond the largest code of the
-            // largest scale (of int8; e4m3's, 448, is larger)
-            const bool odd = amax_u > __float_as_uint(127.0f * FKV_PAGE_MAX_SCALE);
-            if (odd) {
-                // rare: the largest finite magnitude
-                float amax = 0.0f;
-                for (int i = row0; i < len; i += R) {
-                    float v[16];
-                    row_of(t + i, v);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        amax = fmaxf(amax, finite_abs(v[e]));
-                }
-                amax_u = __float_as_uint(amax);
-                join();
-            }
-            const float want = amax_u ? scale_of<FMT>(__uint_as_float(amax_u)) : FKV_PAGE_MIN_SCALE;
-            // a page's scale never shrinks while it has rows
-            const float now = was >= want ? was : want;
-            const float inv = __frcp_rn(now);
-            auto put = [&](int row, const uint4 &q) {
-                uint8_t *const p = page + row * a.st;
-                *reinterpret_cast<uint2 *>(p + g.d0) = make_uint2(q.x, q.y);
-                *reinterpret_cast<uint2 *>(p + g.d1) = make_uint2(q.z, q.w);
-            };
-            if (!odd) {
+                uint32_t amax_u = 0;
 #pragma unroll
                 for (int k = 0; k < KEEP; ++k)
                     if (row0 + k * R < len) {
                         float v[16];
                         turned(keep[k], t + row0 + k * R, v);
-                        put(off + row0 + k * R, codes16_inside<FMT>(v, inv));
+                        amax_u = most_of(v, amax_u);
                     }
-            }
-            for (int i = odd ? row0 : row0 + KEEP * R; i < len; i += R) {
-                float v[16];
-                row_of(t + i, v);
-                nan |= drop_nan(v);
-                put(off + i, codes16<FMT>(v, inv));
-            }
-            __syncwarp();
-            if (now != was) {
-                const float ratio = __fmul_rn(was, inv);
-                for (int i = row0; i < off; i += R) {
-                    uint4 *p = reinterpret_cast<uint4 *>(page + i * a.st + c * 16);
+                for (int i = row0 + KEEP * R; i < len; i += R) {
                     float v[16];
-                    values16<FMT>(*p, v);
-                    *p = codes16<FMT>(v, ratio);
+                    row_of(t + i, v);
+                    amax_u = most_of(v, amax_u);
                 }
-                if (tid == 0)
-                    *sp = now;
+                auto join = [&]() {
+                    amax_u = __reduce_max_sync(~0u, amax_u);
+                    if (GT > 32) {
+                        __syncthreads();       // red is free (also: every thread has read the page's old scale)
+                        if (lane == 0)
+                            red[threadIdx.x >> 5] = amax_u;
+                        __syncthreads();
+#pragma unroll
+                        for (int w = 0; w < GT / 32; ++w)
+                            amax_u = max(amax_u, red[w]);
+                    }
+                };
+                join();
+                // infinities or NaN among the values, or some beyond the largest code of the
+                // largest scale (of int8; e4m3's, 448, is larger)
+                const bool odd = amax_u > __float_as_uint(127.0f * FKV_PAGE_MAX_SCALE);
+                if (odd) {
+                    // rare: the largest finite magnitude
+                    float amax = 0.0f;
+                    for (int i = row0; i < len; i += R) {
+                        float v[16];
+                        row_of(t + i, v);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            amax = fmaxf(amax, finite_abs(v[e]));
+                    }
+                    amax_u = __float_as_uint(amax);
+                    join();
+                }
+                const float want = amax_u ? scale_of<FMT>(__uint_as_float(amax_u)) : FKV_PAGE_MIN_SCALE;
+                // a page's scale never shrinks while it has rows
+                const float now = was >= want ? was : want;
+                const float inv = __frcp_rn(now);
+                auto put = [&](int row, const uint4 &q) {
+                    uint8_t *const p = page + row * a.st;
+                    *reinterpret_cast<uint2 *>(p + g.d0) = make_uint2(q.x, q.y);
+                    *reinterpret_cast<uint2 *>(p + g.d1) = make_uint2(q.z, q.w);
+                };
+                if (!odd) {
+#pragma unroll
+                    for (int k = 0; k < KEEP; ++k)
+                        if (row0 + k * R < len) {
+                            float v[16];
+                            turned(keep[k], t + row0 + k * R, v);
+                            put(off + row0 + k * R, codes16_inside<FMT>(v, inv));
+                        }
+                }
+                for (int i = odd ? row0 : row0 + KEEP * R; i < len; i += R) {
+                    float v[16];
+                    row_of(t + i, v);
+                    nan |= drop_nan(v);
+                    put(off + i, codes16<FMT>(v, inv));
+                }
+                __syncwarp();
+                if (now != was) {
+                    const float ratio = __fmul_rn(was, inv);
+                    for (int i = row0; i < off; i += R) {
+                        uint4 *p = reinterpret_cast<uint4 *>(page + i * a.st + c * 16);
+                        float v[16];
+                        values16<FMT>(*p, v);
+                        *p = codes16<FMT>(v, ratio);
+                    }
+                    if (tid == 0)
+                        *sp = now;
+                }
             }
+            x -= (h1 - h0) * x_head;
         }
     }
     if (nan)
@@ -418,7 +421,8 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
 // Bytes bound long calls, and a few blocks an SM more or less what is in flight of them: 9
 // prompts of 1,000 to 8,192 tokens (32 query and 8 KV heads of 128, bf16) into 4-bit pages
 // 193 us, 5.6 TB/s, with six blocks an SM, 216 without the limit, 252 with eight (spills); into
-// e4m3 pages 242 us with five, 277 with six, 335 with turned rows kept in fp32 (238 in this order).
+// e4m3 pages 207 us with five (with one head a run 242, 277 with six blocks, 335 with turned
+// rows kept in fp32).
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads, FMT == FKV_UINT4 ? 6 : 5) k_page_append(const AppendArgs a)
 {
     if constexpr (FMT == FKV_UINT4) {
@@ -442,16 +446,18 @@ int append_heads(const fkv_ctx *ctx, int64_t groups, int heads)
     return static_cast<int>(per < 1 ? 1 : per > 16 ? 16 : per);
 }
 
+// Whether a run is a warp's: a step's, and where that makes four rows a lane at most: a
+// block's other threads would have none (13 GPT-2-shaped prompts, pages of 16: 31 us against 52).
+bool warp_runs(const AppendArgs &a, int dim) { return a.stretch == 1 || a.block * (dim / 16) <= 32 * 4; }
+
 template <int D, int FMT, typename T> cudaError_t append_as(const AppendArgs &a, cudaStream_t st)
 {
     if (FMT == FKV_UINT4) {
         k_page_append<D, FMT, T, 32><<<a.row_blocks, kAppendThreads, 0, st>>>(a);
         return cudaGetLastError();
     }
-    const int64_t items = (a.T + a.stretch - 1) / a.stretch * 2 * a.heads;
-    // a warp a run where it takes four rows a lane at most: a block's other threads had none
-    // (13 GPT-2-shaped prompts, pages of 16: 31 us against 52)
-    if (a.stretch == 1 || a.block * (D / 16) <= 32 * 4)
+    const int64_t items = (a.T + a.stretch - 1) / a.stretch * 2 * a.run_chunks;
+    if (warp_runs(a, D))
         k_page_append<D, FMT, T, 32><<<a.row_blocks + static_cast<unsigned>((items + 3) / 4), kAppendThreads, 0, st>>>(a);
     else
         k_page_append<D, FMT, T, FMT == FKV_UINT4 ? 32 : kAppendThreads>
@@ -499,7 +505,15 @@ cudaError_t launch_page_append(const fkv_ctx *ctx, const fkv_pages *p, const fkv
     a.per = append_heads(ctx, groups, a.row_heads);
     a.chunks = (a.row_heads + a.per - 1) / a.per;
     a.row_blocks = static_cast<unsigned>((groups * a.chunks + kAppendThreads / 32 - 1) / (kAppendThreads / 32));
-    a.by_block = FastDiv::make(static_cast<unsigned>(p->block)), a.by_heads = FastDiv::make(static_cast<unsigned>(p->n_heads));
+    // Heads a run is looked up for: up to four, in equal parts, while an SM keeps 32 warps or 8
+    // blocks of runs (60 GPT-2-shaped prompts 86 us, 101 with one, 111 with twelve; Llama-shaped
+    // ones 207, 242, 199 with eight).
+    const int64_t runs = (a.T + a.stretch - 1) / a.stretch * 2, room = static_cast<int64_t>(ctx->sms) * (warp_runs(a, p->dim) ? 32 : 8);
+    const int64_t want = a.stretch == 1 ? 1 : runs * a.heads / room;
+    const int at_most = static_cast<int>(want < 1 ? 1 : want > 4 ? 4 : want);
+    a.run_chunks = (a.heads + at_most - 1) / at_most;
+    a.run_heads = (a.heads + a.run_chunks - 1) / a.run_chunks;
+    a.by_block = FastDiv::make(static_cast<unsigned>(p->block)), a.by_heads = FastDiv::make(static_cast<unsigned>(a.run_chunks));
     a.by_chunks = FastDiv::make(static_cast<unsigned>(a.chunks ? a.chunks : 1));
     switch (p->format) {
     case FKV_E4M3:

@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = warp >> 2;
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     auto bar = [&](int i) { return smem_u32(bars) + 8 * i; };
+
     // the last rows of a causal prompt see the most keys: they go first
     int x = blockIdx.x;
     const int h = x % a.H;

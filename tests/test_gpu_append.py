@@ -131,6 +131,28 @@ def test_append(fkv, ctx, fmt, dtype, D, rot, pairs, block, how):
     assert torch.equal(q.cpu()[live], want[live])
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8", "uint4"])
+@pytest.mark.parametrize("H,D,block", [(7, 64, 16), (12, 64, 16), (11, 128, 64), (8, 128, 32)])
+def test_append_of_many_tokens(fkv, ctx, fmt, H, D, block):
+    """So many runs that several heads share one look-up, heads that do not divide evenly among them, pages that grow."""
+    rng = np.random.default_rng(12)
+    lens = [(5, 9000), (0, 17), (block - 1, 6000), (3, 1), (0, 2500)]
+    nb = sum(n // block + 3 for _, n in lens)
+    slots, pos = _slots(rng, lens, nb, block)
+    T = len(slots)
+    pool = Pool(fkv, rng, nb, H, D, block, fmt)
+    x = torch.from_numpy(rng.standard_normal((T, 1 + 2 * H, D)).astype(np.float32)).bfloat16().cuda()
+    x[5999] *= 100                                           # a page's scale is one row's
+    cos, sin = _table(9100, D // 4)
+    out = ctx.page_append(pool.pages, x[:, 1:1 + H], x[:, 1 + H:], _cuda(slots), _cuda(pos), _cuda(cos), _cuda(sin), q=x[:, :1])
+    assert ctx.sync_status() == 0
+    h = x.float().cpu().numpy()
+    t = paged.turn(h[:, :1 + H], pos, cos, sin, D // 2)
+    assert torch.equal(out.cpu(), torch.from_numpy(t[:, :1]).bfloat16())
+    pool.write(t[:, 1:], h[:, 1 + H:], slots)
+    pool.same()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("D,block,T", [(64, 16, 1), (128, 32, 5), (128, 1024, 700), (64, 48, 3000)])
 def test_write_of_4_bits(fkv, ctx, D, block, T, dtype):
