@@ -569,8 +569,8 @@ int fkv_page_write(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rows *k, cons
  * of a negative position is left out: nothing of it is stored, its row of q_out left
  * as it is; one of a position past the tables too, and FKV_ERANGE is set (in 8-bit
  * pages either ends its run).  A token of a negative slot has its query turned all the
- * same.  q_out may be q itself; its
- * rows overlap nothing else of the call.  q and q_out may be NULL. */
+ * same.  q_out may be q itself; its rows overlap nothing else of the call.  q and
+ * q_out may be NULL. */
 typedef struct {
     const void *q;               /* vectors by (token, head) as fkv_rows, all of `dtype`: */
     void *q_out;                 /*   16-byte boundaries, element strides below */
