@@ -505,10 +505,10 @@ cudaError_t launch_page_append(const fkv_ctx *ctx, const fkv_pages *p, const fkv
     a.per = append_heads(ctx, groups, a.row_heads);
     a.chunks = (a.row_heads + a.per - 1) / a.per;
     a.row_blocks = static_cast<unsigned>((groups * a.chunks + kAppendThreads / 32 - 1) / (kAppendThreads / 32));
-    // Heads a run is looked up for: up to four, in equal parts, while an SM keeps 32 warps or 8
+    // Heads a run is looked up for: up to four, in equal parts, while an SM keeps 64 warps or 16
     // blocks of runs (60 GPT-2-shaped prompts 86 us, 101 with one, 111 with twelve; Llama-shaped
     // ones 207, 242, 199 with eight).
-    const int64_t runs = (a.T + a.stretch - 1) / a.stretch * 2, room = static_cast<int64_t>(ctx->sms) * (warp_runs(a, p->dim) ? 32 : 8);
+    const int64_t runs = (a.T + a.stretch - 1) / a.stretch * 2, room = static_cast<int64_t>(ctx->sms) * (warp_runs(a, p->dim) ? 64 : 16);
     const int64_t want = a.stretch == 1 ? 1 : runs * a.heads / room;
     const int at_most = static_cast<int>(want < 1 ? 1 : want > 4 ? 4 : want);
     a.run_chunks = (a.heads + at_most - 1) / at_most;

@@ -132,7 +132,7 @@ def test_append(fkv, ctx, fmt, dtype, D, rot, pairs, block, how):
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8", "uint4"])
-@pytest.mark.parametrize("H,D,block", [(7, 64, 16), (12, 64, 16), (11, 128, 64), (8, 128, 32)])
+@pytest.mark.parametrize("H,D,block", [(7, 64, 16), (12, 64, 16), (13, 64, 16), (11, 128, 64), (8, 128, 32)])
 def test_append_of_many_tokens(fkv, ctx, fmt, H, D, block):
     """So many runs that several heads share one look-up, heads that do not divide evenly among them, pages that grow."""
     rng = np.random.default_rng(12)
