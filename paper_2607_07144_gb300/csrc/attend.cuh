@@ -55,6 +55,8 @@ struct Seen {
     // Whether any of the rows sees one of the 16 keys from k on.  Others of a tile are
     // not looked up: their pages may be gone.
     __device__ __forceinline__ bool of(int k) const { return k < lo || (k + 16 > begin && k < end); }
+    // Whether any of them sees key j.
+    __device__ __forceinline__ bool one(int j) const { return j < lo || (j >= begin && j < end); }
 };
 
 // The tiles that rows at positions pa .. pb see: the first positions', then the window's.

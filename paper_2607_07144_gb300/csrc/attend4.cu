@@ -331,16 +331,15 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
         const uint32_t *const num = reinterpret_cast<const uint32_t *>(base + (nums - sbase)) + it % ST * (2 * KW) + lane;
 
         // a lane a key: its numbers, and what its value's step gives its weights.  Those of
-        // keys behind the request's end, or that were not loaded, may be anything.
-        const bool all_loaded = units == (1u << U) - 1 && key + KW <= q.len;
+        // keys that a row does not see may be anything: their scores are replaced, and what
+        // multiplies their weights of zero is finite (share_of always is).
 #pragma unroll
         for (int x = 0; x < KW; x += 32) {
-            uint32_t kn = num[x], vn = num[KW + x];
-            if (!all_loaded && (!(units >> ((x + lane) >> 4) & 1) || key + x + lane >= q.len))
-                kn = vn = 0;
+            const uint32_t kn = num[x], vn = num[KW + x];
             const float vs = value_scale(__uint_as_float(vn << 16)), share = share_of(vs);
+            const float vmid = share * __uint_as_float(vn & 0xffff0000u);
             keys_s[x + lane] = make_float4(__uint_as_float(kn << 16), __uint_as_float(kn & 0xffff0000u), lg2(vs), share);
-            mids_s[x + lane] = share * __uint_as_float(vn & 0xffff0000u);
+            mids_s[x + lane] = fabsf(vmid) <= 3.402823466e38f ? vmid : 0.0f;
         }
 
         // the units' keys gid and gid + 8; a unit that was not loaded gives

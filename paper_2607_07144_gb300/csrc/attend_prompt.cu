@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             return p.id;
         };
         uint4 v[3][NL];
-        uint32_t num[2];                       // of keys lane and 32 + lane % 16; 0: not the request's, or not looked at
+        uint32_t num[2];                       // of keys lane and 32 + lane % 16; 0: not looked at
         auto load = [&](uint4 (&x)[3][NL], int j, int id) {
             int64_t from = -1, from_n = -1;
             if (id >= 0) {
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                     x[u][i] = at[u] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(pool + at[u] + i * RP * a.st)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int y = 0; y < 2; ++y)
-                num[y] = at_n[y] >= 0 && first(j) + (y ? 32 + (lane & 15) : lane) < q.len ? __ldg(numbers + at_n[y] + (lane & 15)) : 0;
+                num[y] = at_n[y] >= 0 && first(j) + (y ? 32 + (lane & 15) : lane) < tiles.lim ? __ldg(numbers + at_n[y] + (lane & 15)) : 0;
         };
         const Page start = ask(0);
         Page after = ask(1);
@@ -384,11 +384,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
         int nid = check(after);
         for (int j = 0; j < n_it; ++j) {
             // nid: checked ids of tile j + 1.  All shuffles of an iteration come before its loads.
+            // Keys that no row sees hold anything: 0.  (Those behind the last row's were not loaded.
+            // The test of a key before a window, where its loads are, took 7 to 10 %.)
+            if (a.window) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    if (!rows_see.one(first(j) + (y ? 32 + (lane & 15) : lane)))
+                        num[y] = 0;
+            }
             uint32_t by[2];                    // step and middle as they go into the tile
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const float step = __uint_as_float(num[y] << 16), mid = __uint_as_float(num[y] & 0xffff0000u);
-                float most = fmaf(8.0f, step, fabsf(mid));
+                float step = __uint_as_float(num[y] << 16), mid = __uint_as_float(num[y] & 0xffff0000u);
+                float most = fmaf(8.0f, fabsf(step), fabsf(mid));
+                // (so do those of a token that was never stored, seen by its own row: what no written
+                // row has, NaN and infinities among it, would reach the tile's other rows)
+                if (!(most <= 0x1p120f))
+                    step = mid = most = 0.0f;
 #pragma unroll
                 for (int o = 1; o < 16; o <<= 1)
                     most = fmaxf(most, __shfl_xor_sync(~0u, most, o));

@@ -515,3 +515,51 @@ def test_refusals(fkv, ctx):
     odd = wide[:, :64].unflatten(1, (2, 16, 2))
     refused(lambda: go(pages=fkv.Pages(*[torch.zeros((20, 2, 16, 32), dtype=torch.uint8, device="cuda")] * 2, odd, odd)))
     assert (out == 7).all() and ctx.sync_status() == 0
+
+
+def _fill(how, shape, rng):
+    """Numbers (step, middle) as memory that was never written may hold them."""
+    if how == "random":
+        return (rng.integers(0, 1 << 16, shape + (2,)).astype(np.uint32) << 16).view(np.float32)
+    one = {"nan": (np.nan, np.nan), "middle": (0.25, np.inf), "step": (np.inf, 0.5), "minus": (-np.inf, -np.inf),
+           "large": (2.0 ** 100, -2.0 ** 116), "small": (0.0, 2.0 ** 100)}[how]
+    return np.broadcast_to(np.asarray(one, np.float32), shape + (2,))
+
+
+def _leave_unwritten(fkv, b, how, where):
+    """Pages as b's, but for the numbers of the positions where[r] of request r; what the oracle reads stays."""
+    rng = np.random.default_rng(90)
+    dev = []
+    for s in b.numbers:
+        s = s.copy()
+        for r, j in enumerate(where):
+            s[b.table[r, j // b.block], :, j % b.block] = _fill(how, (len(j), b.H), rng)
+        dev.append(torch.from_numpy(s).bfloat16().cuda())
+    b.pages = fkv.Pages(b.pages.k, b.pages.v, *dev)
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(softcap=20.0), dict(slopes=[0.1, 0.02, -0.01, 0.0])])
+@pytest.mark.parametrize("how", ["nan", "middle", "step", "minus", "large", "small", "random"])
+@pytest.mark.parametrize("new", [1, 7, 80])
+@pytest.mark.parametrize("D,dtype,block", [(64, "f16", 48), (128, "bf16", 16)])
+def test_positions_that_no_row_sees_hold_anything(fkv, ctx, D, dtype, block, new, how, opt):
+    """Before a window and behind the sinks, in units of 16 positions of which rows see others."""
+    b = Batch(fkv, 26, [(300, new), (45, new), (1000, new)], 2, 2, D, block, dtype)
+    seen = [paged.visible(new, x, window=40, sinks=5).any(0) for x in b.len]
+    assert all((~s).any() for s in seen[::2])
+    _leave_unwritten(fkv, b, how, [np.flatnonzero(~s) for s in seen])
+    b.check(ctx, rows=[0, new // 2, new - 1], window=40, sinks=5, **opt)
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(slopes=[0.1, 0.02, -0.01, 0.0])])
+@pytest.mark.parametrize("how", ["nan", "middle", "step", "minus"])
+@pytest.mark.parametrize("new", [4, 15, 80])
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "bf16"), (128, "f16")])
+def test_padded_tokens_do_not_reach_the_others(fkv, ctx, D, dtype, new, how, opt):
+    """The last tokens of each request were never stored: theirs are no one's rows, and the others' are as ever."""
+    b = Batch(fkv, 27, [(300, new), (45, new), (7, new)], 2, 2, D, 16, dtype)
+    _leave_unwritten(fkv, b, how, [np.arange(x - 3, x) for x in b.len])
+    given = {k: torch.tensor(v, dtype=torch.float32, device="cuda") for k, v in opt.items()}
+    out, lse = b.run(ctx, **given)
+    assert ctx.sync_status() == 0
+    b.compare(out, lse, np.arange(new - 3), None, opt.get("slopes"), 0.0, D ** -0.5, (), {})
