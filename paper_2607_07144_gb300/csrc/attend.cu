@@ -400,8 +400,8 @@ __global__ void __launch_bounds__(128, 3)
                 pf[n][1] = transpose8(pack_half(p[2], p[3]));
             }
             // value rows 2t, 2t + 1, 2t + 8, 2t + 9 of the unit, D / 8 dimensions
-            // each; rows behind the request's end hold any bytes, NaN codes among
-            // them: read as zeros
+            // each; those that a row does not see hold any bytes, and a weight of zero
+            // does not undo a NaN code
             uint32_t w[4][D / 32];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
@@ -415,14 +415,12 @@ __global__ void __launch_bounds__(128, 3)
                     w[x][0] = v.x, w[x][1] = v.y;
                 }
             }
-            if (key + 16 * u + 16 > q.len) {
+            if (FMT == FKV_E4M3 && !full) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
-                    if (key + 16 * u + 2 * t + (x & 1) + 8 * (x >> 1) >= q.len) {
 #pragma unroll
-                        for (int k = 0; k < D / 32; ++k)
-                            w[x][k] = 0;
-                    }
+                    for (int k = 0; k < D / 32; ++k)
+                        w[x][k] = without_nan(w[x][k]);
             }
 #pragma unroll
             for (int k = 0; k < D / 32; ++k)

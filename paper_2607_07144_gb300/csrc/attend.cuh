@@ -96,6 +96,13 @@ __device__ __forceinline__ bool all_see(const AttendArgs &a, const Request &q, i
            (k1 <= q.pre || ((!a.causal || k1 - 1 <= pa) && (!a.window || k0 > pb - a.window || k1 <= a.sinks)));
 }
 
+// Four e4m3 codes with NaN (0x7f and 0xff) as zero.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w)
+{
+    const uint32_t m = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return w & ~((m << 1) - (m >> 7));
+}
+
 __device__ __forceinline__ uint32_t pack_half(float a, float b)
 {
     const __half2 h = __floats2half2_rn(a, b);

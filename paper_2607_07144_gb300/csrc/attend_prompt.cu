@@ -552,6 +552,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             const int w = warp & 1;
             const int c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
             const int r0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+            // the keys between these are seen by every row
+            const int seen_from = a.window ? pb - a.window + 1 : 0;
+            const int seen_to = pa < 0 ? 0 : max(a.window ? 0 : q.pre, a.causal ? min(q.len, pa + 1) : q.len);
             const bool v_side = warp & 2;
             const uint8_t *const pool = static_cast<const uint8_t *>(v_side ? a.pool_v : a.pool_k) + h * a.sh + c * 16 + r0 * a.st;
             const float *const scale_of = (v_side ? a.vs : a.ks) + h * a.sch;
@@ -630,15 +633,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
                 const int st = j & 1;
                 if (j >= 2 && ok)
                     ok = mbar_park(bar(empty_bar + st), ((j >> 1) - 1) & 1, a.status);
-                const int first_key = first(j);
-                if (v_side && first_key + 64 > q.len) {
-                    // rows behind the request's end hold any bytes, NaN codes among them
+                if (FMT == FKV_E4M3 && v_side && (first(j) < seen_from || first(j) + 64 > seen_to)) {
+                    // keys that some row does not see hold any bytes, and a weight of zero does
+                    // not undo a NaN code
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
 #pragma unroll
-                        for (int i = 0; i < NL; ++i)
-                            if (first_key + 16 * u + r0 + i * RP >= q.len)
-                                v[u][i] = make_uint4(0, 0, 0, 0);
+                        for (int i = 0; i < NL; ++i) {
+                            v[u][i].x = without_nan(v[u][i].x), v[u][i].y = without_nan(v[u][i].y);
+                            v[u][i].z = without_nan(v[u][i].z), v[u][i].w = without_nan(v[u][i].w);
+                        }
                 }
                 const uint32_t tile = at0 + st * S::tile;
 #pragma unroll

@@ -263,6 +263,46 @@ def test_masked_nan_and_infinite_values_do_not_spread(fkv, ctx):
     b.check(ctx)
 
 
+def _nan_codes(b, where):
+    """NaN codes at the positions where[r] of request r; what the oracle reads stays."""
+    for t in (b.pages.k, b.pages.v):
+        t = t.view(torch.uint8)
+        for r, js in enumerate(where):
+            for j in js:
+                t[b.table[r, j // b.block], :, j % b.block] = 0x7f if j % 2 else 0xff
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(softcap=20.0), dict(slopes=[0.1, 0.02, 0.01, 0.0])])
+@pytest.mark.parametrize("new", [1, 7, 80])
+@pytest.mark.parametrize("D,dtype,block", [(64, "f16", 48), (128, "bf16", 16)])
+def test_positions_that_no_row_sees_hold_anything(fkv, ctx, D, dtype, block, new, opt):
+    """Before a window and behind the sinks, in units of 16 positions of which rows see others."""
+    b = Batch(fkv, 26, [(300, new), (45, new), (1000, new)], 2, 2, D, block, "e4m3", dtype)
+    seen = [paged.visible(new, x, window=40, sinks=5).any(0) for x in b.len]
+    assert all((~s).any() for s in seen[::2])
+    _nan_codes(b, [np.flatnonzero(~s) for s in seen])
+    b.check(ctx, rows=[0, new // 2, new - 1], window=40, sinks=5, **opt)
+
+
+@pytest.mark.parametrize("new", [4, 15, 80, 200])
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "bf16")])
+def test_padded_tokens_do_not_reach_the_others(fkv, ctx, D, dtype, new):
+    """The last tokens of each request were never stored, of one nothing of their page: theirs are no one's rows, and
+    the others' are as ever: twice what either may be off by, 2^-10 covering weights and scores, and 14 the largest value."""
+    b = Batch(fkv, 27, [(288 + (19 - new) % 16, new), (45, new), (7, new)], 2, 2, D, 16, "e4m3", dtype)
+    want, lse = b.run(ctx)
+    _nan_codes(b, [np.arange(x - 3, x) for x in b.len])
+    for s in (b.pages.k_scale, b.pages.v_scale):
+        s[b.table[0, b.len[0] // 16]] = float("nan")
+    out, lse2 = b.run(ctx)
+    assert ctx.sync_status() == 0
+    eps = torch.finfo(b.q.dtype).eps / 2
+    for x in b.cu[:-1]:
+        o, w = (y[x:x + new - 3].double() for y in (out, want))
+        assert ((o - w).abs() <= 2 * (eps * w.abs() + 2.0 ** -10 * 14)).all()
+        assert ((lse2 - lse)[x:x + new - 3].abs() <= 2.0 ** -10).all()
+
+
 def test_padded_rows_and_skipped_requests_stay(fkv, ctx):
     b = Batch(fkv, 9, [(40, 1), (60, 5), (20, 1)], 2, 2, 64, 16, "e4m3", "bf16", gap=5)
     good, _ = b.run(ctx)
