@@ -624,7 +624,9 @@ int fkv_page_append(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rotary *a, v
  * the row's values are unspecified.
  * FKV_UINT4: k_j and v_j are middle + (c - 7.5) step.  Elements of a query below
  * 2^-22 of its largest are rounded to 2^-33 of that, and that largest times a step
- * of K and `scale` has to be below 2^100.  What is said above of a weight times V's
+ * of K and `scale` has to be below 2^100.  With scale taken for 2 scale / cap where
+ * that is more, the largest times scale and K's values times scale have to be below
+ * 2^126.  What is said above of a weight times V's
  * scale holds for it times V's step, and for more than 32 rows a KV head (max_new x
  * query heads a KV head) times a power of two near the largest value of 16
  * positions; a bfloat16 q of that many rows has V's values rounded to fp16 as well

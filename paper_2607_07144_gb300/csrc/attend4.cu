@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
     const uint32_t sbase = (smem_u32(raw) + 1023) & ~1023u;
     uint8_t *const base = raw + (sbase - smem_u32(raw));
     uint2 *const q_s = reinterpret_cast<uint2 *>(base + S::ring);
-    // a warp's keys: K's step and middle, log2 of V's step; what a weight counts, and times V's middle
+    // a warp's keys: K's step and middle times 2^11, log2 of V's step; what a weight counts, and times V's middle
     float4 *const keys_s = reinterpret_cast<float4 *>(base + S::ring + S::q) + KW * warp;
     float *const mids_s = reinterpret_cast<float *>(base + S::ring + S::q + 4 * KW * 16) + KW * warp;
     typedef float RowPair[2][R];                 // a warp's maxima and sums
@@ -264,11 +264,13 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
         sum += __shfl_xor_sync(~0u, sum, 1);
         sum += __shfl_xor_sync(~0u, sum, 2);
         // a lane's scores are of rows 2t and 2t + 1: what a product (in 2^-24) and the sum of
-        // the query are multiplied by beside step and middle, and where a product starts
+        // the query are multiplied by beside step and middle, and where a product starts.  (Step
+        // and middle come times 2^11, which leaves these two below 2^127 scale: all in one of
+        // them, queries above 2^117 gave infinity, whatever the keys.)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const float by = __shfl_sync(~0u, down, (2 * t + c) * 4) * mul0, all = __shfl_sync(~0u, sum, (2 * t + c) * 4);
-            rowmul[n][c] = by * 0x1p24f, rowsum[n][c] = by * all, start[n][c] = -7.5f * 0x1p-24f * all;
+            rowmul[n][c] = by * 0x1p13f, rowsum[n][c] = by * (all * 0x1p-11f), start[n][c] = -7.5f * 0x1p-24f * all;
             const int rw = row0 + 8 * n + 2 * t + c;
             const bool live_c = rw < rows;
             const int ii = live_c ? static_cast<int>(a.gdiv.div(rw)) : 0;
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(128, step4_blocks(NT))
             const uint32_t kn = num[x], vn = num[KW + x];
             const float vs = value_scale(__uint_as_float(vn << 16)), share = share_of(vs);
             const float vmid = share * __uint_as_float(vn & 0xffff0000u);
-            keys_s[x + lane] = make_float4(__uint_as_float(kn << 16), __uint_as_float(kn & 0xffff0000u), lg2(vs), share);
+            keys_s[x + lane] = make_float4(__uint_as_float(kn << 16) * 0x1p11f, __uint_as_float(kn & 0xffff0000u) * 0x1p11f, lg2(vs), share);
             mids_s[x + lane] = fabsf(vmid) <= 3.402823466e38f ? vmid : 0.0f;
         }
 

@@ -563,3 +563,63 @@ def test_padded_tokens_do_not_reach_the_others(fkv, ctx, D, dtype, new, how, opt
     out, lse = b.run(ctx, **given)
     assert ctx.sync_status() == 0
     b.compare(out, lse, np.arange(new - 3), None, opt.get("slopes"), 0.0, D ** -0.5, (), {})
+
+
+@pytest.mark.parametrize("slopes", [None, [0.01, -0.02]])
+@pytest.mark.parametrize("new", [1, 5, 60])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_near_the_largest_numbers(fkv, ctx, D, new, slopes):
+    """Query rows of 2^121, whose elements cancel, against keys whose dimensions are alike: every score is zero before the
+    bias, and every product and sum on the way an integer of few bits times a power of two.  What is left of the bounds
+    above are the weights' and the values' roundings, the bias's error and the exponential's."""
+    b = Batch(fkv, 28, [(150, new), (17, new)], 1, 2, D, 16, "bf16")
+    c = b.codes[0]
+    c[:] = (c[..., :1] & 15) * 17
+    b.numbers[0] = b.numbers[0] * np.float32(2.0 ** -28)
+    b.pages = fkv.Pages(torch.from_numpy(c).cuda(), b.pages.v, *(torch.from_numpy(s).bfloat16().cuda() for s in b.numbers))
+    rng = np.random.default_rng(91)
+    sign = rng.permuted(np.broadcast_to(np.arange(D) % 2 * 2 - 1, tuple(b.q.shape)), axis=-1)
+    b.q = torch.from_numpy(np.ascontiguousarray(sign * 2.0 ** 121, np.float32)).bfloat16().cuda()
+    opt = {} if slopes is None else dict(slopes=torch.tensor(slopes, device="cuda"))
+    out, lse = b.run(ctx, scale=0.5, **opt)
+    assert ctx.sync_status() == 0
+    o, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r, length in enumerate(b.len):
+        v = paged.gather4(b.codes[1], b.numbers[1], b.table[r], length)[0]
+        for i in range(new):
+            p = b.before[r] + i
+            for u in range(2):
+                x = (0.0 if slopes is None else slopes[u]) * (np.arange(p + 1) - p)
+                w = np.exp(x)
+                want, mass = w @ v[:p + 1] / w.sum(), np.abs(v[:p + 1]).max()
+                ds = 2.0 ** -20 * (np.abs(x).max() + abs(np.log(w.sum())) + 16)
+                # (a value is at most twice the mass in |c - 7.5| step + |middle|)
+                bound = 2.0 ** -9 * np.abs(want) + (2.0 ** -10 + ds + length * 2.0 ** -30) * 2 * mass
+                assert (np.abs(o[b.cu[r] + i, u] - want) <= bound).all()
+                assert abs(l[b.cu[r] + i, u] - np.log(w.sum())) <= ds
+
+
+@pytest.mark.parametrize("new", [1, 6, 70])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_far_above_one(fkv, ctx, D, new):
+    """Rows of 2^50 to 2^66 against keys as much below."""
+    b = Batch(fkv, 29, [(200, new), (33, new)], 1, 2, D, 32, "bf16")
+    far = torch.exp2(torch.randint(50, 67, b.q.shape[:2] + (1,), device="cuda").float())
+    b.q = (b.q.float() * far).bfloat16()
+    b.numbers[0] = b.numbers[0] * np.float32(2.0 ** -60)
+    b.pages = fkv.Pages(b.pages.k, b.pages.v, *(torch.from_numpy(s).bfloat16().cuda() for s in b.numbers))
+    b.check(ctx, rows=[0, 1, new // 2, new - 1])
+
+
+@pytest.mark.parametrize("new", [1, 7, 80])
+@pytest.mark.parametrize("D,dtype", [(64, "f16"), (128, "bf16")])
+def test_keys_of_any_size(fkv, ctx, D, dtype, new):
+    """Keys' steps and middles apart by factors up to 2^60, and values' as well."""
+    b = Batch(fkv, 30, [(200, new), (20, new)], 1, 2, D, 16, dtype, spread=0.1)
+    rng = np.random.default_rng(61)
+    for kv in (0, 1):
+        far = np.exp2(rng.integers(-60, 1, b.numbers[kv].shape[:3]))[..., None].astype(np.float32)
+        with np.errstate(invalid="ignore"):
+            b.numbers[kv] = b.numbers[kv] * far
+    b.pages = fkv.Pages(b.pages.k, b.pages.v, *(torch.from_numpy(s).bfloat16().cuda() for s in b.numbers))
+    b.check(ctx, rows=[0, new // 2, new - 1])
