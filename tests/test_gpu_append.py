@@ -153,6 +153,88 @@ def test_append_of_many_tokens(fkv, ctx, fmt, H, D, block):
     pool.same()
 
 
+# So many tokens that a block of threads takes a run (its rule: more than 64 (token, head, K or V) an SM, and rows
+# enough in a page for a block), in runs of up to 1,024 rows: more than its threads keep.
+BLOCKS = [(64, 64, False, 48), (64, 32, True, 128), (128, 128, True, 48), (128, 128, False, 1024), (128, 64, False, 128),
+          (64, 48, True, 1024)]
+
+
+def _by_blocks(fkv, seed, fmt, dtype, D, block):
+    rng = np.random.default_rng(seed)
+    H, Hq = 8, 3
+    lens = [(0, 500), (37, 400), (block - 1, 300), (1000, 1), (5, 1150), (block, 37)]
+    nb = sum(n // block + 3 for _, n in lens)
+    slots, pos = _slots(rng, lens, nb, block)
+    T = len(slots)
+    assert T * H * 2 > 64 * torch.cuda.get_device_properties(0).multi_processor_count and block * (D // 16) > 128
+    pool = Pool(fkv, rng, nb, H, D, block, fmt)
+    x = torch.from_numpy((rng.standard_normal((T, Hq + 2 * H, D)) * np.exp(rng.standard_normal((T, 1, 1))))
+                         .astype(np.float32)).to(DT[dtype])
+    return H, Hq, lens, slots, pos, pool, x
+
+
+def _append_by_blocks(ctx, H, Hq, slots, pos, pool, x, rot, pairs, status):
+    cos, sin = _table(2300, rot // 2)
+    d = x.cuda()
+    out = torch.full((len(slots), Hq, x.shape[2]), 7.0, dtype=x.dtype, device="cuda")
+    ctx.page_append(pool.pages, d[:, Hq:Hq + H], d[:, Hq + H:], _cuda(slots), _cuda(pos), _cuda(cos), _cuda(sin), q=d[:, :Hq],
+                    q_out=out, interleaved=pairs)
+    assert ctx.sync_status() == status
+    h = x.float().numpy()
+    turned = paged.turn(h[:, :Hq + H], pos, cos, sin, rot, pairs)
+    off = (pos < 0) | (pos >= len(cos))
+    want = torch.from_numpy(turned[:, :Hq]).to(x.dtype)
+    want[torch.from_numpy(off)] = 7.0
+    assert torch.equal(out.cpu(), want)
+    pool.write(turned[:, Hq:], h[:, Hq + H:], np.where(off, -1, slots))
+    pool.same()
+
+
+@pytest.mark.parametrize("D,rot,pairs,block", BLOCKS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_runs_of_a_block_of_threads(fkv, ctx, fmt, dtype, D, rot, pairs, block):
+    """Runs that end early: at tokens of no slot, and of negative positions, at requests' and pages' ends."""
+    H, Hq, lens, slots, pos, pool, x = _by_blocks(fkv, 13, fmt, dtype, D, block)
+    ends = np.cumsum([n for _, n in lens]) - 1
+    slots[ends[0]], pos[ends[1]] = -1, -1
+    last = np.flatnonzero(slots % block == block - 1)
+    slots[last[0]], pos[last[-1]] = -1, -1
+    _append_by_blocks(ctx, H, Hq, slots, pos, pool, x, rot, pairs, 0)
+
+
+@pytest.mark.parametrize("D,rot,pairs,block", BLOCKS)
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_runs_of_a_block_with_positions_and_slots_outside(fkv, ctx, fmt, D, rot, pairs, block):
+    H, Hq, lens, slots, pos, pool, x = _by_blocks(fkv, 14, fmt, "bf16", D, block)
+    ends = np.cumsum([n for _, n in lens]) - 1
+    pos[ends[0]], pos[ends[2]], pos[ends[4]] = 2300, 2 ** 31 - 1, -5
+    _append_by_blocks(ctx, H, Hq, slots, pos, pool, x, rot, pairs, -2)
+    slots = slots.copy()
+    slots[ends[1]], slots[ends[5]] = 1 << 40, len(pool.codes[0]) * block
+    pos[ends[0]] = pos[ends[2]] = -1
+    _append_by_blocks(ctx, H, Hq, slots, pos, pool, x, rot, pairs, -2)
+
+
+@pytest.mark.parametrize("D,rot,pairs,block", BLOCKS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_runs_of_a_block_with_values_that_are_no_numbers(fkv, ctx, fmt, dtype, D, rot, pairs, block):
+    """NaN, infinities and values beyond the scales' range in some rows of a run, in its first ones and in its last."""
+    H, Hq, lens, slots, pos, pool, x = _by_blocks(fkv, 15, fmt, dtype, D, block)
+    x[3, Hq + 1, 5], x[499, Hq + H + 7, D - 1], x[700, Hq + 2, 0] = float("nan"), float("inf"), float("-inf")
+    x[1300, Hq + H, 9], x[1301, Hq + H, 9], x[40, 1, 3] = float("inf"), float("nan"), float("nan")
+    if dtype != "f16":
+        x[1700, Hq + 3], x[2000, Hq + H + 3] = 1.5e38, -2e36
+    cos, sin = _table(2300, rot // 2)
+    d = x.cuda()
+    ctx.page_append(pool.pages, d[:, Hq:Hq + H], d[:, Hq + H:], _cuda(slots), _cuda(pos), _cuda(cos), _cuda(sin), interleaved=pairs)
+    assert ctx.sync_status() == -5
+    h = x.float().numpy()
+    pool.write(paged.turn(h[:, Hq:Hq + H], pos, cos, sin, rot, pairs), h[:, Hq + H:], slots)
+    pool.same()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("D,block,T", [(64, 16, 1), (128, 32, 5), (128, 1024, 700), (64, 48, 3000)])
 def test_write_of_4_bits(fkv, ctx, D, block, T, dtype):
