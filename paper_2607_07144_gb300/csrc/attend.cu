@@ -519,73 +519,6 @@ template <int D, typename T> __global__ void __launch_bounds__(128) k_attend_com
 // A window that holds every position is none.
 int window_of(const fkv_attend &c) { return c.window >= FKV_PAGE_MAX_LEN ? 0 : static_cast<int>(c.window); }
 
-struct Plan {
-    int nt, row_tiles, splits, chunk;
-    bool cluster;                // the splits of a row are one cluster
-    bool fits;                   // the blocks are few enough for one launch
-};
-
-// Which kernel serves the call, and how many shares the keys are split into.
-// Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step
-// kernel, more to the tensor-memory one (nt = 0): for 24 sequences of 3-16k
-// positions and 8 heads of 128 in 8-bit pages, 63 rows take 384 us against 236; 28 rows 265
-// against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
-// 4,096 and 283 against 364 with a cap.  (4-bit pages: 28 rows 205 us, 32 rows 217,
-// 36 by the tensor-memory kernel 324.)  A block's time is its keys plus a fixed
-// part (its launch, the first loads' latency and its end: about that of 384 keys);
-// the blocks run in waves of `slots`.  The split with the least waves x time wins.
-// Up to eight shares of the step kernel are joined in their cluster (about 100
-// keys' time) if all blocks run at once: where blocks queue,
-// those of a cluster hold their places until its last one is done (64 ragged
-// sequences of 16-32k positions: 561 us, and 499 with the shares joined by
-// another launch, which costs 512 keys' time and 8 a share).
-Plan plan_of(const fkv_ctx *ctx, const fkv_attend &c)
-{
-    Plan p;
-    const int H = c.pages->n_heads, G = c.n_q_heads / H, window = window_of(c);
-    const int64_t most = c.max_new * G;
-    p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
-    const int per = p.nt ? 8 * p.nt : prompt_rows();
-    p.row_tiles = static_cast<int>((most + per - 1) / per);
-    const int64_t blocks = c.n_req * H * p.row_tiles, slots = ctx->sms * (p.nt == 0 ? 1 : c.pages->format == FKV_UINT4 ? step4_blocks(p.nt) : 3);
-    // Of 4-bit pages, the blocks that will have rows, as far as the number of tokens tells:
-    // others end at once, and no wave has to be saved for them (24 requests of 2 to 7 tokens,
-    // 4 query heads each: 66 us, 83 with all their second tiles counted).
-    int64_t busy = blocks;
-    if (c.pages->format == FKV_UINT4) {
-        const int64_t tiles = std::max(std::min(c.n_req, c.n_tok), (c.n_tok * G + per - 1) / per + c.n_req / 3);
-        busy = H * std::min(tiles, c.n_req * p.row_tiles);
-    }
-    // all that a block of rows may look at: with a window, that and the sinks (whose
-    // tiles end apart); a prefix may be of any length
-    int64_t span = c.max_len;
-    const int64_t seen = c.window + c.max_new + 2 * kTile + (c.sinks > 0 ? c.sinks + kTile : 0);
-    if (window && !c.prefix && c.sinks < FKV_PAGE_MAX_LEN && seen < span)
-        span = seen;
-    const int tiles = static_cast<int>((span + kTile - 1) / kTile);
-    double best = 0.0;
-    p.splits = 1;
-    p.chunk = tiles > 0 ? tiles : 1;
-    // blocks, and rows of partial results, are counted in a grid dimension
-    p.fits = blocks <= INT32_MAX;
-    const int64_t room = INT32_MAX / (blocks > 0 ? blocks : 1);
-    const int most_splits = c.n_tok * c.n_q_heads > INT32_MAX ? 1 : static_cast<int>(room < kMaxSplits ? room : kMaxSplits);
-    for (int s = 1; s <= most_splits && s <= tiles; ++s) {
-        const int chunk = (tiles + s - 1) / s;
-        const int64_t waves = (busy * s + slots - 1) / slots;
-        const bool in_cluster = p.nt && s > 1 && s <= kMaxCluster && blocks * s <= slots;
-        const double join = s == 1 ? 0.0 : in_cluster ? 100.0 : 512.0 + 8.0 * s;
-        const double cost = waves * (chunk * kTile + 384.0) + join;
-        if (s == 1 || cost < best) {
-            best = cost;
-            p.splits = (tiles + chunk - 1) / chunk;
-            p.chunk = chunk;
-        }
-    }
-    p.cluster = p.nt && p.splits > 1 && p.splits <= kMaxCluster && blocks * p.splits <= slots;
-    return p;
-}
-
 template <int D, int FMT, typename T, int NT>
 cudaError_t step_rows(const fkv_ctx *ctx, const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t st)
 {
@@ -635,30 +568,76 @@ cudaError_t step_dt(const fkv_ctx *ctx, const AttendArgs &a, int dtype, int nt, 
 
 }  // namespace
 
-// A load takes as many units of 16 positions as lie in a page, up to a warp's group
-// (attend4.cu); of 8-bit pages one.
-int page_attend_box(const fkv_ctx *ctx, const fkv_attend &c)
+// Which kernel serves the call, and how many shares the keys are split into.
+// Up to 32 rows a KV head (in tiles of nt = 1 or 2 columns of 8) go to the step
+// kernel, more to the tensor-memory one (nt = 0): for 24 sequences of 3-16k
+// positions and 8 heads of 128 in 8-bit pages, 63 rows take 384 us against 236; 28 rows 265
+// against 224 and 274 against 263 with a bias, but 84 against 110 with a window of
+// 4,096 and 283 against 364 with a cap.  (4-bit pages: 28 rows 205 us, 32 rows 217,
+// 36 by the tensor-memory kernel 324.)  A block's time is its keys plus a fixed
+// part (its launch, the first loads' latency and its end: about that of 384 keys);
+// the blocks run in waves of `slots`.  The split with the least waves x time wins.
+// Up to eight shares of the step kernel are joined in their cluster (about 100
+// keys' time) if all blocks run at once: where blocks queue,
+// those of a cluster hold their places until its last one is done (64 ragged
+// sequences of 16-32k positions: 561 us, and 499 with the shares joined by
+// another launch, which costs 512 keys' time and 8 a share).
+fkv_attend_plan page_attend_plan(const fkv_ctx *ctx, const fkv_attend &c)
 {
-    if (c.pages->format != FKV_UINT4)
-        return 16;
-    const int most = plan_of(ctx, c).nt ? kStep4Keys : 16;
-    int box = 16;
-    while (box < most && c.pages->block % (2 * box) == 0)
-        box *= 2;
-    return box;
+    fkv_attend_plan p;
+    const int H = c.pages->n_heads, G = c.n_q_heads / H, window = window_of(c);
+    const int64_t most = c.max_new * G;
+    p.nt = most <= 8 ? 1 : most <= 32 ? 2 : 0;
+    const int per = p.nt ? 8 * p.nt : prompt_rows();
+    p.row_tiles = static_cast<int>((most + per - 1) / per);
+    const int64_t blocks = c.n_req * H * p.row_tiles, slots = ctx->sms * (p.nt == 0 ? 1 : c.pages->format == FKV_UINT4 ? step4_blocks(p.nt) : 3);
+    // Of 4-bit pages, the blocks that will have rows, as far as the number of tokens tells:
+    // others end at once, and no wave has to be saved for them (24 requests of 2 to 7 tokens,
+    // 4 query heads each: 66 us, 83 with all their second tiles counted).
+    int64_t busy = blocks;
+    if (c.pages->format == FKV_UINT4) {
+        const int64_t tiles = std::max(std::min(c.n_req, c.n_tok), (c.n_tok * G + per - 1) / per + c.n_req / 3);
+        busy = H * std::min(tiles, c.n_req * p.row_tiles);
+    }
+    // all that a block of rows may look at: with a window, that and the sinks (whose
+    // tiles end apart); a prefix may be of any length
+    int64_t span = c.max_len;
+    const int64_t seen = c.window + c.max_new + 2 * kTile + (c.sinks > 0 ? c.sinks + kTile : 0);
+    if (window && !c.prefix && c.sinks < FKV_PAGE_MAX_LEN && seen < span)
+        span = seen;
+    const int tiles = static_cast<int>((span + kTile - 1) / kTile);
+    double best = 0.0;
+    p.splits = 1;
+    p.chunk = tiles > 0 ? tiles : 1;
+    // blocks, and rows of partial results, are counted in a grid dimension
+    const bool fits = blocks <= INT32_MAX;
+    const int64_t room = INT32_MAX / (blocks > 0 ? blocks : 1);
+    const int most_splits = c.n_tok * c.n_q_heads > INT32_MAX ? 1 : static_cast<int>(room < kMaxSplits ? room : kMaxSplits);
+    for (int s = 1; s <= most_splits && s <= tiles; ++s) {
+        const int chunk = (tiles + s - 1) / s;
+        const int64_t waves = (busy * s + slots - 1) / slots;
+        const bool in_cluster = p.nt && s > 1 && s <= kMaxCluster && blocks * s <= slots;
+        const double join = s == 1 ? 0.0 : in_cluster ? 100.0 : 512.0 + 8.0 * s;
+        const double cost = waves * (chunk * kTile + 384.0) + join;
+        if (s == 1 || cost < best) {
+            best = cost;
+            p.splits = (tiles + chunk - 1) / chunk;
+            p.chunk = chunk;
+        }
+    }
+    p.cluster = p.nt && p.splits > 1 && p.splits <= kMaxCluster && blocks * p.splits <= slots;
+    // A load takes as many units of 16 positions as lie in a page, up to a warp's group
+    // (attend4.cu); of 8-bit pages one.
+    p.box = 16;
+    if (c.pages->format == FKV_UINT4 && p.nt)
+        while (p.box < kStep4Keys && c.pages->block % (2 * p.box) == 0)
+            p.box *= 2;
+    p.workspace = !fits ? -1 : p.splits == 1 || p.cluster ? 0
+                : (static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * (c.pages->dim + 1) * 4 + 255) / 256 * 256;
+    return p;
 }
 
-int64_t page_attend_workspace(const fkv_ctx *ctx, const fkv_attend &c)
-{
-    const Plan p = plan_of(ctx, c);
-    if (!p.fits)
-        return -1;
-    if (p.splits == 1 || p.cluster)
-        return 0;
-    return (static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * (c.pages->dim + 1) * 4 + 255) / 256 * 256;
-}
-
-cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws, const CUtensorMap &mk,
+cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, const fkv_attend_plan &p, void *ws, const CUtensorMap &mk,
                                const CUtensorMap &mv, cudaStream_t st)
 {
     const fkv_pages *pg = c.pages;
@@ -680,8 +659,7 @@ cudaError_t launch_page_attend(const fkv_ctx *ctx, const fkv_attend &c, void *ws
     // (a cap next to float32's largest has a reciprocal of zero: y is zero, f(s) is s)
     a.cap2 = c.softcap * kLog2e, a.cap_inv = c.softcap > 0.0f ? 1.0f / a.cap2 : 0.0f;
     a.div = FastDiv::make(pg->block), a.gdiv = FastDiv::make(a.G);
-    const Plan p = plan_of(ctx, c);
-    a.box = __builtin_ctz(static_cast<unsigned>(page_attend_box(ctx, c))) - 4;
+    a.box = __builtin_ctz(static_cast<unsigned>(p.box)) - 4;
     a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk, a.cluster = p.cluster;
     a.ws_o = static_cast<float *>(ws);
     a.ws_lse = a.ws_o ? a.ws_o + static_cast<int64_t>(p.splits) * c.n_tok * c.n_q_heads * pg->dim : nullptr;

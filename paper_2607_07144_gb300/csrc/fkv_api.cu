@@ -1236,7 +1236,7 @@ int64_t fkv_page_attend_workspace(const fkv_ctx *ctx, const fkv_attend *a)
 {
     if (!ctx || check_attend_sizes(a))
         return 0;
-    const int64_t need = page_attend_workspace(ctx, *a);
+    const int64_t need = page_attend_plan(ctx, *a).workspace;
     return need < 0 ? 0 : need;
 }
 
@@ -1250,7 +1250,8 @@ int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t 
         return FKV_OK;
     if (const char *why = check_attend(a))
         return fail(ctx, FKV_EINVAL, why);
-    const int64_t need = page_attend_workspace(ctx, *a);
+    const fkv_attend_plan plan = page_attend_plan(ctx, *a);
+    const int64_t need = plan.workspace;
     if (need < 0)
         return fail(ctx, FKV_EINVAL, "too many requests times new tokens for one launch");
     if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256)))
@@ -1259,10 +1260,9 @@ int fkv_page_attend(fkv_ctx *ctx, const fkv_attend *a, void *workspace, int64_t 
         return fail(ctx, FKV_EINVAL, why);
     EncodeTiledFn enc = encode_tiled();
     CUtensorMap mk, mv;
-    const int box = page_attend_box(ctx, *a);
-    if (!enc || !page_map(enc, a->pages, a->pages->k, box, &mk) || !page_map(enc, a->pages, a->pages->v, box, &mv))
+    if (!enc || !page_map(enc, a->pages, a->pages->k, plan.box, &mk) || !page_map(enc, a->pages, a->pages->v, plan.box, &mv))
         return fail(ctx, FKV_ECUDA, "cuTensorMapEncodeTiled failed");
-    CK(launch_page_attend(ctx, *a, need ? workspace : nullptr, mk, mv, as_stream(stream)), "page attention launch");
+    CK(launch_page_attend(ctx, *a, plan, need ? workspace : nullptr, mk, mv, as_stream(stream)), "page attention launch");
     return FKV_OK;
 }
 

@@ -209,11 +209,17 @@ int64_t page_append_blocks(const fkv_pages *p, const fkv_rotary &r);
 cudaError_t launch_page_read(const fkv_ctx *c, const fkv_pages *p, const int32_t *kv_len, int64_t n_req,
                              const int32_t *table, int64_t table_stride, int64_t width, int64_t t0, int64_t t1,
                              int64_t layer, const fkv_cache *k_out, const fkv_cache *v_out, cudaStream_t st);
-// mk, mv: TMA maps over the pools as [page][head][position][dim] bytes, 16 positions a box
-// bytes, or -1: too many blocks for one launch
-int64_t page_attend_workspace(const fkv_ctx *c, const fkv_attend &a);
-int page_attend_box(const fkv_ctx *c, const fkv_attend &a);      // positions a load takes of a page
-cudaError_t launch_page_attend(const fkv_ctx *c, const fkv_attend &a, void *ws, const CUtensorMap &mk,
+// How a page attention call is launched (attend.cu): made once a call, as the maps and the
+// kernel have to agree on it.
+struct fkv_attend_plan {
+    int nt, row_tiles, splits, chunk;
+    int box;                     // positions a load takes of a page
+    bool cluster;                // the splits of a row are one cluster
+    int64_t workspace;           // bytes, or -1: too many blocks for one launch
+};
+fkv_attend_plan page_attend_plan(const fkv_ctx *c, const fkv_attend &a);
+// mk, mv: TMA maps over the pools as [page][head][position][row] bytes, p.box positions a box
+cudaError_t launch_page_attend(const fkv_ctx *c, const fkv_attend &a, const fkv_attend_plan &p, void *ws, const CUtensorMap &mk,
                                const CUtensorMap &mv, cudaStream_t st);
 
 // ------------------------------------------------------- device helpers
