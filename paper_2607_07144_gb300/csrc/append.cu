@@ -51,14 +51,16 @@ struct Groups {
     }
 };
 
-template <typename T> __device__ __forceinline__ Raw<T> load_groups(const T *row, const Groups &g)
+// (FIXED: the launch writes nothing of what is read.  Queries may be written in place.)
+template <bool FIXED, typename T> __device__ __forceinline__ Raw<T> load_groups(const T *row, const Groups &g)
 {
     constexpr int H = sizeof(T) / 2;         // 16-byte words a group
+    const uint4 *const p0 = reinterpret_cast<const uint4 *>(row + g.d0), *const p1 = reinterpret_cast<const uint4 *>(row + g.d1);
     Raw<T> r;
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-        r.v[i] = __ldg(reinterpret_cast<const uint4 *>(row + g.d0) + i);
-        r.v[H + i] = __ldg(reinterpret_cast<const uint4 *>(row + g.d1) + i);
+        r.v[i] = FIXED ? __ldg(p0 + i) : p0[i];
+        r.v[H + i] = FIXED ? __ldg(p1 + i) : p1[i];
     }
     return r;
 }
@@ -212,7 +214,7 @@ template <int D, int FMT, typename T> __device__ __forceinline__ void append_row
             const int kind = FMT != FKV_UINT4 || u + k < a.q_heads ? 0 : u + k < a.q_heads + a.heads ? 1 : 2;
             const int h = u + k - (kind == 0 ? 0 : kind == 1 ? a.q_heads : a.q_heads + a.heads);
             if (u + k < u1 && live)
-                raw[k] = load_groups<T>(static_cast<const T *>(a.x[kind]) + t * a.x_tok[kind] + h * a.x_head[kind], g);
+                raw[k] = load_groups<false, T>(static_cast<const T *>(a.x[kind]) + t * a.x_tok[kind] + h * a.x_head[kind], g);
             else
 #pragma unroll
                 for (int i = 0; i < static_cast<int>(sizeof(T)); ++i)
@@ -270,7 +272,7 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
     };
     // the thread's elements of a token's row, and what they are turned (twice, for the largest
     // magnitude and the codes: kept turned they would take twice the registers)
-    auto raw_of = [&](int64_t t) { return load_groups<T>(x + t * x_tok, g); };
+    auto raw_of = [&](int64_t t) { return load_groups<true, T>(x + t * x_tok, g); };
     auto turned = [&](const Raw<T> &r, int64_t t, float *v) {
         load16<T>(reinterpret_cast<const T *>(&r), v);
         if (g.f >= 0) {
