@@ -455,7 +455,7 @@ typedef struct {
     void *v;
     float *k_scale;
     float *v_scale;
-    int format;             /* FKV_E4M3 or FKV_INT8 */
+    int format;             /* FKV_E4M3, FKV_INT8 or FKV_UINT4 */
     int n_heads;
     int dim;
     int block;
@@ -613,24 +613,31 @@ int fkv_page_append(fkv_ctx *ctx, const fkv_pages *pages, const fkv_rotary *a, v
  * rounded to q's type, in `out` (n_tok x n_q_heads, q's dtype).  lse (float32
  * [n_tok][n_q_heads], or NULL) receives log sum_j exp(s_j).  A row that sees
  * nothing gets zeros and -infinity.  What masked positions and slots past a
- * request's end hold does not matter, nor does the table's entry of a page that
- * none of the request's rows sees (one behind the window may be gone).  Sums, maxima and weights are held in
- * float32, a weight times V's scale as a normal number up to 2^15: one that lies
- * more than 2^130 below the row's largest counts as zero (which takes pages of
- * V scales that far apart, or nearly).  For the product with V they are rounded
- * to fp16, and to zero below 2^-30 of the largest.  Elements of a bfloat16 query
- * below 2^-31 of its largest are rounded to 2^-39 of that.  A score, and a query's
- * largest element times K's scale and `scale`, have to be float32 numbers, else
- * the row's values are unspecified.
+ * request's end hold does not matter (a position that one row sees and another
+ * does not has to be valid for the one alone), nor does the table's entry of a
+ * page that none of the request's rows sees (one behind the window may be gone).
+ * Sums, maxima and weights are held in float32, a weight times V's scale as a
+ * normal number up to 2^15: one that lies more than 2^130 below the row's largest
+ * counts as zero (which takes pages of V scales that far apart, or nearly).  For
+ * the product with V they are rounded to fp16, and to zero below 2^-30 of the
+ * largest.  Elements of a bfloat16 query below 2^-31 of its largest are rounded to
+ * 2^-39 of that.  A score, and a query's largest element times K's scale and
+ * `scale`, have to be float32 numbers, else the row's values are unspecified.
  * FKV_UINT4: k_j and v_j are middle + (c - 7.5) step.  Elements of a query below
- * 2^-22 of its largest are rounded to 2^-33 of that, and that largest times a step
+ * 2^-21 of its largest are rounded to 2^-32 of that, and that largest times a step
  * of K and `scale` has to be below 2^100.  With scale taken for 2 scale / cap where
  * that is more, the largest times scale and K's values times scale have to be below
- * 2^126.  What is said above of a weight times V's
- * scale holds for it times V's step, and for more than 32 rows a KV head (max_new x
- * query heads a KV head) times a power of two near the largest value of 16
- * positions; a bfloat16 q of that many rows has V's values rounded to fp16 as well
- * (those below 2^-29 of that largest to 2^-40 of it).
+ * 2^126.  What is said above of a weight times V's scale holds for it times V's step.
+ * With more than 32 rows a KV head (max_new x query heads a KV head) it holds for it
+ * times a power of two near the largest of 16 positions' 8 step + |middle|, those of
+ * positions that any row of the request sees, and the numbers themselves are rounded
+ * in places:
+ *     a sum of a query's elements, which K's middles are multiplied by, to 2^-22 of
+ *     itself;
+ *     steps and middles of K, and of V for a float16 q, to multiples of 2^-38 of that
+ *     largest (exact from 2^-30 of it on);
+ *     values of V for a bfloat16 q to fp16 (below 2^-28 of that largest to 2^-35 of
+ *     it).
  * table, table_stride and width as in fkv_page_plan.  max_new and max_len bound
  * n_new and kv_len of every request (they size the launch).  A request whose
  * numbers do not hold together (cu not increasing or past n_tok, a length past

@@ -422,8 +422,8 @@ template <int D, int FMT, typename T, int GT> __device__ __forceinline__ void ap
 
 // Bytes bound long calls, and a few blocks an SM more or less what is in flight of them: 9
 // prompts of 1,000 to 8,192 tokens (32 query and 8 KV heads of 128, bf16) into 4-bit pages
-// 193 us, 5.6 TB/s, with six blocks an SM, 216 without the limit, 252 with eight (spills); into
-// e4m3 pages 207 us with five (with one head a run 242, 277 with six blocks, 335 with turned
+// 193 us, 5.6 TB/s, with six blocks an SM (80 registers, 24 to 48 bytes a thread spilled), 216
+// without the limit, 252 with eight (64 registers, more spilled); into e4m3 pages 207 us with five (with one head a run 242, 277 with six blocks, 335 with turned
 // rows kept in fp32).
 template <int D, int FMT, typename T, int GT> __global__ void __launch_bounds__(kAppendThreads, FMT == FKV_UINT4 ? 6 : 5) k_page_append(const AppendArgs a)
 {

@@ -593,7 +593,9 @@ fkv_attend_plan page_attend_plan(const fkv_ctx *ctx, const fkv_attend &c)
     const int64_t blocks = c.n_req * H * p.row_tiles, slots = ctx->sms * (p.nt == 0 ? 1 : c.pages->format == FKV_UINT4 ? step4_blocks(p.nt) : 3);
     // Of 4-bit pages, the blocks that will have rows, as far as the number of tokens tells:
     // others end at once, and no wave has to be saved for them (24 requests of 2 to 7 tokens,
-    // 4 query heads each: 66 us, 83 with all their second tiles counted).
+    // 4 query heads each: 66 us, 83 with all their second tiles counted).  n_req / 3 is what
+    // those requests' last tiles lack of full ones; it has been measured there alone, and a
+    // wrong guess costs a share more or less.
     int64_t busy = blocks;
     if (c.pages->format == FKV_UINT4) {
         const int64_t tiles = std::max(std::min(c.n_req, c.n_tok), (c.n_tok * G + per - 1) / per + c.n_req / 3);

@@ -1,4 +1,4 @@
-// What the two attention kernels over the paged cache share (attend.cu,
+// What the attention kernels over the paged cache share (attend.cu, attend4.cu,
 // attend_prompt.cu): arguments, the visible range of a request's rows, and how
 // the value scales enter.
 #pragma once

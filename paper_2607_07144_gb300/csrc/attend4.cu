@@ -16,7 +16,7 @@
 // A code needs no conversion: as the low four bits of an fp16 number it is the
 // subnormal c 2^-24, and one place to the left c 2^-20.  A word of eight codes is four
 // operands of two after four masks and a shift; the factor 16 between neighbours is
-// taken out of the query for K, exactly but for elements of it below 2^-25 of its largest
+// taken out of the query for K, exactly but for elements of it below 2^-24 of its largest
 // (rounded to 2^-35 of that), and of the output for V.
 //
 // Half of the bytes of 8-bit pages bring the same work: what bounds these kernels is no longer

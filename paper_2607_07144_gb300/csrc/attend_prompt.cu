@@ -24,18 +24,20 @@
 // 4-bit pages: a key, middle + (c - 7.5) step, is (c - 8) step, whose 11 bits fp16 holds,
 // and middle + step / 2 in every dimension.  K's tile holds the former over the power of
 // two that brings the largest of 16 keys' 8 step + |middle| to [2^14, 2^15), the unit's
-// scale (where a step is below 2^-28 of that, to 2^-40); the latter times the query's sum is
-// a step of 16 more dimensions: middle, middle, step / 2, step / 2 against the sum's upper
-// and lower half, twice.  So scores come out exactly as over 8-bit pages, without a number
-// of the key's in the softmax (with two there, 8 bytes of shared memory a score: 2,334 us
-// against 1,678).  V's tile holds whole values over such a power of two, rounded to fp16
+// scale (steps and middles below 2^-30 of that are rounded to multiples of fp16's 2^-24, 2^-38
+// of it); the latter times the query's sum is a step of 16 more dimensions: middle, middle,
+// step / 2, step / 2 against the sum's upper and lower half, twice, which leave out 2^-22 of
+// the sum: an error of 2^-22 |middle sum q|, next to fp32's of as large a product.  So scores
+// come out as over 8-bit pages, without a number of the key's in the softmax (with two there,
+// 8 bytes of shared memory a score: 2,334 us against 1,678).  V's tile holds whole values over such a power of two, rounded to fp16
 // once, as the weights are (for bfloat16 outputs; see EXACT).  Eight codes of a word lie in a
 // tile in the order 0 4 1 5 2 6 3 7, as masks give them two at a time; so do the queries'
 // elements, and the outputs' are put back.
 //
-// The pieces above: 1,678 us, 1.14 PFLOP/s (float16 1,848), GPT-2-shaped prompts 47 us (float16).
-// Without the codes' loads 1,471: a shuffle behind a load in flight waits for it, so that an
-// iteration's come before its loads (1,682 against 2,138); with the table's look-up left for the
+// The pieces above: 1,692 us, 1.13 PFLOP/s (float16 1,872), GPT-2-shaped prompts 47 us (float16);
+// 15 us of it are what keeps numbers of masked positions out (1,678 before).  Without the codes'
+// loads 1,471: a shuffle behind a load in flight waits for it, so that an iteration's come before
+// its loads (1,682 against 2,138); with the table's look-up left for the
 // iteration after 2,134.  Seven warps convert instead of four, all with the same statements:
 // those for K and V apart compete for the instruction cache.
 #include "attend.cuh"
@@ -693,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_prompt(const AttendArgs 
             {
                 constexpr int LR = D / 8, RI = 32 / LR;                  // rows at a time
                 // (with 4-bit keys rows of either type are scaled, and to less, so that fp16
-                // holds their sums: elements below 2^-22 of the largest are rounded to 2^-33 of it)
+                // holds their sums: elements below 2^-21 of the largest are rounded to 2^-32 of it)
                 constexpr int TOP = FOUR ? 7 : 14;
                 float all = 0.0f;                                        // the lane's row's sum
                 const int c = lane % LR, rr = lane / LR;

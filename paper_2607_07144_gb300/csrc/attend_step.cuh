@@ -6,7 +6,7 @@
 
 namespace fkvd {
 
-constexpr float kPBits = 8.0f;     // P is at most 2^8
+constexpr float kPBits = 8.0f;     // the reference's own weight is 2^8: P is at most that over 8-bit pages, 2^15 over 4-bit ones
 constexpr int kMaxCluster = 8;     // blocks of a portable cluster
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
